@@ -73,7 +73,7 @@ typedef enum {
                           bits 2 (c % 16).  bits <= 2, C % 16 == 0; as a layer input it needs
                           stride 1 and W % 4 == 0 (H W % 4 == 0 for 1x1 layers).  A quarter
                           of the bytes of PQ_CODES_C16. */
-    PQ_CODES_C32F4 = 4  /* 2-bit codes as packed FP4: two to a byte, channel-blocked in
+    PQ_CODES_C32F4 = 4, /* 2-bit codes as packed FP4: two to a byte, channel-blocked in
                           32-channel blocks of 16 bytes per position; code of channel c in the
                           4 bits at byte ((((n*(C/32) + c/32)*H + h)*W + w)*16 + (c%32)/2),
                           low nibble for even c, high nibble for odd c.  A code v <= 3 is the
@@ -81,6 +81,9 @@ typedef enum {
                           path reads it in place.  bits <= 2, C % 32 == 0; as a layer format it
                           also needs Cin_g % 64 == 0, Cout_g % 32 == 0, bits_w <= 3, and no
                           channel shuffle.  Half the bytes of PQ_CODES_C16. */
+    PQ_CODES_F16 = 5    /* tokens' signed 8-bit codes as IEEE half values (exact), rows of K:
+                          the operand of the dense layer's tensor-core path.  Only for
+                          palquant_quantize_tokens and palquant_linear_i8. */
 } pq_code_format;
 
 /* Output channel permutation (Sec. 4.2).  kind:
@@ -336,7 +339,8 @@ pq_status palquant_cyclic_shuffle_module(const void* q_dev, const void* w_packed
 
 /* Synchronise `stream`, then read and clear the device error word of the
  * current device.  Returns PQ_ETIMEOUT if any kernel's bounded wait ran out
- * since the last check, PQ_ECUDA on a CUDA error, else PQ_OK. */
+ * since the last check, PQ_EINVAL if one met a cache page out of range, PQ_ECUDA
+ * on a CUDA error, else PQ_OK. */
 pq_status palquant_sync_check(pq_stream_t stream);
 
 /* Limit, in nanoseconds, of every in-kernel wait of kernels launched after this
@@ -487,6 +491,137 @@ pq_status palquant_fake_quant_backward(const float* x_dev, const float* dy_dev, 
                                        double* du_dev, int64_t P, int32_t G, int32_t Cg, int32_t bits, int32_t kind,
                                        const float* l_host, const float* u_host, void* scratch_dev,
                                        size_t scratch_bytes, pq_stream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* 8-bit transformer layers.  The paper has no counterpart: these carry the  */
+/* library's integer products and group-wise scales to dense layers over     */
+/* tokens and to attention over a cache.  Signed 8-bit codes, one fp32 scale  */
+/* for each token, output channel, or block of cached tokens and head:       */
+/*   s = fl(amax * fl(1/127)), inv = fl(1/s), code = clamp(rint(fl(x * inv)), */
+/*   -127, 127)                                                              */
+/* with amax the largest magnitude under the scale and every operation one    */
+/* fp32 rounding (half to even).  An s below the smallest normal fp32 number   */
+/* counts as 0: codes 0, scale 0.  A NaN or an infinity under a scale makes   */
+/* that scale NaN and its codes 0: what is computed from them is NaN and        */
+/* nothing else is touched.                                                   */
+/* ------------------------------------------------------------------------ */
+
+/* Element type of activations. */
+typedef enum { PQ_F32 = 0, PQ_F16 = 1, PQ_BF16 = 2 } pq_float_type;
+
+/* A dense layer y = x W^T: x [M, K] of x_type, W [N, K] signed 8-bit codes, y
+ * [M, N] of y_type.  ldx, ldw, ldy: elements from one row to the next (at least
+ * the row's length).  The last dimension is contiguous. */
+typedef struct {
+    int64_t M;
+    int32_t N, K;        /* K <= 131072: every sum of 127 * 128 products fits int32 */
+    int32_t x_type, y_type; /* pq_float_type */
+    int64_t ldx, ldw, ldy;
+} pq_linear_desc;
+
+/* Codes and scale of every token (row): x_dev [M, K] of x_type, ldx elements
+ * from one row to the next.  code_format PQ_CODES_INT8 (signed bytes) or
+ * PQ_CODES_F16 (the codes as IEEE half values), q_dev [M, ldq], s_dev M floats.
+ * Any alignment of the type; rows on 16-byte boundaries are read and written 16
+ * bytes at a time.  M = 0 does nothing. */
+pq_status palquant_quantize_tokens(const void* x_dev, int32_t x_type, int64_t ldx, int64_t M, int32_t K,
+                                   int32_t code_format, void* q_dev, int64_t ldq, float* s_dev, pq_stream_t stream);
+
+/* The code format in which palquant_linear_i8 is fastest for a layer of this size
+ * (PQ_CODES_INT8 or PQ_CODES_F16); both give the same result.  Host only. */
+int32_t palquant_linear_code_format(const pq_linear_desc* d);
+
+/* The layer on codes (those of palquant_quantize_tokens, or any in [-127, 127]):
+ *   acc[m, n] = sum_k q[m, k] w[n, k]                    (exact, int32)
+ *   y[m, n] = fl(fl((float)acc * s_x[m]) * s_w[n]), then fl(y + bias[n]) if
+ *   bias_dev != NULL, rounded to y_type once.
+ * q_dev [M, ldq] in code_format; s_x_dev M floats, s_w_dev and bias_dev N floats;
+ * acc_dev (int32 [M, N], contiguous) and y_dev may each be NULL, not both (s_x_dev
+ * and s_w_dev may be NULL when y_dev is).  d->x_type and d->ldx are not read.
+ * M = 0 does nothing. */
+pq_status palquant_linear_i8(const void* q_dev, int32_t code_format, int64_t ldq, const float* s_x_dev,
+                             const int8_t* w_dev, const float* s_w_dev, const float* bias_dev, int32_t* acc_dev,
+                             void* y_dev, const pq_linear_desc* d, pq_stream_t stream);
+
+/* Bytes of device scratch palquant_linear_q8 needs (the tokens' codes and scales);
+ * 0 for a descriptor that it refuses. */
+size_t palquant_linear_q8_scratch_bytes(const pq_linear_desc* d);
+
+/* palquant_quantize_tokens into scratch_dev (16-byte aligned), then
+ * palquant_linear_i8: x_dev to y_dev. */
+pq_status palquant_linear_q8(const void* x_dev, const int8_t* w_dev, const float* s_w_dev, const float* bias_dev,
+                             void* y_dev, const pq_linear_desc* d, void* scratch_dev, size_t scratch_bytes,
+                             pq_stream_t stream);
+
+/* A paged cache of keys and values: codes [num_pages][Hkv][page_tokens][D] and one
+ * scale for each page and head [num_pages][Hkv], for each side.  The token at
+ * position p of sequence b sits in page page_table[b][p / page_tokens], slot
+ * p % page_tokens.  page_tokens is 16, 32, 64 or 128; D a multiple of 16, 16 to 256;
+ * codes 16-byte aligned.  A page id outside [0, num_pages) that a call meets is
+ * skipped (nothing is read or written there) and reported by palquant_sync_check as
+ * PQ_EINVAL. */
+typedef struct {
+    int32_t num_pages, page_tokens, Hkv, D;
+    int8_t *k_dev, *v_dev;
+    float *k_scale_dev, *v_scale_dev;
+} pq_kv8_cache;
+
+/* Runs of tokens of B sequences.  Sequence b's run has cu_dev[b + 1] - cu_dev[b]
+ * tokens (0 to max_n; cu_dev[0] = 0), at positions start_dev[b] and up; its i-th
+ * token is row cu_dev[b] + i of the float tensors, whose rows hold Hkv heads of D
+ * contiguous elements: element (row, h, d) at row * token stride + h * head stride
+ * + d.  page_table_dev: int32 [B][table_pitch].  cu_dev, start_dev and
+ * page_table_dev are device arrays of int32; a position whose page lies beyond
+ * table_pitch is skipped and reported as a page id out of range is. */
+typedef struct {
+    int32_t type; /* pq_float_type of k and v */
+    int32_t B, max_n, table_pitch;
+    int64_t k_token_stride, k_head_stride, v_token_stride, v_head_stride;
+    const int32_t *cu_dev, *start_dev, *page_table_dev;
+} pq_kv8_tokens;
+
+/* Quantise the runs into the cache.  A page whose first token is in the run starts
+ * afresh.  In a page that holds earlier tokens (slots below start % page_tokens)
+ * with scale s_old, the scale becomes s = max(s_old, s of the new tokens) and the
+ * earlier codes, where s grew, clamp(rint(fl(code * fl(s_old * inv))), -127, 127).  Slots
+ * after the run are left as they are.  No page may be touched by two sequences of
+ * one call. */
+pq_status palquant_kv8_append(const pq_kv8_cache* cache, const void* k_dev, const void* v_dev,
+                              const pq_kv8_tokens* t, pq_stream_t stream);
+
+/* The values of the runs' tokens, fl(code * scale) rounded to the type: k_dev and
+ * v_dev are written (each may be NULL). */
+pq_status palquant_kv8_read(const pq_kv8_cache* cache, void* k_dev, void* v_dev, const pq_kv8_tokens* t,
+                            pq_stream_t stream);
+
+/* Attention over the cache.  Sequence b has len_dev[b] cached tokens and
+ * n = cu_q_dev[b + 1] - cu_q_dev[b] queries (0 to max_q; cu_q_dev[0] = 0), rows
+ * cu_q_dev[b] and up of q and o, Hq heads of D each; query head h reads cache head
+ * h / (Hq / Hkv).  With causal = 1 the queries are the sequence's last tokens: query
+ * i stands at position p = len - n + i and sees the tokens up to p, with window > 0
+ * only the last `window` of them.  With causal = 0 every query sees all tokens
+ * (window must be 0).  With a score = scale * q . k for each token seen,
+ *   o = sum softmax(score) v;        a query that sees no token gives 0.
+ * Scores, softmax statistics and sums are fp32.  Queries of PQ_F16 and PQ_BF16
+ * enter the products as half values scaled by a power of two for each row, and
+ * the probabilities as half values; PQ_F32 carries a second half value for the rest of
+ * each.  max_len >= every len_dev[b], max_q >= every n (both on the host, so that
+ * the call does not wait for the device); Hq / Hkv <= 64. */
+typedef struct {
+    int32_t type; /* pq_float_type of q and o */
+    int32_t B, Hq, max_q, max_len;
+    int32_t causal, window, table_pitch;
+    float scale;
+    int64_t q_token_stride, q_head_stride, o_token_stride, o_head_stride;
+    const int32_t *cu_q_dev, *len_dev, *page_table_dev;
+} pq_kv8_attn;
+
+/* Bytes of device scratch palquant_kv8_attention needs; 0 where it needs none or
+ * would refuse the descriptors. */
+size_t palquant_kv8_attention_scratch_bytes(const pq_kv8_cache* cache, const pq_kv8_attn* a);
+
+pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, void* o_dev, const pq_kv8_attn* a,
+                                 void* scratch_dev, size_t scratch_bytes, pq_stream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Introspection (host only; no GPU needed).                                */

@@ -18,7 +18,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libpalquant.so")
 
 PQ_OK, PQ_EINVAL, PQ_EUNSUPPORTED, PQ_ECUDA, PQ_ETIMEOUT = 0, -1, -2, -3, -4
-PQ_CODES_INT8, PQ_CODES_E4M3, PQ_CODES_C16, PQ_CODES_C16P2, PQ_CODES_C32F4 = 0, 1, 2, 3, 4
+PQ_CODES_INT8, PQ_CODES_E4M3, PQ_CODES_C16, PQ_CODES_C16P2, PQ_CODES_C32F4, PQ_CODES_F16 = 0, 1, 2, 3, 4, 5
+PQ_F32, PQ_F16, PQ_BF16 = 0, 1, 2
 PQ_LAYER_INPUTS_READY = 1  # pq_layer_desc.flags: the previous kernel on the stream writes neither input nor weights
 
 # Every symbol include/palquant.h declares.
@@ -36,6 +37,9 @@ EXPORTS = [
     "palquant_bitsplit_pack_weight_codes_host", "palquant_bitsplit_act", "palquant_bitsplit_conv",
     "palquant_pack_weights_odd_host", "palquant_fake_quant_forward", "palquant_fake_quant_scratch_bytes",
     "palquant_fake_quant_backward", "palquant_quantize_act_lu", "palquant_quantize_layer_fused_lu",
+    "palquant_quantize_tokens", "palquant_linear_code_format", "palquant_linear_i8",
+    "palquant_linear_q8_scratch_bytes", "palquant_linear_q8", "palquant_kv8_append", "palquant_kv8_read",
+    "palquant_kv8_attention_scratch_bytes", "palquant_kv8_attention",
 ]
 
 
@@ -63,6 +67,29 @@ class ConvPlan(ctypes.Structure):
 
     def as_dict(self):
         return {name: getattr(self, name) for name, _ in self._fields_}
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("M", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("N", "K", "x_type", "y_type")] + \
+        [(n, ctypes.c_int64) for n in ("ldx", "ldw", "ldy")]
+
+
+class KV8Cache(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("num_pages", "page_tokens", "Hkv", "D")] + \
+        [(n, ctypes.c_void_p) for n in ("k_dev", "v_dev", "k_scale_dev", "v_scale_dev")]
+
+
+class KV8Tokens(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("type", "B", "max_n", "table_pitch")] + \
+        [(n, ctypes.c_int64) for n in ("k_token_stride", "k_head_stride", "v_token_stride", "v_head_stride")] + \
+        [(n, ctypes.c_void_p) for n in ("cu_dev", "start_dev", "page_table_dev")]
+
+
+class KV8Attn(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("type", "B", "Hq", "max_q", "max_len", "causal", "window", "table_pitch")] + \
+        [("scale", ctypes.c_float)] + \
+        [(n, ctypes.c_int64) for n in ("q_token_stride", "q_head_stride", "o_token_stride", "o_head_stride")] + \
+        [(n, ctypes.c_void_p) for n in ("cu_q_dev", "len_dev", "page_table_dev")]
 
 
 _P = ctypes.c_void_p
@@ -148,6 +175,24 @@ def _load():
     L.palquant_fake_quant_backward.restype = _I32
     L.palquant_fake_quant_backward.argtypes = [_P, _P, _P, _P, _P, _I64, _I32, _I32, _I32, _I32, _P, _P, _P,
                                                ctypes.c_size_t, _P]
+    L.palquant_quantize_tokens.restype = _I32
+    L.palquant_quantize_tokens.argtypes = [_P, _I32, _I64, _I64, _I32, _I32, _P, _I64, _P, _P]
+    L.palquant_linear_code_format.restype = _I32
+    L.palquant_linear_code_format.argtypes = [ctypes.POINTER(LinearDesc)]
+    L.palquant_linear_i8.restype = _I32
+    L.palquant_linear_i8.argtypes = [_P, _I32, _I64, _P, _P, _P, _P, _P, _P, ctypes.POINTER(LinearDesc), _P]
+    L.palquant_linear_q8_scratch_bytes.restype = ctypes.c_size_t
+    L.palquant_linear_q8_scratch_bytes.argtypes = [ctypes.POINTER(LinearDesc)]
+    L.palquant_linear_q8.restype = _I32
+    L.palquant_linear_q8.argtypes = [_P, _P, _P, _P, _P, ctypes.POINTER(LinearDesc), _P, ctypes.c_size_t, _P]
+    for name in ("palquant_kv8_append", "palquant_kv8_read"):
+        getattr(L, name).restype = _I32
+        getattr(L, name).argtypes = [ctypes.POINTER(KV8Cache), _P, _P, ctypes.POINTER(KV8Tokens), _P]
+    L.palquant_kv8_attention_scratch_bytes.restype = ctypes.c_size_t
+    L.palquant_kv8_attention_scratch_bytes.argtypes = [ctypes.POINTER(KV8Cache), ctypes.POINTER(KV8Attn)]
+    L.palquant_kv8_attention.restype = _I32
+    L.palquant_kv8_attention.argtypes = [ctypes.POINTER(KV8Cache), _P, _P, ctypes.POINTER(KV8Attn), _P, ctypes.c_size_t,
+                                         _P]
     return L
 
 
@@ -168,6 +213,11 @@ def _ptr(obj):
         assert obj.is_contiguous(), "tensors passed to libpalquant must be contiguous"
         return obj.data_ptr()
     raise TypeError(f"cannot pass {type(obj)} as a pointer")
+
+
+def _strided(obj):
+    """As _ptr, for a tensor whose strides are in its descriptor."""
+    return obj.data_ptr() if hasattr(obj, "data_ptr") else _ptr(obj)
 
 
 def _stream(stream):
@@ -456,3 +506,135 @@ def palquant_quantize_layer_fused_lu(x_dev, l, u, w_packed_dev, d: LayerDesc, m_
                                                 _ptr(mo), _ptr(mr), shuf or shuffle(1, 1), _ptr(shortcut_dev),
                                                 _ptr(acc_out_dev), _ptr(y_out_dev), _ptr(q_out_dev), _stream(stream)),
            "palquant_quantize_layer_fused_lu")
+
+
+# ---------------------------------------------------------------- 8-bit transformer layers
+def _float_type(t) -> int:
+    import torch
+
+    types = {torch.float32: PQ_F32, torch.float16: PQ_F16, torch.bfloat16: PQ_BF16}
+    if t.dtype not in types:
+        raise TypeError(f"activations are float32, float16 or bfloat16, not {t.dtype}")
+    return types[t.dtype]
+
+
+def _rows(t, name, columns=None):
+    """Row pitch of a matrix with contiguous rows (any pitch for a single row)."""
+    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{name}: a matrix with contiguous rows"
+    assert columns is None or t.shape[1] == columns, f"{name}: {columns} columns"
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+def _heads(t, name):
+    """(token stride, head stride) of [tokens, heads, D] with contiguous D."""
+    assert t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] <= 1), f"{name}: [tokens, heads, D] with contiguous D"
+    return t.stride(0), t.stride(1)
+
+
+def _index(t, name):
+    import torch
+
+    assert t.dtype == torch.int32 and t.is_contiguous(), f"{name}: a contiguous int32 tensor"
+    return t
+
+
+def linear_desc(x, w, y) -> LinearDesc:
+    """Descriptor of y [M, N] = x [M, K] w [N, K]^T from the tensors (w: int8 codes)."""
+    import torch
+
+    assert w.dtype == torch.int8, "w: int8 codes"
+    (M, K), N = x.shape, w.shape[0]
+    assert y.shape == (M, N), "y: [M, N]"
+    return LinearDesc(M, N, K, _float_type(x), _float_type(y), _rows(x, "x"), _rows(w, "w", K), _rows(y, "y"))
+
+
+def kv8_cache(k, v, k_scale, v_scale) -> KV8Cache:
+    """Descriptor of a paged 8-bit cache: codes [pages, Hkv, page_tokens, D] int8, scales [pages, Hkv] fp32.
+    It keeps the tensors alive."""
+    import torch
+
+    pages, H, T, D = k.shape
+    assert k.dtype == v.dtype == torch.int8 and v.shape == k.shape, "codes: two int8 tensors of one shape"
+    assert k_scale.dtype == v_scale.dtype == torch.float32 and k_scale.shape == v_scale.shape == (pages, H), \
+        "scales: two float32 tensors [pages, Hkv]"
+    c = KV8Cache(pages, T, H, D, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
+    c._keep = (k, v, k_scale, v_scale)
+    return c
+
+
+def kv8_tokens(k, v, cu, start, page_table, max_n) -> KV8Tokens:
+    """Descriptor of the runs that k and v [tokens, Hkv, D] hold (any token and head strides; v or k may be None
+    for palquant_kv8_read).  cu [B + 1], start [B], page_table [B, pages]: int32.  It keeps the index tensors alive."""
+    some = k if k is not None else v
+    B = start.numel()
+    assert cu.numel() == B + 1 and page_table.shape[0] == B, "cu: B + 1 values, page_table: B rows"
+    assert k is None or v is None or k.dtype == v.dtype, "k and v have one type"
+    ks, vs = ((0, 0) if t is None else _heads(t, n) for t, n in ((k, "k"), (v, "v")))
+    t = KV8Tokens(_float_type(some), B, int(max_n), page_table.shape[1], *ks, *vs, _ptr(_index(cu, "cu")),
+                  _ptr(_index(start, "start")), _ptr(_index(page_table, "page_table")))
+    t._keep = (cu, start, page_table)
+    return t
+
+
+def kv8_attn(q, o, cu_q, lens, page_table, max_q, max_len, scale, causal=True, window=0) -> KV8Attn:
+    """Descriptor of one attention call: q and o [tokens, Hq, D] (any token and head strides), cu_q [B + 1], lens [B],
+    page_table [B, pages]: int32.  It keeps the index tensors alive."""
+    B = lens.numel()
+    assert cu_q.numel() == B + 1 and page_table.shape[0] == B, "cu_q: B + 1 values, page_table: B rows"
+    assert o.shape == q.shape and o.dtype == q.dtype, "o: as q"
+    a = KV8Attn(_float_type(q), B, q.shape[1], int(max_q), int(max_len), int(bool(causal)), int(window),
+                page_table.shape[1], float(scale), *_heads(q, "q"), *_heads(o, "o"), _ptr(_index(cu_q, "cu_q")),
+                _ptr(_index(lens, "lens")), _ptr(_index(page_table, "page_table")))
+    a._keep = (cu_q, lens, page_table)
+    return a
+
+
+def palquant_quantize_tokens(x_dev, x_type, ldx, M, K, code_format, q_dev, ldq, s_dev, stream=None):
+    """Signed 8-bit codes and one scale for each token (row); code_format PQ_CODES_INT8 or PQ_CODES_F16."""
+    _check(lib.palquant_quantize_tokens(_strided(x_dev), x_type, ldx, M, K, code_format, _strided(q_dev), ldq,
+                                        _ptr(s_dev), _stream(stream)), "palquant_quantize_tokens")
+
+
+def palquant_linear_code_format(d: LinearDesc) -> int:
+    return lib.palquant_linear_code_format(ctypes.byref(d))
+
+
+def palquant_linear_i8(q_dev, code_format, ldq, s_x_dev, w_dev, s_w_dev, bias_dev, acc_dev, y_dev, d: LinearDesc,
+                       stream=None):
+    """Dense layer on token codes: exact int32 sums, scales for each token and output channel."""
+    _check(lib.palquant_linear_i8(_strided(q_dev), code_format, ldq, _ptr(s_x_dev), _strided(w_dev), _ptr(s_w_dev),
+                                  _ptr(bias_dev), _ptr(acc_dev), _strided(y_dev), ctypes.byref(d), _stream(stream)),
+           "palquant_linear_i8")
+
+
+def palquant_linear_q8_scratch_bytes(d: LinearDesc) -> int:
+    return lib.palquant_linear_q8_scratch_bytes(ctypes.byref(d))
+
+
+def palquant_linear_q8(x_dev, w_dev, s_w_dev, bias_dev, y_dev, d: LinearDesc, scratch_dev, scratch_bytes, stream=None):
+    """Token quantiser and dense layer: x to y."""
+    _check(lib.palquant_linear_q8(_strided(x_dev), _strided(w_dev), _ptr(s_w_dev), _ptr(bias_dev), _strided(y_dev),
+                                  ctypes.byref(d), _ptr(scratch_dev), scratch_bytes, _stream(stream)),
+           "palquant_linear_q8")
+
+
+def palquant_kv8_append(cache: KV8Cache, k_dev, v_dev, t: KV8Tokens, stream=None):
+    """Quantise runs of tokens into the cache (one scale for each page and head)."""
+    _check(lib.palquant_kv8_append(ctypes.byref(cache), _strided(k_dev), _strided(v_dev), ctypes.byref(t),
+                                   _stream(stream)), "palquant_kv8_append")
+
+
+def palquant_kv8_read(cache: KV8Cache, k_dev, v_dev, t: KV8Tokens, stream=None):
+    """The values that runs of cached tokens stand for; k_dev or v_dev may be None."""
+    _check(lib.palquant_kv8_read(ctypes.byref(cache), _strided(k_dev), _strided(v_dev), ctypes.byref(t),
+                                 _stream(stream)), "palquant_kv8_read")
+
+
+def palquant_kv8_attention_scratch_bytes(cache: KV8Cache, a: KV8Attn) -> int:
+    return lib.palquant_kv8_attention_scratch_bytes(ctypes.byref(cache), ctypes.byref(a))
+
+
+def palquant_kv8_attention(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, scratch_dev, scratch_bytes, stream=None):
+    """Attention over the cache: single tokens, chunks and prompts, grouped heads."""
+    _check(lib.palquant_kv8_attention(ctypes.byref(cache), _strided(q_dev), _strided(o_dev), ctypes.byref(a),
+                                      _ptr(scratch_dev), scratch_bytes, _stream(stream)), "palquant_kv8_attention")

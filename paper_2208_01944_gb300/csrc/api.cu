@@ -921,6 +921,10 @@ pq_status layer_fused_impl(const void* q_dev, const void* w_packed_dev, const pq
 
 }  // namespace
 
+namespace pq {
+uint64_t wait_limit_ns() { return g_wait_limit_ns.load(); }
+}  // namespace pq
+
 // ===========================================================================
 // Public ABI
 // ===========================================================================
@@ -1345,6 +1349,7 @@ pq_status palquant_sync_check(pq_stream_t stream) {
     if (cudaDeviceSynchronize() != cudaSuccess) return PQ_ECUDA;
   }
   if (h & PQ_ERR_TIMEOUT) return PQ_ETIMEOUT;
+  if (h & PQ_ERR_PAGE) return PQ_EINVAL;
   return PQ_OK;
 }
 

@@ -1,0 +1,246 @@
+// The paged 8-bit cache of keys and values: append (quantise in) and read (values
+// out).  One scale covers a page's tokens of one head, so a block of threads owns
+// one (page, head, side): it finds the scale of what the page will hold, rewrites
+// the earlier codes where the scale grew, and writes the new ones.  New tokens stay
+// in registers between the search for their largest magnitude and the rounding.
+// Bound by HBM: each new element is read once and each code written once.
+#include <cuda_runtime.h>
+
+#include "palquant.h"
+#include "pq_internal.h"
+#include "pq_tokens.cuh"
+
+namespace pq {
+namespace {
+
+constexpr int kKvThreads = 256;
+
+struct KvArgs {
+  pq_kv8_cache c;
+  pq_kv8_tokens t;
+  const void* in[2];  // k, v (append)
+  void* out[2];       // k, v (read); either may be NULL
+  int blocks;         // pages of a sequence that a run can touch
+  unsigned int* err;
+  bool wide[2];  // rows of the float tensor on 16-byte boundaries
+};
+
+// What a block of threads works on: side, head, and the run's tokens in one page.
+struct KvUnit {
+  int side, h;
+  int64_t row;      // float row of the run's first token in the page
+  int first, count; // slots [first, first + count) of the page belong to the run
+  int64_t page;     // -1: none (nothing to do)
+};
+
+__device__ __forceinline__ KvUnit kv_unit(const KvArgs& a) {
+  KvUnit u;
+  unsigned r = blockIdx.x;
+  u.side = r & 1;
+  r >>= 1;
+  u.h = r % a.c.Hkv;
+  r /= a.c.Hkv;
+  const int blk = r % a.blocks, b = r / a.blocks;
+  const int T = a.c.page_tokens;
+  const int start = a.t.start_dev[b], cu = a.t.cu_dev[b];
+  const int n = min(a.t.cu_dev[b + 1] - cu, a.t.max_n);
+  const int page = start / T + blk;
+  const int64_t lo = max(static_cast<int64_t>(start), static_cast<int64_t>(page) * T);
+  const int64_t hi = min(static_cast<int64_t>(start) + n, static_cast<int64_t>(page + 1) * T);
+  u.page = -1;
+  if (start < 0 || n <= 0 || lo >= hi) return u;
+  u.row = cu + (lo - start);
+  u.first = static_cast<int>(lo - static_cast<int64_t>(page) * T);
+  u.count = static_cast<int>(hi - lo);
+  int id = -1;
+  if (page < a.t.table_pitch) id = a.t.page_table_dev[static_cast<int64_t>(b) * a.t.table_pitch + page];
+  if (id < 0 || id >= a.c.num_pages) {
+    if (threadIdx.x == 0) atomicOr(a.err, PQ_ERR_PAGE);
+    return u;
+  }
+  u.page = id;
+  return u;
+}
+
+// NV: vectors of 8 elements that a thread keeps; 0: the tokens are read twice.
+template <typename T, int NV>
+__global__ void __launch_bounds__(kKvThreads) pq_kv8_append(const __grid_constant__ KvArgs a) {
+  __shared__ uint32_t red[8];
+  const KvUnit u = kv_unit(a);
+  if (u.page < 0) return;
+  const int D8 = a.c.D / 8;
+  const int64_t ts = u.side ? a.t.v_token_stride : a.t.k_token_stride;
+  const int64_t hs = u.side ? a.t.v_head_stride : a.t.k_head_stride;
+  const T* x = static_cast<const T*>(a.in[u.side]) + u.row * ts + u.h * hs;
+  const int64_t slot0 = (u.page * a.c.Hkv + u.h) * a.c.page_tokens;
+  int8_t* q = (u.side ? a.c.v_dev : a.c.k_dev) + slot0 * a.c.D;
+  float* sp = (u.side ? a.c.v_scale_dev : a.c.k_scale_dev) + u.page * a.c.Hkv + u.h;
+  const bool wide = a.wide[u.side];
+  const int nvec = u.count * D8;
+  const float was = u.first > 0 ? *sp : 0.0f;
+  auto get = [&](int v) { return load8(x + (v / D8) * ts + (v % D8) * 8, 8, wide); };
+
+  Vec8<T> keep[NV > 0 ? NV : 1];
+  uint32_t top = 0;
+  if (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = threadIdx.x + i * kKvThreads;
+      if (v < nvec) {
+        keep[i] = get(v);
+        top = max(top, amax8(keep[i]));
+      }
+    }
+  } else {
+    for (int v = threadIdx.x; v < nvec; v += kKvThreads) top = max(top, amax8(get(v)));
+  }
+  top = block_max(top, red);  // every thread has read the old scale before it
+  const float fresh = scale_of_amax(top);
+  const float scale = (fresh != fresh || was != was) ? __int_as_float(0x7FC00000) : fmaxf(was, fresh);
+  const float inv = inverse_of_scale(scale);
+  if (threadIdx.x == 0) *sp = scale;
+  if (u.first > 0 && scale != was) {  // also where either is NaN
+    const float ratio = __fmul_rn(was, inv);
+    uint32_t* w = reinterpret_cast<uint32_t*>(q);
+    for (int v = threadIdx.x; v < u.first * a.c.D / 4; v += kKvThreads) {
+      const uint32_t o = w[v];
+      int c[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) c[i] = code_of(static_cast<float>(static_cast<int8_t>(o >> (8 * i))), ratio);
+      w[v] = pack_bytes(c[0], c[1], c[2], c[3]);
+    }
+  }
+  uint2* dst = reinterpret_cast<uint2*>(q + static_cast<int64_t>(u.first) * a.c.D);
+  if (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = threadIdx.x + i * kKvThreads;
+      if (v < nvec) dst[v] = codes8(keep[i], inv);
+    }
+  } else {
+    for (int v = threadIdx.x; v < nvec; v += kKvThreads) dst[v] = codes8(get(v), inv);
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kKvThreads) pq_kv8_read(const __grid_constant__ KvArgs a) {
+  const KvUnit u = kv_unit(a);
+  if (u.page < 0 || a.out[u.side] == nullptr) return;
+  const int D8 = a.c.D / 8;
+  const int64_t ts = u.side ? a.t.v_token_stride : a.t.k_token_stride;
+  const int64_t hs = u.side ? a.t.v_head_stride : a.t.k_head_stride;
+  T* x = static_cast<T*>(a.out[u.side]) + u.row * ts + u.h * hs;
+  const int64_t slot0 = (u.page * a.c.Hkv + u.h) * a.c.page_tokens + u.first;
+  const uint2* q = reinterpret_cast<const uint2*>((u.side ? a.c.v_dev : a.c.k_dev) + slot0 * a.c.D);
+  const float scale = (u.side ? a.c.v_scale_dev : a.c.k_scale_dev)[u.page * a.c.Hkv + u.h];
+  const bool wide = a.wide[u.side];
+  for (int v = threadIdx.x; v < u.count * D8; v += kKvThreads) {
+    const uint2 c = q[v];
+    Vec8<T> r;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      r.v[i] = from_f32<T>(__fmul_rn(static_cast<float>(static_cast<int8_t>((i < 4 ? c.x : c.y) >> (8 * (i & 3)))), scale));
+    store8(x + (v / D8) * ts + (v % D8) * 8, r, 8, wide);
+  }
+}
+
+template <typename T>
+void launch_append(const KvArgs& a, unsigned grid, cudaStream_t s) {
+  const int vecs = a.c.page_tokens * (a.c.D / 8);
+  const int most = (vecs < a.t.max_n * (a.c.D / 8) ? vecs : a.t.max_n * (a.c.D / 8));
+  const int nv = (most + kKvThreads - 1) / kKvThreads;
+  if (nv <= 1)
+    pq_kv8_append<T, 1><<<grid, kKvThreads, 0, s>>>(a);
+  else if (nv <= 2)
+    pq_kv8_append<T, 2><<<grid, kKvThreads, 0, s>>>(a);
+  else if (nv <= 4)
+    pq_kv8_append<T, 4><<<grid, kKvThreads, 0, s>>>(a);
+  else if (nv <= 8)
+    pq_kv8_append<T, 8><<<grid, kKvThreads, 0, s>>>(a);
+  else
+    pq_kv8_append<T, 0><<<grid, kKvThreads, 0, s>>>(a);
+}
+
+}  // namespace
+
+bool valid_kv8_cache(const pq_kv8_cache* c) {
+  return c != nullptr && c->num_pages >= 1 && c->Hkv >= 1 &&
+         (c->page_tokens == 16 || c->page_tokens == 32 || c->page_tokens == 64 || c->page_tokens == 128) &&
+         c->D >= 16 && c->D <= 256 && c->D % 16 == 0 && c->k_dev != nullptr && c->v_dev != nullptr &&
+         c->k_scale_dev != nullptr && c->v_scale_dev != nullptr && is_aligned(c->k_dev, 16) &&
+         is_aligned(c->v_dev, 16) && is_aligned(c->k_scale_dev, 4) && is_aligned(c->v_scale_dev, 4);
+}
+
+namespace {
+
+// Checks what both calls share and fills the launch; *grid = 0: nothing to do.
+pq_status kv_args(const pq_kv8_cache* c, const pq_kv8_tokens* t, const void* k, const void* v, KvArgs* a,
+                  unsigned* grid) {
+  *grid = 0;
+  if (!valid_kv8_cache(c) || t == nullptr) return PQ_EINVAL;
+  if (t->type != PQ_F32 && t->type != PQ_F16 && t->type != PQ_BF16) return PQ_EINVAL;
+  if (t->B < 0 || t->max_n < 0 || t->table_pitch < 0) return PQ_EINVAL;
+  if (t->B == 0 || t->max_n == 0) return PQ_OK;
+  if (t->cu_dev == nullptr || t->start_dev == nullptr || t->page_table_dev == nullptr || !is_aligned(t->cu_dev, 4) ||
+      !is_aligned(t->start_dev, 4) || !is_aligned(t->page_table_dev, 4))
+    return PQ_EINVAL;
+  const size_t e = bytes_of_type(t->type);
+  if (!is_aligned(k, e) || !is_aligned(v, e)) return PQ_EINVAL;
+  if (t->k_token_stride < 0 || t->k_head_stride < 0 || t->v_token_stride < 0 || t->v_head_stride < 0) return PQ_EINVAL;
+  a->c = *c;
+  a->t = *t;
+  a->wide[0] = is_aligned(k, 16) && t->k_token_stride * e % 16 == 0 && t->k_head_stride * e % 16 == 0;
+  a->wide[1] = is_aligned(v, 16) && t->v_token_stride * e % 16 == 0 && t->v_head_stride * e % 16 == 0;
+  a->blocks = static_cast<int>((static_cast<int64_t>(t->max_n) + c->page_tokens - 2) / c->page_tokens + 1);
+  a->err = device_error_word();
+  if (a->err == nullptr) return PQ_ECUDA;
+  const int64_t units = 2ll * c->Hkv * a->blocks;
+  if (units > 0x7FFFFFFFll / t->B) return PQ_EUNSUPPORTED;
+  *grid = static_cast<unsigned>(units * t->B);
+  return PQ_OK;
+}
+
+}  // namespace
+}  // namespace pq
+
+extern "C" {
+
+pq_status palquant_kv8_append(const pq_kv8_cache* cache, const void* k_dev, const void* v_dev,
+                              const pq_kv8_tokens* t, pq_stream_t stream) {
+  if (t != nullptr && t->B > 0 && t->max_n > 0 && (k_dev == nullptr || v_dev == nullptr)) return PQ_EINVAL;
+  pq::KvArgs a = {};
+  unsigned grid = 0;
+  const pq_status st = pq::kv_args(cache, t, k_dev, v_dev, &a, &grid);
+  if (st != PQ_OK || grid == 0) return st;
+  a.in[0] = k_dev;
+  a.in[1] = v_dev;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (t->type == PQ_F32)
+    pq::launch_append<float>(a, grid, s);
+  else if (t->type == PQ_F16)
+    pq::launch_append<__half>(a, grid, s);
+  else
+    pq::launch_append<__nv_bfloat16>(a, grid, s);
+  return cudaGetLastError() == cudaSuccess ? PQ_OK : PQ_ECUDA;
+}
+
+pq_status palquant_kv8_read(const pq_kv8_cache* cache, void* k_dev, void* v_dev, const pq_kv8_tokens* t,
+                            pq_stream_t stream) {
+  if (t != nullptr && t->B > 0 && t->max_n > 0 && k_dev == nullptr && v_dev == nullptr) return PQ_EINVAL;
+  pq::KvArgs a = {};
+  unsigned grid = 0;
+  const pq_status st = pq::kv_args(cache, t, k_dev, v_dev, &a, &grid);
+  if (st != PQ_OK || grid == 0) return st;
+  a.out[0] = k_dev;
+  a.out[1] = v_dev;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  if (t->type == PQ_F32)
+    pq::pq_kv8_read<float><<<grid, pq::kKvThreads, 0, s>>>(a);
+  else if (t->type == PQ_F16)
+    pq::pq_kv8_read<__half><<<grid, pq::kKvThreads, 0, s>>>(a);
+  else
+    pq::pq_kv8_read<__nv_bfloat16><<<grid, pq::kKvThreads, 0, s>>>(a);
+  return cudaGetLastError() == cudaSuccess ? PQ_OK : PQ_ECUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,559 @@
+// Attention over the paged 8-bit cache for few query rows (single tokens, short
+// chunks; any other case, tile by tile).
+//
+// Mathematics.  With codes kc, vc and one scale for each page and head,
+//   x_ij = scale log2(e) s_k(j) sum_d q_id kc_jd,   w_ij = 2^(x_ij + log2 s_v(j) - m_i),
+//   o_id = sum_j w_ij vc_jd / sum_j w_ij / s_v(j),
+// m_i the running maximum of x_ij + log2 s_v(j).  Folding the value scale into the exponent keeps
+// every w in (0, 1] whatever the pages' scales are, so w can be a half value and the
+// products with the codes run without a scale inside the MMA.  (A page whose value
+// scale is 0 holds zeros only; it counts with scale 1.)
+//
+// Split.  Bound by the cache's bytes: each must be read once for all heads of a
+// group.  A block takes one cache head, up to 16 query rows and a part of the token
+// range; its 8 warps take 16-token steps in turn, each with a running maximum, sum
+// and output of its own, joined through shared memory at the end.  Scores are computed
+// transposed (tokens are the MMA's 16 rows, query rows its 8 columns: a group of up to
+// 8 heads fills it), the probabilities turn into the second product's operand by
+// an 8 x 8 transpose in registers, and the outputs are transposed too (16 rows of D).
+// Codes go from memory to registers to halves; no shared memory in the loop.
+// Few query rows are spread over the chip by splitting the tokens; the parts' maxima,
+// sums and outputs are joined by pq_kv8_join.
+//
+// Rounding.  Queries enter as halves scaled by a power of two for each row so that their largest
+// element lies in [2^7, 2^8) (exact for 16-bit queries down to 2^-22 of it), w as
+// halves (scaled by 2^8: small ones stay normal); fp32 queries and their w carry a
+// second half for the remainder (22 bits).  All sums are fp32.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "palquant.h"
+#include "pq_internal.h"
+#include "pq_kv8.h"
+#include "pq_tokens.cuh"
+
+namespace pq {
+namespace {
+
+constexpr int kAttnWarps = 8;
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kWShift = 8.0f;
+constexpr float kNone = -INFINITY;
+
+__device__ __forceinline__ float exp2_approx(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+// Tokens that the query rows [r0, r0 + rows) of sequence b may see: [lo, hi).
+struct Span {
+  int n, len;  // queries and tokens of the sequence
+  int lo, hi;
+};
+
+__device__ __forceinline__ Span span_of(const AttnArgs& p, int b, int r0, int rows) {
+  Span s;
+  s.n = min(p.a.cu_q_dev[b + 1] - p.a.cu_q_dev[b], p.a.max_q);
+  s.len = max(0, min(p.a.len_dev[b], p.a.max_len));
+  s.lo = 0;
+  s.hi = s.len;
+  if (p.a.causal) {
+    const int last = min(s.n * p.group, r0 + rows) - 1;
+    s.hi = min(s.len, s.len - s.n + last / p.group + 1);
+    if (p.a.window > 0) s.lo = max(0, s.len - s.n + r0 / p.group + 1 - p.a.window);
+  }
+  return s;
+}
+
+// The block's share of the grid: the row tile changes fastest (its neighbours read
+// the same codes).
+struct Place {
+  int tile, split, h, b;
+};
+
+__device__ __forceinline__ Place place_of(const AttnArgs& p) {
+  Place r;
+  unsigned i = blockIdx.x;
+  r.tile = i % p.row_tiles;
+  i /= p.row_tiles;
+  r.split = i % p.splits;
+  i /= p.splits;
+  r.h = i % p.c.Hkv;
+  r.b = i / p.c.Hkv;
+  return r;
+}
+
+// DP: D rounded up to 64, 128 or 256; NT: tiles of 8 query rows; TWO: fp32 queries
+// and outputs, each operand in two halves.
+template <typename T, int DP, int NT, bool TWO>
+__global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_constant__ AttnArgs p) {
+  constexpr int kC = DP / 64;        // 64-wide pieces of a key row
+  constexpr int kJ = DP / 16;        // 16-row tiles of the transposed output
+  constexpr int kRows = 8 * NT;
+  constexpr int kHalves = TWO ? 2 : 1;
+  __shared__ float row_factor[kRows];
+  __shared__ float join_m[kAttnWarps][kRows], join_l[kAttnWarps][kRows];
+  __shared__ float join_o[kAttnWarps / 2][kJ * NT * 4][32];
+  const Place w = place_of(p);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int r0 = w.tile * kRows;
+  const Span sp = span_of(p, w.b, r0, kRows);
+  const int rows = sp.n * p.group;
+  if (r0 >= rows) return;
+  const int first = sp.lo & ~15;
+  const int from = first + w.split * p.chunk;
+  const int to = min(sp.hi, from + p.chunk);
+  if (w.split > 0 && from >= sp.hi) return;
+  const int D = p.c.D;
+
+  // ---- queries: row 8 j + g, columns 64 c + 16 t and up, as the MMA's second operand
+  uint32_t qf[kHalves][NT][kC][8];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+    const int r = r0 + 8 * j + g;
+    const bool there = r < rows;
+    const int64_t tok = p.a.cu_q_dev[w.b] + (there ? r / p.group : 0);
+    const T* src = static_cast<const T*>(p.q) + tok * p.a.q_token_stride +
+                   static_cast<int64_t>(w.h * p.group + (there ? r % p.group : 0)) * p.a.q_head_stride;
+    Vec8<T> v[kC][2];
+    uint32_t top = 0;
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int d = 64 * c + 16 * t + 8 * i;
+        v[c][i] = load8(src + d, there && d < D ? 8 : 0, there && d < D && p.wide_q);
+        top = max(top, amax8(v[c][i]));
+      }
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+    // 2^e <= largest magnitude < 2^(e+1); the row is scaled by 2^(7 - e)
+    const int e = top >= 0x7F800000u ? 0 : max(static_cast<int>(top >> 23) - 127, -100);
+    const float f = __int_as_float((127 + 7 - e) << 23);
+    if (warp == 0 && t == 0) row_factor[8 * j + g] = p.a.scale * kLog2e * __int_as_float((127 - 7 + e) << 23);
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const float a = to_f32(v[c][i].v[2 * k]) * f, b = to_f32(v[c][i].v[2 * k + 1]) * f;
+          const uint32_t h = pack_half2(a, b);
+          qf[0][j][c][4 * i + k] = h;
+          if (TWO) {
+            const __half2 hh = *reinterpret_cast<const __half2*>(&h);
+            qf[kHalves - 1][j][c][4 * i + k] = pack_half2(a - __low2float(hh), b - __high2float(hh));
+          }
+        }
+  }
+  __syncthreads();
+  // ---- this lane's score columns: rows 8 j + 2 t and 8 j + 2 t + 1
+  float factor[NT][2];
+  int lo[NT][2], hi[NT][2];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = r0 + 8 * j + 2 * t + i;
+      factor[j][i] = row_factor[8 * j + 2 * t + i];
+      const int at = sp.len - sp.n + r / p.group + 1;
+      hi[j][i] = r >= rows ? 0 : p.a.causal ? min(at, sp.len) : sp.len;
+      lo[j][i] = p.a.window > 0 ? max(0, at - p.a.window) : 0;
+    }
+
+  float m[NT][2], l[NT][2], o[kJ][NT][4];
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) m[j][i] = kNone, l[j][i] = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kJ; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[i][j][e] = 0.0f;
+
+  const int* table = p.a.page_table_dev + static_cast<int64_t>(w.b) * p.a.table_pitch;
+  for (int s = from + 16 * warp; s < to; s += 16 * kAttnWarps) {
+    const int slot = s >> p.page_shift;
+    const int id = slot < p.a.table_pitch ? table[slot] : -1;
+    if (id < 0 || id >= p.c.num_pages) {
+      if (lane == 0) atomicOr(p.err, PQ_ERR_PAGE);
+      continue;
+    }
+    const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
+    const int64_t base = ((ph << p.page_shift) + (s & (p.c.page_tokens - 1))) * D;
+    const int8_t* kp = p.c.k_dev + base;
+    const int8_t* vp = p.c.v_dev + base;
+    // ---- codes: key rows g and g + 8; value rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+    uint4 kr[kC][2];
+#pragma unroll
+    for (int c = 0; c < kC; ++c)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        kr[c][i] = 64 * c + 16 * t < D ? *reinterpret_cast<const uint4*>(kp + (g + 8 * i) * D + 64 * c + 16 * t)
+                                       : make_uint4(0, 0, 0, 0);
+    uint32_t vr[4][DP / 32];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int8_t* src = vp + (2 * t + (i & 1) + 8 * (i >> 1)) * D + g * (DP / 8);
+      if (DP == 64) {
+        const uint2 v = g * 8 < D ? *reinterpret_cast<const uint2*>(src) : make_uint2(0, 0);
+        vr[i][0] = v.x, vr[i][1] = v.y;
+      } else {
+#pragma unroll
+        for (int c = 0; c < DP / 128; ++c) {
+          const uint4 v = g * (DP / 8) + 16 * c < D ? *reinterpret_cast<const uint4*>(src + 16 * c) : make_uint4(0, 0, 0, 0);
+          vr[i][4 * c] = v.x, vr[i][4 * c + 1] = v.y, vr[i][4 * c + 2] = v.z, vr[i][4 * c + 3] = v.w;
+        }
+      }
+    }
+    const float sk = p.c.k_scale_dev[ph];
+    const float sv0 = p.c.v_scale_dev[ph];
+    const float sv = sv0 == 0.0f ? 1.0f : sv0;
+    const float lv = log2f(sv), inv_v = 1.0f / sv;
+
+    // ---- scores
+    float x[NT][4];
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[j][e] = 0.0f;
+#pragma unroll
+    for (int c = 0; c < kC; ++c) {
+      const uint32_t a[4] = {kr[c][0].x, kr[c][0].y, kr[c][0].z, kr[c][0].w};
+      const uint32_t b[4] = {kr[c][1].x, kr[c][1].y, kr[c][1].z, kr[c][1].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t a0, a1, a2, a3;
+        half_of_codes(a[i], a0, a2);
+        half_of_codes(b[i], a1, a3);
+#pragma unroll
+        for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            mma_16x8x16(x[j], a0, a1, a2, a3, qf[hf][j][c][2 * i], qf[hf][j][c][2 * i + 1]);
+      }
+    }
+    // ---- probabilities
+    uint32_t pf[kHalves][NT][2];
+    bool grew = false;
+    float alpha[NT][2];
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+      float wv[4];
+      bool seen[4];
+      float top[2] = {m[j][0], m[j][1]};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int i = e & 1, at = s + g + 8 * (e >> 1);
+        seen[e] = at >= lo[j][i] && at < hi[j][i];
+        wv[e] = fmaf(x[j][e], sk * factor[j][i], lv);
+        if (seen[e]) top[i] = fmaxf(top[i], wv[e]);
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], d));
+        const float at = top[i] == kNone ? 0.0f : top[i];
+        alpha[j][i] = exp2_approx(m[j][i] - at);
+        grew |= top[i] != m[j][i];
+        m[j][i] = top[i];
+        top[i] = at - kWShift;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) wv[e] = seen[e] ? exp2_approx(wv[e] - top[e & 1]) : 0.0f;
+#pragma unroll
+      for (int i = 0; i < 2; ++i)  // a page that the row does not see adds nothing, even with a NaN scale
+        l[j][i] = l[j][i] * alpha[j][i] + (seen[i] || seen[i + 2] ? (wv[i] + wv[i + 2]) * inv_v : 0.0f);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t h = pack_half2(wv[2 * i], wv[2 * i + 1]);
+        pf[0][j][i] = transpose_8x8(h);
+        if (TWO) {
+          const __half2 hh = *reinterpret_cast<const __half2*>(&h);
+          pf[kHalves - 1][j][i] = transpose_8x8(pack_half2(wv[2 * i] - __low2float(hh), wv[2 * i + 1] - __high2float(hh)));
+        }
+      }
+    }
+    if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+      for (int i = 0; i < kJ; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][j][e] *= alpha[j][e & 1];
+    }
+    // ---- outputs: tile i holds D rows g (DP/8) + 2 i (its rows 0-7) and + 2 i + 1 (rows 8-15)
+#pragma unroll
+    for (int c = 0; c < DP / 32; ++c) {
+      uint32_t a01[4], a23[4];
+      half_pairs_of_codes(vr[0][c], vr[1][c], a01);
+      half_pairs_of_codes(vr[2][c], vr[3][c], a23);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int hf = 0; hf < kHalves; ++hf)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            mma_16x8x16(o[2 * c + i][j], a01[2 * i], a01[2 * i + 1], a23[2 * i], a23[2 * i + 1], pf[hf][j][0], pf[hf][j][1]);
+    }
+  }
+  // ---- join the warps: sums over the lanes, then pairs of warps
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int d = 4; d < 32; d <<= 1) l[j][i] += __shfl_xor_sync(0xffffffffu, l[j][i], d);
+#pragma unroll
+  for (int half = kAttnWarps / 2; half > 0; half >>= 1) {
+    if (warp >= half && warp < 2 * half) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (g == 0) join_m[warp][8 * j + 2 * t + i] = m[j][i], join_l[warp][8 * j + 2 * t + i] = l[j][i];
+#pragma unroll
+        for (int i = 0; i < kJ; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) join_o[warp - half][(i * NT + j) * 4 + e][lane] = o[i][j][e];
+      }
+    }
+    __syncthreads();
+    if (warp < half) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        float mine[2], other[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const float mo = join_m[warp + half][8 * j + 2 * t + i];
+          const float top = fmaxf(m[j][i], mo), at = top == kNone ? 0.0f : top;
+          mine[i] = exp2_approx(m[j][i] - at);
+          other[i] = exp2_approx(mo - at);
+          l[j][i] = l[j][i] * mine[i] + join_l[warp + half][8 * j + 2 * t + i] * other[i];
+          m[j][i] = top;
+        }
+#pragma unroll
+        for (int i = 0; i < kJ; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            o[i][j][e] = o[i][j][e] * mine[e & 1] + join_o[warp][(i * NT + j) * 4 + e][lane] * other[e & 1];
+      }
+    }
+    __syncthreads();
+  }
+  if (warp != 0) return;
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int r = r0 + 8 * j + 2 * t + i;
+      if (r >= rows) continue;
+      const int qi = r / p.group, hq = w.h * p.group + r % p.group;
+      const int d0 = g * (DP / 8);
+      if (p.splits > 1) {
+        const int64_t at = ((static_cast<int64_t>(w.b) * p.a.max_q + qi) * p.a.Hq + hq) * p.splits + w.split;
+        if (g == 0) p.ml[at] = make_float2(m[j][i], l[j][i]);
+        float* dst = p.part + at * D + d0;
+#pragma unroll
+        for (int k = 0; k < kJ; ++k)
+          if (d0 + 2 * k < D) *reinterpret_cast<float2*>(dst + 2 * k) = make_float2(o[k][j][i], o[k][j][i + 2]);
+        continue;
+      }
+      const float inv = l[j][i] == 0.0f ? 0.0f : 1.0f / l[j][i];
+      T* dst = static_cast<T*>(p.o) + (static_cast<int64_t>(p.a.cu_q_dev[w.b]) + qi) * p.a.o_token_stride +
+               static_cast<int64_t>(hq) * p.a.o_head_stride + d0;
+#pragma unroll
+      for (int k = 0; k < kJ; k += 4) {
+        Vec8<T> v;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          v.v[2 * u] = from_f32<T>(o[k + u][j][i] * inv);
+          v.v[2 * u + 1] = from_f32<T>(o[k + u][j][i + 2] * inv);
+        }
+        if (d0 + 2 * k < D) store8(dst + 2 * k, v, 8, p.wide_o);
+      }
+    }
+}
+
+// Joins the parts of one query row: a warp each.
+template <typename T>
+__global__ void __launch_bounds__(256) pq_kv8_join(const __grid_constant__ AttnArgs p, int tile_rows) {
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  const int hq = static_cast<int>(at % p.a.Hq);
+  const int64_t rest = at / p.a.Hq;
+  const int qi = static_cast<int>(rest % p.a.max_q);
+  const int64_t b = rest / p.a.max_q;
+  wait_previous_kernel();
+  if (b >= p.a.B) return;
+  const int r = qi * p.group + hq % p.group;
+  const Span sp = span_of(p, static_cast<int>(b), r / tile_rows * tile_rows, tile_rows);
+  if (qi >= sp.n) return;
+  // the parts that the row's tile was cut into (at least the first is there)
+  const int first = sp.lo & ~15;
+  const int parts = max(1, min(p.splits, (sp.hi - first + p.chunk - 1) / p.chunk));
+  const float2* ml = p.ml + at * p.splits;
+  float top = kNone;
+  for (int s = 0; s < parts; ++s) top = fmaxf(top, ml[s].x);
+  const float base = top == kNone ? 0.0f : top;
+  float l = 0.0f, o[8] = {};
+  for (int s = 0; s < parts; ++s) {
+    const float2 v = ml[s];
+    const float f = exp2_approx(v.x - base);
+    l += v.y * f;
+    const float* src = p.part + (at * p.splits + s) * p.c.D;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      if (lane + 32 * k < p.c.D) o[k] += src[lane + 32 * k] * f;
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  T* dst = static_cast<T*>(p.o) + (static_cast<int64_t>(p.a.cu_q_dev[b]) + qi) * p.a.o_token_stride +
+           static_cast<int64_t>(hq) * p.a.o_head_stride;
+#pragma unroll
+  for (int k = 0; k < 8; ++k)
+    if (lane + 32 * k < p.c.D) dst[lane + 32 * k] = from_f32<T>(o[k] * inv);
+}
+
+// ---------------------------------------------------------------------- host
+int sm_count() {
+  int dev = 0, sms = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    sms = 0;
+  return sms > 0 ? sms : 152;
+}
+
+int padded_d(int D) { return D <= 64 ? 64 : D <= 128 ? 128 : 256; }
+
+// Tiles of 8 query rows of one block: two where there are more than 8 rows and the
+// outputs of 16 fit the registers.
+int row_tiles_of_block(const pq_kv8_cache* c, const pq_kv8_attn* a) {
+  const int64_t rows = static_cast<int64_t>(a->max_q) * (a->Hq / c->Hkv);
+  return rows <= 8 || padded_d(c->D) == 256 ? 1 : 2;
+}
+
+bool valid_attn(const pq_kv8_cache* c, const pq_kv8_attn* a) {
+  if (!valid_kv8_cache(c) || a == nullptr) return false;
+  if (a->type != PQ_F32 && a->type != PQ_F16 && a->type != PQ_BF16) return false;
+  if (a->B < 0 || a->max_q < 0 || a->max_len < 0 || a->table_pitch < 0 || a->window < 0) return false;
+  if (a->Hq < 1 || a->Hq % c->Hkv != 0 || a->Hq / c->Hkv > 64) return false;
+  if ((a->causal != 0 && a->causal != 1) || (a->causal == 0 && a->window != 0)) return false;
+  if (a->q_token_stride < 0 || a->q_head_stride < 0 || a->o_token_stride < 0 || a->o_head_stride < 0) return false;
+  return !(a->scale != a->scale);
+}
+
+// Parts of the token range: enough blocks to fill the chip four times over where
+// there are few rows, none shorter than 256 tokens (two steps of every warp).
+void plan_split(const pq_kv8_cache* c, const pq_kv8_attn* a, AttnArgs* p) {
+  const int rows = 8 * row_tiles_of_block(c, a);
+  p->row_tiles = static_cast<int>((static_cast<int64_t>(a->max_q) * (a->Hq / c->Hkv) + rows - 1) / rows);
+  // tokens that one row tile can see, from a multiple of 16 on
+  int64_t range = a->max_len;
+  if (a->window > 0) range = std::min<int64_t>(range, static_cast<int64_t>(a->window) + rows + 15);
+  range = std::max<int64_t>(range, 1);
+  const int64_t units = static_cast<int64_t>(a->B) * c->Hkv * p->row_tiles;
+  const int64_t want = (4ll * sm_count() + units - 1) / units;
+  const int64_t most = (range + 255) / 256;
+  const int64_t splits = std::max<int64_t>(1, std::min(want, most));
+  const int64_t chunk = ((range + splits - 1) / splits + 127) / 128 * 128;
+  p->chunk = static_cast<int>(std::min<int64_t>(chunk, 0x7FFFFF80));
+  p->splits = static_cast<int>((range + chunk - 1) / chunk);
+}
+
+template <typename T, bool TWO>
+cudaError_t launch_rows(const AttnArgs& p, unsigned grid, int nt, cudaStream_t s) {
+  const int dp = padded_d(p.c.D);
+  if (dp == 64 && nt == 1)
+    pq_kv8_rows<T, 64, 1, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
+  else if (dp == 64)
+    pq_kv8_rows<T, 64, 2, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
+  else if (dp == 128 && nt == 1)
+    pq_kv8_rows<T, 128, 1, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
+  else if (dp == 128)
+    pq_kv8_rows<T, 128, 2, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
+  else
+    pq_kv8_rows<T, 256, 1, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
+  cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess || p.splits <= 1) return e;
+  const int64_t rows = static_cast<int64_t>(p.a.B) * p.a.max_q * p.a.Hq;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>((rows + 7) / 8));
+  cfg.blockDim = dim3(256);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, pq_kv8_join<T>, p, 8 * nt);
+}
+
+size_t scratch_of(const AttnArgs& p) {
+  if (p.splits <= 1) return 0;
+  const size_t parts = static_cast<size_t>(p.a.B) * p.a.max_q * p.a.Hq * p.splits;
+  return parts * sizeof(float2) + parts * p.c.D * sizeof(float);
+}
+
+}  // namespace
+}  // namespace pq
+
+extern "C" {
+
+size_t palquant_kv8_attention_scratch_bytes(const pq_kv8_cache* cache, const pq_kv8_attn* a) {
+  if (!pq::valid_attn(cache, a) || a->B == 0 || a->max_q == 0) return 0;
+  pq::AttnArgs p = {};
+  p.c = *cache;
+  p.a = *a;
+  pq::plan_split(cache, a, &p);
+  return pq::scratch_of(p);
+}
+
+pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, void* o_dev, const pq_kv8_attn* a,
+                                 void* scratch_dev, size_t scratch_bytes, pq_stream_t stream) {
+  if (!pq::valid_attn(cache, a)) return PQ_EINVAL;
+  if (a->B == 0 || a->max_q == 0) return PQ_OK;
+  const size_t e = pq::bytes_of_type(a->type);
+  if (q_dev == nullptr || o_dev == nullptr || a->cu_q_dev == nullptr || a->len_dev == nullptr ||
+      (a->page_table_dev == nullptr && a->max_len > 0) || !pq::is_aligned(q_dev, e) || !pq::is_aligned(o_dev, e) ||
+      !pq::is_aligned(a->cu_q_dev, 4) || !pq::is_aligned(a->len_dev, 4) || !pq::is_aligned(a->page_table_dev, 4))
+    return PQ_EINVAL;
+  pq::AttnArgs p = {};
+  p.c = *cache;
+  p.a = *a;
+  p.q = q_dev;
+  p.o = o_dev;
+  p.group = a->Hq / cache->Hkv;
+  p.page_shift = cache->page_tokens == 16 ? 4 : cache->page_tokens == 32 ? 5 : cache->page_tokens == 64 ? 6 : 7;
+  p.wide_q = pq::is_aligned(q_dev, 16) && a->q_token_stride * e % 16 == 0 && a->q_head_stride * e % 16 == 0;
+  p.wide_o = pq::is_aligned(o_dev, 16) && a->o_token_stride * e % 16 == 0 && a->o_head_stride * e % 16 == 0;
+  pq::plan_split(cache, a, &p);
+  const size_t need = pq::scratch_of(p);
+  if (need > 0 && (scratch_dev == nullptr || scratch_bytes < need || !pq::is_aligned(scratch_dev, 16))) return PQ_EINVAL;
+  if (p.splits > 1) {
+    const size_t parts = static_cast<size_t>(a->B) * a->max_q * a->Hq * p.splits;
+    p.ml = static_cast<float2*>(scratch_dev);
+    p.part = reinterpret_cast<float*>(p.ml + parts);
+  }
+  const int64_t units = static_cast<int64_t>(p.row_tiles) * p.splits * cache->Hkv;
+  if (units > 0x7FFFFFFFll / a->B || static_cast<int64_t>(a->max_q) * a->Hq > (0x7FFFFFFFll * 8) / a->B)
+    return PQ_EUNSUPPORTED;
+  const unsigned grid = static_cast<unsigned>(units * a->B);
+  p.err = pq::device_error_word();
+  if (p.err == nullptr) return PQ_ECUDA;
+  const int nt = pq::row_tiles_of_block(cache, a);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t st;
+  if (a->type == PQ_F32)
+    st = pq::launch_rows<float, true>(p, grid, nt, s);
+  else if (a->type == PQ_F16)
+    st = pq::launch_rows<__half, false>(p, grid, nt, s);
+  else
+    st = pq::launch_rows<__nv_bfloat16, false>(p, grid, nt, s);
+  return st == cudaSuccess && cudaGetLastError() == cudaSuccess ? PQ_OK : PQ_ECUDA;
+}
+
+}  // extern "C"

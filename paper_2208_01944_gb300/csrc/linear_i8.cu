@@ -1,0 +1,364 @@
+// Dense layers on signed 8-bit codes, y = (q W^T) s_x s_w + bias, and the token
+// quantiser before them.
+//
+// pq_quantize_tokens: one block per token; the token stays in registers between
+// the search for its largest magnitude and the rounding (one read of x, one write
+// of the codes; HBM-bound).
+//
+// pq_linear_rows: any size, any alignment; the kernel of few tokens, where the
+// weights' bytes are what counts.  mma.sync on 8-bit integers runs at 158 TOPS on
+// this chip, far below the half-precision rate, and 8-bit codes are exact half
+// values, so the codes are turned into halves in registers (1.25 instructions a
+// code) and multiplied with fp32 sums.  Those are exact as long as they stay below 2^24:
+// 127 * 128 * 1024 = 16646144 < 2^24, so every warp adds its fp32 sums to int32
+// ones after at most 1024 of K.  The weights are the 16-row operand of the MMA and
+// the tokens its 8 columns, so few tokens waste little.  The warps of a block share
+// 16 output channels and take turns along K, each lane reading 16 contiguous
+// bytes; within a 64-wide step the order of K is the lanes' own, the same for both
+// operands.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+
+#include "palquant.h"
+#include "pq_internal.h"
+#include "pq_tokens.cuh"
+
+namespace pq {
+namespace {
+
+constexpr int kTokThreads = 256;
+
+// NV: vectors of 8 elements that a thread keeps; 0: the token is read twice.
+template <typename T, bool HALF, int NV>
+__global__ void __launch_bounds__(kTokThreads) pq_quantize_tokens(const T* __restrict__ x, int64_t ldx, int K,
+                                                                  void* __restrict__ q, int64_t ldq,
+                                                                  float* __restrict__ s, bool wide_x, bool wide_q) {
+  __shared__ uint32_t red[8];
+  const int64_t m = blockIdx.x;
+  const T* row = x + m * ldx;
+  const int nvec = (K + 7) / 8;
+  let_next_kernel_start();
+  Vec8<T> keep[NV > 0 ? NV : 1];
+  uint32_t top = 0;
+  if (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = threadIdx.x + i * blockDim.x;
+      if (v < nvec) {
+        keep[i] = load8(row + 8 * v, K - 8 * v, wide_x && 8 * v + 8 <= K);
+        top = max(top, amax8(keep[i]));
+      }
+    }
+  } else {
+    for (int v = threadIdx.x; v < nvec; v += blockDim.x)
+      top = max(top, amax8(load8(row + 8 * v, K - 8 * v, wide_x && 8 * v + 8 <= K)));
+  }
+  top = block_max(top, red);
+  const float scale = scale_of_amax(top), inv = inverse_of_scale(scale);
+  if (threadIdx.x == 0) s[m] = scale;
+  auto put = [&](int v, const Vec8<T>& r) {
+    const int left = K - 8 * v;
+    const bool wide = wide_q && left >= 8;
+    if (HALF) {
+      Vec8<__half> h;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) h.v[i] = __int2half_rn(code_of(to_f32(r.v[i]), inv));
+      store8(static_cast<__half*>(q) + m * ldq + 8 * v, h, left, wide);
+    } else {
+      const uint2 c = codes8(r, inv);
+      int8_t* dst = static_cast<int8_t*>(q) + m * ldq + 8 * v;
+      if (wide) {
+        *reinterpret_cast<uint2*>(dst) = c;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if (i < left) dst[i] = static_cast<int8_t>((i < 4 ? c.x : c.y) >> (8 * (i & 3)));
+      }
+    }
+  };
+  if (NV > 0) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int v = threadIdx.x + i * blockDim.x;
+      if (v < nvec) put(v, keep[i]);
+    }
+  } else {
+    for (int v = threadIdx.x; v < nvec; v += blockDim.x)
+      put(v, load8(row + 8 * v, K - 8 * v, wide_x && 8 * v + 8 <= K));
+  }
+}
+
+template <typename T, bool HALF>
+cudaError_t launch_tokens(const void* x, int64_t ldx, int64_t M, int K, void* q, int64_t ldq, float* s,
+                          cudaStream_t stream) {
+  const bool wide_x = is_aligned(x, 16) && ldx * sizeof(T) % 16 == 0;
+  const size_t qe = HALF ? 2 : 1;
+  const bool wide_q = is_aligned(q, 8 * qe) && ldq % 8 == 0;
+  const int nvec = (K + 7) / 8;
+  const int threads = std::min(kTokThreads, (nvec + 31) / 32 * 32);
+  const int nv = (nvec + threads - 1) / threads;
+  const T* xt = static_cast<const T*>(x);
+  const unsigned grid = static_cast<unsigned>(M);
+  if (nv <= 1)
+    pq_quantize_tokens<T, HALF, 1><<<grid, threads, 0, stream>>>(xt, ldx, K, q, ldq, s, wide_x, wide_q);
+  else if (nv <= 2)
+    pq_quantize_tokens<T, HALF, 2><<<grid, threads, 0, stream>>>(xt, ldx, K, q, ldq, s, wide_x, wide_q);
+  else if (nv <= 4)
+    pq_quantize_tokens<T, HALF, 4><<<grid, threads, 0, stream>>>(xt, ldx, K, q, ldq, s, wide_x, wide_q);
+  else if (nv <= 8)
+    pq_quantize_tokens<T, HALF, 8><<<grid, threads, 0, stream>>>(xt, ldx, K, q, ldq, s, wide_x, wide_q);
+  else
+    pq_quantize_tokens<T, HALF, 0><<<grid, threads, 0, stream>>>(xt, ldx, K, q, ldq, s, wide_x, wide_q);
+  return cudaGetLastError();
+}
+
+// ------------------------------------------------------------------ products
+struct LinearArgs {
+  const void* q;
+  int64_t ldq;
+  const float* s_x;
+  const int8_t* w;
+  int64_t ldw;
+  const float* s_w;
+  const float* bias;
+  int32_t* acc;
+  void* y;
+  int64_t ldy;
+  int64_t M;
+  int N, K;
+  int y_type;
+};
+
+__device__ __forceinline__ void put_result(const LinearArgs& a, int64_t m, int n, int acc) {
+  if (a.acc != nullptr) a.acc[m * a.N + n] = acc;
+  if (a.y == nullptr) return;
+  float y = __fmul_rn(__fmul_rn(__int2float_rn(acc), a.s_x[m]), a.s_w[n]);
+  if (a.bias != nullptr) y = __fadd_rn(y, a.bias[n]);
+  const int64_t at = m * a.ldy + n;
+  if (a.y_type == PQ_F32)
+    static_cast<float*>(a.y)[at] = y;
+  else if (a.y_type == PQ_F16)
+    static_cast<__half*>(a.y)[at] = __float2half_rn(y);
+  else
+    static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(y);
+}
+
+// 16 codes of a row from column k on as bytes, zeros past K.
+template <bool WIDE>
+__device__ __forceinline__ uint4 codes16(const int8_t* row, int k, int K) {
+  if (WIDE && k + 16 <= K) return *reinterpret_cast<const uint4*>(row + k);
+  uint32_t w[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (k + i < K) w[i >> 2] |= static_cast<uint32_t>(static_cast<uint8_t>(row[k + i])) << (8 * (i & 3));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// The same 16 columns as halves, from bytes or from halves.
+template <bool HALF, bool WIDE>
+__device__ __forceinline__ void half16(const void* q, int64_t row, int k, int K, uint32_t (&r)[8]) {
+  if (HALF) {
+    const __half* p = static_cast<const __half*>(q) + row + k;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const Vec8<__half> v = load8(p + 8 * j, K - k - 8 * j, WIDE && k + 8 * j + 8 <= K);
+      const uint4 u = *reinterpret_cast<const uint4*>(&v);
+      r[4 * j] = u.x, r[4 * j + 1] = u.y, r[4 * j + 2] = u.z, r[4 * j + 3] = u.w;
+    }
+  } else {
+    const uint4 u = codes16<WIDE>(static_cast<const int8_t*>(q) + row, k, K);
+    half_of_codes(u.x, r[0], r[1]);
+    half_of_codes(u.y, r[2], r[3]);
+    half_of_codes(u.z, r[4], r[5]);
+    half_of_codes(u.w, r[6], r[7]);
+  }
+}
+
+constexpr int kRowWarps = 8;
+constexpr int kExactSteps = 16;  // 64-wide steps whose fp32 sums are exact
+
+// A block: 16 output channels x 8 NT tokens.
+template <int NT, bool HALF, bool WIDE>
+__global__ void __launch_bounds__(32 * kRowWarps) pq_linear_rows(const __grid_constant__ LinearArgs a) {
+  __shared__ int32_t part[kRowWarps][NT][8][17];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int n0 = blockIdx.x * 16;
+  const int64_t m0 = static_cast<int64_t>(blockIdx.y) * (8 * NT);
+  const int steps = (a.K + 63) / 64;
+  // rows past the end read the last row again; their sums are not stored
+  const int8_t* w0 = a.w + static_cast<int64_t>(min(n0 + g, a.N - 1)) * a.ldw;
+  const int8_t* w1 = a.w + static_cast<int64_t>(min(n0 + g + 8, a.N - 1)) * a.ldw;
+  int64_t tok[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) tok[j] = min(m0 + 8 * j + g, a.M - 1) * a.ldq;
+
+  int32_t sum[NT][4] = {};
+  wait_previous_kernel();
+  for (int s0 = warp; s0 < steps; s0 += kExactSteps * kRowWarps) {
+    float d[NT][4] = {};
+#pragma unroll 4
+    for (int i = 0; i < kExactSteps; ++i) {
+      const int s = s0 + i * kRowWarps;
+      if (s >= steps) break;
+      const int k = s * 64 + t * 16;
+      const uint4 u0 = codes16<WIDE>(w0, k, a.K), u1 = codes16<WIDE>(w1, k, a.K);
+      uint32_t b[NT][8];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) half16<HALF, WIDE>(a.q, tok[j], k, a.K, b[j]);
+      const uint32_t x0[4] = {u0.x, u0.y, u0.z, u0.w}, x1[4] = {u1.x, u1.y, u1.z, u1.w};
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t r0, r1, r2, r3;
+        half_of_codes(x0[c], r0, r2);
+        half_of_codes(x1[c], r1, r3);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) mma_16x8x16(d[j], r0, r1, r2, r3, b[j][2 * c], b[j][2 * c + 1]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum[j][e] += __float2int_rn(d[j][e]);
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) part[warp][j][2 * t + (e & 1)][g + 8 * (e >> 1)] = sum[j][e];
+  __syncthreads();
+  for (int e = threadIdx.x; e < NT * 128; e += 32 * kRowWarps) {
+    const int r = e & 15, c = (e >> 4) & 7, j = e >> 7;
+    const int n = n0 + r;
+    const int64_t m = m0 + 8 * j + c;
+    if (n >= a.N || m >= a.M) continue;
+    int32_t acc = 0;
+#pragma unroll
+    for (int w = 0; w < kRowWarps; ++w) acc += part[w][j][c][r];
+    put_result(a, m, n, acc);
+  }
+}
+
+template <int NT, bool HALF, bool WIDE>
+cudaError_t launch_rows_as(const LinearArgs& a, bool after_tokens, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>((a.N + 15) / 16), static_cast<unsigned>((a.M + 8 * NT - 1) / (8 * NT)));
+  cfg.blockDim = dim3(32 * kRowWarps);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = after_tokens ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, pq_linear_rows<NT, HALF, WIDE>, a);
+}
+
+template <bool HALF, bool WIDE>
+cudaError_t launch_rows(const LinearArgs& a, bool after_tokens, cudaStream_t stream) {
+  if (a.M <= 8) return launch_rows_as<1, HALF, WIDE>(a, after_tokens, stream);
+  if (a.M <= 16) return launch_rows_as<2, HALF, WIDE>(a, after_tokens, stream);
+  return launch_rows_as<4, HALF, WIDE>(a, after_tokens, stream);
+}
+
+bool valid_type(int32_t t) { return t == PQ_F32 || t == PQ_F16 || t == PQ_BF16; }
+
+bool valid_linear(const pq_linear_desc* d) {
+  return d != nullptr && d->M >= 0 && d->N >= 1 && d->K >= 1 && d->K <= 131072 && valid_type(d->x_type) &&
+         valid_type(d->y_type) && d->ldx >= d->K && d->ldw >= d->K && d->ldy >= d->N;
+}
+
+// The scratch: codes (rows padded to 16 elements), then scales.
+int64_t padded_k(const pq_linear_desc* d) { return (static_cast<int64_t>(d->K) + 15) / 16 * 16; }
+size_t code_bytes(const pq_linear_desc* d) {
+  const size_t e = palquant_linear_code_format(d) == PQ_CODES_F16 ? 2 : 1;
+  return static_cast<size_t>(d->M) * static_cast<size_t>(padded_k(d)) * e;
+}
+
+pq_status linear_codes(const void* q_dev, int32_t code_format, int64_t ldq, const float* s_x_dev, const int8_t* w_dev,
+                       const float* s_w_dev, const float* bias_dev, int32_t* acc_dev, void* y_dev,
+                       const pq_linear_desc* d, bool after_tokens, pq_stream_t stream) {
+  if (!valid_linear(d)) return PQ_EINVAL;
+  if (code_format != PQ_CODES_INT8 && code_format != PQ_CODES_F16) return PQ_EINVAL;
+  if (d->M == 0) return PQ_OK;
+  if (q_dev == nullptr || w_dev == nullptr || ldq < d->K || (acc_dev == nullptr && y_dev == nullptr)) return PQ_EINVAL;
+  if (y_dev != nullptr && (s_x_dev == nullptr || s_w_dev == nullptr)) return PQ_EINVAL;
+  if (!is_aligned(y_dev, bytes_of_type(d->y_type)) || !is_aligned(acc_dev, 4) || !is_aligned(s_x_dev, 4) ||
+      !is_aligned(s_w_dev, 4) || !is_aligned(bias_dev, 4) || (code_format == PQ_CODES_F16 && !is_aligned(q_dev, 2)))
+    return PQ_EINVAL;
+  if (d->M > 8ll * 65535 * 4) return PQ_EUNSUPPORTED;  // blocks along the grid's second axis
+  const LinearArgs a = {q_dev,   ldq,   s_x_dev, w_dev,  d->ldw, s_w_dev, bias_dev,
+                        acc_dev, y_dev, d->ldy,  d->M,   d->N,   d->K,    d->y_type};
+  const size_t qe = code_format == PQ_CODES_F16 ? 2 : 1;
+  const bool wide = is_aligned(q_dev, 16) && ldq * qe % 16 == 0 && is_aligned(w_dev, 16) && d->ldw % 16 == 0;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (code_format == PQ_CODES_F16)
+    e = wide ? launch_rows<true, true>(a, after_tokens, s) : launch_rows<true, false>(a, after_tokens, s);
+  else
+    e = wide ? launch_rows<false, true>(a, after_tokens, s) : launch_rows<false, false>(a, after_tokens, s);
+  return e == cudaSuccess && cudaGetLastError() == cudaSuccess ? PQ_OK : PQ_ECUDA;
+}
+
+}  // namespace
+}  // namespace pq
+
+extern "C" {
+
+pq_status palquant_quantize_tokens(const void* x_dev, int32_t x_type, int64_t ldx, int64_t M, int32_t K,
+                                   int32_t code_format, void* q_dev, int64_t ldq, float* s_dev, pq_stream_t stream) {
+  if (!pq::valid_type(x_type) || M < 0 || K < 1 || ldx < K || ldq < K) return PQ_EINVAL;
+  if (code_format != PQ_CODES_INT8 && code_format != PQ_CODES_F16) return PQ_EINVAL;
+  if (M == 0) return PQ_OK;
+  if (M > 0x7FFFFFFF) return PQ_EUNSUPPORTED;
+  const bool half = code_format == PQ_CODES_F16;
+  if (x_dev == nullptr || q_dev == nullptr || s_dev == nullptr || !pq::is_aligned(x_dev, pq::bytes_of_type(x_type)) ||
+      !pq::is_aligned(q_dev, half ? 2 : 1) || !pq::is_aligned(s_dev, 4))
+    return PQ_EINVAL;
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (x_type == PQ_F32)
+    e = half ? pq::launch_tokens<float, true>(x_dev, ldx, M, K, q_dev, ldq, s_dev, s)
+             : pq::launch_tokens<float, false>(x_dev, ldx, M, K, q_dev, ldq, s_dev, s);
+  else if (x_type == PQ_F16)
+    e = half ? pq::launch_tokens<__half, true>(x_dev, ldx, M, K, q_dev, ldq, s_dev, s)
+             : pq::launch_tokens<__half, false>(x_dev, ldx, M, K, q_dev, ldq, s_dev, s);
+  else
+    e = half ? pq::launch_tokens<__nv_bfloat16, true>(x_dev, ldx, M, K, q_dev, ldq, s_dev, s)
+             : pq::launch_tokens<__nv_bfloat16, false>(x_dev, ldx, M, K, q_dev, ldq, s_dev, s);
+  return e == cudaSuccess ? PQ_OK : PQ_ECUDA;
+}
+
+int32_t palquant_linear_code_format(const pq_linear_desc* d) {
+  (void)d;
+  return PQ_CODES_INT8;
+}
+
+pq_status palquant_linear_i8(const void* q_dev, int32_t code_format, int64_t ldq, const float* s_x_dev,
+                             const int8_t* w_dev, const float* s_w_dev, const float* bias_dev, int32_t* acc_dev,
+                             void* y_dev, const pq_linear_desc* d, pq_stream_t stream) {
+  return pq::linear_codes(q_dev, code_format, ldq, s_x_dev, w_dev, s_w_dev, bias_dev, acc_dev, y_dev, d, false, stream);
+}
+
+size_t palquant_linear_q8_scratch_bytes(const pq_linear_desc* d) {
+  if (!pq::valid_linear(d)) return 0;
+  return (pq::code_bytes(d) + 15) / 16 * 16 + static_cast<size_t>(d->M) * sizeof(float);
+}
+
+pq_status palquant_linear_q8(const void* x_dev, const int8_t* w_dev, const float* s_w_dev, const float* bias_dev,
+                             void* y_dev, const pq_linear_desc* d, void* scratch_dev, size_t scratch_bytes,
+                             pq_stream_t stream) {
+  if (!pq::valid_linear(d)) return PQ_EINVAL;
+  if (d->M == 0) return PQ_OK;
+  if (x_dev == nullptr || w_dev == nullptr || s_w_dev == nullptr || y_dev == nullptr || scratch_dev == nullptr ||
+      !pq::is_aligned(scratch_dev, 16) || scratch_bytes < palquant_linear_q8_scratch_bytes(d) ||
+      !pq::is_aligned(y_dev, pq::bytes_of_type(d->y_type)) || !pq::is_aligned(s_w_dev, 4) ||
+      !pq::is_aligned(bias_dev, 4))
+    return PQ_EINVAL;
+  const int32_t format = palquant_linear_code_format(d);
+  const int64_t ldq = pq::padded_k(d);
+  float* s_x = reinterpret_cast<float*>(static_cast<char*>(scratch_dev) + (pq::code_bytes(d) + 15) / 16 * 16);
+  const pq_status st = palquant_quantize_tokens(x_dev, d->x_type, d->ldx, d->M, d->K, format, scratch_dev, ldq, s_x, stream);
+  if (st != PQ_OK) return st;
+  return pq::linear_codes(scratch_dev, format, ldq, s_x, w_dev, s_w_dev, bias_dev, nullptr, y_dev, d, true, stream);
+}
+
+}  // extern "C"

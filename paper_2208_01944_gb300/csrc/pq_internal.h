@@ -13,6 +13,7 @@
 #define PQ_ERR_EPILOGUE 8u    // ... in the epilogue role
 #define PQ_ERR_TEARDOWN 16u   // ... while draining in-flight copies / MMAs
 #define PQ_ERR_SELFTEST 32u   // ... in the watchdog self-test kernel
+#define PQ_ERR_PAGE 64u       // a cache page out of range (skipped)
 
 namespace pq {
 
@@ -195,5 +196,6 @@ int launch_act_sum(const float* x, int64_t P, int G, int Cg, double* partial, in
 int launch_act_sum_finish(const double* partial, int nblocks, int G, double* sums, cudaStream_t stream);
 int launch_watchdog_selftest(unsigned int* err, uint64_t limit_ns, cudaStream_t stream);
 unsigned int* device_error_word();  // device address of the current device's error word
+uint64_t wait_limit_ns();           // limit of in-kernel waits (palquant_set_wait_limit_ns)
 
 }  // namespace pq
