@@ -15,6 +15,7 @@
 
 #include "palquant.h"
 #include "pq_internal.h"
+#include "pq_linear.h"
 
 using pq::ConvParams;
 
@@ -923,6 +924,16 @@ pq_status layer_fused_impl(const void* q_dev, const void* w_packed_dev, const pq
 
 namespace pq {
 uint64_t wait_limit_ns() { return g_wait_limit_ns.load(); }
+
+bool encode_map_2d(CUtensorMap* map, CUtensorMapDataType type, const void* base, uint64_t cols, uint64_t rows,
+                   uint64_t pitch_bytes, uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn enc = encode_fn();
+  if (enc == nullptr) return false;
+  const cuuint64_t dims[2] = {cols, rows}, pitch[1] = {pitch_bytes};
+  const cuuint32_t box[2] = {box_cols, box_rows}, step[2] = {1, 1};
+  return enc(map, type, 2, const_cast<void*>(base), dims, pitch, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 }  // namespace pq
 
 // ===========================================================================

@@ -22,6 +22,7 @@
 
 #include "palquant.h"
 #include "pq_internal.h"
+#include "pq_linear.h"
 #include "pq_tokens.cuh"
 
 namespace pq {
@@ -114,36 +115,6 @@ cudaError_t launch_tokens(const void* x, int64_t ldx, int64_t M, int K, void* q,
 }
 
 // ------------------------------------------------------------------ products
-struct LinearArgs {
-  const void* q;
-  int64_t ldq;
-  const float* s_x;
-  const int8_t* w;
-  int64_t ldw;
-  const float* s_w;
-  const float* bias;
-  int32_t* acc;
-  void* y;
-  int64_t ldy;
-  int64_t M;
-  int N, K;
-  int y_type;
-};
-
-__device__ __forceinline__ void put_result(const LinearArgs& a, int64_t m, int n, int acc) {
-  if (a.acc != nullptr) a.acc[m * a.N + n] = acc;
-  if (a.y == nullptr) return;
-  float y = __fmul_rn(__fmul_rn(__int2float_rn(acc), a.s_x[m]), a.s_w[n]);
-  if (a.bias != nullptr) y = __fadd_rn(y, a.bias[n]);
-  const int64_t at = m * a.ldy + n;
-  if (a.y_type == PQ_F32)
-    static_cast<float*>(a.y)[at] = y;
-  else if (a.y_type == PQ_F16)
-    static_cast<__half*>(a.y)[at] = __float2half_rn(y);
-  else
-    static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(y);
-}
-
 // 16 codes of a row from column k on as bytes, zeros past K.
 template <bool WIDE>
 __device__ __forceinline__ uint4 codes16(const int8_t* row, int k, int K) {
@@ -234,7 +205,7 @@ __global__ void __launch_bounds__(32 * kRowWarps) pq_linear_rows(const __grid_co
     int32_t acc = 0;
 #pragma unroll
     for (int w = 0; w < kRowWarps; ++w) acc += part[w][j][c][r];
-    put_result(a, m, n, acc);
+    put_result(a, m, n, acc, a.s_w != nullptr ? a.s_w[n] : 0.0f, a.bias != nullptr ? a.bias[n] : 0.0f);
   }
 }
 
@@ -284,14 +255,17 @@ pq_status linear_codes(const void* q_dev, int32_t code_format, int64_t ldq, cons
   if (!is_aligned(y_dev, bytes_of_type(d->y_type)) || !is_aligned(acc_dev, 4) || !is_aligned(s_x_dev, 4) ||
       !is_aligned(s_w_dev, 4) || !is_aligned(bias_dev, 4) || (code_format == PQ_CODES_F16 && !is_aligned(q_dev, 2)))
     return PQ_EINVAL;
-  if (d->M > 8ll * 65535 * 4) return PQ_EUNSUPPORTED;  // blocks along the grid's second axis
   const LinearArgs a = {q_dev,   ldq,   s_x_dev, w_dev,  d->ldw, s_w_dev, bias_dev,
                         acc_dev, y_dev, d->ldy,  d->M,   d->N,   d->K,    d->y_type};
   const size_t qe = code_format == PQ_CODES_F16 ? 2 : 1;
   const bool wide = is_aligned(q_dev, 16) && ldq * qe % 16 == 0 && is_aligned(w_dev, 16) && d->ldw % 16 == 0;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (code_format == PQ_CODES_F16)
+  if (!(code_format == PQ_CODES_F16 && linear_tc_takes(a)) && d->M > 32ll * 65535)
+    return PQ_EUNSUPPORTED;  // blocks along the grid's second axis
+  if (code_format == PQ_CODES_F16 && linear_tc_takes(a))
+    e = launch_linear_tc(a, after_tokens, s);
+  else if (code_format == PQ_CODES_F16)
     e = wide ? launch_rows<true, true>(a, after_tokens, s) : launch_rows<true, false>(a, after_tokens, s);
   else
     e = wide ? launch_rows<false, true>(a, after_tokens, s) : launch_rows<false, false>(a, after_tokens, s);
@@ -328,8 +302,7 @@ pq_status palquant_quantize_tokens(const void* x_dev, int32_t x_type, int64_t ld
 }
 
 int32_t palquant_linear_code_format(const pq_linear_desc* d) {
-  (void)d;
-  return PQ_CODES_INT8;
+  return pq::valid_linear(d) && d->M > 16 ? PQ_CODES_F16 : PQ_CODES_INT8;
 }
 
 pq_status palquant_linear_i8(const void* q_dev, int32_t code_format, int64_t ldq, const float* s_x_dev,
