@@ -4,24 +4,24 @@
 // tcgen05 kind (and mma.sync on 8-bit integers runs at 158 TOPS), but 8-bit codes
 // are exact half values: kind::f16 multiplies them exactly and its fp32 sums of
 // integers stay exact below 2^24, that is for 1024 of K (127 * 128 * 1024 < 2^24).  Every
-// 1024 of K the sums move from tensor memory into int32 registers.
+// 1024 of K the sums move from tensor memory into int32 registers; two accumulators
+// take turns, so that one is read while the other is written.
 //
-// Tile.  128 output channels (the MMA's rows) x BN tokens (its columns).  The weights stay
-// 8-bit in memory: four warps turn each 128 x 64 block into halves and put it into
-// tensor memory, from where the MMA takes its first operand, so the halves cost neither
-// memory traffic nor shared-memory bandwidth.  The tokens come as halves
+// Tile.  128 output channels (the MMA's rows) x BN tokens (its columns) a block.  The
+// weights stay 8-bit in memory: four warps turn each 128 x 64 block into halves and put
+// it into tensor memory, from where the MMA takes its first operand, so the halves cost
+// neither memory traffic nor shared-memory bandwidth.  The tokens come as halves
 // (PQ_CODES_F16, written by the token quantiser) by TMA, in the 128-byte swizzle that
-// the MMA reads.  Bound by the tensor rate for many tokens, by the weights' bytes for few.
+// the MMA reads.  With many tiles two blocks work as a pair (cta_group::2): 256 channels
+// x BN tokens, each block holding half of the tokens, so that an SM takes in
+// (8 + BN / 16) KB for each 64 of K instead of (8 + BN / 8).  Single blocks of 128 x 192 were bound by
+// that: 32 KB in every 384 cycles is more than the 64 bytes a cycle that L2 gives an SM.
+// Bound by the tensor rate for many tokens, by the weights' bytes for few.
 //
-// Drain.  Two accumulators take turns, so that one is read while the other is
-// written: with 256 tokens they are the tile's two halves, and the issue order runs two
-// K blocks of the first half, then the same two of the second, which leaves the
-// first half's drain the time of two K blocks; with fewer tokens they alternate
-// from one 1024-wide stretch (or tile) to the next.
-//
-// Roles (16 warps): 0 loads, 1 issues the MMAs, 4-7 convert, 8-15 drain and write.
-// Few tiles: the blocks of a cluster take parts of K of one tile and add their
-// int32 sums through distributed shared memory (in a fixed order; exact anyway).
+// Roles (16 warps): 0 loads, 1 issues the MMAs (of the pair, in its first block), 4-7
+// convert, 8-15 drain and write.  Few tiles: the blocks of a cluster take parts of K of
+// one tile and add their int32 sums through distributed shared memory (in a fixed
+// order; exact anyway).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -38,29 +38,25 @@ constexpr int kTcThreads = 512;
 constexpr int kTcBK = 64;           // K of one stage: 64 bytes of a weight row, 128 of a token row
 constexpr int kTcExact = 16;        // stages whose fp32 sums are exact
 constexpr int kTcWBytes = 128 * kTcBK;
-constexpr int kTcMaxStages = 8;
+constexpr int kTcStages = 8;        // of the loads' ring
 
-struct TcShape {
-  int halves, nb, stages;  // accumulators of one tile, their columns, stages of the ring
-};
-__host__ __device__ constexpr TcShape tc_shape(int BN) {
-  return BN == 256 ? TcShape{2, 128, 5} : TcShape{1, BN, 8};
-}
-__host__ __device__ constexpr int tc_smem(int BN) {
-  return tc_shape(BN).stages * (kTcWBytes + BN * 128) + 1024 /* alignment */ + 512 /* barriers */;
+// Stages of converted weights in tensor memory, 32 columns each, beside two accumulators.
+__host__ __device__ constexpr int tc_a_stages(int BN) { return BN <= 128 ? 8 : 4; }
+__host__ __device__ constexpr int tc_tok_bytes(int BN, bool pair) { return (pair ? BN / 2 : BN) * 128; }
+__host__ __device__ constexpr int tc_smem(int BN, bool pair) {
+  return kTcStages * (kTcWBytes + tc_tok_bytes(BN, pair)) + 1024 /* alignment */ + 512 /* barriers */;
 }
 
-// Barriers, 8 bytes each: w_full, b_full, a_full, empty (a ring each), acc_full,
-// acc_empty (two each), done.
+// Barriers, 8 bytes each: loaded (a stage's bytes), full (its weights are halves too, in
+// both blocks of a pair), empty (a ring each), acc_full, acc_empty (two each), done.
 struct TcBars {
   uint32_t base;
-  __device__ uint32_t w_full(int s) const { return base + 8u * s; }
-  __device__ uint32_t b_full(int s) const { return base + 8u * (kTcMaxStages + s); }
-  __device__ uint32_t a_full(int s) const { return base + 8u * (2 * kTcMaxStages + s); }
-  __device__ uint32_t empty(int s) const { return base + 8u * (3 * kTcMaxStages + s); }
-  __device__ uint32_t acc_full(int i) const { return base + 8u * (4 * kTcMaxStages + i); }
-  __device__ uint32_t acc_empty(int i) const { return base + 8u * (4 * kTcMaxStages + 2 + i); }
-  __device__ uint32_t done() const { return base + 8u * (4 * kTcMaxStages + 4); }
+  __device__ uint32_t loaded(int s) const { return base + 8u * s; }
+  __device__ uint32_t full(int s) const { return base + 8u * (kTcStages + s); }
+  __device__ uint32_t empty(int s) const { return base + 8u * (2 * kTcStages + s); }
+  __device__ uint32_t acc_full(int i) const { return base + 8u * (3 * kTcStages + i); }
+  __device__ uint32_t acc_empty(int i) const { return base + 8u * (3 * kTcStages + 2 + i); }
+  __device__ uint32_t done() const { return base + 8u * (3 * kTcStages + 4); }
 };
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, int c0, int c1, uint32_t bar) {
@@ -77,21 +73,59 @@ __device__ __forceinline__ uint64_t sw128_desc(uint32_t addr) {
          (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
 }
 
-// Instruction descriptor of kind::f16: half operands, fp32 sums, K-major, M = 128.
-__host__ __device__ constexpr uint32_t idesc_f16_f32(int N) {
-  return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(128 >> 4) << 24);
+// Instruction descriptor of kind::f16: half operands, fp32 sums, K-major.
+__host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N) {
+  return (1u << 4) | (static_cast<uint32_t>(N >> 3) << 17) | (static_cast<uint32_t>(M >> 4) << 24);
 }
 
 // Four MMAs (64 of K) with the first operand in tensor memory; the whole warp calls, one lane issues.
+#define PQ_TC_MMA_X4(group)                                                                                            \
+  asm volatile(                                                                                                        \
+      "{\n.reg .pred p, q, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %10, 0;\nsetp.eq.b32 q, 0, 0;\n"            \
+      "@e tcgen05.mma.cta_group::" group ".kind::f16 [%0], [%1], %5, %9, p;\n"                                         \
+      "@e tcgen05.mma.cta_group::" group ".kind::f16 [%0], [%2], %6, %9, q;\n"                                         \
+      "@e tcgen05.mma.cta_group::" group ".kind::f16 [%0], [%3], %7, %9, q;\n"                                         \
+      "@e tcgen05.mma.cta_group::" group ".kind::f16 [%0], [%4], %8, %9, q;\n}" ::"r"(d),                              \
+      "r"(a), "r"(a + 8), "r"(a + 16), "r"(a + 24), "l"(b), "l"(b + 2), "l"(b + 4), "l"(b + 6), "r"(idesc),            \
+      "r"(accumulate)                                                                                                  \
+      : "memory")
+template <bool PAIR>
 __device__ __forceinline__ void tc_mma_f16_ts_x4(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n.reg .pred p, q, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %10, 0;\nsetp.eq.b32 q, 0, 0;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %5, %9, p;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%2], %6, %9, q;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%3], %7, %9, q;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%4], %8, %9, q;\n}" ::"r"(d),
-      "r"(a), "r"(a + 8), "r"(a + 16), "r"(a + 24), "l"(b), "l"(b + 2), "l"(b + 4), "l"(b + 6), "r"(idesc), "r"(accumulate)
-      : "memory");
+  if (PAIR)
+    PQ_TC_MMA_X4("2");
+  else
+    PQ_TC_MMA_X4("1");
+}
+#undef PQ_TC_MMA_X4
+
+// Arrive once the MMAs issued so far are done: here, or on the same barrier of both blocks of the pair.
+template <bool PAIR>
+__device__ __forceinline__ void tc_commit_group(uint32_t bar) {
+  if (PAIR)
+    asm volatile(
+        "{\n.reg .pred e;\nelect.sync _|e, 0xffffffff;\n"
+        "@e tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n}" ::"r"(bar),
+        "h"(static_cast<uint16_t>(3))
+        : "memory");
+  else
+    tc_commit_warp(bar);
+}
+
+template <bool PAIR>
+__device__ __forceinline__ void tmem_alloc_group(uint32_t dst_smem, uint32_t ncols) {
+  if (PAIR) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(dst_smem), "r"(ncols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  } else {
+    tmem_alloc(dst_smem, ncols);
+  }
+}
+template <bool PAIR>
+__device__ __forceinline__ void tmem_dealloc_group(uint32_t taddr, uint32_t ncols) {
+  if (PAIR)
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
+  else
+    tmem_dealloc(taddr, ncols);
 }
 
 // 32 columns of this warp's 32 tensor-memory lanes.
@@ -128,6 +162,15 @@ __device__ __forceinline__ int32_t load_of_peer(uint32_t addr, uint32_t rank) {
   return v;
 }
 
+// Arrive on a barrier of the pair's first block.  What it announces (tensor memory
+// written or read) is ordered by the tcgen05 fences around it; a release at cluster
+// scope would wait for this thread's stores to memory, and made a tile three times slower.
+__device__ __forceinline__ void arrive_at_first(uint32_t bar) {
+  uint32_t a;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(bar));
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(a) : "memory");
+}
+
 // Position in the ring.
 struct Ring {
   int s = 0;
@@ -137,47 +180,51 @@ struct Ring {
   }
 };
 
-// Tile t: channel tiles in bands of 16, the tokens' tiles along a band, so that the
-// tiles at work at one time share weights and tokens in L2.
-__device__ __forceinline__ void tile_origin(const LinearTc& p, int t, int BN, int* n0, int64_t* m0) {
-  const int band = t / (16 * p.m_tiles), in = t - band * 16 * p.m_tiles;
-  const int width = min(16, p.n_tiles - band * 16);
-  *n0 = (band * 16 + in % width) * 128;
+// Tile t: channel tiles in bands, the tokens' tiles along a band, so that the tiles
+// at work at one time share weights and tokens in L2.
+__device__ __forceinline__ void tile_origin(const LinearTc& p, int t, int channels, int BN, int* n0, int64_t* m0) {
+  const int high = 2048 / channels;  // channel tiles of a band
+  const int band = t / (high * p.m_tiles), in = t - band * high * p.m_tiles;
+  const int width = min(high, p.n_tiles - band * high);
+  *n0 = (band * high + in % width) * channels;
   *m0 = static_cast<int64_t>(in / width) * BN;
 }
 
-template <int BN>
+template <int BN, bool PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
     pq_linear_tc(const __grid_constant__ LinearTc p, const __grid_constant__ CUtensorMap map_w,
                  const __grid_constant__ CUtensorMap map_q) {
-  constexpr TcShape kS = tc_shape(BN);
-  constexpr int kCols = kS.nb / 2;  // columns of an accumulator that one of its two draining warps takes
-  constexpr uint32_t kABase = 256;  // first tensor-memory column of the weights' stages
-  static_assert(2 * kS.nb <= 256 && 256 + 32 * kS.stages <= 512, "tensor memory");
+  constexpr int kAStages = tc_a_stages(BN);
+  constexpr int kTok = tc_tok_bytes(BN, PAIR);
+  constexpr int kCols = BN / 2;           // columns of an accumulator that one of its two draining warps takes
+  constexpr uint32_t kABase = 2 * BN;     // first tensor-memory column of the weights' stages
+  constexpr int kChannels = PAIR ? 256 : 128;
+  static_assert(kABase + 32 * kAStages <= 512 && kTcStages % kAStages == 0, "tensor memory");
   extern __shared__ uint8_t raw[];
   __shared__ int abort_flag;
   __shared__ uint32_t tmem_base;
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
-  const uint32_t tok_base = smem, w_base = smem + kS.stages * BN * 128u;
-  const TcBars bars{w_base + kS.stages * kTcWBytes};
+  const uint32_t tok_base = smem, w_base = smem + kTcStages * kTok;
+  const TcBars bars{w_base + kTcStages * kTcWBytes};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = PAIR || p.k_parts > 1 ? static_cast<int>(cluster_rank()) : 0;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kS.stages; ++s) {
-      mbar_init(bars.w_full(s), 1);
-      mbar_init(bars.b_full(s), 1);
-      mbar_init(bars.a_full(s), 4);
+    for (int s = 0; s < kTcStages; ++s) {
+      mbar_init(bars.loaded(s), 1);
+      mbar_init(bars.full(s), PAIR ? 8 : 4);
       mbar_init(bars.empty(s), 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(bars.acc_full(i), 1);
-      mbar_init(bars.acc_empty(i), 8);
+      mbar_init(bars.acc_empty(i), PAIR ? 16 : 8);
     }
     mbar_init(bars.done(), 1);
     abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 1) tmem_alloc(smem_u32(&tmem_base), 512);
+  if (PAIR) cluster_sync();  // the other block arrives on these barriers
+  if (warp == 1) tmem_alloc_group<PAIR>(smem_u32(&tmem_base), 512);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -185,10 +232,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 
   // this block's part of K, in stages, and its tiles
   const int all = (p.a.K + kTcBK - 1) / kTcBK;
-  const int rank = p.k_parts > 1 ? static_cast<int>(cluster_rank()) : 0;
-  const int kb0 = static_cast<int>(static_cast<int64_t>(all) * rank / p.k_parts);
-  const int kbs = static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / p.k_parts) - kb0;
-  const int first_tile = blockIdx.x / p.k_parts, tile_step = gridDim.x / p.k_parts;
+  const int kb0 = PAIR ? 0 : static_cast<int>(static_cast<int64_t>(all) * rank / p.k_parts);
+  const int kbs = PAIR ? all : static_cast<int>(static_cast<int64_t>(all) * (rank + 1) / p.k_parts) - kb0;
+  const int share = PAIR ? 2 : p.k_parts;  // blocks of one tile
+  const int first_tile = blockIdx.x / share, tile_step = gridDim.x / share;
   const int tiles = p.n_tiles * p.m_tiles;
   WaitCtx ctx{&abort_flag, p.err, p.wait_limit_ns, PQ_ERR_PRODUCER};
 
@@ -197,79 +244,61 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     if (warp == 0 && lane == 0) {
       // ---- loads.  The weights do not depend on the kernel before this one.
       Ring r;
-      int issued = 0;
       int n0;
       int64_t m0;
-      tile_origin(p, first_tile, BN, &n0, &m0);
-      const int ahead = first_tile < tiles ? min(kS.stages, kbs) : 0;
+      tile_origin(p, first_tile, kChannels, BN, &n0, &m0);
+      const int ahead = first_tile < tiles ? min(kTcStages, kbs) : 0;
       auto load_w = [&](int s, int kb) {
-        mbar_arrive_expect_tx(bars.w_full(s), kTcWBytes);
-        tma_load_2d(w_base + s * kTcWBytes, &map_w, (kb0 + kb) * kTcBK, n0, bars.w_full(s));
+        mbar_arrive_expect_tx(bars.loaded(s), kTcWBytes + kTok);
+        tma_load_2d(w_base + s * kTcWBytes, &map_w, (kb0 + kb) * kTcBK, n0 + (PAIR ? 128 * rank : 0), bars.loaded(s));
       };
       for (int i = 0; i < ahead; ++i) load_w(i, i);
       wait_previous_kernel();
       bool ok = true;
-      int total = 0;
+      int issued = 0;
       for (int t = first_tile; ok && t < tiles; t += tile_step) {
-        tile_origin(p, t, BN, &n0, &m0);
-        for (int kb = 0; kb < kbs; ++kb, ++total) {
-          if (total >= kS.stages && !mbar_wait(bars.empty(r.s), r.phase ^ 1u, ctx)) {
+        tile_origin(p, t, kChannels, BN, &n0, &m0);
+        const int tok = static_cast<int>(m0) + (PAIR ? BN / 2 * rank : 0);
+        for (int kb = 0; kb < kbs; ++kb, ++issued) {
+          if (issued >= kTcStages && !mbar_wait(bars.empty(r.s), r.phase ^ 1u, ctx)) {
             ok = false;
             break;
           }
-          if (total >= ahead) load_w(r.s, kb);
-          mbar_arrive_expect_tx(bars.b_full(r.s), BN * 128);
-          tma_load_2d(tok_base + r.s * BN * 128, &map_q, (kb0 + kb) * kTcBK, static_cast<int>(m0), bars.b_full(r.s));
-          ++issued;
-          r.next(kS.stages);
+          if (issued >= ahead) load_w(r.s, kb);
+          tma_load_2d(tok_base + r.s * kTok, &map_q, (kb0 + kb) * kTcBK, tok, bars.loaded(r.s));
+          r.next(kTcStages);
         }
       }
-      // what was loaded last may still be on its way (all of `ahead` was issued)
-      const int w_issued = max(issued, ahead);
-      for (int k = max(0, w_issued - kS.stages); k < w_issued; ++k)
-        mbar_wait_drain(bars.w_full(k % kS.stages), (k / kS.stages) & 1, p.wait_limit_ns, p.err);
-      for (int k = max(0, issued - kS.stages); k < issued; ++k)
-        mbar_wait_drain(bars.b_full(k % kS.stages), (k / kS.stages) & 1, p.wait_limit_ns, p.err);
-    } else if (warp == 1) {
+      // what was loaded last may still be on its way
+      for (int k = max(0, issued - kTcStages); k < issued; ++k)
+        mbar_wait_drain(bars.loaded(k % kTcStages), (k / kTcStages) & 1, p.wait_limit_ns, p.err);
+    } else if (warp == 1 && (!PAIR || rank == 0)) {
       // ---- MMAs
       ctx.err_bits = PQ_ERR_MMA;
-      constexpr uint32_t idesc = idesc_f16_f32(kS.nb);
-      auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)); };
+      constexpr uint32_t idesc = idesc_f16_f32(kChannels, BN);
+      auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)) != 0; };
       Ring r;
       uint32_t stretch = 0;  // exact stretches of K so far, over all tiles
       bool ok = true;
       for (int t = first_tile; ok && t < tiles; t += tile_step) {
-        for (int c0 = 0; ok && c0 < kbs; c0 += kTcExact) {
+        for (int c0 = 0; ok && c0 < kbs; c0 += kTcExact, ++stretch) {
           const int c1 = min(kbs, c0 + kTcExact);
-          // times that this stretch's accumulators were used before
-          const uint32_t uses = kS.halves == 2 ? stretch : stretch >> 1;
-          for (int g0 = c0; ok && g0 < c1; g0 += 2) {
-            const int g1 = min(c1, g0 + 2);
-            const Ring start = r;
-#pragma unroll
-            for (int h = 0; h < kS.halves; ++h) {
-              const int buf = kS.halves == 2 ? h : stretch & 1;
-              Ring x = start;
-              for (int kb = g0; kb < g1; ++kb) {
-                if (kb == c0 && uses > 0) ok = ok && wait(bars.acc_empty(buf), (uses - 1) & 1);
-                if (h == 0) ok = ok && wait(bars.a_full(x.s), x.phase) && wait(bars.b_full(x.s), x.phase);
-                if (!ok) break;
-                tc_fence_after();
-                tc_mma_f16_ts_x4(tmem + buf * kS.nb, tmem + kABase + 32 * x.s,
-                                 sw128_desc(tok_base + x.s * BN * 128 + h * 128 * 128), idesc, kb != c0);
-                if (h == kS.halves - 1) tc_commit_warp(bars.empty(x.s));
-                x.next(kS.stages);
-              }
-              if (!ok) break;
-              if (g1 == c1) tc_commit_warp(bars.acc_full(buf));
-              r = x;
-            }
+          const uint32_t acc = stretch & 1, uses = stretch >> 1;
+          if (uses > 0) ok = wait(bars.acc_empty(acc), (uses - 1) & 1);
+          for (int kb = c0; ok && kb < c1; ++kb) {
+            ok = wait(bars.full(r.s), r.phase);
+            if (!ok) break;
+            tc_fence_after();
+            tc_mma_f16_ts_x4<PAIR>(tmem + acc * BN, tmem + kABase + 32 * (r.s % kAStages),
+                                   sw128_desc(tok_base + r.s * kTok), idesc, kb != c0);
+            tc_commit_group<PAIR>(bars.empty(r.s));
+            r.next(kTcStages);
           }
-          ++stretch;
+          if (ok) tc_commit_group<PAIR>(bars.acc_full(acc));
         }
       }
       // every MMA issued must be over before the tensor memory is given back
-      tc_commit_warp(bars.done());
+      tc_commit_group<PAIR>(bars.done());
       if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
       __syncwarp();
     }
@@ -277,31 +306,43 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     // ---- weights to halves: this thread's row of each block
     ctx.err_bits = PQ_ERR_EPILOGUE;
-    const int row = 32 * (warp - 4) + lane;
+    const int row = 32 * (warp & 3) + lane;
     const uint32_t swizzle = (row >> 1) & 3;
-    const uint32_t lanes = static_cast<uint32_t>(32 * (warp - 4)) << 16;
+    const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
     Ring r;
     bool ok = true;
+    int i = 0;
     for (int t = first_tile; ok && t < tiles; t += tile_step)
-      for (int kb = 0; kb < kbs; ++kb) {
-        ok = __all_sync(0xffffffffu, mbar_wait(bars.w_full(r.s), r.phase, ctx));
+      for (int kb = 0; kb < kbs; ++kb, ++i) {
+        // with fewer stages in tensor memory than in the ring: block i - kAStages must be over
+        if (kAStages < kTcStages && i >= kAStages) {
+          const int k = i - kAStages;
+          ok = mbar_wait(bars.empty(k % kTcStages), (k / kTcStages) & 1, ctx);
+        }
+        ok = __all_sync(0xffffffffu, ok && mbar_wait(bars.loaded(r.s), r.phase, ctx)) != 0;
         if (!ok) break;
         const uint32_t src = w_base + r.s * kTcWBytes + row * kTcBK;
         uint32_t h[32];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint4 v = lds128(src + ((i ^ swizzle) << 4));
-          half_of_codes(v.x, h[8 * i], h[8 * i + 1]);
-          half_of_codes(v.y, h[8 * i + 2], h[8 * i + 3]);
-          half_of_codes(v.z, h[8 * i + 4], h[8 * i + 5]);
-          half_of_codes(v.w, h[8 * i + 6], h[8 * i + 7]);
+        for (int c = 0; c < 4; ++c) {
+          const uint4 v = lds128(src + ((c ^ swizzle) << 4));
+          half_of_codes(v.x, h[8 * c], h[8 * c + 1]);
+          half_of_codes(v.y, h[8 * c + 2], h[8 * c + 3]);
+          half_of_codes(v.z, h[8 * c + 4], h[8 * c + 5]);
+          half_of_codes(v.w, h[8 * c + 6], h[8 * c + 7]);
         }
-        tmem_st32(tmem + lanes + kABase + 32 * r.s, h);
+        tc_fence_after();
+        tmem_st32(tmem + lanes + kABase + 32 * (r.s % kAStages), h);
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bars.a_full(r.s));
-        r.next(kS.stages);
+        if (lane == 0) {
+          if (PAIR)
+            arrive_at_first(bars.full(r.s));
+          else
+            mbar_arrive(bars.full(r.s));
+        }
+        r.next(kTcStages);
       }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
@@ -310,69 +351,62 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     const int quarter = warp & 3, side = (warp - 8) >> 2;
     const uint32_t from = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + side * kCols;
     wait_previous_kernel();  // the tokens' scales
-    int32_t sum[kS.halves][kCols];
+    int32_t sum[kCols];
     uint32_t stretch = 0;
     bool ok = true;
     for (int t = first_tile; ok && t < tiles; t += tile_step) {
 #pragma unroll
-      for (int h = 0; h < kS.halves; ++h)
+      for (int j = 0; j < kCols; ++j) sum[j] = 0;
+      for (int c0 = 0; ok && c0 < kbs; c0 += kTcExact, ++stretch) {
+        const uint32_t acc = stretch & 1;
+        ok = __all_sync(0xffffffffu, mbar_wait(bars.acc_full(acc), (stretch >> 1) & 1, ctx)) != 0;
+        if (!ok) break;
+        tc_fence_after();
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) sum[h][j] = 0;
-      for (int c0 = 0; ok && c0 < kbs; c0 += kTcExact) {
+        for (int j = 0; j < kCols; j += 16) {
+          uint32_t v[16];
+          tmem_ld16(from + acc * BN + j, v);
+          tmem_wait_ld();
 #pragma unroll
-        for (int h = 0; h < kS.halves; ++h) {
-          const int buf = kS.halves == 2 ? h : stretch & 1;
-          const uint32_t uses = kS.halves == 2 ? stretch : stretch >> 1;
-          ok = ok && __all_sync(0xffffffffu, mbar_wait(bars.acc_full(buf), uses & 1, ctx));
-          if (!ok) break;
-          tc_fence_after();
-#pragma unroll
-          for (int j = 0; j < kCols; j += 16) {
-            uint32_t v[16];
-            tmem_ld16(from + buf * kS.nb + j, v);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sum[h][j + i] += __float2int_rn(__uint_as_float(v[i]));
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bars.acc_empty(buf));
+          for (int i = 0; i < 16; ++i) sum[j + i] += __float2int_rn(__uint_as_float(v[i]));
         }
-        ++stretch;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR)
+            arrive_at_first(bars.acc_empty(acc));
+          else
+            mbar_arrive(bars.acc_empty(acc));
+        }
       }
       if (!ok) break;
-      if (p.k_parts > 1) {
+      if (!PAIR && p.k_parts > 1) {
         // the ring is idle: this block's only tile is over (the last accumulator was full)
-        if (BN <= 128) {
 #pragma unroll
-          for (int j = 0; j < kCols; ++j)
-            asm volatile("st.shared.s32 [%0], %1;" ::"r"(tok_base + ((side * kCols + j) * 128 + 32 * quarter + lane) * 4),
-                         "r"(sum[0][j])
-                         : "memory");
-        }
+        for (int j = 0; j < kCols; ++j)
+          asm volatile("st.shared.s32 [%0], %1;" ::"r"(tok_base + ((side * kCols + j) * 128 + 32 * quarter + lane) * 4),
+                       "r"(sum[j])
+                       : "memory");
         break;
       }
       int n0;
       int64_t m0;
-      tile_origin(p, t, BN, &n0, &m0);
-      const int n = n0 + 32 * quarter + lane;
+      tile_origin(p, t, kChannels, BN, &n0, &m0);
+      const int n = n0 + (PAIR ? 128 * rank : 0) + 32 * quarter + lane;
       if (n < p.a.N) {
         const float s_w = p.a.s_w != nullptr ? p.a.s_w[n] : 0.0f, bias = p.a.bias != nullptr ? p.a.bias[n] : 0.0f;
+        const int64_t m = m0 + side * kCols;
 #pragma unroll
-        for (int h = 0; h < kS.halves; ++h) {
-          const int64_t m = m0 + h * 128 + side * kCols;
-#pragma unroll
-          for (int j = 0; j < kCols; ++j)
-            if (m + j < p.a.M) put_result(p.a, m + j, n, sum[h][j], s_w, bias);
-        }
+        for (int j = 0; j < kCols; ++j)
+          if (m + j < p.a.M) put_result(p.a, m + j, n, sum[j], s_w, bias);
       }
     }
-    if (p.k_parts > 1) {
+    if (!PAIR && p.k_parts > 1) {
       // add the cluster's parts: every block writes a share of the tokens
       cluster_sync();
       int n0;
       int64_t m0;
-      tile_origin(p, first_tile, BN, &n0, &m0);
+      tile_origin(p, first_tile, kChannels, BN, &n0, &m0);
       const int c = threadIdx.x & 127, n = n0 + c;
       const int j0 = BN * rank / p.k_parts, j1 = BN * (rank + 1) / p.k_parts;
       if (ok && n < p.a.N) {
@@ -387,50 +421,59 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     }
   }
   // the blocks of a cluster leave together: their sums are read by the others
-  if (p.k_parts > 1 && warp < 8) {
+  if (!PAIR && p.k_parts > 1 && warp < 8) {
     cluster_sync();
     cluster_sync();
   }
   tc_fence_before();
   __syncthreads();
+  // a pair's MMAs work on both blocks' memory, and its barriers are arrived on from both
+  if (PAIR) cluster_sync();
   if (warp == 1) {
+    __syncwarp();
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc_group<PAIR>(tmem, 512);
   }
 }
 
-template <int BN>
-cudaError_t launch(const LinearTc& p, const CUtensorMap& w, const CUtensorMap& q, int grid, bool after_tokens,
+template <int BN, bool PAIR>
+cudaError_t launch(const LinearTc& p, const CUtensorMap& w, const CUtensorMap& q, int sms, bool after_tokens,
                    cudaStream_t stream) {
-  static int attr_set[64] = {0};
+  static int most[64] = {0};  // clusters of two that fit the device at one time
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  if (dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(pq_linear_tc<BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, tc_smem(BN));
-    if (e != cudaSuccess) return e;
-    if (dev < 64) attr_set[dev] = 1;
-  }
+  if (dev >= 64) return cudaErrorInvalidDevice;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
   cfg.blockDim = dim3(kTcThreads);
-  cfg.dynamicSmemBytes = tc_smem(BN);
+  cfg.dynamicSmemBytes = tc_smem(BN, PAIR);
   cfg.stream = stream;
   cudaLaunchAttribute attr[2];
-  int n = 0;
-  if (after_tokens) {
-    attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[n++].val.programmaticStreamSerializationAllowed = 1;
-  }
-  if (p.k_parts > 1) {
-    attr[n].id = cudaLaunchAttributeClusterDimension;
-    attr[n].val.clusterDim.x = static_cast<unsigned>(p.k_parts);
-    attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
-    ++n;
-  }
+  const int cluster = PAIR ? 2 : p.k_parts;
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = n;
-  return cudaLaunchKernelEx(&cfg, pq_linear_tc<BN>, p, w, q);
+  if (most[dev] == 0) {
+    e = cudaFuncSetAttribute(pq_linear_tc<BN, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, tc_smem(BN, PAIR));
+    if (e != cudaSuccess) return e;
+    int n = sms;
+    if (PAIR) {
+      cfg.gridDim = dim3(static_cast<unsigned>(sms / 2 * 2));
+      cfg.numAttrs = 1;
+      e = cudaOccupancyMaxActiveClusters(&n, pq_linear_tc<BN, PAIR>, &cfg);
+      if (e != cudaSuccess || n < 1) return e != cudaSuccess ? e : cudaErrorInvalidConfiguration;
+    }
+    most[dev] = n;
+  }
+  const int64_t tiles = static_cast<int64_t>(p.n_tiles) * p.m_tiles;
+  // a cluster that shares K has one tile; otherwise as many blocks as there are at one time take the tiles in turn
+  const int64_t at_once = p.k_parts > 1 ? tiles : std::min<int64_t>(tiles, most[dev]);
+  cfg.gridDim = dim3(static_cast<unsigned>(at_once * cluster));
+  cfg.numAttrs = after_tokens ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, pq_linear_tc<BN, PAIR>, p, w, q);
 }
 
 }  // namespace
@@ -449,29 +492,42 @@ cudaError_t launch_linear_tc(const LinearArgs& a, bool after_tokens, cudaStream_
   p.err = device_error_word();
   p.wait_limit_ns = wait_limit_ns();
   if (p.err == nullptr) return cudaErrorInitializationError;
-  p.n_tiles = (a.N + 127) / 128;
-  auto tiles_of = [&](int bn) { return static_cast<int64_t>(p.n_tiles) * ((a.M + bn - 1) / bn); };
-  auto cost = [&](int bn) { return (tiles_of(bn) + sms - 1) / sms * bn; };
-  // tokens of a tile: the fewest that hold all of them, beyond 128 what leaves the
-  // last round of tiles the fullest
-  const int bn = a.M <= 32 ? 32 : a.M <= 64 ? 64 : a.M <= 128 ? 128 : cost(128) < cost(256) ? 128 : 256;
-  p.m_tiles = static_cast<int>((a.M + bn - 1) / bn);
-  const int64_t tiles = tiles_of(bn);
-  if (tiles > 0x7FFFFFFF) return cudaErrorInvalidValue;
-  // parts of K: while the chip is less than half full and each part keeps 256 of K
+  // Tiles.  Up to 128 tokens: single blocks, one tile of tokens, the fewest columns
+  // that hold them.  More: the cheaper of single blocks of 128 tokens and pairs of 128,
+  // 160 or 192, by rounds of tiles x columns (a single block takes a quarter longer
+  // for a column).  Single blocks share K while the chip is less than half full and
+  // each part keeps 256 of K.
+  auto ceil_div = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+  int bn = a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
+  const int64_t singles = ceil_div(a.N, 128) * ceil_div(a.M, bn);
   p.k_parts = 1;
-  while (bn <= 128 && p.k_parts < 8 && tiles * p.k_parts * 2 <= sms && a.K / (p.k_parts * 2) >= 256) p.k_parts *= 2;
-  const int grid = p.k_parts > 1 ? static_cast<int>(tiles) * p.k_parts : static_cast<int>(std::min<int64_t>(tiles, sms));
+  while (p.k_parts < 8 && singles * p.k_parts * 2 <= sms && a.K / (p.k_parts * 2) >= 256) p.k_parts *= 2;
+  bool pair = false;
+  if (a.M > 128) {
+    double best = 1.25 * static_cast<double>(ceil_div(singles * p.k_parts, sms)) * bn / p.k_parts;
+    for (int c = 192; c >= 128; c -= 32) {
+      const double cost = static_cast<double>(ceil_div(ceil_div(a.N, 256) * ceil_div(a.M, c), std::max(1, sms / 2))) * c;
+      if (cost < best) best = cost, bn = c, pair = true;
+    }
+  }
+  if (pair) p.k_parts = 1;
+  p.n_tiles = static_cast<int>(ceil_div(a.N, pair ? 256 : 128));
+  const int64_t m_tiles = ceil_div(a.M, bn);
+  if (p.n_tiles * m_tiles > 0x7FFFFFFF) return cudaErrorInvalidValue;
+  p.m_tiles = static_cast<int>(m_tiles);
   CUtensorMap w, q;
   if (!encode_map_2d(&w, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.w, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.N),
                      static_cast<uint64_t>(a.ldw), kTcBK, 128, CU_TENSOR_MAP_SWIZZLE_64B) ||
       !encode_map_2d(&q, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a.q, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M),
-                     static_cast<uint64_t>(a.ldq) * 2, kTcBK, static_cast<uint32_t>(bn), CU_TENSOR_MAP_SWIZZLE_128B))
+                     static_cast<uint64_t>(a.ldq) * 2, kTcBK, static_cast<uint32_t>(pair ? bn / 2 : bn),
+                     CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorInvalidValue;
-  if (bn == 32) return launch<32>(p, w, q, grid, after_tokens, stream);
-  if (bn == 64) return launch<64>(p, w, q, grid, after_tokens, stream);
-  if (bn == 128) return launch<128>(p, w, q, grid, after_tokens, stream);
-  return launch<256>(p, w, q, grid, after_tokens, stream);
+  if (pair && bn == 192) return launch<192, true>(p, w, q, sms, after_tokens, stream);
+  if (pair && bn == 160) return launch<160, true>(p, w, q, sms, after_tokens, stream);
+  if (pair) return launch<128, true>(p, w, q, sms, after_tokens, stream);
+  if (bn == 32) return launch<32, false>(p, w, q, sms, after_tokens, stream);
+  if (bn == 64) return launch<64, false>(p, w, q, sms, after_tokens, stream);
+  return launch<128, false>(p, w, q, sms, after_tokens, stream);
 }
 
 }  // namespace pq
