@@ -18,10 +18,12 @@
 // that: 32 KB in every 384 cycles is more than the 64 bytes a cycle that L2 gives an SM.
 // Bound by the tensor rate for many tokens, by the weights' bytes for few.
 //
-// Roles (16 warps): 0 loads, 1 issues the MMAs (of the pair, in its first block), 4-7
-// convert, 8-15 drain and write.  Few tiles: the blocks of a cluster take parts of K of
-// one tile and add their int32 sums through distributed shared memory (in a fixed
-// order; exact anyway).
+// Roles (20 warps): 0 and 2 load (weights, tokens), 1 issues the MMAs (of the pair, in
+// its first block), 4-7 and 8-11 convert a half each of every stage, 12-19 drain and
+// write.  A stage is 128 of K: waiting for one and freeing it costs the issuing warp about
+// 130 cycles beside its MMAs, more than there are to spare with stages of 64.  Few
+// tiles: the blocks of a cluster take parts of K of one tile and add their int32 sums
+// through distributed shared memory (in a fixed order; exact anyway).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -34,29 +36,36 @@
 namespace pq {
 namespace {
 
-constexpr int kTcThreads = 512;
-constexpr int kTcBK = 64;           // K of one stage: 64 bytes of a weight row, 128 of a token row
-constexpr int kTcExact = 16;        // stages whose fp32 sums are exact
+constexpr int kTcThreads = 640;     // warpgroups: 0 loads and MMAs, 1 and 2 convert, 3 and 4 drain
+constexpr int kTcBK = 128;          // K of one stage: 128 bytes of a weight row, twice 128 of a token row
+constexpr int kTcExact = 8;         // stages whose fp32 sums are exact
 constexpr int kTcWBytes = 128 * kTcBK;
-constexpr int kTcStages = 8;        // of the loads' ring
+constexpr int kTcMaxStages = 8;
 
-// Stages of converted weights in tensor memory, 32 columns each, beside two accumulators.
-__host__ __device__ constexpr int tc_a_stages(int BN) { return BN <= 128 ? 8 : 4; }
-__host__ __device__ constexpr int tc_tok_bytes(int BN, bool pair) { return (pair ? BN / 2 : BN) * 128; }
-__host__ __device__ constexpr int tc_smem(int BN, bool pair) {
-  return kTcStages * (kTcWBytes + tc_tok_bytes(BN, pair)) + 1024 /* alignment */ + 512 /* barriers */;
+// Tokens' rows of a block, the bytes of its stage, and the stages that fit.
+__host__ __device__ constexpr int tc_rows(int BN, bool pair) { return pair ? BN / 2 : BN; }
+__host__ __device__ constexpr int tc_stage_bytes(int BN, bool pair) { return kTcWBytes + tc_rows(BN, pair) * 256; }
+__host__ __device__ constexpr int tc_stages(int BN, bool pair) {
+  return 204800 / tc_stage_bytes(BN, pair) < kTcMaxStages ? 204800 / tc_stage_bytes(BN, pair) : kTcMaxStages;
 }
+__host__ __device__ constexpr int tc_smem(int BN, bool pair) {
+  return tc_stages(BN, pair) * tc_stage_bytes(BN, pair) + 1024 /* alignment */ + 512 /* barriers */;
+}
+// Half stages of converted weights in tensor memory, 32 columns each, beside two accumulators.
+__host__ __device__ constexpr int tc_a_slots(int BN) { return BN <= 128 ? 8 : BN <= 160 ? 6 : 4; }
 
 // Barriers, 8 bytes each: loaded (a stage's bytes), full (its weights are halves too, in
-// both blocks of a pair), empty (a ring each), acc_full, acc_empty (two each), done.
+// both blocks of a pair), empty (a ring each), a_empty (a slot of converted weights is
+// free), acc_full, acc_empty (two each), done.
 struct TcBars {
   uint32_t base;
   __device__ uint32_t loaded(int s) const { return base + 8u * s; }
-  __device__ uint32_t full(int s) const { return base + 8u * (kTcStages + s); }
-  __device__ uint32_t empty(int s) const { return base + 8u * (2 * kTcStages + s); }
-  __device__ uint32_t acc_full(int i) const { return base + 8u * (3 * kTcStages + i); }
-  __device__ uint32_t acc_empty(int i) const { return base + 8u * (3 * kTcStages + 2 + i); }
-  __device__ uint32_t done() const { return base + 8u * (3 * kTcStages + 4); }
+  __device__ uint32_t full(int s) const { return base + 8u * (kTcMaxStages + s); }
+  __device__ uint32_t empty(int s) const { return base + 8u * (2 * kTcMaxStages + s); }
+  __device__ uint32_t a_empty(int s) const { return base + 8u * (3 * kTcMaxStages + s); }
+  __device__ uint32_t acc_full(int i) const { return base + 8u * (4 * kTcMaxStages + i); }
+  __device__ uint32_t acc_empty(int i) const { return base + 8u * (4 * kTcMaxStages + 2 + i); }
+  __device__ uint32_t done() const { return base + 8u * (4 * kTcMaxStages + 4); }
 };
 
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, int c0, int c1, uint32_t bar) {
@@ -180,6 +189,48 @@ struct Ring {
   }
 };
 
+// One channel's results of kCols tokens from m on: the warp's 32 lanes write 32
+// consecutive channels of one token at a time.  s_x: the tokens' scales in shared memory.
+template <int kCols, typename T>
+__device__ __forceinline__ void put_column_as(const LinearArgs& a, int64_t m, int n, const int32_t (&sum)[kCols],
+                                              const float* s_x) {
+  const float s_w = a.s_w[n], bias = a.bias != nullptr ? a.bias[n] : 0.0f;
+  const bool add = a.bias != nullptr;
+  const int left = static_cast<int>(min(static_cast<int64_t>(kCols), a.M - m));
+  T* y = static_cast<T*>(a.y) + m * a.ldy + n;
+  const float4* s4 = reinterpret_cast<const float4*>(s_x);
+#pragma unroll
+  for (int j = 0; j < kCols; j += 4) {
+    const float4 f = s4[j / 4];
+    float v[4] = {f.x, f.y, f.z, f.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = __fmul_rn(__fmul_rn(__int2float_rn(sum[j + i]), v[i]), s_w);
+      if (add) v[i] = __fadd_rn(v[i], bias);
+      if (j + i < left) *y = from_f32<T>(v[i]);
+      y += a.ldy;
+    }
+  }
+}
+
+template <int kCols>
+__device__ __forceinline__ void put_column(const LinearArgs& a, int64_t m, int n, const int32_t (&sum)[kCols],
+                                           const float* s_x) {
+  if (n >= a.N) return;
+  if (a.acc != nullptr) {
+#pragma unroll
+    for (int j = 0; j < kCols; ++j)
+      if (m + j < a.M) a.acc[(m + j) * a.N + n] = sum[j];
+  }
+  if (a.y == nullptr) return;
+  if (a.y_type == PQ_F32)
+    put_column_as<kCols, float>(a, m, n, sum, s_x);
+  else if (a.y_type == PQ_F16)
+    put_column_as<kCols, __half>(a, m, n, sum, s_x);
+  else
+    put_column_as<kCols, __nv_bfloat16>(a, m, n, sum, s_x);
+}
+
 // Tile t: channel tiles in bands, the tokens' tiles along a band, so that the tiles
 // at work at one time share weights and tokens in L2.
 __device__ __forceinline__ void tile_origin(const LinearTc& p, int t, int channels, int BN, int* n0, int64_t* m0) {
@@ -194,27 +245,31 @@ template <int BN, bool PAIR>
 __global__ void __launch_bounds__(kTcThreads, 1)
     pq_linear_tc(const __grid_constant__ LinearTc p, const __grid_constant__ CUtensorMap map_w,
                  const __grid_constant__ CUtensorMap map_q) {
-  constexpr int kAStages = tc_a_stages(BN);
-  constexpr int kTok = tc_tok_bytes(BN, PAIR);
+  constexpr int kStages = tc_stages(BN, PAIR);
+  constexpr int kSlots = tc_a_slots(BN);
+  constexpr int kTok = tc_rows(BN, PAIR) * 128;  // bytes of 64 of K of the block's tokens
   constexpr int kCols = BN / 2;           // columns of an accumulator that one of its two draining warps takes
+  constexpr int kStep = kCols % 32 == 0 ? 32 : 16;
   constexpr uint32_t kABase = 2 * BN;     // first tensor-memory column of the weights' stages
   constexpr int kChannels = PAIR ? 256 : 128;
-  static_assert(kABase + 32 * kAStages <= 512 && kTcStages % kAStages == 0, "tensor memory");
+  static_assert(kABase + 32 * kSlots <= 512 && kSlots <= kTcMaxStages && kStages >= 3, "memory");
   extern __shared__ uint8_t raw[];
   __shared__ int abort_flag;
   __shared__ uint32_t tmem_base;
+  __shared__ alignas(16) float scales[8][kCols];  // of each draining warp's tokens
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
-  const uint32_t tok_base = smem, w_base = smem + kTcStages * kTok;
-  const TcBars bars{w_base + kTcStages * kTcWBytes};
+  const uint32_t tok_base = smem, w_base = smem + kStages * 2 * kTok;
+  const TcBars bars{w_base + kStages * kTcWBytes};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR || p.k_parts > 1 ? static_cast<int>(cluster_rank()) : 0;
 
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kTcStages; ++s) {
-      mbar_init(bars.loaded(s), 1);
-      mbar_init(bars.full(s), PAIR ? 8 : 4);
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(bars.loaded(s), 2);
+      mbar_init(bars.full(s), PAIR ? 16 : 8);
       mbar_init(bars.empty(s), 1);
     }
+    for (int s = 0; s < kSlots; ++s) mbar_init(bars.a_empty(s), 1);
     for (int i = 0; i < 2; ++i) {
       mbar_init(bars.acc_full(i), 1);
       mbar_init(bars.acc_empty(i), PAIR ? 16 : 8);
@@ -241,43 +296,48 @@ __global__ void __launch_bounds__(kTcThreads, 1)
 
   if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 0 && lane == 0) {
-      // ---- loads.  The weights do not depend on the kernel before this one.
+    if ((warp == 0 || warp == 2) && lane == 0) {
+      // ---- loads: the weights (warp 0), which do not depend on the kernel before this
+      // one, and the tokens.  One thread for both took longer for a stage than its MMAs do.
+      const bool weights = warp == 0;
       Ring r;
-      int n0;
-      int64_t m0;
-      tile_origin(p, first_tile, kChannels, BN, &n0, &m0);
-      const int ahead = first_tile < tiles ? min(kTcStages, kbs) : 0;
-      auto load_w = [&](int s, int kb) {
-        mbar_arrive_expect_tx(bars.loaded(s), kTcWBytes + kTok);
-        tma_load_2d(w_base + s * kTcWBytes, &map_w, (kb0 + kb) * kTcBK, n0 + (PAIR ? 128 * rank : 0), bars.loaded(s));
-      };
-      for (int i = 0; i < ahead; ++i) load_w(i, i);
-      wait_previous_kernel();
       bool ok = true;
       int issued = 0;
+      if (!weights) wait_previous_kernel();
       for (int t = first_tile; ok && t < tiles; t += tile_step) {
+        int n0;
+        int64_t m0;
         tile_origin(p, t, kChannels, BN, &n0, &m0);
-        const int tok = static_cast<int>(m0) + (PAIR ? BN / 2 * rank : 0);
+        const int row = weights ? n0 + (PAIR ? 128 * rank : 0) : static_cast<int>(m0) + (PAIR ? BN / 2 * rank : 0);
         for (int kb = 0; kb < kbs; ++kb, ++issued) {
-          if (issued >= kTcStages && !mbar_wait(bars.empty(r.s), r.phase ^ 1u, ctx)) {
+          if (issued >= kStages && !mbar_wait(bars.empty(r.s), r.phase ^ 1u, ctx)) {
             ok = false;
             break;
           }
-          if (issued >= ahead) load_w(r.s, kb);
-          tma_load_2d(tok_base + r.s * kTok, &map_q, (kb0 + kb) * kTcBK, tok, bars.loaded(r.s));
-          r.next(kTcStages);
+          const uint32_t bar = bars.loaded(r.s);
+          const int k = (kb0 + kb) * kTcBK;
+          mbar_arrive_expect_tx(bar, weights ? kTcWBytes : 2 * kTok);
+          if (weights) {
+            tma_load_2d(w_base + r.s * kTcWBytes, &map_w, k, row, bar);
+          } else {
+            tma_load_2d(tok_base + r.s * 2 * kTok, &map_q, k, row, bar);
+            tma_load_2d(tok_base + r.s * 2 * kTok + kTok, &map_q, k + 64, row, bar);
+          }
+          r.next(kStages);
         }
       }
-      // what was loaded last may still be on its way
-      for (int k = max(0, issued - kTcStages); k < issued; ++k)
-        mbar_wait_drain(bars.loaded(k % kTcStages), (k / kTcStages) & 1, p.wait_limit_ns, p.err);
+      // What was loaded last may still be on its way.  After a wait that ran out, one of
+      // the two may have stopped short of the other, whose last stages then never fill:
+      // their own wait ends at its limit.
+      for (int k = max(0, issued - kStages); k < issued; ++k)
+        mbar_wait_drain(bars.loaded(k % kStages), (k / kStages) & 1, p.wait_limit_ns, p.err);
     } else if (warp == 1 && (!PAIR || rank == 0)) {
       // ---- MMAs
       ctx.err_bits = PQ_ERR_MMA;
       constexpr uint32_t idesc = idesc_f16_f32(kChannels, BN);
       auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)) != 0; };
       Ring r;
+      int slot = 0;
       uint32_t stretch = 0;  // exact stretches of K so far, over all tiles
       bool ok = true;
       for (int t = first_tile; ok && t < tiles; t += tile_step) {
@@ -289,10 +349,15 @@ __global__ void __launch_bounds__(kTcThreads, 1)
             ok = wait(bars.full(r.s), r.phase);
             if (!ok) break;
             tc_fence_after();
-            tc_mma_f16_ts_x4<PAIR>(tmem + acc * BN, tmem + kABase + 32 * (r.s % kAStages),
-                                   sw128_desc(tok_base + r.s * kTok), idesc, kb != c0);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              tc_mma_f16_ts_x4<PAIR>(tmem + acc * BN, tmem + kABase + 32 * slot,
+                                     sw128_desc(tok_base + (2 * r.s + h) * kTok), idesc, h > 0 || kb != c0);
+              tc_commit_group<PAIR>(bars.a_empty(slot));
+              if (++slot == kSlots) slot = 0;
+            }
             tc_commit_group<PAIR>(bars.empty(r.s));
-            r.next(kTcStages);
+            r.next(kStages);
           }
           if (ok) tc_commit_group<PAIR>(bars.acc_full(acc));
         }
@@ -302,59 +367,65 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
       __syncwarp();
     }
-  } else if (warp < 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-    // ---- weights to halves: this thread's row of each block
+  } else if (warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    // ---- weights to halves: this thread's row of every block, one half (64 of K) of it
     ctx.err_bits = PQ_ERR_EPILOGUE;
-    const int row = 32 * (warp & 3) + lane;
-    const uint32_t swizzle = (row >> 1) & 3;
-    const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
+    const int row = 32 * (warp & 3) + lane, half = (warp - 4) >> 2;
+    const uint32_t swizzle = row & 7;
+    const uint32_t to = tmem + kABase + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
+    const int total = first_tile < tiles ? ((tiles - first_tile - 1) / tile_step + 1) * kbs : 0;
     Ring r;
-    bool ok = true;
-    int i = 0;
-    for (int t = first_tile; ok && t < tiles; t += tile_step)
-      for (int kb = 0; kb < kbs; ++kb, ++i) {
-        // with fewer stages in tensor memory than in the ring: block i - kAStages must be over
-        if (kAStages < kTcStages && i >= kAStages) {
-          const int k = i - kAStages;
-          ok = mbar_wait(bars.empty(k % kTcStages), (k / kTcStages) & 1, ctx);
-        }
-        ok = __all_sync(0xffffffffu, ok && mbar_wait(bars.loaded(r.s), r.phase, ctx)) != 0;
-        if (!ok) break;
-        const uint32_t src = w_base + r.s * kTcWBytes + row * kTcBK;
-        uint32_t h[32];
+    int slot = half;
+    uint32_t round = 0;  // times that the slot was used before
+    for (int i = 0; i < total; ++i) {
+      if (!__all_sync(0xffffffffu, mbar_wait(bars.loaded(r.s), r.phase, ctx))) break;
+      const uint32_t src = w_base + r.s * kTcWBytes + row * kTcBK;
+      uint32_t h[32];
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint4 v = lds128(src + ((c ^ swizzle) << 4));
-          half_of_codes(v.x, h[8 * c], h[8 * c + 1]);
-          half_of_codes(v.y, h[8 * c + 2], h[8 * c + 3]);
-          half_of_codes(v.z, h[8 * c + 4], h[8 * c + 5]);
-          half_of_codes(v.w, h[8 * c + 6], h[8 * c + 7]);
-        }
-        tc_fence_after();
-        tmem_st32(tmem + lanes + kABase + 32 * (r.s % kAStages), h);
-        tmem_wait_st();
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) {
-          if (PAIR)
-            arrive_at_first(bars.full(r.s));
-          else
-            mbar_arrive(bars.full(r.s));
-        }
-        r.next(kTcStages);
+      for (int c = 0; c < 4; ++c) {
+        const uint4 v = lds128(src + (((4 * half + c) ^ swizzle) << 4));
+        half_of_codes(v.x, h[8 * c], h[8 * c + 1]);
+        half_of_codes(v.y, h[8 * c + 2], h[8 * c + 3]);
+        half_of_codes(v.z, h[8 * c + 4], h[8 * c + 5]);
+        half_of_codes(v.w, h[8 * c + 6], h[8 * c + 7]);
       }
+      if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(bars.a_empty(slot), (round - 1) & 1, ctx))) break;
+      tc_fence_after();
+      tmem_st32(to + 32 * slot, h);
+      tmem_wait_st();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (PAIR)
+          arrive_at_first(bars.full(r.s));
+        else
+          mbar_arrive(bars.full(r.s));
+      }
+      r.next(kStages);
+      slot += 2;
+      if (slot >= kSlots) slot = half, ++round;
+    }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
     // ---- sums and outputs: this thread's channel, half of each accumulator's tokens
     ctx.err_bits = PQ_ERR_EPILOGUE;
-    const int quarter = warp & 3, side = (warp - 8) >> 2;
+    const int quarter = warp & 3, side = (warp - 12) >> 2;
     const uint32_t from = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + side * kCols;
     wait_previous_kernel();  // the tokens' scales
     int32_t sum[kCols];
     uint32_t stretch = 0;
     bool ok = true;
     for (int t = first_tile; ok && t < tiles; t += tile_step) {
+      int n0;
+      int64_t m0;
+      tile_origin(p, t, kChannels, BN, &n0, &m0);
+      __syncwarp();
+      for (int j = lane; j < kCols; j += 32) {
+        const int64_t m = m0 + side * kCols + j;
+        scales[warp - 12][j] = p.a.s_x != nullptr && m < p.a.M ? p.a.s_x[m] : 0.0f;
+      }
+      __syncwarp();
 #pragma unroll
       for (int j = 0; j < kCols; ++j) sum[j] = 0;
       for (int c0 = 0; ok && c0 < kbs; c0 += kTcExact, ++stretch) {
@@ -363,12 +434,15 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         if (!ok) break;
         tc_fence_after();
 #pragma unroll
-        for (int j = 0; j < kCols; j += 16) {
-          uint32_t v[16];
-          tmem_ld16(from + acc * BN + j, v);
+        for (int j = 0; j < kCols; j += kStep) {
+          uint32_t v[kStep];
+          if constexpr (kStep == 32)
+            tmem_ld32(from + acc * BN + j, v);
+          else
+            tmem_ld16(from + acc * BN + j, v);
           tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 16; ++i) sum[j + i] += __float2int_rn(__uint_as_float(v[i]));
+          for (int i = 0; i < kStep; ++i) sum[j + i] += __float2int_rn(__uint_as_float(v[i]));
         }
         tc_fence_before();
         __syncwarp();
@@ -389,17 +463,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
                        : "memory");
         break;
       }
-      int n0;
-      int64_t m0;
-      tile_origin(p, t, kChannels, BN, &n0, &m0);
-      const int n = n0 + (PAIR ? 128 * rank : 0) + 32 * quarter + lane;
-      if (n < p.a.N) {
-        const float s_w = p.a.s_w != nullptr ? p.a.s_w[n] : 0.0f, bias = p.a.bias != nullptr ? p.a.bias[n] : 0.0f;
-        const int64_t m = m0 + side * kCols;
-#pragma unroll
-        for (int j = 0; j < kCols; ++j)
-          if (m + j < p.a.M) put_result(p.a, m + j, n, sum[j], s_w, bias);
-      }
+      put_column<kCols>(p.a, m0 + side * kCols, n0 + (PAIR ? 128 * rank : 0) + 32 * quarter + lane, sum, scales[warp - 12]);
     }
     if (!PAIR && p.k_parts > 1) {
       // add the cluster's parts: every block writes a share of the tokens
@@ -421,7 +485,7 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     }
   }
   // the blocks of a cluster leave together: their sums are read by the others
-  if (!PAIR && p.k_parts > 1 && warp < 8) {
+  if (!PAIR && p.k_parts > 1 && warp < 12) {
     cluster_sync();
     cluster_sync();
   }
@@ -494,9 +558,9 @@ cudaError_t launch_linear_tc(const LinearArgs& a, bool after_tokens, cudaStream_
   if (p.err == nullptr) return cudaErrorInitializationError;
   // Tiles.  Up to 128 tokens: single blocks, one tile of tokens, the fewest columns
   // that hold them.  More: the cheaper of single blocks of 128 tokens and pairs of 128,
-  // 160 or 192, by rounds of tiles x columns (a single block takes a quarter longer
-  // for a column).  Single blocks share K while the chip is less than half full and
-  // each part keeps 256 of K.
+  // 160 or 192, by rounds of tiles x the time of 64 of K, which was 384, 404 and 423 cycles for
+  // the pairs (about bn + 500 in units of 0.6 cycles).  Single blocks share K while the
+  // chip is less than half full and each part keeps 256 of K.
   auto ceil_div = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
   int bn = a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
   const int64_t singles = ceil_div(a.N, 128) * ceil_div(a.M, bn);
@@ -504,9 +568,10 @@ cudaError_t launch_linear_tc(const LinearArgs& a, bool after_tokens, cudaStream_
   while (p.k_parts < 8 && singles * p.k_parts * 2 <= sms && a.K / (p.k_parts * 2) >= 256) p.k_parts *= 2;
   bool pair = false;
   if (a.M > 128) {
-    double best = 1.25 * static_cast<double>(ceil_div(singles * p.k_parts, sms)) * bn / p.k_parts;
+    double best = static_cast<double>(ceil_div(singles * p.k_parts, sms)) * (bn + 500) / p.k_parts;
     for (int c = 192; c >= 128; c -= 32) {
-      const double cost = static_cast<double>(ceil_div(ceil_div(a.N, 256) * ceil_div(a.M, c), std::max(1, sms / 2))) * c;
+      const double cost =
+          static_cast<double>(ceil_div(ceil_div(a.N, 256) * ceil_div(a.M, c), std::max(1, sms / 2))) * (c + 500);
       if (cost < best) best = cost, bn = c, pair = true;
     }
   }
@@ -517,9 +582,9 @@ cudaError_t launch_linear_tc(const LinearArgs& a, bool after_tokens, cudaStream_
   p.m_tiles = static_cast<int>(m_tiles);
   CUtensorMap w, q;
   if (!encode_map_2d(&w, CU_TENSOR_MAP_DATA_TYPE_UINT8, a.w, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.N),
-                     static_cast<uint64_t>(a.ldw), kTcBK, 128, CU_TENSOR_MAP_SWIZZLE_64B) ||
+                     static_cast<uint64_t>(a.ldw), kTcBK, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
       !encode_map_2d(&q, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a.q, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M),
-                     static_cast<uint64_t>(a.ldq) * 2, kTcBK, static_cast<uint32_t>(pair ? bn / 2 : bn),
+                     static_cast<uint64_t>(a.ldq) * 2, 64, static_cast<uint32_t>(pair ? bn / 2 : bn),
                      CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorInvalidValue;
   if (pair && bn == 192) return launch<192, true>(p, w, q, sms, after_tokens, stream);
