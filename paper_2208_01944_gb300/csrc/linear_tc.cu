@@ -163,11 +163,14 @@ __device__ __forceinline__ uint32_t cluster_rank() {
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
 }
-__device__ __forceinline__ int32_t load_of_peer(uint32_t addr, uint32_t rank) {
+__device__ __forceinline__ int4 load_of_peer(uint32_t addr, uint32_t rank) {
   uint32_t a;
-  int32_t v;
+  int4 v;
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
-  asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(a) : "memory");
+  asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "r"(a)
+               : "memory");
   return v;
 }
 
@@ -466,20 +469,28 @@ __global__ void __launch_bounds__(kTcThreads, 1)
       put_column<kCols>(p.a, m0 + side * kCols, n0 + (PAIR ? 128 * rank : 0) + 32 * quarter + lane, sum, scales[warp - 12]);
     }
     if (!PAIR && p.k_parts > 1) {
-      // add the cluster's parts: every block writes a share of the tokens
+      // add the cluster's parts: every block writes a share of the tokens, a warp one
+      // token's 128 channels at a time, four a lane
       cluster_sync();
       int n0;
       int64_t m0;
       tile_origin(p, first_tile, kChannels, BN, &n0, &m0);
-      const int c = threadIdx.x & 127, n = n0 + c;
-      const int j0 = BN * rank / p.k_parts, j1 = BN * (rank + 1) / p.k_parts;
-      if (ok && n < p.a.N) {
-        const float s_w = p.a.s_w != nullptr ? p.a.s_w[n] : 0.0f, bias = p.a.bias != nullptr ? p.a.bias[n] : 0.0f;
-        for (int j = j0 + side; j < j1 && m0 + j < p.a.M; j += 2) {
-          int32_t acc = 0;
-          for (int b = 0; b < p.k_parts; ++b) acc += load_of_peer(tok_base + (j * 128 + c) * 4, b);
-          put_result(p.a, m0 + j, n, acc, s_w, bias);
+      const int j1 = BN * (rank + 1) / p.k_parts;
+#pragma unroll 4
+      for (int j = BN * rank / p.k_parts + warp - 12; j < j1; j += 8) {
+        if (!ok || m0 + j >= p.a.M) break;
+        const int n = n0 + 4 * lane;
+        int4 acc = make_int4(0, 0, 0, 0);
+        for (int b = 0; b < p.k_parts; ++b) {
+          const int4 v = load_of_peer(tok_base + (j * 128 + 4 * lane) * 4, b);
+          acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
         }
+        const int sums[4] = {acc.x, acc.y, acc.z, acc.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n + i < p.a.N)
+            put_result(p.a, m0 + j, n + i, sums[i], p.a.s_w != nullptr ? p.a.s_w[n + i] : 0.0f,
+                       p.a.bias != nullptr ? p.a.bias[n + i] : 0.0f);
       }
       cluster_sync();
     }
@@ -560,12 +571,13 @@ cudaError_t launch_linear_tc(const LinearArgs& a, bool after_tokens, cudaStream_
   // that hold them.  More: the cheaper of single blocks of 128 tokens and pairs of 128,
   // 160 or 192, by rounds of tiles x the time of 64 of K, which was 384, 404 and 423 cycles for
   // the pairs (about bn + 500 in units of 0.6 cycles).  Single blocks share K while the
-  // chip is less than half full and each part keeps 256 of K.
+  // chip is less than half full and each part keeps 256 of K; eight parts of 128 tokens
+  // take longer to add than they save (16 tiles of K = 8192: 22 us, four parts 15 us).
   auto ceil_div = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
   int bn = a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
   const int64_t singles = ceil_div(a.N, 128) * ceil_div(a.M, bn);
   p.k_parts = 1;
-  while (p.k_parts < 8 && singles * p.k_parts * 2 <= sms && a.K / (p.k_parts * 2) >= 256) p.k_parts *= 2;
+  while (p.k_parts < (bn < 128 ? 8 : 4) && singles * p.k_parts * 2 <= sms && a.K / (p.k_parts * 2) >= 256) p.k_parts *= 2;
   bool pair = false;
   if (a.M > 128) {
     double best = static_cast<double>(ceil_div(singles * p.k_parts, sms)) * (bn + 500) / p.k_parts;
