@@ -30,42 +30,14 @@
 
 #include "palquant.h"
 #include "pq_internal.h"
-#include "pq_kv8.h"
+#include "pq_kv8.cuh"
 #include "pq_tokens.cuh"
 
 namespace pq {
 namespace {
 
 constexpr int kAttnWarps = 8;
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kWShift = 8.0f;
-constexpr float kNone = -INFINITY;
-
-__device__ __forceinline__ float exp2_approx(float x) {
-  float r;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-  return r;
-}
-
-// Tokens that the query rows [r0, r0 + rows) of sequence b may see: [lo, hi).
-struct Span {
-  int n, len;  // queries and tokens of the sequence
-  int lo, hi;
-};
-
-__device__ __forceinline__ Span span_of(const AttnArgs& p, int b, int r0, int rows) {
-  Span s;
-  s.n = min(p.a.cu_q_dev[b + 1] - p.a.cu_q_dev[b], p.a.max_q);
-  s.len = max(0, min(p.a.len_dev[b], p.a.max_len));
-  s.lo = 0;
-  s.hi = s.len;
-  if (p.a.causal) {
-    const int last = min(s.n * p.group, r0 + rows) - 1;
-    s.hi = min(s.len, s.len - s.n + last / p.group + 1);
-    if (p.a.window > 0) s.lo = max(0, s.len - s.n + r0 / p.group + 1 - p.a.window);
-  }
-  return s;
-}
 
 // The block's share of the grid: the row tile changes fastest (its neighbours read
 // the same codes).
@@ -102,7 +74,7 @@ __global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_cons
   const Span sp = span_of(p, w.b, r0, kRows);
   const int rows = sp.n * p.group;
   if (r0 >= rows) return;
-  const int first = sp.lo & ~15;
+  const int first = sp.lo & ~(p.align - 1);
   const int from = first + w.split * p.chunk;
   const int to = min(sp.hi, from + p.chunk);
   if (w.split > 0 && from >= sp.hi) return;
@@ -394,7 +366,7 @@ __global__ void __launch_bounds__(256) pq_kv8_join(const __grid_constant__ AttnA
   const Span sp = span_of(p, static_cast<int>(b), r / tile_rows * tile_rows, tile_rows);
   if (qi >= sp.n) return;
   // the parts that the row's tile was cut into (at least the first is there)
-  const int first = sp.lo & ~15;
+  const int first = sp.lo & ~(p.align - 1);
   const int parts = max(1, min(p.splits, (sp.hi - first + p.chunk - 1) / p.chunk));
   const float2* ml = p.ml + at * p.splits;
   float top = kNone;
@@ -446,22 +418,47 @@ bool valid_attn(const pq_kv8_cache* c, const pq_kv8_attn* a) {
   return !(a->scale != a->scale);
 }
 
-// Parts of the token range: enough blocks to fill the chip four times over where
-// there are few rows, none shorter than 256 tokens (two steps of every warp).
-void plan_split(const pq_kv8_cache* c, const pq_kv8_attn* a, AttnArgs* p) {
-  const int rows = 8 * row_tiles_of_block(c, a);
-  p->row_tiles = static_cast<int>((static_cast<int64_t>(a->max_q) * (a->Hq / c->Hkv) + rows - 1) / rows);
-  // tokens that one row tile can see, from a multiple of 16 on
+// Which kernel, its row tiles, and the parts of the token range.  Few query rows are
+// spread over the chip by cutting the tokens: four blocks an SM of at least 256 tokens
+// (two steps of every warp), or, on the tensor cores, one block an SM of at least 512.
+struct Plan {
+  bool tc;
+  int rows;  // query rows of a tile
+};
+
+Plan plan_attention(const pq_kv8_cache* c, const pq_kv8_attn* a, AttnArgs* p) {
+  Plan plan;
+  plan.tc = attn_tc_takes(*c, *a);
+  plan.rows = plan.tc ? kAttnTcRows : 8 * row_tiles_of_block(c, a);
+  p->align = plan.tc ? kAttnTcTokens : 16;
+  p->row_tiles = static_cast<int>((static_cast<int64_t>(a->max_q) * (a->Hq / c->Hkv) + plan.rows - 1) / plan.rows);
+  // tokens that one row tile can see, from a multiple of `align` on
   int64_t range = a->max_len;
-  if (a->window > 0) range = std::min<int64_t>(range, static_cast<int64_t>(a->window) + rows + 15);
+  if (a->window > 0) range = std::min<int64_t>(range, static_cast<int64_t>(a->window) + plan.rows + p->align);
   range = std::max<int64_t>(range, 1);
   const int64_t units = static_cast<int64_t>(a->B) * c->Hkv * p->row_tiles;
-  const int64_t want = (4ll * sm_count() + units - 1) / units;
-  const int64_t most = (range + 255) / 256;
-  const int64_t splits = std::max<int64_t>(1, std::min(want, most));
+  const int64_t want = ((plan.tc ? 1 : 4) * static_cast<int64_t>(sm_count()) + units - 1) / units;
+  const int64_t least = plan.tc ? 512 : 256;
+  const int64_t splits = std::max<int64_t>(1, std::min(want, (range + least - 1) / least));
   const int64_t chunk = ((range + splits - 1) / splits + 127) / 128 * 128;
   p->chunk = static_cast<int>(std::min<int64_t>(chunk, 0x7FFFFF80));
   p->splits = static_cast<int>((range + chunk - 1) / chunk);
+  return plan;
+}
+
+template <typename T>
+cudaError_t launch_join(const AttnArgs& p, int tile_rows, cudaStream_t s) {
+  const int64_t rows = static_cast<int64_t>(p.a.B) * p.a.max_q * p.a.Hq;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>((rows + 7) / 8));
+  cfg.blockDim = dim3(256);
+  cfg.stream = s;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, pq_kv8_join<T>, p, tile_rows);
 }
 
 template <typename T, bool TWO>
@@ -477,19 +474,7 @@ cudaError_t launch_rows(const AttnArgs& p, unsigned grid, int nt, cudaStream_t s
     pq_kv8_rows<T, 128, 2, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
   else
     pq_kv8_rows<T, 256, 1, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
-  cudaError_t e = cudaGetLastError();
-  if (e != cudaSuccess || p.splits <= 1) return e;
-  const int64_t rows = static_cast<int64_t>(p.a.B) * p.a.max_q * p.a.Hq;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>((rows + 7) / 8));
-  cfg.blockDim = dim3(256);
-  cfg.stream = s;
-  cudaLaunchAttribute attr[1];
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, pq_kv8_join<T>, p, 8 * nt);
+  return cudaGetLastError();
 }
 
 size_t scratch_of(const AttnArgs& p) {
@@ -508,7 +493,7 @@ size_t palquant_kv8_attention_scratch_bytes(const pq_kv8_cache* cache, const pq_
   pq::AttnArgs p = {};
   p.c = *cache;
   p.a = *a;
-  pq::plan_split(cache, a, &p);
+  pq::plan_attention(cache, a, &p);
   return pq::scratch_of(p);
 }
 
@@ -530,7 +515,8 @@ pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, v
   p.page_shift = cache->page_tokens == 16 ? 4 : cache->page_tokens == 32 ? 5 : cache->page_tokens == 64 ? 6 : 7;
   p.wide_q = pq::is_aligned(q_dev, 16) && a->q_token_stride * e % 16 == 0 && a->q_head_stride * e % 16 == 0;
   p.wide_o = pq::is_aligned(o_dev, 16) && a->o_token_stride * e % 16 == 0 && a->o_head_stride * e % 16 == 0;
-  pq::plan_split(cache, a, &p);
+  const pq::Plan plan = pq::plan_attention(cache, a, &p);
+  p.wait_limit_ns = pq::wait_limit_ns();
   const size_t need = pq::scratch_of(p);
   if (need > 0 && (scratch_dev == nullptr || scratch_bytes < need || !pq::is_aligned(scratch_dev, 16))) return PQ_EINVAL;
   if (p.splits > 1) {
@@ -544,15 +530,24 @@ pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, v
   const unsigned grid = static_cast<unsigned>(units * a->B);
   p.err = pq::device_error_word();
   if (p.err == nullptr) return PQ_ECUDA;
-  const int nt = pq::row_tiles_of_block(cache, a);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t st;
-  if (a->type == PQ_F32)
-    st = pq::launch_rows<float, true>(p, grid, nt, s);
+  if (plan.tc)
+    st = pq::launch_attn_tc(p, grid, s);
+  else if (a->type == PQ_F32)
+    st = pq::launch_rows<float, true>(p, grid, plan.rows / 8, s);
   else if (a->type == PQ_F16)
-    st = pq::launch_rows<__half, false>(p, grid, nt, s);
+    st = pq::launch_rows<__half, false>(p, grid, plan.rows / 8, s);
   else
-    st = pq::launch_rows<__nv_bfloat16, false>(p, grid, nt, s);
+    st = pq::launch_rows<__nv_bfloat16, false>(p, grid, plan.rows / 8, s);
+  if (st == cudaSuccess && p.splits > 1) {
+    if (a->type == PQ_F32)
+      st = pq::launch_join<float>(p, plan.rows, s);
+    else if (a->type == PQ_F16)
+      st = pq::launch_join<__half>(p, plan.rows, s);
+    else
+      st = pq::launch_join<__nv_bfloat16>(p, plan.rows, s);
+  }
   return st == cudaSuccess && cudaGetLastError() == cudaSuccess ? PQ_OK : PQ_ECUDA;
 }
 

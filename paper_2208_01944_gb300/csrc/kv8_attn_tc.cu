@@ -1,0 +1,485 @@
+// Attention over the paged 8-bit cache for many query rows (prompts, long chunks), on
+// the 5th-generation tensor cores.  The mathematics is that of pq_kv8_rows.
+//
+// Split.  A block takes one cache head and 256 query rows (queries x heads of the group)
+// as two tiles of 128, and walks through the tokens 128 at a time.  Each step's codes
+// are turned into halves once, for both tiles, on their way into shared memory.
+// Scores are 128 rows x 128 tokens in tensor memory, a row a thread, so the softmax needs
+// no exchange between threads; the probabilities go back over the scores as halves
+// and are the second product's first operand from there.  While one tile's softmax
+// runs, the tensor core works on the other tile: its issue order is
+//   P0 V(j), Q0 K(j+1), P1 V(j), Q1 K(j+1),
+// and one thread's MMAs run in order, so scores never overwrite probabilities in use.
+// The outputs stay in tensor memory; they are rescaled only when a row's maximum has grown
+// by more than 2^8 (w stays below 2^8, a half holds 2^16), which is rare.
+// Bound by the softmax's instructions and the tensor rate (512 cycles for each of
+// the four products of a step at D = 128).
+//
+// Roles (16 warps): 0 issues the MMAs, 4-7 convert, 8-11 and 12-15 are the tiles'
+// softmax.  Tiles with the most tokens come first.
+#include <cuda_runtime.h>
+
+#include "palquant.h"
+#include "pq_internal.h"
+#include "pq_kv8.cuh"
+#include "pq_tokens.cuh"
+
+namespace pq {
+namespace {
+
+constexpr int kTokens = kAttnTcTokens;  // of one step
+constexpr int kThreads = 512;
+constexpr int kSub = 128 * 128;         // 128 rows of 64 halves
+constexpr float kGrow = 8.0f;           // log2 by which a maximum may grow without a rescale
+constexpr int kPageRing = 4;            // steps whose scales are kept
+
+__host__ __device__ constexpr int attn_smem(int DP) { return 6 * (DP / 64) * kSub + 1024 /* alignment */; }
+
+struct AttnBars {
+  uint32_t base;
+  __device__ uint32_t q_full() const { return base; }
+  __device__ uint32_t done() const { return base + 8u; }
+  __device__ uint32_t k_full(int s) const { return base + 16u + 8u * s; }
+  __device__ uint32_t k_empty(int s) const { return base + 32u + 8u * s; }
+  __device__ uint32_t v_full(int s) const { return base + 48u + 8u * s; }
+  __device__ uint32_t v_empty(int s) const { return base + 64u + 8u * s; }
+  __device__ uint32_t s_full(int t) const { return base + 80u + 8u * t; }
+  __device__ uint32_t p_full(int t) const { return base + 96u + 8u * t; }
+};
+constexpr int kBars = 14;
+
+// Operand whose rows are K (tokens) and whose 64-wide columns are N (D), 128-byte
+// swizzle: groups of 8 rows 1024 bytes apart, 64-wide column blocks kSub apart.
+__device__ __forceinline__ uint64_t sw128_desc_n_major(uint32_t addr) {
+  return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (static_cast<uint64_t>(kSub >> 4) << 16) |
+         (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
+}
+
+// One MMA; the whole warp calls, one lane issues.
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %4, 0;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %4, 0;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
+      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]),
+      "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
+}
+
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// Where the block works: the row tile is the slowest part, the last ones (which see
+// the most tokens) first.
+struct TcPlace {
+  int tile, split, h, b;
+};
+__device__ __forceinline__ TcPlace tc_place(const AttnArgs& p) {
+  TcPlace r;
+  unsigned i = blockIdx.x;
+  r.h = i % p.c.Hkv;
+  i /= p.c.Hkv;
+  r.split = i % p.splits;
+  i /= p.splits;
+  r.b = i % p.a.B;
+  r.tile = p.row_tiles - 1 - static_cast<int>(i / p.a.B);
+  return r;
+}
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constant__ AttnArgs p) {
+  constexpr int kSubs = DP / 64;
+  constexpr uint32_t kO = 256;  // tensor memory: scores of both tiles, then their outputs
+  extern __shared__ uint8_t raw[];
+  __shared__ alignas(8) uint64_t bar_words[kBars];
+  __shared__ float4 pages[kPageRing][8];  // scale of the keys, log2 and inverse of the values' scale
+  __shared__ int abort_flag;
+  __shared__ uint32_t tmem_base;
+  const TcPlace w = tc_place(p);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int r0 = w.tile * kAttnTcRows;
+  const Span sp = span_of(p, w.b, r0, kAttnTcRows);
+  const int rows = sp.n * p.group;
+  if (r0 >= rows) return;
+  const int first = sp.lo & ~(p.align - 1);
+  const int from = first + w.split * p.chunk;
+  if (w.split > 0 && from >= sp.hi) return;
+  const int to = min(sp.hi, from + p.chunk);
+  const int steps = to > from ? (to - from + kTokens - 1) / kTokens : 0;
+  const int tiles = rows - r0 > 128 ? 2 : 1;
+  const int D = p.c.D;
+  const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
+  const uint32_t q_base = smem, k_base = q_base + 2 * kSubs * kSub, v_base = k_base + 2 * kSubs * kSub;
+  const AttnBars bars{smem_u32(bar_words)};
+
+  if (threadIdx.x == 0) {
+    mbar_init(bars.q_full(), 4 * tiles);
+    mbar_init(bars.done(), 1);
+    for (int s = 0; s < 2; ++s) {
+      mbar_init(bars.k_full(s), 4);
+      mbar_init(bars.k_empty(s), 1);
+      mbar_init(bars.v_full(s), 4);
+      mbar_init(bars.v_empty(s), 1);
+      mbar_init(bars.s_full(s), 1);
+      mbar_init(bars.p_full(s), 4);
+    }
+    abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 0) tmem_alloc(smem_u32(&tmem_base), 512);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_base;
+  WaitCtx ctx{&abort_flag, p.err, p.wait_limit_ns, PQ_ERR_MMA};
+
+  if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 0) {
+      // ---- MMAs
+      auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)) != 0; };
+      const uint32_t idesc_s = (1u << 4) | (16u << 17) | (8u << 24);                                       // N = 128 tokens
+      const uint32_t idesc_o = (1u << 4) | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (8u << 24);  // N = D
+      auto scores = [&](int t, int s) {
+#pragma unroll
+        for (int k = 0; k < DP / 16; ++k)
+          if (16 * k < D)
+            mma_ss(tmem + 128 * t, sw128_desc(q_base + (t * kSubs + k / 4) * kSub) + 2 * (k & 3),
+                   sw128_desc(k_base + (s * kSubs + k / 4) * kSub) + 2 * (k & 3), idesc_s, k > 0);
+        tc_commit_warp(bars.s_full(t));
+      };
+      auto outputs = [&](int t, int s, bool accumulate) {
+#pragma unroll
+        for (int k = 0; k < kTokens / 16; ++k)
+          mma_ts(tmem + kO + t * DP, tmem + 128 * t + 8 * k, sw128_desc_n_major(v_base + s * kSubs * kSub + 2048 * k),
+                 idesc_o, accumulate || k > 0);
+      };
+      bool ok = steps > 0 && wait(bars.q_full(), 0) && wait(bars.k_full(0), 0);
+      if (ok) {
+        tc_fence_after();
+        for (int t = 0; t < tiles; ++t) scores(t, 0);
+        tc_commit_warp(bars.k_empty(0));
+      }
+      for (int j = 0; ok && j < steps; ++j) {
+        const int s = j & 1, n = s ^ 1;
+        ok = wait(bars.v_full(s), (j >> 1) & 1);
+        for (int t = 0; ok && t < tiles; ++t) {
+          ok = wait(bars.p_full(t), j & 1);
+          if (!ok) break;
+          tc_fence_after();
+          outputs(t, s, j > 0);
+          if (j + 1 < steps) {
+            if (t == 0) ok = wait(bars.k_full(n), ((j + 1) >> 1) & 1);
+            if (!ok) break;
+            tc_fence_after();
+            scores(t, n);
+          }
+        }
+        if (!ok) break;
+        tc_commit_warp(bars.v_empty(s));
+        if (j + 1 < steps) tc_commit_warp(bars.k_empty(n));
+      }
+      // every MMA issued is over: the outputs are whole, the tensor memory may be given back
+      tc_commit_warp(bars.done());
+      if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
+      __syncwarp();
+    }
+  } else if (warp < 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    // ---- codes to halves
+    ctx.err_bits = PQ_ERR_PRODUCER;
+    const int tid = threadIdx.x - 128;
+    const int C = D / 16;  // 16-byte pieces of a token
+    const int* table = p.a.page_table_dev + static_cast<int64_t>(w.b) * p.a.table_pitch;
+    // piece i of this thread: piece (i * 128 + tid) of the step's 128 C
+    int token[DP / 16], piece[DP / 16];
+#pragma unroll
+    for (int i = 0; i < DP / 16; ++i) {
+      token[i] = (i * 128 + tid) / C;
+      piece[i] = (i * 128 + tid) % C;
+    }
+    // page of a position: -1 where nothing is to be read (outside the rows' span, or out of range)
+    auto page_of = [&](int at) {
+      const int slot = at >> p.page_shift, start = slot << p.page_shift;
+      if (start >= sp.hi || start + p.c.page_tokens <= sp.lo) return -1;
+      const int id = slot < p.a.table_pitch ? table[slot] : -1;
+      return id < p.c.num_pages ? id : -1;
+    };
+    auto fetch = [&](const int8_t* codes, int j, uint4 (&r)[DP / 16]) {
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i) {
+        r[i] = make_uint4(0, 0, 0, 0);
+        if (i < C) {
+          const int at = from + j * kTokens + token[i];
+          const int id = page_of(at);
+          if (id >= 0) {
+            const int64_t row = ((static_cast<int64_t>(id) * p.c.Hkv + w.h) << p.page_shift) + (at & (p.c.page_tokens - 1));
+            r[i] = *reinterpret_cast<const uint4*>(codes + row * D + 16 * piece[i]);
+          }
+        }
+      }
+    };
+    auto store = [&](uint32_t base, const uint4 (&r)[DP / 16]) {
+#pragma unroll
+      for (int i = 0; i < DP / 16; ++i)
+        if (i < C) {
+          uint32_t h[8];
+          half_of_codes(r[i].x, h[0], h[1]);
+          half_of_codes(r[i].y, h[2], h[3]);
+          half_of_codes(r[i].z, h[4], h[5]);
+          half_of_codes(r[i].w, h[6], h[7]);
+          const uint32_t row = base + (piece[i] >> 2) * kSub + token[i] * 128;
+          const uint32_t at = 2 * (piece[i] & 3), x = token[i] & 7;
+          // the pieces of the second 64 columns in the other order: no bank conflicts
+          const bool flip = (piece[i] >> 2) & 1;
+          const uint32_t a0 = row + (((at + (flip ? 1 : 0)) ^ x) << 4), a1 = row + (((at + (flip ? 0 : 1)) ^ x) << 4);
+          sts128(a0, flip ? h[4] : h[0], flip ? h[5] : h[1], flip ? h[6] : h[2], flip ? h[7] : h[3]);
+          sts128(a1, flip ? h[0] : h[4], flip ? h[1] : h[5], flip ? h[2] : h[6], flip ? h[3] : h[7]);
+        }
+    };
+    auto publish = [&](uint32_t bar) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    };
+    uint4 kr[DP / 16], vr[DP / 16];
+    if (steps > 0) fetch(p.c.k_dev, 0, kr);
+    for (int j = 0; j < steps; ++j) {
+      const int s = j & 1;
+      fetch(p.c.v_dev, j, vr);
+      // the step's scales; those of four steps before are no longer read (the keys of two
+      // steps before are done with, so all softmax before that is)
+      if (j > 1 && !__all_sync(0xffffffffu, mbar_wait(bars.k_empty(s), ((j >> 1) - 1) & 1, ctx))) break;
+      if (tid < kTokens >> p.page_shift) {
+        const int at = from + j * kTokens + (tid << p.page_shift);
+        const int id = page_of(at);
+        float4 f = make_float4(0.0f, kNone, 0.0f, 0.0f);
+        if (id >= 0) {
+          const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
+          const float sv0 = p.c.v_scale_dev[ph], sv = sv0 == 0.0f ? 1.0f : sv0;
+          f = make_float4(p.c.k_scale_dev[ph], log2f(sv), 1.0f / sv, 0.0f);
+        } else if (at < sp.hi && at + p.c.page_tokens > sp.lo) {
+          atomicOr(p.err, PQ_ERR_PAGE);
+        }
+        pages[j % kPageRing][tid] = f;
+      }
+      store(k_base + s * kSubs * kSub, kr);
+      publish(bars.k_full(s));
+      if (j + 1 < steps) fetch(p.c.k_dev, j + 1, kr);
+      if (j > 1 && !__all_sync(0xffffffffu, mbar_wait(bars.v_empty(s), ((j >> 1) - 1) & 1, ctx))) break;
+      store(v_base + s * kSubs * kSub, vr);
+      publish(bars.v_full(s));
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    // ---- softmax: this thread's row
+    ctx.err_bits = PQ_ERR_EPILOGUE;
+    const int t = (warp - 8) >> 2;
+    if (t < tiles) {
+      const int in = 32 * (warp & 3) + lane, r = r0 + 128 * t + in;
+      const bool mine = r < rows;
+      const int qi = mine ? r / p.group : 0, hq = w.h * p.group + (mine ? r % p.group : 0);
+      const int64_t tok = static_cast<int64_t>(p.a.cu_q_dev[w.b]) + qi;
+      const uint32_t lanes = static_cast<uint32_t>(32 * (warp & 3)) << 16;
+      const uint32_t s_mem = tmem + lanes + 128 * t, o_mem = tmem + lanes + kO + t * DP;
+      float factor;
+      {
+        // the row as halves, scaled so that its largest element lies in [2^7, 2^8)
+        const T* src = static_cast<const T*>(p.q) + tok * p.a.q_token_stride + static_cast<int64_t>(hq) * p.a.q_head_stride;
+        Vec8<T> v[DP / 8];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) {
+          const bool there = mine && 8 * i < D;
+          v[i] = load8(src + 8 * i, there ? 8 : 0, there && p.wide_q);
+          top = max(top, amax8(v[i]));
+        }
+        const int e = top >= 0x7F800000u ? 0 : max(static_cast<int>(top >> 23) - 127, -100);
+        const float f = __int_as_float((127 + 7 - e) << 23);
+        factor = p.a.scale * kLog2e * __int_as_float((127 - 7 + e) << 23);
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) {
+          uint32_t h[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) h[k] = pack_half2(to_f32(v[i].v[2 * k]) * f, to_f32(v[i].v[2 * k + 1]) * f);
+          sts128(q_base + (t * kSubs + i / 8) * kSub + in * 128 + (((i & 7) ^ (in & 7)) << 4), h[0], h[1], h[2], h[3]);
+        }
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars.q_full());
+      }
+      const int at = sp.len - sp.n + qi + 1;
+      const int hi = !mine ? 0 : p.a.causal ? min(at, sp.len) : sp.len;
+      const int lo = p.a.window > 0 ? max(0, at - p.a.window) : 0;
+      float m = kNone, l = 0.0f;
+      bool ok = true;
+      for (int j = 0; j < steps; ++j) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bars.s_full(t), j & 1, ctx)) != 0;
+        if (!ok) break;
+        tc_fence_after();
+        float x[kTokens];
+#pragma unroll
+        for (int c = 0; c < kTokens; c += 32) {
+          uint32_t v[32];
+          tmem_ld32(s_mem + c, v);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[c + i] = __uint_as_float(v[i]);
+        }
+        tmem_wait_ld();
+        const float4* scale = pages[j % kPageRing];
+        const int j0 = from + j * kTokens;
+        const bool whole = __all_sync(0xffffffffu, j0 >= lo && j0 + kTokens <= hi) != 0;
+        float top[4] = {m, m, m, m};
+        if (whole) {
+#pragma unroll
+          for (int c = 0; c < kTokens; c += 16) {
+            const float4 f = scale[c >> p.page_shift];
+            const float g = f.x * factor;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              x[c + i] = fmaf(x[c + i], g, f.y);
+              top[i & 3] = fmaxf(top[i & 3], x[c + i]);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int c = 0; c < kTokens; c += 16) {
+            const float4 f = scale[c >> p.page_shift];
+            const float g = f.x * factor;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const bool seen = j0 + c + i >= lo && j0 + c + i < hi;
+              x[c + i] = seen ? fmaf(x[c + i], g, f.y) : kNone;
+              top[i & 3] = fmaxf(top[i & 3], x[c + i]);
+            }
+          }
+        }
+        const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+        const bool grew = high > m + kGrow;
+        if (__any_sync(0xffffffffu, grew)) {
+          const float next = grew ? high : m;
+          const float alpha = next == kNone ? 1.0f : exp2_approx(m - next);
+          m = next;
+          l *= alpha;
+          if (j > 0) {
+            // the product before has finished: it was issued before these scores
+#pragma unroll
+            for (int c = 0; c < DP; c += 16) {
+              if (c < D) {
+                uint32_t v[16];
+                tmem_ld16(o_mem + c, v);
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+                tmem_st16(o_mem + c, v);
+              }
+            }
+          }
+        }
+        const float base = m == kNone ? 0.0f : m;
+#pragma unroll
+        for (int c = 0; c < kTokens; c += 32) {
+          uint32_t h[16];
+#pragma unroll
+          for (int u = 0; u < 32; u += 16) {
+            float sum = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+              const float a = exp2_approx(x[c + u + i] - base), b = exp2_approx(x[c + u + i + 1] - base);
+              sum += a + b;
+              h[(u + i) / 2] = pack_half2(a, b);
+            }
+            // a page that the row does not see adds nothing, even with a NaN scale
+            l += whole || sum != 0.0f ? sum * scale[(c + u) >> p.page_shift].z : 0.0f;
+          }
+          tmem_st16(s_mem + c / 2, h);
+        }
+        tmem_wait_st();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars.p_full(t));
+      }
+      // ---- outputs
+      if (ok && steps > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars.done(), 0, ctx)) != 0;
+      tc_fence_after();
+      const float inv = p.splits > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
+      const int64_t part = ((static_cast<int64_t>(w.b) * p.a.max_q + qi) * p.a.Hq + hq) * p.splits + w.split;
+      if (p.splits > 1 && mine) p.ml[part] = make_float2(m, l);
+      T* dst = static_cast<T*>(p.o) + tok * p.a.o_token_stride + static_cast<int64_t>(hq) * p.a.o_head_stride;
+#pragma unroll
+      for (int c = 0; c < DP; c += 16) {
+        if (c < D) {
+          uint32_t v[16];
+          tmem_ld16(o_mem + c, v);
+          tmem_wait_ld();
+          if (!ok || !mine) continue;
+          if (p.splits > 1) {
+#pragma unroll
+            for (int i = 0; i < 16; i += 2)
+              *reinterpret_cast<float2*>(p.part + part * D + c + i) =
+                  steps > 0 ? make_float2(__uint_as_float(v[i]), __uint_as_float(v[i + 1])) : make_float2(0.0f, 0.0f);
+          } else {
+#pragma unroll
+            for (int u = 0; u < 16; u += 8) {
+              Vec8<T> r;
+#pragma unroll
+              for (int i = 0; i < 8; ++i)
+                r.v[i] = from_f32<T>(steps > 0 && l != 0.0f ? __uint_as_float(v[u + i]) * inv : 0.0f);
+              store8(dst + c + u, r, 8, p.wide_o);
+            }
+          }
+        }
+      }
+      tc_fence_before();
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 0) {
+    __syncwarp();
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <typename T, int DP>
+cudaError_t launch(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
+  static int attr_set[64] = {0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !attr_set[dev]) {
+    e = cudaFuncSetAttribute(pq_kv8_tiles<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(DP));
+    if (e != cudaSuccess) return e;
+    if (dev < 64) attr_set[dev] = 1;
+  }
+  pq_kv8_tiles<T, DP><<<grid, kThreads, attn_smem(DP), stream>>>(p);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool attn_tc_takes(const pq_kv8_cache& c, const pq_kv8_attn& a) {
+  return a.type != PQ_F32 && c.D <= 128 && static_cast<int64_t>(a.max_q) * (a.Hq / c.Hkv) > 64;
+}
+
+cudaError_t launch_attn_tc(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
+  if (p.a.type == PQ_F16) return p.c.D <= 64 ? launch<__half, 64>(p, grid, stream) : launch<__half, 128>(p, grid, stream);
+  return p.c.D <= 64 ? launch<__nv_bfloat16, 64>(p, grid, stream) : launch<__nv_bfloat16, 128>(p, grid, stream);
+}
+
+}  // namespace pq
