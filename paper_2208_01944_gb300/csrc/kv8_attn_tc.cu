@@ -31,7 +31,7 @@ constexpr int kTokens = kAttnTcTokens;  // of one step
 constexpr int kThreads = 512;
 constexpr int kSub = 128 * 128;         // 128 rows of 64 halves
 constexpr float kGrow = 8.0f;           // log2 by which a maximum may grow without a rescale
-constexpr int kPageRing = 4;            // steps whose scales are kept
+constexpr int kPageRing = 8;            // steps whose pages are looked up ahead
 
 __host__ __device__ constexpr int attn_smem(int DP) { return 6 * (DP / 64) * kSub + 1024 /* alignment */; }
 
@@ -45,8 +45,17 @@ struct AttnBars {
   __device__ uint32_t v_empty(int s) const { return base + 64u + 8u * s; }
   __device__ uint32_t s_full(int t) const { return base + 80u + 8u * t; }
   __device__ uint32_t p_full(int t) const { return base + 96u + 8u * t; }
+  __device__ uint32_t page_full(int i) const { return base + 112u + 8u * i; }
+  __device__ uint32_t page_empty(int i) const { return base + 112u + 8u * kPageRing + 8u * i; }
 };
-constexpr int kBars = 14;
+constexpr int kBars = 14 + 2 * kPageRing;
+
+// A page of a step: scale of the keys, log2 and inverse of the values' scale, and where
+// the head's codes begin (absent pages: -1).
+struct alignas(8) StepPage {
+  float k, log2_v, inv_v;
+  int64_t codes;
+};
 
 // Operand whose rows are K (tokens) and whose 64-wide columns are N (D), 128-byte
 // swizzle: groups of 8 rows 1024 bytes apart, 64-wide column blocks kSub apart.
@@ -106,7 +115,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
   constexpr uint32_t kO = 256;  // tensor memory: scores of both tiles, then their outputs
   extern __shared__ uint8_t raw[];
   __shared__ alignas(8) uint64_t bar_words[kBars];
-  __shared__ float4 pages[kPageRing][8];  // scale of the keys, log2 and inverse of the values' scale
+  __shared__ StepPage pages[kPageRing][8];
   __shared__ int abort_flag;
   __shared__ uint32_t tmem_base;
   const TcPlace w = tc_place(p);
@@ -136,6 +145,10 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
       mbar_init(bars.v_empty(s), 1);
       mbar_init(bars.s_full(s), 1);
       mbar_init(bars.p_full(s), 4);
+    }
+    for (int i = 0; i < kPageRing; ++i) {
+      mbar_init(bars.page_full(i), 1);
+      mbar_init(bars.page_empty(i), 1);
     }
     abort_flag = 0;
     fence_mbar_init();
@@ -191,12 +204,41 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         }
         if (!ok) break;
         tc_commit_warp(bars.v_empty(s));
+        tc_commit_warp(bars.page_empty(j % kPageRing));
         if (j + 1 < steps) tc_commit_warp(bars.k_empty(n));
       }
       // every MMA issued is over: the outputs are whole, the tensor memory may be given back
       tc_commit_warp(bars.done());
       if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
       __syncwarp();
+    } else if (warp == 1) {
+      // ---- the steps' pages, a lane each, up to kPageRing steps ahead of the codes (two
+      // dependent loads that would otherwise stand in every step's way)
+      ctx.err_bits = PQ_ERR_PRODUCER;
+      const int* table = p.a.page_table_dev + static_cast<int64_t>(w.b) * p.a.table_pitch;
+      for (int j = 0; j < steps; ++j) {
+        const int i = j % kPageRing;
+        if (j >= kPageRing &&
+            !__all_sync(0xffffffffu, mbar_wait(bars.page_empty(i), (j / kPageRing - 1) & 1, ctx)))
+          break;
+        if (lane < kTokens >> p.page_shift) {
+          const int start = from + j * kTokens + (lane << p.page_shift), slot = start >> p.page_shift;
+          StepPage page = {0.0f, kNone, 0.0f, -1};
+          if (start < sp.hi && start + p.c.page_tokens > sp.lo) {  // within the rows' span
+            const int id = slot < p.a.table_pitch ? table[slot] : -1;
+            if (id >= 0 && id < p.c.num_pages) {
+              const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
+              const float sk = p.c.k_scale_dev[ph], sv0 = p.c.v_scale_dev[ph], sv = sv0 == 0.0f ? 1.0f : sv0;
+              page = {sk, log2f(sv), 1.0f / sv, (ph << p.page_shift) * D};
+            } else {
+              atomicOr(p.err, PQ_ERR_PAGE);
+            }
+          }
+          pages[i][lane] = page;
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bars.page_full(i));
+      }
     }
   } else if (warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
@@ -204,85 +246,68 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
     ctx.err_bits = PQ_ERR_PRODUCER;
     const int tid = threadIdx.x - 128;
     const int C = D / 16;  // 16-byte pieces of a token
-    const int* table = p.a.page_table_dev + static_cast<int64_t>(w.b) * p.a.table_pitch;
-    // piece i of this thread: piece (i * 128 + tid) of the step's 128 C
-    int token[DP / 16], piece[DP / 16];
+    // A thread takes one 16-byte piece of every (128 / kP)th token.  Eight neighbours hold
+    // four pieces of two tokens, whose halves lie in different banks.
+    constexpr int kP = DP / 16, kTokStep = 128 / kP;
+    const int piece = kP == 8 ? (tid & 3) | ((tid >> 1) & 4) : tid & 3;
+    const int token = kP == 8 ? ((tid >> 3) & ~1) | ((tid >> 2) & 1) : tid >> 2;
+    const bool there = piece < C;
+    const uint32_t row = (piece >> 2) * kSub + token * 128;
+    const uint32_t at0 = row + (((2 * (piece & 3)) ^ (token & 7)) << 4), at1 = row + (((2 * (piece & 3) + 1) ^ (token & 7)) << 4);
+    auto fetch = [&](const int8_t* codes, int j, uint4 (&r)[kP]) {
+      const StepPage* page = pages[j % kPageRing];
 #pragma unroll
-    for (int i = 0; i < DP / 16; ++i) {
-      token[i] = (i * 128 + tid) / C;
-      piece[i] = (i * 128 + tid) % C;
-    }
-    // page of a position: -1 where nothing is to be read (outside the rows' span, or out of range)
-    auto page_of = [&](int at) {
-      const int slot = at >> p.page_shift, start = slot << p.page_shift;
-      if (start >= sp.hi || start + p.c.page_tokens <= sp.lo) return -1;
-      const int id = slot < p.a.table_pitch ? table[slot] : -1;
-      return id < p.c.num_pages ? id : -1;
-    };
-    auto fetch = [&](const int8_t* codes, int j, uint4 (&r)[DP / 16]) {
-#pragma unroll
-      for (int i = 0; i < DP / 16; ++i) {
+      for (int i = 0; i < kP; ++i) {
+        const int k = token + i * kTokStep;
+        const int64_t base = page[k >> p.page_shift].codes;
         r[i] = make_uint4(0, 0, 0, 0);
-        if (i < C) {
-          const int at = from + j * kTokens + token[i];
-          const int id = page_of(at);
-          if (id >= 0) {
-            const int64_t row = ((static_cast<int64_t>(id) * p.c.Hkv + w.h) << p.page_shift) + (at & (p.c.page_tokens - 1));
-            r[i] = *reinterpret_cast<const uint4*>(codes + row * D + 16 * piece[i]);
-          }
-        }
+        if (there && base >= 0)
+          r[i] = *reinterpret_cast<const uint4*>(codes + base + (k & (p.c.page_tokens - 1)) * D + 16 * piece);
       }
     };
-    auto store = [&](uint32_t base, const uint4 (&r)[DP / 16]) {
+    auto store = [&](uint32_t base, const uint4 (&r)[kP]) {
+      if (!there) return;
 #pragma unroll
-      for (int i = 0; i < DP / 16; ++i)
-        if (i < C) {
-          uint32_t h[8];
-          half_of_codes(r[i].x, h[0], h[1]);
-          half_of_codes(r[i].y, h[2], h[3]);
-          half_of_codes(r[i].z, h[4], h[5]);
-          half_of_codes(r[i].w, h[6], h[7]);
-          const uint32_t row = base + (piece[i] >> 2) * kSub + token[i] * 128;
-          const uint32_t at = 2 * (piece[i] & 3), x = token[i] & 7;
-          // the pieces of the second 64 columns in the other order: no bank conflicts
-          const bool flip = (piece[i] >> 2) & 1;
-          const uint32_t a0 = row + (((at + (flip ? 1 : 0)) ^ x) << 4), a1 = row + (((at + (flip ? 0 : 1)) ^ x) << 4);
-          sts128(a0, flip ? h[4] : h[0], flip ? h[5] : h[1], flip ? h[6] : h[2], flip ? h[7] : h[3]);
-          sts128(a1, flip ? h[0] : h[4], flip ? h[1] : h[5], flip ? h[2] : h[6], flip ? h[3] : h[7]);
-        }
+      for (int i = 0; i < kP; ++i) {
+        uint32_t h[8];
+        half_of_codes(r[i].x, h[0], h[1]);
+        half_of_codes(r[i].y, h[2], h[3]);
+        half_of_codes(r[i].z, h[4], h[5]);
+        half_of_codes(r[i].w, h[6], h[7]);
+        sts128(base + at0 + i * kTokStep * 128, h[0], h[1], h[2], h[3]);
+        sts128(base + at1 + i * kTokStep * 128, h[4], h[5], h[6], h[7]);
+      }
     };
     auto publish = [&](uint32_t bar) {
       fence_proxy_async_smem();
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
-    uint4 kr[DP / 16], vr[DP / 16];
-    if (steps > 0) fetch(p.c.k_dev, 0, kr);
-    for (int j = 0; j < steps; ++j) {
+    auto look = [&](int j) {
+      return __all_sync(0xffffffffu, mbar_wait(bars.page_full(j % kPageRing), (j / kPageRing) & 1, ctx)) != 0;
+    };
+    uint4 kr[kP], vr[kP];
+    bool ok = steps > 0 && look(0);
+    if (ok) {
+      fetch(p.c.k_dev, 0, kr);
+      fetch(p.c.v_dev, 0, vr);
+    }
+    for (int j = 0; ok && j < steps; ++j) {
       const int s = j & 1;
-      fetch(p.c.v_dev, j, vr);
-      // the step's scales; those of four steps before are no longer read (the keys of two
-      // steps before are done with, so all softmax before that is)
-      if (j > 1 && !__all_sync(0xffffffffu, mbar_wait(bars.k_empty(s), ((j >> 1) - 1) & 1, ctx))) break;
-      if (tid < kTokens >> p.page_shift) {
-        const int at = from + j * kTokens + (tid << p.page_shift);
-        const int id = page_of(at);
-        float4 f = make_float4(0.0f, kNone, 0.0f, 0.0f);
-        if (id >= 0) {
-          const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
-          const float sv0 = p.c.v_scale_dev[ph], sv = sv0 == 0.0f ? 1.0f : sv0;
-          f = make_float4(p.c.k_scale_dev[ph], log2f(sv), 1.0f / sv, 0.0f);
-        } else if (at < sp.hi && at + p.c.page_tokens > sp.lo) {
-          atomicOr(p.err, PQ_ERR_PAGE);
-        }
-        pages[j % kPageRing][tid] = f;
-      }
+      if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.k_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
+      if (!ok) break;
       store(k_base + s * kSubs * kSub, kr);
       publish(bars.k_full(s));
-      if (j + 1 < steps) fetch(p.c.k_dev, j + 1, kr);
-      if (j > 1 && !__all_sync(0xffffffffu, mbar_wait(bars.v_empty(s), ((j >> 1) - 1) & 1, ctx))) break;
+      if (j + 1 < steps) {
+        ok = look(j + 1);
+        if (!ok) break;
+        fetch(p.c.k_dev, j + 1, kr);
+      }
+      if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.v_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
+      if (!ok) break;
       store(v_base + s * kSubs * kSub, vr);
       publish(bars.v_full(s));
+      if (j + 1 < steps) fetch(p.c.v_dev, j + 1, vr);
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
@@ -340,30 +365,30 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
           for (int i = 0; i < 32; ++i) x[c + i] = __uint_as_float(v[i]);
         }
         tmem_wait_ld();
-        const float4* scale = pages[j % kPageRing];
+        const StepPage* page = pages[j % kPageRing];
         const int j0 = from + j * kTokens;
         const bool whole = __all_sync(0xffffffffu, j0 >= lo && j0 + kTokens <= hi) != 0;
         float top[4] = {m, m, m, m};
         if (whole) {
 #pragma unroll
           for (int c = 0; c < kTokens; c += 16) {
-            const float4 f = scale[c >> p.page_shift];
-            const float g = f.x * factor;
+            const StepPage f = page[c >> p.page_shift];
+            const float g = f.k * factor;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-              x[c + i] = fmaf(x[c + i], g, f.y);
+              x[c + i] = fmaf(x[c + i], g, f.log2_v);
               top[i & 3] = fmaxf(top[i & 3], x[c + i]);
             }
           }
         } else {
 #pragma unroll
           for (int c = 0; c < kTokens; c += 16) {
-            const float4 f = scale[c >> p.page_shift];
-            const float g = f.x * factor;
+            const StepPage f = page[c >> p.page_shift];
+            const float g = f.k * factor;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const bool seen = j0 + c + i >= lo && j0 + c + i < hi;
-              x[c + i] = seen ? fmaf(x[c + i], g, f.y) : kNone;
+              x[c + i] = seen ? fmaf(x[c + i], g, f.log2_v) : kNone;
               top[i & 3] = fmaxf(top[i & 3], x[c + i]);
             }
           }
@@ -404,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
               h[(u + i) / 2] = pack_half2(a, b);
             }
             // a page that the row does not see adds nothing, even with a NaN scale
-            l += whole || sum != 0.0f ? sum * scale[(c + u) >> p.page_shift].z : 0.0f;
+            l += whole || sum != 0.0f ? sum * page[(c + u) >> p.page_shift].inv_v : 0.0f;
           }
           tmem_st16(s_mem + c / 2, h);
         }
