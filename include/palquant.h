@@ -557,7 +557,7 @@ pq_status palquant_linear_q8(const void* x_dev, const int8_t* w_dev, const float
  * scale for each page and head [num_pages][Hkv], for each side.  The token at
  * position p of sequence b sits in page page_table[b][p / page_tokens], slot
  * p % page_tokens.  page_tokens is 16, 32, 64 or 128; D a multiple of 16, 16 to 256;
- * codes 16-byte aligned.  A page id outside [0, num_pages) that a call meets is
+ * codes 16-byte aligned; scales not negative, and 0, NaN or between 2^-100 and 2^100.  A page id outside [0, num_pages) that a call meets is
  * skipped (nothing is read or written there) and reported by palquant_sync_check as
  * PQ_EINVAL. */
 typedef struct {

@@ -64,19 +64,29 @@ __device__ __forceinline__ uint64_t sw128_desc_n_major(uint32_t addr) {
          (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
 }
 
-// One MMA; the whole warp calls, one lane issues.
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// Four MMAs (64 of K); the whole warp calls, one lane issues.  One election and no
+// branch between them: a branch around each made the issue of an MMA take longer than
+// the MMA.  The first operand from shared memory (32 bytes of K a step) or tensor memory.
+__device__ __forceinline__ void mma_ss_x4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n.reg .pred p, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %4, 0;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{\n.reg .pred p, q, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %10, 0;\nsetp.eq.b32 q, 0, 0;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %5, %9, p;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %2, %6, %9, q;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %3, %7, %9, q;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %4, %8, %9, q;\n}" ::"r"(d),
+      "l"(a), "l"(a + 2), "l"(a + 4), "l"(a + 6), "l"(b), "l"(b + 2), "l"(b + 4), "l"(b + 6), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// (16 rows of the second operand, 2048 bytes, a step)
+__device__ __forceinline__ void mma_ts_x4(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n.reg .pred p, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %4, 0;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}" ::"r"(d),
-      "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{\n.reg .pred p, q, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %10, 0;\nsetp.eq.b32 q, 0, 0;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %5, %9, p;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%2], %6, %9, q;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%3], %7, %9, q;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%4], %8, %9, q;\n}" ::"r"(d),
+      "r"(a), "r"(a + 8), "r"(a + 16), "r"(a + 24), "l"(b), "l"(b + 128), "l"(b + 256), "l"(b + 384), "r"(idesc),
+      "r"(accumulate)
       : "memory");
 }
 
@@ -90,6 +100,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
 
 __device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// (s0, s1) += (a, b), packed.
+__device__ __forceinline__ void add_pair(float& s0, float& s1, float a, float b) {
+  asm("{\n.reg .b64 s, t;\nmov.b64 s, {%0, %1};\nmov.b64 t, {%2, %3};\nadd.rn.f32x2 s, s, t;\nmov.b64 {%0, %1}, s;\n}"
+      : "+f"(s0), "+f"(s1)
+      : "f"(a), "f"(b));
 }
 
 // Where the block works: the row tile is the slowest part, the last ones (which see
@@ -169,17 +186,15 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
       const uint32_t idesc_o = (1u << 4) | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (8u << 24);  // N = D
       auto scores = [&](int t, int s) {
 #pragma unroll
-        for (int k = 0; k < DP / 16; ++k)
-          if (16 * k < D)
-            mma_ss(tmem + 128 * t, sw128_desc(q_base + (t * kSubs + k / 4) * kSub) + 2 * (k & 3),
-                   sw128_desc(k_base + (s * kSubs + k / 4) * kSub) + 2 * (k & 3), idesc_s, k > 0);
+        for (int c = 0; c < kSubs; ++c)
+          mma_ss_x4(tmem + 128 * t, sw128_desc(q_base + (t * kSubs + c) * kSub), sw128_desc(k_base + (s * kSubs + c) * kSub),
+                    idesc_s, c > 0);
         tc_commit_warp(bars.s_full(t));
       };
       auto outputs = [&](int t, int s, bool accumulate) {
-#pragma unroll
-        for (int k = 0; k < kTokens / 16; ++k)
-          mma_ts(tmem + kO + t * DP, tmem + 128 * t + 8 * k, sw128_desc_n_major(v_base + s * kSubs * kSub + 2048 * k),
-                 idesc_o, accumulate || k > 0);
+        const uint64_t v = sw128_desc_n_major(v_base + s * kSubs * kSub);
+        mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t, v, idesc_o, accumulate);
+        mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + 32, v + 512, idesc_o, 1);
       };
       bool ok = steps > 0 && wait(bars.q_full(), 0) && wait(bars.k_full(0), 0);
       if (ok) {
@@ -265,8 +280,8 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
           r[i] = *reinterpret_cast<const uint4*>(codes + base + (k & (p.c.page_tokens - 1)) * D + 16 * piece);
       }
     };
+    // (columns past D are zeros: the scores' products run over whole blocks of 64)
     auto store = [&](uint32_t base, const uint4 (&r)[kP]) {
-      if (!there) return;
 #pragma unroll
       for (int i = 0; i < kP; ++i) {
         uint32_t h[8];
@@ -334,8 +349,9 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
           top = max(top, amax8(v[i]));
         }
         const int e = top >= 0x7F800000u ? 0 : max(static_cast<int>(top >> 23) - 127, -100);
-        const float f = __int_as_float((127 + 7 - e) << 23);
-        factor = p.a.scale * kLog2e * __int_as_float((127 - 7 + e) << 23);
+        // (negated where the call's scale is negative: the scores' factor is not)
+        const float f = __int_as_float((127 + 7 - e) << 23) * (p.a.scale < 0.0f ? -1.0f : 1.0f);
+        factor = fabsf(p.a.scale) * kLog2e * __int_as_float((127 - 7 + e) << 23);
 #pragma unroll
         for (int i = 0; i < DP / 8; ++i) {
           uint32_t h[4];
@@ -368,32 +384,31 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         const StepPage* page = pages[j % kPageRing];
         const int j0 = from + j * kTokens;
         const bool whole = __all_sync(0xffffffffu, j0 >= lo && j0 + kTokens <= hi) != 0;
-        float top[4] = {m, m, m, m};
+        // the row's maximum: within 16 tokens of one page that of the raw scores (the scales
+        // are not negative)
+        float high = m;
         if (whole) {
 #pragma unroll
           for (int c = 0; c < kTokens; c += 16) {
-            const StepPage f = page[c >> p.page_shift];
-            const float g = f.k * factor;
+            const StepPage& f = page[c >> p.page_shift];
+            float top = fmaxf(x[c], x[c + 1]);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              x[c + i] = fmaf(x[c + i], g, f.log2_v);
-              top[i & 3] = fmaxf(top[i & 3], x[c + i]);
-            }
+            for (int i = 2; i < 16; i += 2) top = fmaxf(top, fmaxf(x[c + i], x[c + i + 1]));
+            high = fmaxf(high, fmaf(top, f.k * factor, f.log2_v));
           }
         } else {
 #pragma unroll
           for (int c = 0; c < kTokens; c += 16) {
-            const StepPage f = page[c >> p.page_shift];
-            const float g = f.k * factor;
+            const StepPage& f = page[c >> p.page_shift];
+            const float g = f.k * factor, lv = f.log2_v;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const bool seen = j0 + c + i >= lo && j0 + c + i < hi;
-              x[c + i] = seen ? fmaf(x[c + i], g, f.log2_v) : kNone;
-              top[i & 3] = fmaxf(top[i & 3], x[c + i]);
+              x[c + i] = seen ? fmaf(x[c + i], g, lv) : kNone;
+              high = fmaxf(high, x[c + i]);
             }
           }
         }
-        const float high = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
         const bool grew = high > m + kGrow;
         if (__any_sync(0xffffffffu, grew)) {
           const float next = grew ? high : m;
@@ -421,15 +436,22 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
           uint32_t h[16];
 #pragma unroll
           for (int u = 0; u < 32; u += 16) {
-            float sum = 0.0f;
+            const StepPage& f = page[(c + u) >> p.page_shift];
+            // seen as a whole: the scores are still raw
+            const float g = whole ? f.k * factor : 1.0f, shift = whole ? f.log2_v - base : -base;
+            float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
-              const float a = exp2_approx(x[c + u + i] - base), b = exp2_approx(x[c + u + i + 1] - base);
-              sum += a + b;
+              float a, b;
+              fma2_rn(x[c + u + i], x[c + u + i + 1], g, shift, a, b);
+              a = exp2_approx(a);
+              b = exp2_approx(b);
+              add_pair(s0, s1, a, b);
               h[(u + i) / 2] = pack_half2(a, b);
             }
             // a page that the row does not see adds nothing, even with a NaN scale
-            l += whole || sum != 0.0f ? sum * page[(c + u) >> p.page_shift].inv_v : 0.0f;
+            const float sum = s0 + s1;
+            l += whole || sum != 0.0f ? sum * f.inv_v : 0.0f;
           }
           tmem_st16(s_mem + c / 2, h);
         }
