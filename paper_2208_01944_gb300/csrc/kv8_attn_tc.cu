@@ -3,20 +3,21 @@
 //
 // Split.  A block takes one cache head and 256 query rows (queries x heads of the group)
 // as two tiles of 128, and walks through the tokens 128 at a time.  Each step's codes
-// are turned into halves once, for both tiles, on their way into shared memory.
-// Scores are 128 rows x 128 tokens in tensor memory, a row a thread, so the softmax needs
-// no exchange between threads; the probabilities go back over the scores as halves
-// and are the second product's first operand from there.  While one tile's softmax
-// runs, the tensor core works on the other tile: its issue order is
-//   P0 V(j), Q0 K(j+1), P1 V(j), Q1 K(j+1),
-// and one thread's MMAs run in order, so scores never overwrite probabilities in use.
-// The outputs stay in tensor memory; they are rescaled only when a row's maximum has grown
-// by more than 2^8 (w stays below 2^8, a half holds 2^16), which is rare.
-// Bound by the softmax's instructions and the tensor rate (512 cycles for each of
-// the four products of a step at D = 128).
+// are turned into halves once, for both tiles, on their way into shared memory.  The
+// softmax works on half a step: scores are 128 rows x 64 tokens in tensor memory, a row
+// a thread, so it needs no exchange between threads; the probabilities go back over the
+// scores as halves and are the second product's first operand from there.  Each tile has
+// two such buffers: the next half's scores are computed while this one's softmax runs
+// (with one buffer of 128 tokens the softmax waited for its own product and the next scores,
+// 4600 cycles a step).  One thread's MMAs run in order, so scores never overwrite
+// probabilities in use.  The outputs stay in tensor memory; they are rescaled only when
+// a row's maximum has grown by more than 2^8 (w stays below 2^8, a half holds 2^16).
+// Bound by the softmax's instructions, then by the tensor rate (at D = 128 a step's
+// products take 2560 cycles: scores of 64 tokens wait for shared memory, 48 cycles an MMA
+// instead of 32).
 //
-// Roles (16 warps): 0 issues the MMAs, 4-7 convert, 8-11 and 12-15 are the tiles'
-// softmax.  Tiles with the most tokens come first.
+// Roles (16 warps): 0 issues the MMAs, 4 looks up pages, the other six below 8 convert
+// (none of them on the issuing warp's scheduler), 8-11 and 12-15 are the tiles' softmax.  Tiles with the most tokens come first.
 #include <cuda_runtime.h>
 
 #include "palquant.h"
@@ -28,6 +29,7 @@ namespace pq {
 namespace {
 
 constexpr int kTokens = kAttnTcTokens;  // of one step
+constexpr int kHalf = 64;               // of one round of the softmax
 constexpr int kThreads = 512;
 constexpr int kSub = 128 * 128;         // 128 rows of 64 halves
 constexpr float kGrow = 8.0f;           // log2 by which a maximum may grow without a rescale
@@ -43,12 +45,14 @@ struct AttnBars {
   __device__ uint32_t k_empty(int s) const { return base + 32u + 8u * s; }
   __device__ uint32_t v_full(int s) const { return base + 48u + 8u * s; }
   __device__ uint32_t v_empty(int s) const { return base + 64u + 8u * s; }
-  __device__ uint32_t s_full(int t) const { return base + 80u + 8u * t; }
-  __device__ uint32_t p_full(int t) const { return base + 96u + 8u * t; }
-  __device__ uint32_t page_full(int i) const { return base + 112u + 8u * i; }
-  __device__ uint32_t page_empty(int i) const { return base + 112u + 8u * kPageRing + 8u * i; }
+  // both tiles' scores and probabilities in buffer b; their outputs
+  __device__ uint32_t s_full(int b) const { return base + 80u + 8u * b; }
+  __device__ uint32_t p_full(int b) const { return base + 96u + 8u * b; }
+  __device__ uint32_t o_full() const { return base + 112u; }
+  __device__ uint32_t page_full(int i) const { return base + 120u + 8u * i; }
+  __device__ uint32_t page_empty(int i) const { return base + 120u + 8u * kPageRing + 8u * i; }
 };
-constexpr int kBars = 14 + 2 * kPageRing;
+constexpr int kBars = 15 + 2 * kPageRing;
 
 // A page of a step: scale of the keys, log2 and inverse of the values' scale, and where
 // the head's codes begin (absent pages: -1).
@@ -57,36 +61,37 @@ struct alignas(8) StepPage {
   int64_t codes;
 };
 
-// Operand whose rows are K (tokens) and whose 64-wide columns are N (D), 128-byte
-// swizzle: groups of 8 rows 1024 bytes apart, 64-wide column blocks kSub apart.
-__device__ __forceinline__ uint64_t sw128_desc_n_major(uint32_t addr) {
-  return static_cast<uint64_t>((addr >> 4) & 0x3FFFu) | (static_cast<uint64_t>(kSub >> 4) << 16) |
-         (static_cast<uint64_t>(1024 >> 4) << 32) | (static_cast<uint64_t>(1) << 46) | (static_cast<uint64_t>(2) << 61);
-}
+// Operand descriptors in two words.  Both in the 128-byte swizzle, groups of 8 rows 1024
+// bytes apart.  K-major: rows of 64 halves of K.  N-major: rows are K (tokens), their 64-wide
+// column blocks (of D) kSub apart.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_k(uint32_t addr) { return ((addr >> 4) & 0x3FFFu) | (1u << 16); }
+__device__ __forceinline__ uint32_t desc_n(uint32_t addr) { return ((addr >> 4) & 0x3FFFu) | (static_cast<uint32_t>(kSub >> 4) << 16); }
 
 // Four MMAs (64 of K); the whole warp calls, one lane issues.  One election and no
 // branch between them: a branch around each made the issue of an MMA take longer than
 // the MMA.  The first operand from shared memory (32 bytes of K a step) or tensor memory.
-__device__ __forceinline__ void mma_ss_x4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_ss_x4(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n.reg .pred p, q, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %10, 0;\nsetp.eq.b32 q, 0, 0;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %5, %9, p;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %2, %6, %9, q;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %3, %7, %9, q;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %4, %8, %9, q;\n}" ::"r"(d),
-      "l"(a), "l"(a + 2), "l"(a + 4), "l"(a + 6), "l"(b), "l"(b + 2), "l"(b + 4), "l"(b + 6), "r"(idesc), "r"(accumulate)
+      "{\n.reg .pred p, q, e;\n.reg .b64 x, y;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %10, 0;\nsetp.eq.b32 q, 0, 0;\n"
+      "mov.b64 x, {%1, %11};\nmov.b64 y, {%5, %11};\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %9, p;\n"
+      "mov.b64 x, {%2, %11};\nmov.b64 y, {%6, %11};\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %9, q;\n"
+      "mov.b64 x, {%3, %11};\nmov.b64 y, {%7, %11};\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %9, q;\n"
+      "mov.b64 x, {%4, %11};\nmov.b64 y, {%8, %11};\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], x, y, %9, q;\n}" ::"r"(d),
+      "r"(a), "r"(a + 2), "r"(a + 4), "r"(a + 6), "r"(b), "r"(b + 2), "r"(b + 4), "r"(b + 6), "r"(idesc), "r"(accumulate),
+      "r"(kDescHigh)
       : "memory");
 }
 // (16 rows of the second operand, 2048 bytes, a step)
-__device__ __forceinline__ void mma_ts_x4(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+__device__ __forceinline__ void mma_ts_x4(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n.reg .pred p, q, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %10, 0;\nsetp.eq.b32 q, 0, 0;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %5, %9, p;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%2], %6, %9, q;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%3], %7, %9, q;\n"
-      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%4], %8, %9, q;\n}" ::"r"(d),
-      "r"(a), "r"(a + 8), "r"(a + 16), "r"(a + 24), "l"(b), "l"(b + 128), "l"(b + 256), "l"(b + 384), "r"(idesc),
-      "r"(accumulate)
+      "{\n.reg .pred p, q, e;\n.reg .b64 y;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %10, 0;\nsetp.eq.b32 q, 0, 0;\n"
+      "mov.b64 y, {%5, %11};\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], y, %9, p;\n"
+      "mov.b64 y, {%6, %11};\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%2], y, %9, q;\n"
+      "mov.b64 y, {%7, %11};\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%3], y, %9, q;\n"
+      "mov.b64 y, {%8, %11};\n@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%4], y, %9, q;\n}" ::"r"(d),
+      "r"(a), "r"(a + 8), "r"(a + 16), "r"(a + 24), "r"(b), "r"(b + 128), "r"(b + 256), "r"(b + 384), "r"(idesc),
+      "r"(accumulate), "r"(kDescHigh)
       : "memory");
 }
 
@@ -146,6 +151,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
   if (w.split > 0 && from >= sp.hi) return;
   const int to = min(sp.hi, from + p.chunk);
   const int steps = to > from ? (to - from + kTokens - 1) / kTokens : 0;
+  const int halves = to > from ? (to - from + kHalf - 1) / kHalf : 0;
   const int tiles = rows - r0 > 128 ? 2 : 1;
   const int D = p.c.D;
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
@@ -156,13 +162,14 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
     mbar_init(bars.q_full(), 4 * tiles);
     mbar_init(bars.done(), 1);
     for (int s = 0; s < 2; ++s) {
-      mbar_init(bars.k_full(s), 4);
+      mbar_init(bars.k_full(s), 6);
       mbar_init(bars.k_empty(s), 1);
-      mbar_init(bars.v_full(s), 4);
+      mbar_init(bars.v_full(s), 6);
       mbar_init(bars.v_empty(s), 1);
       mbar_init(bars.s_full(s), 1);
-      mbar_init(bars.p_full(s), 4);
+      mbar_init(bars.p_full(s), 4 * tiles);
     }
+    mbar_init(bars.o_full(), 1);
     for (int i = 0; i < kPageRing; ++i) {
       mbar_init(bars.page_full(i), 1);
       mbar_init(bars.page_empty(i), 1);
@@ -174,59 +181,67 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_base;
+  // all 512 columns are this block's: the base is 0 (a constant address costs the issuing
+  // warp no register moves)
+  constexpr uint32_t tmem = 0;
   WaitCtx ctx{&abort_flag, p.err, p.wait_limit_ns, PQ_ERR_MMA};
 
-  if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+  if (warp < 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 0) {
       // ---- MMAs
       auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)) != 0; };
-      const uint32_t idesc_s = (1u << 4) | (16u << 17) | (8u << 24);                                       // N = 128 tokens
+      const uint32_t idesc_s = (1u << 4) | (8u << 17) | (8u << 24);                                        // N = 64 tokens
       const uint32_t idesc_o = (1u << 4) | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (8u << 24);  // N = D
-      auto scores = [&](int t, int s) {
+      // Half i is half i % 2 of step i / 2, whose operands are in stage (i / 2) % 2.  Both
+      // tiles share barriers: a wait or a commit costs this warp about as much as two MMAs.
+      auto scores = [&](int i) {
+        const uint32_t k = k_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128);
 #pragma unroll
-        for (int c = 0; c < kSubs; ++c)
-          mma_ss_x4(tmem + 128 * t, sw128_desc(q_base + (t * kSubs + c) * kSub), sw128_desc(k_base + (s * kSubs + c) * kSub),
-                    idesc_s, c > 0);
-        tc_commit_warp(bars.s_full(t));
+        for (int t = 0; t < 2; ++t)
+          if (t < tiles) {
+#pragma unroll
+            for (int c = 0; c < kSubs; ++c)
+              mma_ss_x4(tmem + 128 * t + kHalf * (i & 1), desc_k(q_base + (t * kSubs + c) * kSub), desc_k(k + c * kSub),
+                        idesc_s, c > 0);
+          }
+        tc_commit_warp(bars.s_full(i & 1));
       };
-      auto outputs = [&](int t, int s, bool accumulate) {
-        const uint64_t v = sw128_desc_n_major(v_base + s * kSubs * kSub);
-        mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t, v, idesc_o, accumulate);
-        mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + 32, v + 512, idesc_o, 1);
+      auto outputs = [&](int i) {
+        const uint32_t v = desc_n(v_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128));
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+          if (t < tiles) mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1), v, idesc_o, i > 0);
+        tc_commit_warp(bars.o_full());
       };
-      bool ok = steps > 0 && wait(bars.q_full(), 0) && wait(bars.k_full(0), 0);
+      bool ok = halves > 0 && wait(bars.q_full(), 0) && wait(bars.k_full(0), 0);
       if (ok) {
         tc_fence_after();
-        for (int t = 0; t < tiles; ++t) scores(t, 0);
-        tc_commit_warp(bars.k_empty(0));
+        scores(0);
       }
-      for (int j = 0; ok && j < steps; ++j) {
-        const int s = j & 1, n = s ^ 1;
-        ok = wait(bars.v_full(s), (j >> 1) & 1);
-        for (int t = 0; ok && t < tiles; ++t) {
-          ok = wait(bars.p_full(t), j & 1);
+      for (int i = 0; ok && i < halves; ++i) {
+        const int j = i >> 1, n = i + 1;
+        if (n < halves) {
+          if (!(n & 1)) ok = wait(bars.k_full((n >> 1) & 1), (n >> 2) & 1);
           if (!ok) break;
           tc_fence_after();
-          outputs(t, s, j > 0);
-          if (j + 1 < steps) {
-            if (t == 0) ok = wait(bars.k_full(n), ((j + 1) >> 1) & 1);
-            if (!ok) break;
-            tc_fence_after();
-            scores(t, n);
-          }
+          scores(n);
         }
+        if (!(i & 1)) {  // both halves of the step's keys have been issued
+          tc_commit_warp(bars.k_empty(j & 1));
+          ok = wait(bars.v_full(j & 1), (j >> 1) & 1);
+        }
+        ok = ok && wait(bars.p_full(i & 1), j & 1);
         if (!ok) break;
-        tc_commit_warp(bars.v_empty(s));
-        tc_commit_warp(bars.page_empty(j % kPageRing));
-        if (j + 1 < steps) tc_commit_warp(bars.k_empty(n));
+        tc_fence_after();
+        outputs(i);
+        if ((i & 1) || n == halves) tc_commit_warp(bars.v_empty(j & 1));
       }
       // every MMA issued is over: the outputs are whole, the tensor memory may be given back
       tc_commit_warp(bars.done());
       if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
       __syncwarp();
-    } else if (warp == 1) {
+    } else if (warp == 4) {
       // ---- the steps' pages, a lane each, up to kPageRing steps ahead of the codes (two
       // dependent loads that would otherwise stand in every step's way)
       ctx.err_bits = PQ_ERR_PRODUCER;
@@ -254,78 +269,81 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         __syncwarp();
         if (lane == 0) mbar_arrive(bars.page_full(i));
       }
-    }
-  } else if (warp < 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    // ---- codes to halves
-    ctx.err_bits = PQ_ERR_PRODUCER;
-    const int tid = threadIdx.x - 128;
-    const int C = D / 16;  // 16-byte pieces of a token
-    // A thread takes one 16-byte piece of every (128 / kP)th token.  Eight neighbours hold
-    // four pieces of two tokens, whose halves lie in different banks.
-    constexpr int kP = DP / 16, kTokStep = 128 / kP;
-    const int piece = kP == 8 ? (tid & 3) | ((tid >> 1) & 4) : tid & 3;
-    const int token = kP == 8 ? ((tid >> 3) & ~1) | ((tid >> 2) & 1) : tid >> 2;
-    const bool there = piece < C;
-    const uint32_t row = (piece >> 2) * kSub + token * 128;
-    const uint32_t at0 = row + (((2 * (piece & 3)) ^ (token & 7)) << 4), at1 = row + (((2 * (piece & 3) + 1) ^ (token & 7)) << 4);
-    auto fetch = [&](const int8_t* codes, int j, uint4 (&r)[kP]) {
-      const StepPage* page = pages[j % kPageRing];
+    } else {
+      // ---- codes to halves, six warps
+      ctx.err_bits = PQ_ERR_PRODUCER;
+      const int tid = 32 * (warp < 4 ? warp - 1 : warp - 2) + lane;
+      const int C = D / 16;  // 16-byte pieces of a token
+      // A thread takes one 16-byte piece of every (192 / kP)th token.  Eight neighbours
+      // hold four pieces of two tokens, whose halves lie in different banks.
+      constexpr int kP = DP / 16, kTokStep = 192 / kP, kTurns = (kTokens + kTokStep - 1) / kTokStep;
+      const int piece = kP == 8 ? (tid & 3) | ((tid >> 1) & 4) : tid & 3;
+      const int token = kP == 8 ? ((tid >> 3) & ~1) | ((tid >> 2) & 1) : tid >> 2;
+      const bool there = piece < C;
+      const uint32_t row = (piece >> 2) * kSub + token * 128;
+      const uint32_t at0 = row + (((2 * (piece & 3)) ^ (token & 7)) << 4), at1 = row + (((2 * (piece & 3) + 1) ^ (token & 7)) << 4);
+      auto fetch = [&](const int8_t* codes, int j, uint4 (&r)[kTurns]) {
+        const StepPage* page = pages[j % kPageRing];
 #pragma unroll
-      for (int i = 0; i < kP; ++i) {
-        const int k = token + i * kTokStep;
-        const int64_t base = page[k >> p.page_shift].codes;
-        r[i] = make_uint4(0, 0, 0, 0);
-        if (there && base >= 0)
-          r[i] = *reinterpret_cast<const uint4*>(codes + base + (k & (p.c.page_tokens - 1)) * D + 16 * piece);
-      }
-    };
-    // (columns past D are zeros: the scores' products run over whole blocks of 64)
-    auto store = [&](uint32_t base, const uint4 (&r)[kP]) {
+        for (int i = 0; i < kTurns; ++i) {
+          const int k = token + i * kTokStep;
+          r[i] = make_uint4(0, 0, 0, 0);
+          if (!there || k >= kTokens) continue;
+          const int64_t base = page[k >> p.page_shift].codes;
+          if (base >= 0)
+            r[i] = *reinterpret_cast<const uint4*>(codes + base + (k & (p.c.page_tokens - 1)) * D + 16 * piece);
+        }
+      };
+      // (columns past D are zeros: the scores' products run over whole blocks of 64)
+      auto store = [&](uint32_t base, const uint4 (&r)[kTurns]) {
 #pragma unroll
-      for (int i = 0; i < kP; ++i) {
-        uint32_t h[8];
-        half_of_codes(r[i].x, h[0], h[1]);
-        half_of_codes(r[i].y, h[2], h[3]);
-        half_of_codes(r[i].z, h[4], h[5]);
-        half_of_codes(r[i].w, h[6], h[7]);
-        sts128(base + at0 + i * kTokStep * 128, h[0], h[1], h[2], h[3]);
-        sts128(base + at1 + i * kTokStep * 128, h[4], h[5], h[6], h[7]);
+        for (int i = 0; i < kTurns; ++i) {
+          if (token + i * kTokStep >= kTokens) break;
+          uint32_t h[8];
+          half_of_codes(r[i].x, h[0], h[1]);
+          half_of_codes(r[i].y, h[2], h[3]);
+          half_of_codes(r[i].z, h[4], h[5]);
+          half_of_codes(r[i].w, h[6], h[7]);
+          sts128(base + at0 + i * kTokStep * 128, h[0], h[1], h[2], h[3]);
+          sts128(base + at1 + i * kTokStep * 128, h[4], h[5], h[6], h[7]);
+        }
+      };
+      auto publish = [&](uint32_t bar) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+      };
+      auto look = [&](int j) {
+        return __all_sync(0xffffffffu, mbar_wait(bars.page_full(j % kPageRing), (j / kPageRing) & 1, ctx)) != 0;
+      };
+      uint4 kr[kTurns], vr[kTurns];
+      bool ok = steps > 0 && look(0);
+      if (ok) {
+        fetch(p.c.k_dev, 0, kr);
+        fetch(p.c.v_dev, 0, vr);
       }
-    };
-    auto publish = [&](uint32_t bar) {
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(bar);
-    };
-    auto look = [&](int j) {
-      return __all_sync(0xffffffffu, mbar_wait(bars.page_full(j % kPageRing), (j / kPageRing) & 1, ctx)) != 0;
-    };
-    uint4 kr[kP], vr[kP];
-    bool ok = steps > 0 && look(0);
-    if (ok) {
-      fetch(p.c.k_dev, 0, kr);
-      fetch(p.c.v_dev, 0, vr);
-    }
-    for (int j = 0; ok && j < steps; ++j) {
-      const int s = j & 1;
-      if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.k_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
-      if (!ok) break;
-      store(k_base + s * kSubs * kSub, kr);
-      publish(bars.k_full(s));
-      if (j + 1 < steps) {
-        ok = look(j + 1);
+      for (int j = 0; ok && j < steps; ++j) {
+        const int s = j & 1;
+        if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.k_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
         if (!ok) break;
-        fetch(p.c.k_dev, j + 1, kr);
+        store(k_base + s * kSubs * kSub, kr);
+        publish(bars.k_full(s));
+        if (j + 1 < steps) {
+          ok = look(j + 1);
+          if (!ok) break;
+          fetch(p.c.k_dev, j + 1, kr);
+        }
+        if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.v_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
+        if (!ok) break;
+        // step j - 2 is over: so is every use of its pages
+        if (j > 1 && warp == 1 && lane == 0) mbar_arrive(bars.page_empty((j - 2) % kPageRing));
+        store(v_base + s * kSubs * kSub, vr);
+        publish(bars.v_full(s));
+        if (j + 1 < steps) fetch(p.c.v_dev, j + 1, vr);
       }
-      if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.v_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
-      if (!ok) break;
-      store(v_base + s * kSubs * kSub, vr);
-      publish(bars.v_full(s));
-      if (j + 1 < steps) fetch(p.c.v_dev, j + 1, vr);
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
     // ---- softmax: this thread's row
     ctx.err_bits = PQ_ERR_EPILOGUE;
     const int t = (warp - 8) >> 2;
@@ -368,44 +386,45 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
       const int lo = p.a.window > 0 ? max(0, at - p.a.window) : 0;
       float m = kNone, l = 0.0f;
       bool ok = true;
-      for (int j = 0; j < steps; ++j) {
-        ok = __all_sync(0xffffffffu, mbar_wait(bars.s_full(t), j & 1, ctx)) != 0;
+      for (int i = 0; i < halves; ++i) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bars.s_full(i & 1), (i >> 1) & 1, ctx)) != 0;
         if (!ok) break;
         tc_fence_after();
-        float x[kTokens];
+        const uint32_t buffer = s_mem + kHalf * (i & 1);
+        float x[kHalf];
 #pragma unroll
-        for (int c = 0; c < kTokens; c += 32) {
+        for (int c = 0; c < kHalf; c += 32) {
           uint32_t v[32];
-          tmem_ld32(s_mem + c, v);
+          tmem_ld32(buffer + c, v);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) x[c + i] = __uint_as_float(v[i]);
+          for (int k = 0; k < 32; ++k) x[c + k] = __uint_as_float(v[k]);
         }
         tmem_wait_ld();
-        const StepPage* page = pages[j % kPageRing];
-        const int j0 = from + j * kTokens;
-        const bool whole = __all_sync(0xffffffffu, j0 >= lo && j0 + kTokens <= hi) != 0;
+        const StepPage* page = pages[(i >> 1) % kPageRing];
+        const int c0 = kHalf * (i & 1), j0 = from + i * kHalf;
+        const bool whole = __all_sync(0xffffffffu, j0 >= lo && j0 + kHalf <= hi) != 0;
         // the row's maximum: within 16 tokens of one page that of the raw scores (the scales
         // are not negative)
         float high = m;
         if (whole) {
 #pragma unroll
-          for (int c = 0; c < kTokens; c += 16) {
-            const StepPage& f = page[c >> p.page_shift];
+          for (int c = 0; c < kHalf; c += 16) {
+            const StepPage& f = page[(c0 + c) >> p.page_shift];
             float top = fmaxf(x[c], x[c + 1]);
 #pragma unroll
-            for (int i = 2; i < 16; i += 2) top = fmaxf(top, fmaxf(x[c + i], x[c + i + 1]));
+            for (int k = 2; k < 16; k += 2) top = fmaxf(top, fmaxf(x[c + k], x[c + k + 1]));
             high = fmaxf(high, fmaf(top, f.k * factor, f.log2_v));
           }
         } else {
 #pragma unroll
-          for (int c = 0; c < kTokens; c += 16) {
-            const StepPage& f = page[c >> p.page_shift];
+          for (int c = 0; c < kHalf; c += 16) {
+            const StepPage& f = page[(c0 + c) >> p.page_shift];
             const float g = f.k * factor, lv = f.log2_v;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const bool seen = j0 + c + i >= lo && j0 + c + i < hi;
-              x[c + i] = seen ? fmaf(x[c + i], g, lv) : kNone;
-              high = fmaxf(high, x[c + i]);
+            for (int k = 0; k < 16; ++k) {
+              const bool seen = j0 + c + k >= lo && j0 + c + k < hi;
+              x[c + k] = seen ? fmaf(x[c + k], g, lv) : kNone;
+              high = fmaxf(high, x[c + k]);
             }
           }
         }
@@ -415,8 +434,11 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
           const float alpha = next == kNone ? 1.0f : exp2_approx(m - next);
           m = next;
           l *= alpha;
-          if (j > 0) {
-            // the product before has finished: it was issued before these scores
+          if (i > 0) {
+            // once the product of the half before is over
+            ok = __all_sync(0xffffffffu, mbar_wait(bars.o_full(), (i - 1) & 1, ctx)) != 0;
+            if (!ok) break;
+            tc_fence_after();
 #pragma unroll
             for (int c = 0; c < DP; c += 16) {
               if (c < D) {
@@ -424,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
                 tmem_ld16(o_mem + c, v);
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) * alpha);
+                for (int k = 0; k < 16; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * alpha);
                 tmem_st16(o_mem + c, v);
               }
             }
@@ -432,33 +454,33 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         }
         const float base = m == kNone ? 0.0f : m;
 #pragma unroll
-        for (int c = 0; c < kTokens; c += 32) {
+        for (int c = 0; c < kHalf; c += 32) {
           uint32_t h[16];
 #pragma unroll
           for (int u = 0; u < 32; u += 16) {
-            const StepPage& f = page[(c + u) >> p.page_shift];
+            const StepPage& f = page[(c0 + c + u) >> p.page_shift];
             // seen as a whole: the scores are still raw
             const float g = whole ? f.k * factor : 1.0f, shift = whole ? f.log2_v - base : -base;
             float s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) {
+            for (int k = 0; k < 16; k += 2) {
               float a, b;
-              fma2_rn(x[c + u + i], x[c + u + i + 1], g, shift, a, b);
+              fma2_rn(x[c + u + k], x[c + u + k + 1], g, shift, a, b);
               a = exp2_approx(a);
               b = exp2_approx(b);
               add_pair(s0, s1, a, b);
-              h[(u + i) / 2] = pack_half2(a, b);
+              h[(u + k) / 2] = pack_half2(a, b);
             }
             // a page that the row does not see adds nothing, even with a NaN scale
             const float sum = s0 + s1;
             l += whole || sum != 0.0f ? sum * f.inv_v : 0.0f;
           }
-          tmem_st16(s_mem + c / 2, h);
+          tmem_st16(buffer + c / 2, h);
         }
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bars.p_full(t));
+        if (lane == 0) mbar_arrive(bars.p_full(i & 1));
       }
       // ---- outputs
       if (ok && steps > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars.done(), 0, ctx)) != 0;
@@ -499,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
   if (warp == 0) {
     __syncwarp();
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem_base, 512);
   }
 }
 
