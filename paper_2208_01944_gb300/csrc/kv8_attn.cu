@@ -16,9 +16,11 @@
 // transposed (tokens are the MMA's 16 rows, query rows its 8 columns: a group of up to
 // 8 heads fills it), the probabilities turn into the second product's operand by
 // an 8 x 8 transpose in registers, and the outputs are transposed too (16 rows of D).
-// Codes go from memory to registers to halves; no shared memory in the loop.
-// Few query rows are spread over the chip by splitting the tokens; the parts' maxima,
-// sums and outputs are joined by pq_kv8_join.
+// Codes come through shared memory, three or four steps of each warp in flight (16-byte
+// asynchronous copies into a ring of the warp's own, no block-wide wait): with loads
+// straight into registers a step waited for its page's id and then for its codes, and a
+// batch of single tokens read 3.9 TB/s.  Few query rows are spread over the chip by splitting
+// the tokens; the parts' maxima, sums and outputs are joined by pq_kv8_join.
 //
 // Rounding.  Queries enter as halves scaled by a power of two for each row so that their largest
 // element lies in [2^7, 2^8) (exact for 16-bit queries down to 2^-22 of it), w as
@@ -57,6 +59,45 @@ __device__ __forceinline__ Place place_of(const AttnArgs& p) {
   return r;
 }
 
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(reinterpret_cast<uint64_t>(src)) : "memory");
+}
+__device__ __forceinline__ uint4 lds_16(uint32_t addr) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 lds_8(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float lds_f32(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// A warp's ring: a step is 16 key rows and 16 value rows of DP bytes, then their scales.
+__host__ __device__ constexpr int ring_steps(int DP) { return DP == 64 ? 4 : 3; }
+__host__ __device__ constexpr int step_bytes(int DP) { return 32 * DP + 16; }
+__host__ __device__ constexpr int ring_bytes(int DP) { return kAttnWarps * ring_steps(DP) * step_bytes(DP); }
+
+// Where 16-byte piece c of a row lies: the pieces are exchanged so that the lanes that
+// read together hit different banks.  Keys: rows g, pieces t; values: rows 2 t (and
+// their odd neighbours), the pieces of D rows g.
+template <int DP>
+__device__ __forceinline__ uint32_t key_at(int row, int c) {
+  return DP == 64 ? row * 64 + c * 16 : row * DP + ((c ^ ((row & 1) << 2)) << 4);
+}
+template <int DP>
+__device__ __forceinline__ uint32_t value_at(int row, int c) {
+  const int t = (row >> 1) & 3;
+  if (DP == 64) return (row >> 1) * 128 + ((((row & 1) * 4 + c) ^ (t << 1)) << 4);
+  if (DP == 128) return row * 128 + ((c ^ (t << 1)) << 4);
+  return row * 256 + ((c ^ ((t & 1) | ((t >> 1) << 2))) << 4);
+}
+
 // DP: D rounded up to 64, 128 or 256; NT: tiles of 8 query rows; TWO: fp32 queries
 // and outputs, each operand in two halves.
 template <typename T, int DP, int NT, bool TWO>
@@ -65,9 +106,14 @@ __global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_cons
   constexpr int kJ = DP / 16;        // 16-row tiles of the transposed output
   constexpr int kRows = 8 * NT;
   constexpr int kHalves = TWO ? 2 : 1;
+  constexpr int kSteps = ring_steps(DP);
+  constexpr int kStep = step_bytes(DP);
+  extern __shared__ __align__(16) uint8_t ring_raw[];
   __shared__ float row_factor[kRows];
   __shared__ float join_m[kAttnWarps][kRows], join_l[kAttnWarps][kRows];
-  __shared__ float join_o[kAttnWarps / 2][kJ * NT * 4][32];
+  // the warps' outputs are joined in the ring's place
+  static_assert(kAttnWarps / 2 * kJ * NT * 4 * 32 * 4 <= ring_bytes(DP), "join buffer");
+  float (*join_o)[kJ * NT * 4][32] = reinterpret_cast<float (*)[kJ * NT * 4][32]>(ring_raw);
   const Place w = place_of(p);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int r0 = w.tile * kRows;
@@ -78,7 +124,56 @@ __global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_cons
   const int from = first + w.split * p.chunk;
   const int to = min(sp.hi, from + p.chunk);
   if (w.split > 0 && from >= sp.hi) return;
-  const int D = p.c.D;
+  const int D = p.c.D, C = D / 16;
+
+  // ---- this warp's steps: tokens from + 16 (warp + 8 i) and up, kSteps - 1 of them ahead
+  const int* table = p.a.page_table_dev + static_cast<int64_t>(w.b) * p.a.table_pitch;
+  const uint32_t ring = smem_u32(ring_raw) + warp * kSteps * kStep;
+  auto page_of = [&](int s) {  // page of a step's tokens
+    const int slot = s >> p.page_shift;
+    return s < to && slot < p.a.table_pitch ? table[slot] : -1;
+  };
+  uint32_t valid = 0;  // bit i: the i-th step from now on that is in flight has a page
+  auto issue = [&](int s, int id, int place, int ahead) {
+    if (s < to) {
+      if (id >= 0 && id < p.c.num_pages) {
+        const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
+        const int64_t base = ((ph << p.page_shift) + (s & (p.c.page_tokens - 1))) * D;
+        const uint32_t at = ring + place * kStep;
+        // 16 C pieces of each side; a token's pieces are neighbours
+#pragma unroll
+        for (int e0 = 0; e0 < DP; e0 += 32) {
+          const int e = e0 + lane;
+          int row, c;
+          if (C == kJ) {
+            row = e / kJ, c = e % kJ;
+          } else {
+            row = e / C, c = e - row * C;
+          }
+          if (row < 16) {
+            cp_async_16(at + key_at<DP>(row, c), p.c.k_dev + base + 16 * e, 16);
+            cp_async_16(at + 16 * DP + value_at<DP>(row, c), p.c.v_dev + base + 16 * e, 16);
+          }
+        }
+        if (lane == 0) cp_async_4(at + 32 * DP, p.c.k_scale_dev + ph);
+        if (lane == 1) cp_async_4(at + 32 * DP + 4, p.c.v_scale_dev + ph);
+        valid |= 1u << ahead;
+      } else if (lane == 0) {
+        atomicOr(p.err, PQ_ERR_PAGE);
+      }
+    }
+    cp_async_commit();
+  };
+  const int s0 = from + 16 * warp;
+  int next_id;
+  {
+    int ids[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) ids[i] = page_of(s0 + 16 * kAttnWarps * i);
+#pragma unroll
+    for (int i = 0; i < kSteps - 1; ++i) issue(s0 + 16 * kAttnWarps * i, ids[i], i, i);
+    next_id = ids[kSteps - 1];
+  }
 
   // ---- queries: row 8 j + g, columns 64 c + 16 t and up, as the MMA's second operand
   uint32_t qf[kHalves][NT][kC][8];
@@ -147,43 +242,46 @@ __global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_cons
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[i][j][e] = 0.0f;
 
-  const int* table = p.a.page_table_dev + static_cast<int64_t>(w.b) * p.a.table_pitch;
-  for (int s = from + 16 * warp; s < to; s += 16 * kAttnWarps) {
-    const int slot = s >> p.page_shift;
-    const int id = slot < p.a.table_pitch ? table[slot] : -1;
-    if (id < 0 || id >= p.c.num_pages) {
-      if (lane == 0) atomicOr(p.err, PQ_ERR_PAGE);
-      continue;
+  int place = 0;
+  for (int s = s0; s < to; s += 16 * kAttnWarps) {
+    cp_async_wait<kSteps - 2>();
+    __syncwarp();  // the step has arrived, and every lane is done with the one before
+    const uint32_t at = ring + place * kStep;
+    {
+      const int ahead = s + 16 * kAttnWarps * (kSteps - 1);
+      const int before = place == 0 ? kSteps - 1 : place - 1;
+      issue(ahead, next_id, before, kSteps - 1);
+      next_id = page_of(ahead + 16 * kAttnWarps);
+      place = place + 1 == kSteps ? 0 : place + 1;
     }
-    const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
-    const int64_t base = ((ph << p.page_shift) + (s & (p.c.page_tokens - 1))) * D;
-    const int8_t* kp = p.c.k_dev + base;
-    const int8_t* vp = p.c.v_dev + base;
+    const bool there = valid & 1;
+    valid >>= 1;
+    if (!there) continue;
     // ---- codes: key rows g and g + 8; value rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9
     uint4 kr[kC][2];
 #pragma unroll
     for (int c = 0; c < kC; ++c)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
-        kr[c][i] = 64 * c + 16 * t < D ? *reinterpret_cast<const uint4*>(kp + (g + 8 * i) * D + 64 * c + 16 * t)
-                                       : make_uint4(0, 0, 0, 0);
+        kr[c][i] = 64 * c + 16 * t < D ? lds_16(at + key_at<DP>(g + 8 * i, 4 * c + t)) : make_uint4(0, 0, 0, 0);
     uint32_t vr[4][DP / 32];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int8_t* src = vp + (2 * t + (i & 1) + 8 * (i >> 1)) * D + g * (DP / 8);
+      const int row = 2 * t + (i & 1) + 8 * (i >> 1);
       if (DP == 64) {
-        const uint2 v = g * 8 < D ? *reinterpret_cast<const uint2*>(src) : make_uint2(0, 0);
+        const uint2 v = g * 8 < D ? lds_8(at + 16 * DP + value_at<DP>(row, g >> 1) + 8 * (g & 1)) : make_uint2(0, 0);
         vr[i][0] = v.x, vr[i][1] = v.y;
       } else {
 #pragma unroll
         for (int c = 0; c < DP / 128; ++c) {
-          const uint4 v = g * (DP / 8) + 16 * c < D ? *reinterpret_cast<const uint4*>(src + 16 * c) : make_uint4(0, 0, 0, 0);
+          const int piece = g * (DP / 128) + c;
+          const uint4 v = piece < C ? lds_16(at + 16 * DP + value_at<DP>(row, piece)) : make_uint4(0, 0, 0, 0);
           vr[i][4 * c] = v.x, vr[i][4 * c + 1] = v.y, vr[i][4 * c + 2] = v.z, vr[i][4 * c + 3] = v.w;
         }
       }
     }
-    const float sk = p.c.k_scale_dev[ph];
-    const float sv0 = p.c.v_scale_dev[ph];
+    const float sk = lds_f32(at + 32 * DP);
+    const float sv0 = lds_f32(at + 32 * DP + 4);
     const float sv = sv0 == 0.0f ? 1.0f : sv0;
     const float lv = log2f(sv), inv_v = 1.0f / sv;
 
@@ -273,6 +371,8 @@ __global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_cons
             mma_16x8x16(o[2 * c + i][j], a01[2 * i], a01[2 * i + 1], a23[2 * i], a23[2 * i + 1], pf[hf][j][0], pf[hf][j][1]);
     }
   }
+  cp_async_wait<0>();
+  __syncthreads();  // the ring is idle
   // ---- join the warps: sums over the lanes, then pairs of warps
 #pragma unroll
   for (int j = 0; j < NT; ++j)
@@ -351,29 +451,34 @@ __global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_cons
     }
 }
 
-// Joins the parts of one query row: a warp each.
-template <typename T>
+// Joins the parts of one query row: W warps each, which take the parts in turn (one
+// warp would wait for hundreds of them one after the other).
+template <typename T, int W>
 __global__ void __launch_bounds__(256) pq_kv8_join(const __grid_constant__ AttnArgs p, int tile_rows) {
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
+  __shared__ float sums[W > 1 ? 8 : 1][W > 1 ? 260 : 1];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, part = warp % W;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * (8 / W) + warp / W;
   const int hq = static_cast<int>(at % p.a.Hq);
   const int64_t rest = at / p.a.Hq;
   const int qi = static_cast<int>(rest % p.a.max_q);
   const int64_t b = rest / p.a.max_q;
   wait_previous_kernel();
-  if (b >= p.a.B) return;
+  const bool row = b < p.a.B;
   const int r = qi * p.group + hq % p.group;
-  const Span sp = span_of(p, static_cast<int>(b), r / tile_rows * tile_rows, tile_rows);
-  if (qi >= sp.n) return;
+  Span sp = {};
+  if (row) sp = span_of(p, static_cast<int>(b), r / tile_rows * tile_rows, tile_rows);
   // the parts that the row's tile was cut into (at least the first is there)
   const int first = sp.lo & ~(p.align - 1);
-  const int parts = max(1, min(p.splits, (sp.hi - first + p.chunk - 1) / p.chunk));
+  const int parts = row && qi < sp.n ? max(1, min(p.splits, (sp.hi - first + p.chunk - 1) / p.chunk)) : 0;
   const float2* ml = p.ml + at * p.splits;
   float top = kNone;
-  for (int s = 0; s < parts; ++s) top = fmaxf(top, ml[s].x);
+  for (int s = lane; s < parts; s += 32) top = fmaxf(top, ml[s].x);
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
   const float base = top == kNone ? 0.0f : top;
   float l = 0.0f, o[8] = {};
-  for (int s = 0; s < parts; ++s) {
+#pragma unroll 4
+  for (int s = part; s < parts; s += W) {
     const float2 v = ml[s];
     const float f = exp2_approx(v.x - base);
     l += v.y * f;
@@ -382,6 +487,19 @@ __global__ void __launch_bounds__(256) pq_kv8_join(const __grid_constant__ AttnA
     for (int k = 0; k < 8; ++k)
       if (lane + 32 * k < p.c.D) o[k] += src[lane + 32 * k] * f;
   }
+  if (W > 1) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) sums[W > 1 ? warp : 0][W > 1 ? lane + 32 * k : 0] = o[k];
+    if (lane == 0) sums[W > 1 ? warp : 0][W > 1 ? 256 : 0] = l;
+    __syncthreads();
+    if (part != 0) return;
+    for (int i = 1; i < W; ++i) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[k] += sums[W > 1 ? warp + i : 0][W > 1 ? lane + 32 * k : 0];
+      l += sums[W > 1 ? warp + i : 0][W > 1 ? 256 : 0];
+    }
+  }
+  if (parts == 0) return;
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
   T* dst = static_cast<T*>(p.o) + (static_cast<int64_t>(p.a.cu_q_dev[b]) + qi) * p.a.o_token_stride +
            static_cast<int64_t>(hq) * p.a.o_head_stride;
@@ -450,7 +568,8 @@ template <typename T>
 cudaError_t launch_join(const AttnArgs& p, int tile_rows, cudaStream_t s) {
   const int64_t rows = static_cast<int64_t>(p.a.B) * p.a.max_q * p.a.Hq;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>((rows + 7) / 8));
+  const bool many = p.splits > 8;
+  cfg.gridDim = dim3(static_cast<unsigned>(many ? rows : (rows + 7) / 8));
   cfg.blockDim = dim3(256);
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -458,23 +577,30 @@ cudaError_t launch_join(const AttnArgs& p, int tile_rows, cudaStream_t s) {
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, pq_kv8_join<T>, p, tile_rows);
+  return many ? cudaLaunchKernelEx(&cfg, pq_kv8_join<T, 8>, p, tile_rows) : cudaLaunchKernelEx(&cfg, pq_kv8_join<T, 1>, p, tile_rows);
+}
+
+template <typename T, int DP, int NT, bool TWO>
+cudaError_t launch_rows_as(const AttnArgs& p, unsigned grid, cudaStream_t s) {
+  static int attr_set[64] = {0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  if (dev >= 64 || !attr_set[dev]) {
+    e = cudaFuncSetAttribute(pq_kv8_rows<T, DP, NT, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(DP));
+    if (e != cudaSuccess) return e;
+    if (dev < 64) attr_set[dev] = 1;
+  }
+  pq_kv8_rows<T, DP, NT, TWO><<<grid, 32 * kAttnWarps, ring_bytes(DP), s>>>(p);
+  return cudaGetLastError();
 }
 
 template <typename T, bool TWO>
 cudaError_t launch_rows(const AttnArgs& p, unsigned grid, int nt, cudaStream_t s) {
   const int dp = padded_d(p.c.D);
-  if (dp == 64 && nt == 1)
-    pq_kv8_rows<T, 64, 1, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
-  else if (dp == 64)
-    pq_kv8_rows<T, 64, 2, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
-  else if (dp == 128 && nt == 1)
-    pq_kv8_rows<T, 128, 1, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
-  else if (dp == 128)
-    pq_kv8_rows<T, 128, 2, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
-  else
-    pq_kv8_rows<T, 256, 1, TWO><<<grid, 32 * kAttnWarps, 0, s>>>(p);
-  return cudaGetLastError();
+  if (dp == 64) return nt == 1 ? launch_rows_as<T, 64, 1, TWO>(p, grid, s) : launch_rows_as<T, 64, 2, TWO>(p, grid, s);
+  if (dp == 128) return nt == 1 ? launch_rows_as<T, 128, 1, TWO>(p, grid, s) : launch_rows_as<T, 128, 2, TWO>(p, grid, s);
+  return launch_rows_as<T, 256, 1, TWO>(p, grid, s);
 }
 
 size_t scratch_of(const AttnArgs& p) {
@@ -525,7 +651,7 @@ pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, v
     p.part = reinterpret_cast<float*>(p.ml + parts);
   }
   const int64_t units = static_cast<int64_t>(p.row_tiles) * p.splits * cache->Hkv;
-  if (units > 0x7FFFFFFFll / a->B || static_cast<int64_t>(a->max_q) * a->Hq > (0x7FFFFFFFll * 8) / a->B)
+  if (units > 0x7FFFFFFFll / a->B || static_cast<int64_t>(a->max_q) * a->Hq > 0x7FFFFFFFll / a->B)
     return PQ_EUNSUPPORTED;
   const unsigned grid = static_cast<unsigned>(units * a->B);
   p.err = pq::device_error_word();
