@@ -4,8 +4,8 @@
 // Mathematics.  With codes kc, vc and one scale for each page and head,
 //   x_ij = scale log2(e) s_k(j) sum_d q_id kc_jd,   w_ij = 2^(x_ij + log2 s_v(j) - m_i),
 //   o_id = sum_j w_ij vc_jd / sum_j w_ij / s_v(j),
-// m_i the running maximum of x_ij + log2 s_v(j).  Folding the value scale into the exponent keeps
-// every w in (0, 1] whatever the pages' scales are, so w can be a half value and the
+// m_i the running maximum of x_ij + log2 s_v(j), up to a factor of 2^8.  Folding the value scale into the exponent keeps
+// every w in the halves' range whatever the pages' scales are, so w can be a half value and the
 // products with the codes run without a scale inside the MMA.  (A page whose value
 // scale is 0 holds zeros only; it counts with scale 1.)
 //
@@ -24,7 +24,7 @@
 //
 // Rounding.  Queries enter as halves scaled by a power of two for each row so that their largest
 // element lies in [2^7, 2^8) (exact for 16-bit queries down to 2^-22 of it), w as
-// halves (scaled by 2^8: small ones stay normal); fp32 queries and their w carry a
+// halves (scaled by 2^6: small ones stay normal, and 2^8 more fit); fp32 queries and their w carry a
 // second half for the remainder (22 bits).  All sums are fp32.
 #include <cuda_runtime.h>
 
@@ -39,7 +39,8 @@ namespace pq {
 namespace {
 
 constexpr int kAttnWarps = 8;
-constexpr float kWShift = 8.0f;
+constexpr float kWShift = 6.0f;
+constexpr float kGrow = 8.0f;  // log2 by which a maximum may grow without a rescale
 
 // The block's share of the grid: the row tile changes fastest (its neighbours read
 // the same codes).
@@ -56,6 +57,12 @@ __device__ __forceinline__ Place place_of(const AttnArgs& p) {
   i /= p.splits;
   r.h = i % p.c.Hkv;
   r.b = i / p.c.Hkv;
+  return r;
+}
+
+__device__ __forceinline__ float log2_approx(float x) {
+  float r;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
@@ -101,7 +108,7 @@ __device__ __forceinline__ uint32_t value_at(int row, int c) {
 // DP: D rounded up to 64, 128 or 256; NT: tiles of 8 query rows; TWO: fp32 queries
 // and outputs, each operand in two halves.
 template <typename T, int DP, int NT, bool TWO>
-__global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_constant__ AttnArgs p) {
+__global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO ? 2 : 1) pq_kv8_rows(const __grid_constant__ AttnArgs p) {
   constexpr int kC = DP / 64;        // 64-wide pieces of a key row
   constexpr int kJ = DP / 16;        // 16-row tiles of the transposed output
   constexpr int kRows = 8 * NT;
@@ -230,6 +237,13 @@ __global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_cons
       lo[j][i] = p.a.window > 0 ? max(0, at - p.a.window) : 0;
     }
 
+  // tokens that every row of the tile sees
+  int all_lo = 0, all_hi = sp.len;
+  if (p.a.causal) {
+    all_hi = max(0, sp.len - sp.n + r0 / p.group + 1);
+    if (p.a.window > 0) all_lo = max(0, sp.len - sp.n + (min(rows, r0 + kRows) - 1) / p.group + 1 - p.a.window);
+  }
+
   float m[NT][2], l[NT][2], o[kJ][NT][4];
 #pragma unroll
   for (int j = 0; j < NT; ++j)
@@ -257,33 +271,17 @@ __global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_cons
     const bool there = valid & 1;
     valid >>= 1;
     if (!there) continue;
-    // ---- codes: key rows g and g + 8; value rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+    // ---- codes: key rows g and g + 8
     uint4 kr[kC][2];
 #pragma unroll
     for (int c = 0; c < kC; ++c)
 #pragma unroll
       for (int i = 0; i < 2; ++i)
         kr[c][i] = 64 * c + 16 * t < D ? lds_16(at + key_at<DP>(g + 8 * i, 4 * c + t)) : make_uint4(0, 0, 0, 0);
-    uint32_t vr[4][DP / 32];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = 2 * t + (i & 1) + 8 * (i >> 1);
-      if (DP == 64) {
-        const uint2 v = g * 8 < D ? lds_8(at + 16 * DP + value_at<DP>(row, g >> 1) + 8 * (g & 1)) : make_uint2(0, 0);
-        vr[i][0] = v.x, vr[i][1] = v.y;
-      } else {
-#pragma unroll
-        for (int c = 0; c < DP / 128; ++c) {
-          const int piece = g * (DP / 128) + c;
-          const uint4 v = piece < C ? lds_16(at + 16 * DP + value_at<DP>(row, piece)) : make_uint4(0, 0, 0, 0);
-          vr[i][4 * c] = v.x, vr[i][4 * c + 1] = v.y, vr[i][4 * c + 2] = v.z, vr[i][4 * c + 3] = v.w;
-        }
-      }
-    }
     const float sk = lds_f32(at + 32 * DP);
     const float sv0 = lds_f32(at + 32 * DP + 4);
     const float sv = sv0 == 0.0f ? 1.0f : sv0;
-    const float lv = log2f(sv), inv_v = 1.0f / sv;
+    const float lv = log2_approx(sv), inv_v = exp2_approx(-lv);  // of one another, whatever the rounding
 
     // ---- scores
     float x[NT][4];
@@ -307,54 +305,79 @@ __global__ void __launch_bounds__(32 * kAttnWarps) pq_kv8_rows(const __grid_cons
             mma_16x8x16(x[j], a0, a1, a2, a3, qf[hf][j][c][2 * i], qf[hf][j][c][2 * i + 1]);
       }
     }
-    // ---- probabilities
+    // ---- probabilities, of the running maximum as it was; only where a score has grown
+    // past it by more than 2^8 (w could leave the halves' range) is it brought up to date
     uint32_t pf[kHalves][NT][2];
-    bool grew = false;
-    float alpha[NT][2];
+    float wv[NT][4];
+    bool seen[NT][4], grew = false;
+    const bool whole = s >= all_lo && s + 16 <= all_hi;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      float wv[4];
-      bool seen[4];
-      float top[2] = {m[j][0], m[j][1]};
+    for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = e & 1, at = s + g + 8 * (e >> 1);
-        seen[e] = at >= lo[j][i] && at < hi[j][i];
-        wv[e] = fmaf(x[j][e], sk * factor[j][i], lv);
-        if (seen[e]) top[i] = fmaxf(top[i], wv[e]);
+        const int i = e & 1, token = s + g + 8 * (e >> 1);
+        seen[j][e] = whole || (token >= lo[j][i] && token < hi[j][i]);
+        wv[j][e] = fmaf(x[j][e], sk * factor[j][i], lv);
+        grew |= seen[j][e] && wv[j][e] > m[j][i] + kGrow;
       }
+    if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int j = 0; j < NT; ++j) {
+        float alpha[2];
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], d));
-        const float at = top[i] == kNone ? 0.0f : top[i];
-        alpha[j][i] = exp2_approx(m[j][i] - at);
-        grew |= top[i] != m[j][i];
-        m[j][i] = top[i];
-        top[i] = at - kWShift;
+        for (int i = 0; i < 2; ++i) {
+          float top = m[j][i];
+          if (seen[j][i]) top = fmaxf(top, wv[j][i]);
+          if (seen[j][i + 2]) top = fmaxf(top, wv[j][i + 2]);
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+          alpha[i] = top == kNone ? 1.0f : exp2_approx(m[j][i] - top);
+          m[j][i] = top;
+          l[j][i] *= alpha[i];
+        }
+#pragma unroll
+        for (int i = 0; i < kJ; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[i][j][e] *= alpha[e & 1];
       }
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) wv[e] = seen[e] ? exp2_approx(wv[e] - top[e & 1]) : 0.0f;
+    for (int j = 0; j < NT; ++j) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float base = m[j][e & 1] == kNone ? 0.0f : m[j][e & 1];
+        wv[j][e] = seen[j][e] ? exp2_approx(wv[j][e] - base + kWShift) : 0.0f;
+      }
 #pragma unroll
       for (int i = 0; i < 2; ++i)  // a page that the row does not see adds nothing, even with a NaN scale
-        l[j][i] = l[j][i] * alpha[j][i] + (seen[i] || seen[i + 2] ? (wv[i] + wv[i + 2]) * inv_v : 0.0f);
+        l[j][i] += seen[j][i] || seen[j][i + 2] ? (wv[j][i] + wv[j][i + 2]) * inv_v : 0.0f;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const uint32_t h = pack_half2(wv[2 * i], wv[2 * i + 1]);
+        const uint32_t h = pack_half2(wv[j][2 * i], wv[j][2 * i + 1]);
         pf[0][j][i] = transpose_8x8(h);
         if (TWO) {
           const __half2 hh = *reinterpret_cast<const __half2*>(&h);
-          pf[kHalves - 1][j][i] = transpose_8x8(pack_half2(wv[2 * i] - __low2float(hh), wv[2 * i + 1] - __high2float(hh)));
+          pf[kHalves - 1][j][i] =
+              transpose_8x8(pack_half2(wv[j][2 * i] - __low2float(hh), wv[j][2 * i + 1] - __high2float(hh)));
         }
       }
     }
-    if (__any_sync(0xffffffffu, grew)) {
+    // ---- codes: value rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+    uint32_t vr[4][DP / 32];
 #pragma unroll
-      for (int i = 0; i < kJ; ++i)
+    for (int i = 0; i < 4; ++i) {
+      const int row = 2 * t + (i & 1) + 8 * (i >> 1);
+      if (DP == 64) {
+        const uint2 v = g * 8 < D ? lds_8(at + 16 * DP + value_at<DP>(row, g >> 1) + 8 * (g & 1)) : make_uint2(0, 0);
+        vr[i][0] = v.x, vr[i][1] = v.y;
+      } else {
 #pragma unroll
-        for (int j = 0; j < NT; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[i][j][e] *= alpha[j][e & 1];
+        for (int c = 0; c < DP / 128; ++c) {
+          const int piece = g * (DP / 128) + c;
+          const uint4 v = piece < C ? lds_16(at + 16 * DP + value_at<DP>(row, piece)) : make_uint4(0, 0, 0, 0);
+          vr[i][4 * c] = v.x, vr[i][4 * c + 1] = v.y, vr[i][4 * c + 2] = v.z, vr[i][4 * c + 3] = v.w;
+        }
+      }
     }
     // ---- outputs: tile i holds D rows g (DP/8) + 2 i (its rows 0-7) and + 2 i + 1 (rows 8-15)
 #pragma unroll
@@ -537,8 +560,10 @@ bool valid_attn(const pq_kv8_cache* c, const pq_kv8_attn* a) {
 }
 
 // Which kernel, its row tiles, and the parts of the token range.  Few query rows are
-// spread over the chip by cutting the tokens: four blocks an SM of at least 256 tokens
-// (two steps of every warp), or, on the tensor cores, one block an SM of at least 512.
+// spread over the chip by cutting the tokens: two blocks an SM (as many as fit) of at
+// least 256 tokens (two steps of every warp), or, on the tensor cores, one block an SM of
+// at least 512.  Four blocks an SM cost the joining kernel more than they won (one token
+// over 130001: 46 us, two 38 us).
 struct Plan {
   bool tc;
   int rows;  // query rows of a tile
@@ -555,7 +580,7 @@ Plan plan_attention(const pq_kv8_cache* c, const pq_kv8_attn* a, AttnArgs* p) {
   if (a->window > 0) range = std::min<int64_t>(range, static_cast<int64_t>(a->window) + plan.rows + p->align);
   range = std::max<int64_t>(range, 1);
   const int64_t units = static_cast<int64_t>(a->B) * c->Hkv * p->row_tiles;
-  const int64_t want = ((plan.tc ? 1 : 4) * static_cast<int64_t>(sm_count()) + units - 1) / units;
+  const int64_t want = ((plan.tc ? 1 : 2) * static_cast<int64_t>(sm_count()) + units - 1) / units;
   const int64_t least = plan.tc ? 512 : 256;
   const int64_t splits = std::max<int64_t>(1, std::min(want, (range + least - 1) / least));
   const int64_t chunk = ((range + splits - 1) / splits + 127) / 128 * 128;
