@@ -585,7 +585,7 @@ typedef struct {
  * with scale s_old, the scale becomes s = max(s_old, s of the new tokens) and the
  * earlier codes, where s grew, clamp(rint(fl(code * fl(s_old * inv))), -127, 127).  Slots
  * after the run are left as they are.  No page may be touched by two sequences of
- * one call. */
+ * one call.  B <= 65535. */
 pq_status palquant_kv8_append(const pq_kv8_cache* cache, const void* k_dev, const void* v_dev,
                               const pq_kv8_tokens* t, pq_stream_t stream);
 

@@ -35,12 +35,9 @@ struct KvUnit {
 
 __device__ __forceinline__ KvUnit kv_unit(const KvArgs& a) {
   KvUnit u;
-  unsigned r = blockIdx.x;
-  u.side = r & 1;
-  r >>= 1;
-  u.h = r % a.c.Hkv;
-  r /= a.c.Hkv;
-  const int blk = r % a.blocks, b = r / a.blocks;
+  const int b = blockIdx.y, blk = (blockIdx.x >> 1) / a.c.Hkv;
+  u.side = blockIdx.x & 1;
+  u.h = (blockIdx.x >> 1) - blk * a.c.Hkv;
   const int T = a.c.page_tokens;
   const int start = a.t.start_dev[b], cu = a.t.cu_dev[b];
   const int n = min(a.t.cu_dev[b + 1] - cu, a.t.max_n);
@@ -85,14 +82,14 @@ __global__ void __launch_bounds__(kKvThreads) pq_kv8_append(const __grid_constan
   if (NV > 0) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int v = threadIdx.x + i * kKvThreads;
+      const int v = threadIdx.x + i * blockDim.x;
       if (v < nvec) {
         keep[i] = get(v);
         top = max(top, amax8(keep[i]));
       }
     }
   } else {
-    for (int v = threadIdx.x; v < nvec; v += kKvThreads) top = max(top, amax8(get(v)));
+    for (int v = threadIdx.x; v < nvec; v += blockDim.x) top = max(top, amax8(get(v)));
   }
   top = block_max(top, red);  // every thread has read the old scale before it
   const float fresh = scale_of_amax(top);
@@ -102,23 +99,23 @@ __global__ void __launch_bounds__(kKvThreads) pq_kv8_append(const __grid_constan
   if (u.first > 0 && scale != was) {  // also where either is NaN
     const float ratio = __fmul_rn(was, inv);
     uint32_t* w = reinterpret_cast<uint32_t*>(q);
-    for (int v = threadIdx.x; v < u.first * a.c.D / 4; v += kKvThreads) {
-      const uint32_t o = w[v];
-      int c[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) c[i] = code_of(static_cast<float>(static_cast<int8_t>(o >> (8 * i))), ratio);
-      w[v] = pack_bytes(c[0], c[1], c[2], c[3]);
+    for (int v = threadIdx.x; v < u.first * a.c.D / 4; v += blockDim.x) {
+      float c[4];
+      floats_of_codes(w[v], c);
+      rounded_pair(c[0], c[1], ratio, c[0], c[1]);
+      rounded_pair(c[2], c[3], ratio, c[2], c[3]);
+      w[v] = ratio > 0.0f ? low_bytes(c[0], c[1], c[2], c[3]) : 0u;
     }
   }
   uint2* dst = reinterpret_cast<uint2*>(q + static_cast<int64_t>(u.first) * a.c.D);
   if (NV > 0) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int v = threadIdx.x + i * kKvThreads;
+      const int v = threadIdx.x + i * blockDim.x;
       if (v < nvec) dst[v] = codes8(keep[i], inv);
     }
   } else {
-    for (int v = threadIdx.x; v < nvec; v += kKvThreads) dst[v] = codes8(get(v), inv);
+    for (int v = threadIdx.x; v < nvec; v += blockDim.x) dst[v] = codes8(get(v), inv);
   }
 }
 
@@ -134,31 +131,40 @@ __global__ void __launch_bounds__(kKvThreads) pq_kv8_read(const __grid_constant_
   const uint2* q = reinterpret_cast<const uint2*>((u.side ? a.c.v_dev : a.c.k_dev) + slot0 * a.c.D);
   const float scale = (u.side ? a.c.v_scale_dev : a.c.k_scale_dev)[u.page * a.c.Hkv + u.h];
   const bool wide = a.wide[u.side];
-  for (int v = threadIdx.x; v < u.count * D8; v += kKvThreads) {
+  for (int v = threadIdx.x; v < u.count * D8; v += blockDim.x) {
     const uint2 c = q[v];
+    float f[2][4];
+    floats_of_codes(c.x, f[0]);
+    floats_of_codes(c.y, f[1]);
     Vec8<T> r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      r.v[i] = from_f32<T>(__fmul_rn(static_cast<float>(static_cast<int8_t>((i < 4 ? c.x : c.y) >> (8 * (i & 3)))), scale));
+    for (int i = 0; i < 8; ++i) r.v[i] = from_f32<T>(__fmul_rn(f[i >> 2][i & 3], scale));
     store8(x + (v / D8) * ts + (v % D8) * 8, r, 8, wide);
   }
 }
 
+// Threads of a block: enough for the vectors of 8 that a page and head can receive.
+int threads_of(const KvArgs& a) {
+  const int tokens = a.c.page_tokens < a.t.max_n ? a.c.page_tokens : a.t.max_n;
+  const int vecs = tokens * (a.c.D / 8);
+  return vecs <= 64 ? 64 : vecs <= 128 ? 128 : kKvThreads;
+}
+
 template <typename T>
-void launch_append(const KvArgs& a, unsigned grid, cudaStream_t s) {
-  const int vecs = a.c.page_tokens * (a.c.D / 8);
-  const int most = (vecs < a.t.max_n * (a.c.D / 8) ? vecs : a.t.max_n * (a.c.D / 8));
-  const int nv = (most + kKvThreads - 1) / kKvThreads;
+void launch_append(const KvArgs& a, dim3 grid, cudaStream_t s) {
+  const int threads = threads_of(a);
+  const int tokens = a.c.page_tokens < a.t.max_n ? a.c.page_tokens : a.t.max_n;
+  const int nv = (tokens * (a.c.D / 8) + threads - 1) / threads;
   if (nv <= 1)
-    pq_kv8_append<T, 1><<<grid, kKvThreads, 0, s>>>(a);
+    pq_kv8_append<T, 1><<<grid, threads, 0, s>>>(a);
   else if (nv <= 2)
-    pq_kv8_append<T, 2><<<grid, kKvThreads, 0, s>>>(a);
+    pq_kv8_append<T, 2><<<grid, threads, 0, s>>>(a);
   else if (nv <= 4)
-    pq_kv8_append<T, 4><<<grid, kKvThreads, 0, s>>>(a);
+    pq_kv8_append<T, 4><<<grid, threads, 0, s>>>(a);
   else if (nv <= 8)
-    pq_kv8_append<T, 8><<<grid, kKvThreads, 0, s>>>(a);
+    pq_kv8_append<T, 8><<<grid, threads, 0, s>>>(a);
   else
-    pq_kv8_append<T, 0><<<grid, kKvThreads, 0, s>>>(a);
+    pq_kv8_append<T, 0><<<grid, threads, 0, s>>>(a);
 }
 
 }  // namespace
@@ -173,10 +179,10 @@ bool valid_kv8_cache(const pq_kv8_cache* c) {
 
 namespace {
 
-// Checks what both calls share and fills the launch; *grid = 0: nothing to do.
+// Checks what both calls share and fills the launch; an empty grid: nothing to do.
 pq_status kv_args(const pq_kv8_cache* c, const pq_kv8_tokens* t, const void* k, const void* v, KvArgs* a,
-                  unsigned* grid) {
-  *grid = 0;
+                  dim3* grid) {
+  *grid = dim3(0);
   if (!valid_kv8_cache(c) || t == nullptr) return PQ_EINVAL;
   if (t->type != PQ_F32 && t->type != PQ_F16 && t->type != PQ_BF16) return PQ_EINVAL;
   if (t->B < 0 || t->max_n < 0 || t->table_pitch < 0) return PQ_EINVAL;
@@ -195,8 +201,8 @@ pq_status kv_args(const pq_kv8_cache* c, const pq_kv8_tokens* t, const void* k, 
   a->err = device_error_word();
   if (a->err == nullptr) return PQ_ECUDA;
   const int64_t units = 2ll * c->Hkv * a->blocks;
-  if (units > 0x7FFFFFFFll / t->B) return PQ_EUNSUPPORTED;
-  *grid = static_cast<unsigned>(units * t->B);
+  if (units > 0x7FFFFFFFll || t->B > 65535) return PQ_EUNSUPPORTED;
+  *grid = dim3(static_cast<unsigned>(units), static_cast<unsigned>(t->B));
   return PQ_OK;
 }
 
@@ -209,9 +215,9 @@ pq_status palquant_kv8_append(const pq_kv8_cache* cache, const void* k_dev, cons
                               const pq_kv8_tokens* t, pq_stream_t stream) {
   if (t != nullptr && t->B > 0 && t->max_n > 0 && (k_dev == nullptr || v_dev == nullptr)) return PQ_EINVAL;
   pq::KvArgs a = {};
-  unsigned grid = 0;
+  dim3 grid(0);
   const pq_status st = pq::kv_args(cache, t, k_dev, v_dev, &a, &grid);
-  if (st != PQ_OK || grid == 0) return st;
+  if (st != PQ_OK || grid.x == 0) return st;
   a.in[0] = k_dev;
   a.in[1] = v_dev;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
@@ -228,18 +234,18 @@ pq_status palquant_kv8_read(const pq_kv8_cache* cache, void* k_dev, void* v_dev,
                             pq_stream_t stream) {
   if (t != nullptr && t->B > 0 && t->max_n > 0 && k_dev == nullptr && v_dev == nullptr) return PQ_EINVAL;
   pq::KvArgs a = {};
-  unsigned grid = 0;
+  dim3 grid(0);
   const pq_status st = pq::kv_args(cache, t, k_dev, v_dev, &a, &grid);
-  if (st != PQ_OK || grid == 0) return st;
+  if (st != PQ_OK || grid.x == 0) return st;
   a.out[0] = k_dev;
   a.out[1] = v_dev;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   if (t->type == PQ_F32)
-    pq::pq_kv8_read<float><<<grid, pq::kKvThreads, 0, s>>>(a);
+    pq::pq_kv8_read<float><<<grid, pq::threads_of(a), 0, s>>>(a);
   else if (t->type == PQ_F16)
-    pq::pq_kv8_read<__half><<<grid, pq::kKvThreads, 0, s>>>(a);
+    pq::pq_kv8_read<__half><<<grid, pq::threads_of(a), 0, s>>>(a);
   else
-    pq::pq_kv8_read<__nv_bfloat16><<<grid, pq::kKvThreads, 0, s>>>(a);
+    pq::pq_kv8_read<__nv_bfloat16><<<grid, pq::threads_of(a), 0, s>>>(a);
   return cudaGetLastError() == cudaSuccess ? PQ_OK : PQ_ECUDA;
 }
 

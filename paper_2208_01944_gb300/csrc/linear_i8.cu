@@ -62,10 +62,7 @@ __global__ void __launch_bounds__(kTokThreads) pq_quantize_tokens(const T* __res
     const int left = K - 8 * v;
     const bool wide = wide_q && left >= 8;
     if (HALF) {
-      Vec8<__half> h;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) h.v[i] = __int2half_rn(code_of(to_f32(r.v[i]), inv));
-      store8(static_cast<__half*>(q) + m * ldq + 8 * v, h, left, wide);
+      store8(static_cast<__half*>(q) + m * ldq + 8 * v, half_codes8(r, inv), left, wide);
     } else {
       const uint2 c = codes8(r, inv);
       int8_t* dst = static_cast<int8_t*>(q) + m * ldq + 8 * v;
@@ -134,7 +131,8 @@ __device__ __forceinline__ void half16(const void* q, int64_t row, int k, int K,
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       const Vec8<__half> v = load8(p + 8 * j, K - k - 8 * j, WIDE && k + 8 * j + 8 <= K);
-      const uint4 u = *reinterpret_cast<const uint4*>(&v);
+      uint4 u;
+      memcpy(&u, &v, sizeof(u));
       r[4 * j] = u.x, r[4 * j + 1] = u.y, r[4 * j + 2] = u.z, r[4 * j + 3] = u.w;
     }
   } else {

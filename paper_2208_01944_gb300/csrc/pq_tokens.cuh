@@ -7,6 +7,7 @@
 
 #include <cfloat>
 #include <cstdint>
+#include <cstring>
 
 #include "pq_device.cuh"
 
@@ -45,9 +46,10 @@ template <typename T>
 __device__ __forceinline__ Vec8<T> load8(const T* p, int n, bool wide) {
   Vec8<T> r;
   if (wide) {
-    uint4* q = reinterpret_cast<uint4*>(&r);
+    uint4 q[sizeof(r) / 16];
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(r) / 16); ++i) q[i] = reinterpret_cast<const uint4*>(p)[i];
+    memcpy(&r, q, sizeof(r));
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) r.v[i] = i < n ? p[i] : from_f32<T>(0.0f);
@@ -58,7 +60,8 @@ __device__ __forceinline__ Vec8<T> load8(const T* p, int n, bool wide) {
 template <typename T>
 __device__ __forceinline__ void store8(T* p, const Vec8<T>& r, int n, bool wide) {
   if (wide) {
-    const uint4* q = reinterpret_cast<const uint4*>(&r);
+    uint4 q[sizeof(r) / 16];
+    memcpy(q, &r, sizeof(r));
 #pragma unroll
     for (int i = 0; i < static_cast<int>(sizeof(r) / 16); ++i) reinterpret_cast<uint4*>(p)[i] = q[i];
   } else {
@@ -73,12 +76,24 @@ __device__ __forceinline__ void store8(T* p, const Vec8<T>& r, int n, bool wide)
 // that of the values, with infinities and NaN above every number.
 __device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
 
+// Of eight elements, as 32-bit float bits.  16-bit elements are compared in pairs.
 template <typename T>
 __device__ __forceinline__ uint32_t amax8(const Vec8<T>& r) {
-  uint32_t m = 0;
+  if constexpr (sizeof(T) == 2) {
+    uint32_t w[4];
+    memcpy(w, &r, sizeof(w));
+    uint32_t m = __vmaxu2(__vmaxu2(w[0] & 0x7FFF7FFFu, w[1] & 0x7FFF7FFFu), __vmaxu2(w[2] & 0x7FFF7FFFu, w[3] & 0x7FFF7FFFu));
+    m = max(m & 0xFFFFu, m >> 16);
+    const unsigned short bits = static_cast<unsigned short>(m);
+    T top;
+    memcpy(&top, &bits, sizeof(top));
+    return abs_bits(to_f32(top));
+  } else {
+    uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) m = max(m, abs_bits(to_f32(r.v[i])));
-  return m;
+    for (int i = 0; i < 8; ++i) m = max(m, abs_bits(to_f32(r.v[i])));
+    return m;
+  }
 }
 
 __device__ __forceinline__ float scale_of_amax(uint32_t bits) {
@@ -90,22 +105,60 @@ __device__ __forceinline__ float scale_of_amax(uint32_t bits) {
 // fl(1/s), 0 for the scales 0 and NaN (whose codes are 0).
 __device__ __forceinline__ float inverse_of_scale(float s) { return s > 0.0f ? __frcp_rn(s) : 0.0f; }
 
-// clamp(rint(fl(x * inv)), -127, 127); 0 where inv is 0, whatever x is.
-__device__ __forceinline__ int code_of(float x, float inv) {
-  const int c = __float2int_rn(__fmul_rn(x, inv));  // NaN (an infinity or NaN under inv = 0) -> 0
-  return min(max(c, -127), 127);
+// clamp(rint(fl(x * inv)), -127, 127) of values that lie under the scale: fl(x * inv) is
+// at most 127 (1 + 2^-22) and needs no clamp, and adding 1.5 * 2^23 rounds it to the nearest
+// integer, half to even, into the low bits of the sum (a conversion to an integer runs at
+// a quarter of the rate of an addition's half).  Where inv is 0 the codes are 0
+// whatever x is.
+constexpr float kRound = 12582912.0f;  // 1.5 * 2^23
+__device__ __forceinline__ float rounded_bits(float x, float inv) { return __fadd_rn(__fmul_rn(x, inv), kRound); }
+
+// (a, b) as rounded_bits.  Not with the packed forms of both operations: the compiler
+// contracts a packed product and sum into one rounding, which decides ties differently.
+__device__ __forceinline__ void rounded_pair(float a, float b, float inv, float& x, float& y) {
+  x = rounded_bits(a, inv);
+  y = rounded_bits(b, inv);
 }
 
-__device__ __forceinline__ uint32_t pack_bytes(int a, int b, int c, int d) {
-  return __byte_perm(__byte_perm(a, b, 0x0040), __byte_perm(c, d, 0x0040), 0x5410);
+__device__ __forceinline__ uint32_t low_bytes(float a, float b, float c, float d) {
+  return __byte_perm(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x0040),
+                     __byte_perm(__float_as_uint(c), __float_as_uint(d), 0x0040), 0x5410);
 }
 
 template <typename T>
 __device__ __forceinline__ uint2 codes8(const Vec8<T>& r, float inv) {
-  int c[8];
+  float c[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) c[i] = code_of(to_f32(r.v[i]), inv);
-  return make_uint2(pack_bytes(c[0], c[1], c[2], c[3]), pack_bytes(c[4], c[5], c[6], c[7]));
+  for (int i = 0; i < 8; i += 2) rounded_pair(to_f32(r.v[i]), to_f32(r.v[i + 1]), inv, c[i], c[i + 1]);
+  const uint2 w = make_uint2(low_bytes(c[0], c[1], c[2], c[3]), low_bytes(c[4], c[5], c[6], c[7]));
+  return inv > 0.0f ? w : make_uint2(0, 0);
+}
+
+// The same codes as halves.
+template <typename T>
+__device__ __forceinline__ Vec8<__half> half_codes8(const Vec8<T>& r, float inv) {
+  Vec8<__half> h;
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    float a, b;
+    rounded_pair(to_f32(r.v[i]), to_f32(r.v[i + 1]), inv, a, b);
+    add2_rn(a, b, -kRound, a, b);
+    uint32_t v;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(v) : "f"(b), "f"(a));
+    w[i / 2] = inv > 0.0f ? v : 0u;
+  }
+  memcpy(&h, w, sizeof(w));
+  return h;
+}
+
+// Four codes as fp32: the byte u = code + 128 in the low bits of 2^23 + u, less 2^23 + 128.
+__device__ __forceinline__ void floats_of_codes(uint32_t w, float (&r)[4]) {
+  const uint32_t u = w ^ 0x80808080u;
+  add2_rn(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7440)), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7441)), -8388736.0f,
+          r[0], r[1]);
+  add2_rn(__uint_as_float(__byte_perm(u, 0x4B000000u, 0x7442)), __uint_as_float(__byte_perm(u, 0x4B000000u, 0x7443)), -8388736.0f,
+          r[2], r[3]);
 }
 
 // Largest of all threads' values, for blocks of up to 8 warps; red: 8 words of
