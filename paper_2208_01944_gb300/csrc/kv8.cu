@@ -1,10 +1,15 @@
 // The paged 8-bit cache of keys and values: append (quantise in) and read (values
 // out).  One scale covers a page's tokens of one head, so a block of threads owns
-// one (page, head, side): it finds the scale of what the page will hold, rewrites
-// the earlier codes where the scale grew, and writes the new ones.  New tokens stay
-// in registers between the search for their largest magnitude and the rounding.
+// a (page, head, side) at a time: it finds the scale of what the page will hold,
+// rewrites the earlier codes where the scale grew, and writes the new ones.  New tokens
+// stay in registers between the search for their largest magnitude and the rounding.
+// Reading, a block takes several heads of a small page: the lookups (run, page) are three
+// dependent loads (16 tokens a page, 8 x 2000 tokens of 8 heads of 128: 28 us one head
+// a block, 21 us eight).
 // Bound by HBM: each new element is read once and each code written once.
 #include <cuda_runtime.h>
+
+#include <algorithm>
 
 #include "palquant.h"
 #include "pq_internal.h"
@@ -21,13 +26,14 @@ struct KvArgs {
   const void* in[2];  // k, v (append)
   void* out[2];       // k, v (read); either may be NULL
   int blocks;         // pages of a sequence that a run can touch
+  int heads;          // heads of one block of threads
   unsigned int* err;
   bool wide[2];  // rows of the float tensor on 16-byte boundaries
 };
 
-// What a block of threads works on: side, head, and the run's tokens in one page.
+// What a block of threads works on: side, heads, and the run's tokens in one page.
 struct KvUnit {
-  int side, h;
+  int side, h, h_end;
   int64_t row;      // float row of the run's first token in the page
   int first, count; // slots [first, first + count) of the page belong to the run
   int64_t page;     // -1: none (nothing to do)
@@ -35,9 +41,11 @@ struct KvUnit {
 
 __device__ __forceinline__ KvUnit kv_unit(const KvArgs& a) {
   KvUnit u;
-  const int b = blockIdx.y, blk = (blockIdx.x >> 1) / a.c.Hkv;
+  const int groups = (a.c.Hkv + a.heads - 1) / a.heads;
+  const int b = blockIdx.y, blk = (blockIdx.x >> 1) / groups;
   u.side = blockIdx.x & 1;
-  u.h = (blockIdx.x >> 1) - blk * a.c.Hkv;
+  u.h = ((blockIdx.x >> 1) - blk * groups) * a.heads;
+  u.h_end = min(u.h + a.heads, a.c.Hkv);
   const int T = a.c.page_tokens;
   const int start = a.t.start_dev[b], cu = a.t.cu_dev[b];
   const int n = min(a.t.cu_dev[b + 1] - cu, a.t.max_n);
@@ -59,9 +67,11 @@ __device__ __forceinline__ KvUnit kv_unit(const KvArgs& a) {
   return u;
 }
 
-// NV: vectors of 8 elements that a thread keeps; 0: the tokens are read twice.
+// NV: vectors of 8 elements that a thread keeps; 0: the tokens are read twice.  Up to 64
+// bytes of them, six blocks fit an SM (42 registers; with the 47 that the compiler would
+// take five fit, and 16 prompts of up to 4096 tokens took 89 us instead of 71).
 template <typename T, int NV>
-__global__ void __launch_bounds__(kKvThreads) pq_kv8_append(const __grid_constant__ KvArgs a) {
+__global__ void __launch_bounds__(kKvThreads, sizeof(T) * NV > 8 ? 1 : 6) pq_kv8_append(const __grid_constant__ KvArgs a) {
   __shared__ uint32_t red[8];
   const KvUnit u = kv_unit(a);
   if (u.page < 0) return;
@@ -83,11 +93,11 @@ __global__ void __launch_bounds__(kKvThreads) pq_kv8_append(const __grid_constan
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int v = threadIdx.x + i * blockDim.x;
-      if (v < nvec) {
-        keep[i] = get(v);
-        top = max(top, amax8(keep[i]));
-      }
+      if (v < nvec) keep[i] = get(v);
     }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+      if (threadIdx.x + i * blockDim.x < nvec) top = max(top, amax8(keep[i]));
   } else {
     for (int v = threadIdx.x; v < nvec; v += blockDim.x) top = max(top, amax8(get(v)));
   }
@@ -126,28 +136,34 @@ __global__ void __launch_bounds__(kKvThreads) pq_kv8_read(const __grid_constant_
   const int D8 = a.c.D / 8;
   const int64_t ts = u.side ? a.t.v_token_stride : a.t.k_token_stride;
   const int64_t hs = u.side ? a.t.v_head_stride : a.t.k_head_stride;
-  T* x = static_cast<T*>(a.out[u.side]) + u.row * ts + u.h * hs;
-  const int64_t slot0 = (u.page * a.c.Hkv + u.h) * a.c.page_tokens + u.first;
-  const uint2* q = reinterpret_cast<const uint2*>((u.side ? a.c.v_dev : a.c.k_dev) + slot0 * a.c.D);
-  const float scale = (u.side ? a.c.v_scale_dev : a.c.k_scale_dev)[u.page * a.c.Hkv + u.h];
+  T* rows = static_cast<T*>(a.out[u.side]) + u.row * ts;
+  const int8_t* codes = u.side ? a.c.v_dev : a.c.k_dev;
+  const float* scales = (u.side ? a.c.v_scale_dev : a.c.k_scale_dev) + u.page * a.c.Hkv;
   const bool wide = a.wide[u.side];
-  for (int v = threadIdx.x; v < u.count * D8; v += blockDim.x) {
-    const uint2 c = q[v];
-    float f[2][4];
-    floats_of_codes(c.x, f[0]);
-    floats_of_codes(c.y, f[1]);
-    Vec8<T> r;
+  for (int h = u.h; h < u.h_end; ++h) {
+    const int64_t slot0 = (u.page * a.c.Hkv + h) * a.c.page_tokens + u.first;
+    const uint2* q = reinterpret_cast<const uint2*>(codes + slot0 * a.c.D);
+    const float scale = scales[h];
+    T* x = rows + h * hs;
+    for (int v = threadIdx.x; v < u.count * D8; v += blockDim.x) {
+      const uint2 c = q[v];
+      float f[2][4];
+      floats_of_codes(c.x, f[0]);
+      floats_of_codes(c.y, f[1]);
+      Vec8<T> r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r.v[i] = from_f32<T>(__fmul_rn(f[i >> 2][i & 3], scale));
-    store8(x + (v / D8) * ts + (v % D8) * 8, r, 8, wide);
+      for (int i = 0; i < 8; ++i) r.v[i] = from_f32<T>(__fmul_rn(f[i >> 2][i & 3], scale));
+      store8(x + (v / D8) * ts + (v % D8) * 8, r, 8, wide);
+    }
   }
 }
 
-// Threads of a block: enough for the vectors of 8 that a page and head can receive.
+// Threads of a block: about four of the vectors of 8 that a page and head can receive
+// for each, so that small pages leave an SM as many bytes in flight as large ones.
 int threads_of(const KvArgs& a) {
   const int tokens = a.c.page_tokens < a.t.max_n ? a.c.page_tokens : a.t.max_n;
   const int vecs = tokens * (a.c.D / 8);
-  return vecs <= 64 ? 64 : vecs <= 128 ? 128 : kKvThreads;
+  return vecs <= 256 ? 64 : vecs <= 512 ? 128 : kKvThreads;
 }
 
 template <typename T>
@@ -180,7 +196,7 @@ bool valid_kv8_cache(const pq_kv8_cache* c) {
 namespace {
 
 // Checks what both calls share and fills the launch; an empty grid: nothing to do.
-pq_status kv_args(const pq_kv8_cache* c, const pq_kv8_tokens* t, const void* k, const void* v, KvArgs* a,
+pq_status kv_args(const pq_kv8_cache* c, const pq_kv8_tokens* t, const void* k, const void* v, bool reading, KvArgs* a,
                   dim3* grid) {
   *grid = dim3(0);
   if (!valid_kv8_cache(c) || t == nullptr) return PQ_EINVAL;
@@ -200,7 +216,13 @@ pq_status kv_args(const pq_kv8_cache* c, const pq_kv8_tokens* t, const void* k, 
   a->blocks = static_cast<int>((static_cast<int64_t>(t->max_n) + c->page_tokens - 2) / c->page_tokens + 1);
   a->err = device_error_word();
   if (a->err == nullptr) return PQ_ECUDA;
-  const int64_t units = 2ll * c->Hkv * a->blocks;
+  // heads that a block reads: up to 2048 vectors of 8, as long as that leaves eight blocks
+  // for every SM of the chip
+  const int vecs = std::min(c->page_tokens, t->max_n) * (c->D / 8);
+  const int64_t pages = 2ll * a->blocks * t->B;
+  a->heads = reading ? std::min(c->Hkv, std::max(1, 2048 / vecs)) : 1;
+  while (a->heads > 1 && pages * ((c->Hkv + a->heads - 1) / a->heads) < 8 * 152) a->heads = (a->heads + 1) / 2;
+  const int64_t units = 2ll * ((c->Hkv + a->heads - 1) / a->heads) * a->blocks;
   if (units > 0x7FFFFFFFll || t->B > 65535) return PQ_EUNSUPPORTED;
   *grid = dim3(static_cast<unsigned>(units), static_cast<unsigned>(t->B));
   return PQ_OK;
@@ -216,7 +238,7 @@ pq_status palquant_kv8_append(const pq_kv8_cache* cache, const void* k_dev, cons
   if (t != nullptr && t->B > 0 && t->max_n > 0 && (k_dev == nullptr || v_dev == nullptr)) return PQ_EINVAL;
   pq::KvArgs a = {};
   dim3 grid(0);
-  const pq_status st = pq::kv_args(cache, t, k_dev, v_dev, &a, &grid);
+  const pq_status st = pq::kv_args(cache, t, k_dev, v_dev, false, &a, &grid);
   if (st != PQ_OK || grid.x == 0) return st;
   a.in[0] = k_dev;
   a.in[1] = v_dev;
@@ -235,7 +257,7 @@ pq_status palquant_kv8_read(const pq_kv8_cache* cache, void* k_dev, void* v_dev,
   if (t != nullptr && t->B > 0 && t->max_n > 0 && k_dev == nullptr && v_dev == nullptr) return PQ_EINVAL;
   pq::KvArgs a = {};
   dim3 grid(0);
-  const pq_status st = pq::kv_args(cache, t, k_dev, v_dev, &a, &grid);
+  const pq_status st = pq::kv_args(cache, t, k_dev, v_dev, true, &a, &grid);
   if (st != PQ_OK || grid.x == 0) return st;
   a.out[0] = k_dev;
   a.out[1] = v_dev;
