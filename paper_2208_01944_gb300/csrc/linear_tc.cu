@@ -248,6 +248,10 @@ __global__ void __launch_bounds__(kTcThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = PAIR || p.k_parts > 1 ? static_cast<int>(cluster_rank()) : 0;
 
+  if (warp == 2 && lane == 0) {
+    prefetch_tmap(&map_w);
+    prefetch_tmap(&map_q);
+  }
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(bars.loaded(s), 2);
@@ -452,27 +456,31 @@ __global__ void __launch_bounds__(kTcThreads, 1)
     }
     if (!PAIR && p.k_parts > 1) {
       // add the cluster's parts: every block writes a share of the tokens, a warp one
-      // token's 128 channels at a time, four a lane
-      cluster_sync();
+      // token's 128 channels at a time, four a lane, whose scales it has by then
       int n0;
       int64_t m0;
       tile_origin(p, first_tile, kChannels, BN, &n0, &m0);
-      const int j1 = BN * (rank + 1) / p.k_parts;
-#pragma unroll 4
-      for (int j = BN * rank / p.k_parts + warp - 12; j < j1; j += 8) {
-        if (!ok || m0 + j >= p.a.M) break;
-        const int n = n0 + 4 * lane;
+      const int n = n0 + 4 * lane;
+      float s_w[4], bias[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        s_w[i] = p.a.s_w != nullptr && n + i < p.a.N ? p.a.s_w[n + i] : 0.0f;
+        bias[i] = p.a.bias != nullptr && n + i < p.a.N ? p.a.bias[n + i] : 0.0f;
+      }
+      cluster_sync();
+      const int j1 = static_cast<int>(min(static_cast<int64_t>(BN * (rank + 1) / p.k_parts), p.a.M - m0));
+#pragma unroll 2
+      for (int j = BN * rank / p.k_parts + warp - 12; ok && j < j1; j += 8) {
         int4 acc = make_int4(0, 0, 0, 0);
         for (int b = 0; b < p.k_parts; ++b) {
           const int4 v = load_of_peer(tok_base + (j * 128 + 4 * lane) * 4, b);
           acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
         }
         const int sums[4] = {acc.x, acc.y, acc.z, acc.w};
+        const float s_x = scales[4 * (j / kCols)][j % kCols];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (n + i < p.a.N)
-            put_result(p.a, m0 + j, n + i, sums[i], p.a.s_w != nullptr ? p.a.s_w[n + i] : 0.0f,
-                       p.a.bias != nullptr ? p.a.bias[n + i] : 0.0f);
+          if (n + i < p.a.N) put_result(p.a, m0 + j, n + i, sums[i], s_x, s_w[i], bias[i]);
       }
       cluster_sync();
     }

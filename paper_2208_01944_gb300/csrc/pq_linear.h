@@ -25,6 +25,7 @@ struct LinearArgs {
   int64_t M;
   int N, K;
   int y_type;
+  bool wide_q;  // token rows on 16-byte boundaries
 };
 
 struct LinearTc {
@@ -35,11 +36,11 @@ struct LinearTc {
   uint64_t wait_limit_ns;
 };
 
-// One output: s_w and bias are channel n's.
-__device__ __forceinline__ void put_result(const LinearArgs& a, int64_t m, int n, int acc, float s_w, float bias) {
+// One output: s_x is token m's, s_w and bias are channel n's.
+__device__ __forceinline__ void put_result(const LinearArgs& a, int64_t m, int n, int acc, float s_x, float s_w, float bias) {
   if (a.acc != nullptr) a.acc[m * a.N + n] = acc;
   if (a.y == nullptr) return;
-  float y = __fmul_rn(__fmul_rn(__int2float_rn(acc), a.s_x[m]), s_w);
+  float y = __fmul_rn(__fmul_rn(__int2float_rn(acc), s_x), s_w);
   if (a.bias != nullptr) y = __fadd_rn(y, bias);
   const int64_t at = m * a.ldy + n;
   if (a.y_type == PQ_F32)
