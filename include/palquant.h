@@ -543,8 +543,10 @@ pq_status palquant_linear_i8(const void* q_dev, int32_t code_format, int64_t ldq
                              const int8_t* w_dev, const float* s_w_dev, const float* bias_dev, int32_t* acc_dev,
                              void* y_dev, const pq_linear_desc* d, pq_stream_t stream);
 
-/* Bytes of device scratch palquant_linear_q8 needs (the tokens' codes and scales);
- * 0 for a descriptor that it refuses. */
+/* Bytes of device scratch palquant_linear_q8 needs: the tokens' codes and scales and,
+ * for weight rows off 16-byte boundaries (ldw not a multiple of 16) under more than 16
+ * tokens and M N K of 2^28 and more, a copy of the weights that it makes in every call; 0
+ * for a descriptor that it refuses. */
 size_t palquant_linear_q8_scratch_bytes(const pq_linear_desc* d);
 
 /* palquant_quantize_tokens into scratch_dev (16-byte aligned), then

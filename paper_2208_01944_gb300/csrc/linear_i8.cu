@@ -150,6 +150,19 @@ __device__ __forceinline__ void load_tokens(const void* q, int64_t row, int k, i
   }
 }
 
+// Weight rows that lie off 16-byte boundaries, copied to rows of `pitch` bytes (a multiple
+// of 16; zeros past K) for the tensor cores' loads.  Bound by the bytes.
+__global__ void __launch_bounds__(256) pq_align_weights(const int8_t* __restrict__ w, int64_t ldw, int N, int K,
+                                                        int8_t* __restrict__ out, int64_t pitch) {
+  const int pieces = static_cast<int>(pitch / 16);
+  const int64_t total = static_cast<int64_t>(N) * pieces, step = static_cast<int64_t>(gridDim.x) * 256;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += step) {
+    const int64_t n = i / pieces;
+    const int k = static_cast<int>(i - n * pieces) * 16;
+    *reinterpret_cast<uint4*>(out + n * pitch + k) = codes16<false>(w + n * ldw, k, K);
+  }
+}
+
 constexpr int kRowWarps = 8;
 constexpr int kExactSteps = 16;  // 64-wide steps whose fp32 sums are exact
 constexpr int kAhead = 2;        // (four took the registers of a fourth block on an SM)
@@ -413,11 +426,26 @@ bool valid_linear(const pq_linear_desc* d) {
          valid_type(d->y_type) && d->ldx >= d->K && d->ldw >= d->K && d->ldy >= d->N;
 }
 
-// The scratch: codes (rows padded to 16 elements), then scales.
+bool aligned_rows(const pq_linear_desc* d) { return d->ldw % 16 == 0; }
+// Weight rows off 16-byte boundaries: the kernels for few tokens read them in place, again for
+// every 16 tokens; the tensor cores' loads want a copy.  With the copy against without (us):
+// 16 x 4001 x 4000 17.0 / 11.8, 24 x 4001 x 4000 17.5 / 23.0, 512 x 4001 x 4000 30 / 200,
+// 128 x 777 x 1001 14.9 / 8.5, 512 x 777 x 1001 15.3 / 19.9.
+bool copies_weights(const pq_linear_desc* d) {
+  return !aligned_rows(d) && d->M > 16 && static_cast<double>(d->M) * d->N * d->K >= 268435456.0;
+}
+int32_t q8_format(const pq_linear_desc* d) {
+  return copies_weights(d) ? PQ_CODES_F16 : palquant_linear_code_format(d);
+}
+
+// The scratch: codes (rows padded to 16 elements), scales, and where it is made the copy
+// of the weights (rows padded to 16 bytes); each part starts on 16 bytes.
 int64_t padded_k(const pq_linear_desc* d) { return (static_cast<int64_t>(d->K) + 15) / 16 * 16; }
-size_t code_bytes(const pq_linear_desc* d) {
-  const size_t e = palquant_linear_code_format(d) == PQ_CODES_F16 ? 2 : 1;
-  return static_cast<size_t>(d->M) * static_cast<size_t>(padded_k(d)) * e;
+size_t scales_at(const pq_linear_desc* d) {
+  return static_cast<size_t>(d->M) * static_cast<size_t>(padded_k(d)) * (q8_format(d) == PQ_CODES_F16 ? 2 : 1);
+}
+size_t weights_at(const pq_linear_desc* d) {
+  return scales_at(d) + (static_cast<size_t>(d->M) * sizeof(float) + 15) / 16 * 16;
 }
 
 pq_status linear_codes(const void* q_dev, int32_t code_format, int64_t ldq, const float* s_x_dev, const int8_t* w_dev,
@@ -481,7 +509,7 @@ pq_status palquant_quantize_tokens(const void* x_dev, int32_t x_type, int64_t ld
 }
 
 int32_t palquant_linear_code_format(const pq_linear_desc* d) {
-  return pq::valid_linear(d) && d->M > 16 ? PQ_CODES_F16 : PQ_CODES_INT8;
+  return pq::valid_linear(d) && d->M > 16 && pq::aligned_rows(d) ? PQ_CODES_F16 : PQ_CODES_INT8;
 }
 
 pq_status palquant_linear_i8(const void* q_dev, int32_t code_format, int64_t ldq, const float* s_x_dev,
@@ -492,7 +520,8 @@ pq_status palquant_linear_i8(const void* q_dev, int32_t code_format, int64_t ldq
 
 size_t palquant_linear_q8_scratch_bytes(const pq_linear_desc* d) {
   if (!pq::valid_linear(d)) return 0;
-  return (pq::code_bytes(d) + 15) / 16 * 16 + static_cast<size_t>(d->M) * sizeof(float);
+  if (!pq::copies_weights(d)) return pq::scales_at(d) + static_cast<size_t>(d->M) * sizeof(float);
+  return pq::weights_at(d) + static_cast<size_t>(d->N) * static_cast<size_t>(pq::padded_k(d));
 }
 
 pq_status palquant_linear_q8(const void* x_dev, const int8_t* w_dev, const float* s_w_dev, const float* bias_dev,
@@ -505,12 +534,24 @@ pq_status palquant_linear_q8(const void* x_dev, const int8_t* w_dev, const float
       !pq::is_aligned(y_dev, pq::bytes_of_type(d->y_type)) || !pq::is_aligned(s_w_dev, 4) ||
       !pq::is_aligned(bias_dev, 4))
     return PQ_EINVAL;
-  const int32_t format = palquant_linear_code_format(d);
-  const int64_t ldq = pq::padded_k(d);
-  float* s_x = reinterpret_cast<float*>(static_cast<char*>(scratch_dev) + (pq::code_bytes(d) + 15) / 16 * 16);
-  const pq_status st = palquant_quantize_tokens(x_dev, d->x_type, d->ldx, d->M, d->K, format, scratch_dev, ldq, s_x, stream);
+  const int32_t format = pq::q8_format(d);
+  const int64_t pitch = pq::padded_k(d);
+  char* scratch = static_cast<char*>(scratch_dev);
+  float* s_x = reinterpret_cast<float*>(scratch + pq::scales_at(d));
+  pq_linear_desc aligned = *d;
+  if (pq::copies_weights(d)) {
+    // before the tokens, so that the copy is complete when the product's first loads start
+    int8_t* copy = reinterpret_cast<int8_t*>(scratch + pq::weights_at(d));
+    const int64_t blocks = (d->N * (pitch / 16) + 255) / 256;
+    pq::pq_align_weights<<<static_cast<unsigned>(blocks < 152 * 16 ? blocks : 152 * 16), 256, 0,
+                           static_cast<cudaStream_t>(stream)>>>(w_dev, d->ldw, d->N, d->K, copy, pitch);
+    if (cudaGetLastError() != cudaSuccess) return PQ_ECUDA;
+    w_dev = copy;
+    aligned.ldw = pitch;
+  }
+  const pq_status st = palquant_quantize_tokens(x_dev, d->x_type, d->ldx, d->M, d->K, format, scratch_dev, pitch, s_x, stream);
   if (st != PQ_OK) return st;
-  return pq::linear_codes(scratch_dev, format, ldq, s_x, w_dev, s_w_dev, bias_dev, nullptr, y_dev, d, true, stream);
+  return pq::linear_codes(scratch_dev, format, pitch, s_x, w_dev, s_w_dev, bias_dev, nullptr, y_dev, &aligned, true, stream);
 }
 
 }  // extern "C"

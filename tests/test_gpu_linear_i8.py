@@ -132,6 +132,25 @@ def test_strides_and_alignments(B, M, N, K):
         assert np.array_equal(sums.cpu().numpy(), acc)
 
 
+@pytest.mark.parametrize("M,N,K,gap", [(17, 40, 131071, 0), (41, 2600, 2601, 0), (400, 700, 1001, 6), (300, 640, 1600, 3)])
+def test_many_tokens_on_weight_rows_off_16_bytes(B, M, N, K, gap):
+    """Weight rows at any address: columns of a wider matrix, `gap` bytes in, or of odd length."""
+    x = _x(M, K, "bf16", K)
+    w, s_w = _weights(N, K, N)
+    wbig = torch.full((N, K + gap), 99, dtype=torch.int8, device="cuda")
+    wd, sd = wbig[:, gap:], torch.from_numpy(s_w).cuda()
+    wd.copy_(torch.from_numpy(w))
+    y = torch.full((M, N), 7.0, device="cuda")
+    d = B.linear_desc(x, wd, y)
+    need = B.palquant_linear_q8_scratch_bytes(d)
+    assert need >= N * K or M * N * K < 2 ** 28  # the copy of the weights
+    scratch = torch.full((need + 64,), 171, dtype=torch.uint8, device="cuda")
+    B.palquant_linear_q8(x, wd, sd, None, y, d, scratch, need)
+    q, s_x = ref.quantize_tokens(_f32(x))
+    _check_y(y, ref.linear(q, w), s_x, s_w, None, "f32")
+    assert bool((scratch[need:] == 171).all())
+
+
 @pytest.mark.parametrize("M", [4, 160])
 def test_non_finite_tokens_poison_themselves_only(B, M):
     K, N = 256, 144

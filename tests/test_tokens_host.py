@@ -33,6 +33,16 @@ def test_linear_descriptors_refused(kw):
         _refused(B.palquant_linear_i8, 64, 0, 131073, 64, 64, 64, None, None, 64, d)
 
 
+@pytest.mark.parametrize("M,ldw,code,copy", [(1, 4096, 0, 0), (16, 4095, 0, 0), (17, 4096, 5, 0), (17, 4095, 0, 4000 * 4096),
+                                             (600, 4095, 0, 4000 * 4096), (600, 4112, 5, 0)])
+def test_linear_code_format_and_scratch(M, ldw, code, copy):
+    d = _linear(M=M, N=4000, K=4095, ldx=4095, ldw=ldw, ldy=4000)
+    assert B.palquant_linear_code_format(d) == code
+    each = 2 if code == B.PQ_CODES_F16 or copy else 1
+    need = B.palquant_linear_q8_scratch_bytes(d)
+    assert M * 4096 * each + 4 * M + copy <= need <= M * 4096 * each + 4 * M + copy + 16
+
+
 def test_linear_arguments_refused():
     d = _linear()
     need = B.palquant_linear_q8_scratch_bytes(d)
