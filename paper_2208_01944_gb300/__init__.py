@@ -9,7 +9,7 @@ convolution (Sec. 4.1); a cyclic permutation moves every group's output to the n
 Importing the package loads nothing; ``binding`` loads the shared library on first use and
 raises if it has not been built.
 """
-__all__ = ["binding", "synth", "workloads"]
+__all__ = ["attention_block", "binding", "synth", "workloads"]
 
 
 def __getattr__(name):

@@ -1,0 +1,128 @@
+"""Self-attention of a transformer layer in 8-bit codes, prompts and single tokens, through the C ABI.
+
+The paper has no counterpart; the block shows the library's 8-bit transformer calls together,
+as a server would use them:
+
+    qkv = x W_qkv^T + b_qkv        palquant_linear_q8: 8-bit codes, one scale for each token and channel
+    cache <- k, v                  palquant_kv8_append: 8-bit codes, one scale for each page and head
+    mixed = attention(q, cache)    palquant_kv8_attention: grouped heads, causal, optional window
+    y = mixed W_out^T              palquant_linear_q8
+
+A block serves a fixed set of sequences.  forward() takes any number of new tokens for each of
+them (none, one, a chunk or a whole prompt), appends them to the cache and attends from them
+to everything cached so far; sequences of different lengths share a call.  reset() ends a
+sequence and makes its pages free for the next one.  q, k and v are read where the first layer
+wrote them (columns of its output), so nothing is copied between the four calls.
+
+    block = AttentionBlock8(w_qkv, w_out, heads=32, kv_heads=8, sequences=4, max_len=4096)
+    y = block.forward(prompts, [900, 17, 2048, 1])    # [2966, hidden]
+    y = block.forward(tokens, [1, 1, 1, 1])           # [4, hidden]
+"""
+from __future__ import annotations
+
+import torch
+
+from . import binding as B
+
+_TYPES = {torch.float32: B.PQ_F32, torch.float16: B.PQ_F16, torch.bfloat16: B.PQ_BF16}
+
+
+def weight_codes(w: torch.Tensor, stream: torch.cuda.Stream | None = None):
+    """Signed 8-bit codes [N, K] and one scale for each output channel (row) of w: the token quantiser on the rows."""
+    if w.dim() != 2 or w.dtype not in _TYPES or w.stride(1) != 1:
+        raise ValueError("w: a float matrix with contiguous rows")
+    codes = torch.empty(w.shape, dtype=torch.int8, device=w.device)
+    scales = torch.empty(w.shape[0], device=w.device)
+    B.palquant_quantize_tokens(w, _TYPES[w.dtype], w.stride(0), w.shape[0], w.shape[1], B.PQ_CODES_INT8, codes,
+                               w.shape[1], scales, stream)
+    return codes, scales
+
+
+class AttentionBlock8:
+    def __init__(self, w_qkv: torch.Tensor, w_out: torch.Tensor, heads: int, kv_heads: int, sequences: int, max_len: int,
+                 b_qkv: torch.Tensor | None = None, page_tokens: int = 64, window: int = 0,
+                 stream: torch.cuda.Stream | None = None):
+        """w_qkv [(heads + 2 kv_heads) D, hidden] (the rows of q, then k, then v) and w_out [hidden, heads D] on the
+        GPU; their type is the activations'."""
+        if heads % kv_heads or w_qkv.shape[0] % (heads + 2 * kv_heads):
+            raise ValueError("heads: a multiple of kv_heads; w_qkv: heads + 2 kv_heads blocks of rows")
+        self.heads, self.kv_heads, self.window = heads, kv_heads, window
+        self.D = w_qkv.shape[0] // (heads + 2 * kv_heads)
+        self.hidden = w_qkv.shape[1]
+        if w_out.shape != (self.hidden, heads * self.D) or w_out.dtype != w_qkv.dtype:
+            raise ValueError("w_out: [hidden, heads D], of w_qkv's type")
+        self.dtype, self.dev, self.stream = w_qkv.dtype, w_qkv.device, stream
+        self.sequences, self.max_len = sequences, max_len
+        self.b_qkv = None if b_qkv is None else b_qkv.to(self.dev, torch.float32).contiguous()
+        self._enter(w_qkv, w_out)
+        with torch.cuda.stream(self.stream):
+            w_qkv, w_out = w_qkv.contiguous(), w_out.contiguous()
+            self.w_qkv, self.s_qkv = weight_codes(w_qkv, stream)
+            self.w_out, self.s_out = weight_codes(w_out, stream)
+            pages = -(-max_len // page_tokens)
+            n = sequences * pages
+            self.k, self.v = (torch.zeros((n, kv_heads, page_tokens, self.D), dtype=torch.int8, device=self.dev)
+                              for _ in range(2))
+            self.k_scale, self.v_scale = (torch.zeros((n, kv_heads), device=self.dev) for _ in range(2))
+            self.cache = B.kv8_cache(self.k, self.v, self.k_scale, self.v_scale)
+            self.table = torch.arange(n, dtype=torch.int32, device=self.dev).view(sequences, pages)
+            self._work = torch.empty(0, dtype=torch.uint8, device=self.dev)
+        self.lens = [0] * sequences  # tokens cached, on the host: no call waits for the device
+
+    def _enter(self, *tensors) -> None:
+        """The block's stream waits for what the caller's has been given, and holds the caller's tensors."""
+        if self.stream is not None:
+            self.stream.wait_stream(torch.cuda.current_stream(self.dev))
+            for t in tensors:
+                t.record_stream(self.stream)
+
+    def _scratch(self, n: int) -> torch.Tensor:
+        """The workspace, grown when a call needs more; the calls of a forward() follow each other on one stream."""
+        if self._work.numel() < n:
+            self._work = torch.empty(n, dtype=torch.uint8, device=self.dev)
+        return self._work
+
+    def _linear(self, x, w, s_w, bias, y):
+        d = B.linear_desc(x, w, y)
+        work = self._scratch(B.palquant_linear_q8_scratch_bytes(d))
+        B.palquant_linear_q8(x, w, s_w, bias, y, d, work, work.numel(), self.stream)
+
+    def reset(self, sequence: int) -> None:
+        self.lens[sequence] = 0
+
+    def forward(self, x: torch.Tensor, counts) -> torch.Tensor:
+        """x [sum(counts), hidden]: counts[b] new tokens of every sequence b, one sequence after the other; returns y
+        of x's shape.  It runs on the block's stream (None: the current one), after what the current stream holds and
+        before what it is given next."""
+        counts = [int(c) for c in counts]
+        if len(counts) != self.sequences or min(counts) < 0 or x.shape != (sum(counts), self.hidden) or x.dtype != self.dtype:
+            raise ValueError("counts: one for each sequence; x: [sum(counts), hidden] of the weights' type")
+        after = [n + c for n, c in zip(self.lens, counts)]
+        if max(after) > self.max_len:
+            raise ValueError(f"a sequence would pass max_len = {self.max_len}")
+        if not sum(counts):
+            return torch.empty_like(x)
+        Hq, Hkv, D, tokens = self.heads, self.kv_heads, self.D, x.shape[0]
+        self._enter(x)
+        with torch.cuda.stream(self.stream):
+            ends = [0]
+            for c in counts:
+                ends.append(ends[-1] + c)
+            index = torch.tensor(ends + self.lens + after, dtype=torch.int32, device=self.dev)
+            cu, start, lens = index.split([self.sequences + 1, self.sequences, self.sequences])
+            qkv = torch.empty((tokens, (Hq + 2 * Hkv) * D), dtype=self.dtype, device=self.dev)
+            self._linear(x, self.w_qkv, self.s_qkv, self.b_qkv, qkv)
+            q, k, v = qkv.view(tokens, Hq + 2 * Hkv, D).split([Hq, Hkv, Hkv], 1)
+            B.palquant_kv8_append(self.cache, k, v, B.kv8_tokens(k, v, cu, start, self.table, max(counts)), self.stream)
+            mixed = torch.empty((tokens, Hq, D), dtype=self.dtype, device=self.dev)
+            a = B.kv8_attn(q, mixed, cu, lens, self.table, max(counts), max(after), D ** -0.5, True, self.window)
+            work = self._scratch(B.palquant_kv8_attention_scratch_bytes(self.cache, a))
+            B.palquant_kv8_attention(self.cache, q, mixed, a, work, work.numel(), self.stream)
+            y = torch.empty((tokens, self.hidden), dtype=self.dtype, device=self.dev)
+            self._linear(mixed.view(tokens, Hq * D), self.w_out, self.s_out, None, y)
+        if self.stream is not None:
+            torch.cuda.current_stream(self.dev).wait_stream(self.stream)
+            y.record_stream(torch.cuda.current_stream(self.dev))
+        self.lens = after
+        self.qkv, self.mixed = qkv, mixed  # the last call's, for inspection
+        return y
