@@ -148,18 +148,19 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
         const int64_t base = ((ph << p.page_shift) + (s & (p.c.page_tokens - 1))) * D;
         const uint32_t at = ring + place * kStep;
         // 16 C pieces of each side; a token's pieces are neighbours
+        const int8_t *k = p.c.k_dev + base + 16 * lane, *v = p.c.v_dev + base + 16 * lane;
+        if (C == kJ) {
 #pragma unroll
-        for (int e0 = 0; e0 < DP; e0 += 32) {
-          const int e = e0 + lane;
-          int row, c;
-          if (C == kJ) {
-            row = e / kJ, c = e % kJ;
-          } else {
-            row = e / C, c = e - row * C;
+          for (int e = 0; e < DP; e += 32) {
+            const int row = (e + lane) / kJ, c = lane % kJ;
+            cp_async_16(at + key_at<DP>(row, c), k + 16 * e, 16);
+            cp_async_16(at + 16 * DP + value_at<DP>(row, c), v + 16 * e, 16);
           }
-          if (row < 16) {
-            cp_async_16(at + key_at<DP>(row, c), p.c.k_dev + base + 16 * e, 16);
-            cp_async_16(at + 16 * DP + value_at<DP>(row, c), p.c.v_dev + base + 16 * e, 16);
+        } else {
+          for (int e = 0; e + lane < 16 * C; e += 32) {
+            const int row = (e + lane) / C, c = e + lane - row * C;
+            cp_async_16(at + key_at<DP>(row, c), k + 16 * e, 16);
+            cp_async_16(at + 16 * DP + value_at<DP>(row, c), v + 16 * e, 16);
           }
         }
         if (lane == 0) cp_async_4(at + 32 * DP, p.c.k_scale_dev + ph);
@@ -308,27 +309,39 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
     // ---- probabilities, of the running maximum as it was; only where a score has grown
     // past it by more than 2^8 (w could leave the halves' range) is it brought up to date
     uint32_t pf[kHalves][NT][2];
-    float wv[NT][4];
-    bool seen[NT][4], grew = false;
-    const bool whole = s >= all_lo && s + 16 <= all_hi;
+    float wv[NT][4], to_l[NT][2];
+    bool grew = false;
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int i = e & 1, token = s + g + 8 * (e >> 1);
-        seen[j][e] = whole || (token >= lo[j][i] && token < hi[j][i]);
-        wv[j][e] = fmaf(x[j][e], sk * factor[j][i], lv);
-        grew |= seen[j][e] && wv[j][e] > m[j][i] + kGrow;
+        wv[j][e] = fmaf(x[j][e], sk * factor[j][e & 1], lv);
+        to_l[j][e & 1] = inv_v;
       }
+    if (s < all_lo || s + 16 > all_hi) {  // tokens that some row does not see
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const bool first_seen = s + g >= lo[j][i] && s + g < hi[j][i];
+          const bool second_seen = s + g + 8 >= lo[j][i] && s + g + 8 < hi[j][i];
+          if (!first_seen) wv[j][i] = kNone;
+          if (!second_seen) wv[j][i + 2] = kNone;
+          // a page that the row does not see adds nothing, even with a NaN scale
+          if (!first_seen && !second_seen) to_l[j][i] = 0.0f;
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) grew |= wv[j][e] > m[j][e & 1] + kGrow;
     if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
         float alpha[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float top = m[j][i];
-          if (seen[j][i]) top = fmaxf(top, wv[j][i]);
-          if (seen[j][i + 2]) top = fmaxf(top, wv[j][i + 2]);
+          float top = fmaxf(m[j][i], fmaxf(wv[j][i], wv[j][i + 2]));
 #pragma unroll
           for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
           alpha[i] = top == kNone ? 1.0f : exp2_approx(m[j][i] - top);
@@ -346,11 +359,10 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float base = m[j][e & 1] == kNone ? 0.0f : m[j][e & 1];
-        wv[j][e] = seen[j][e] ? exp2_approx(wv[j][e] - base + kWShift) : 0.0f;
+        wv[j][e] = exp2_approx(wv[j][e] - base + kWShift);
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i)  // a page that the row does not see adds nothing, even with a NaN scale
-        l[j][i] += seen[j][i] || seen[j][i + 2] ? (wv[j][i] + wv[j][i + 2]) * inv_v : 0.0f;
+      for (int i = 0; i < 2; ++i) l[j][i] += (wv[j][i] + wv[j][i + 2]) * to_l[j][i];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const uint32_t h = pack_half2(wv[j][2 * i], wv[j][2 * i + 1]);
