@@ -406,6 +406,7 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
             mma_16x8x16(o[2 * c + i][j], a01[2 * i], a01[2 * i + 1], a23[2 * i], a23[2 * i + 1], pf[hf][j][0], pf[hf][j][1]);
     }
   }
+  let_next_kernel_start();
   cp_async_wait<0>();
   __syncthreads();  // the ring is idle
   // ---- join the warps: sums over the lanes, then pairs of warps

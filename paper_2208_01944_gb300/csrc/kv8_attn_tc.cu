@@ -542,8 +542,12 @@ cudaError_t launch(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
 
 }  // namespace
 
+// From about 40 query rows of a cache head on: a block's step costs the same for 1 to
+// 128 rows here, and in pq_kv8_rows it grows with every 16 (D = 128, rows of a head, here
+// against there: one sequence of 4000, 24 rows 21 / 21 us, 48 22 / 25; 32 sequences of 3000, 32 rows
+// 111 / 87, 48 111 / 123, 64 112 / 150).
 bool attn_tc_takes(const pq_kv8_cache& c, const pq_kv8_attn& a) {
-  return a.type != PQ_F32 && c.D <= 128 && static_cast<int64_t>(a.max_q) * (a.Hq / c.Hkv) > 64;
+  return a.type != PQ_F32 && c.D <= 128 && static_cast<int64_t>(a.max_q) * (a.Hq / c.Hkv) > 40;
 }
 
 cudaError_t launch_attn_tc(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
