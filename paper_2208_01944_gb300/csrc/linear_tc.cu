@@ -198,6 +198,37 @@ __device__ __forceinline__ void put_column_as(const LinearArgs& a, int64_t m, in
   }
 }
 
+// Four channels of a token.
+__device__ __forceinline__ void put_results4(const LinearArgs& a, int64_t m, int n, int4 acc, float s_x,
+                                             const float (&s_w)[4], const float (&bias)[4], bool wide) {
+  const int sums[4] = {acc.x, acc.y, acc.z, acc.w};
+  if (!wide) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < a.N) put_result(a, m, n + i, sums[i], s_x, s_w[i], bias[i]);
+    return;
+  }
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[i] = __fmul_rn(__fmul_rn(__int2float_rn(sums[i]), s_x), s_w[i]);
+    if (a.bias != nullptr) y[i] = __fadd_rn(y[i], bias[i]);
+  }
+  const int64_t at = m * a.ldy + n;
+  if (a.y_type == PQ_F32) {
+    *reinterpret_cast<float4*>(static_cast<float*>(a.y) + at) = make_float4(y[0], y[1], y[2], y[3]);
+    return;
+  }
+  uint2 h;
+  if (a.y_type == PQ_F16) {
+    h = make_uint2(pack_half2(y[0], y[1]), pack_half2(y[2], y[3]));
+  } else {
+    const __nv_bfloat162 b[2] = {__floats2bfloat162_rn(y[0], y[1]), __floats2bfloat162_rn(y[2], y[3])};
+    memcpy(&h, b, sizeof(h));
+  }
+  *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.y) + at) = h;
+}
+
 template <int kCols>
 __device__ __forceinline__ void put_column(const LinearArgs& a, int64_t m, int n, const int32_t (&sum)[kCols],
                                            const float* s_x) {
@@ -214,6 +245,33 @@ __device__ __forceinline__ void put_column(const LinearArgs& a, int64_t m, int n
     put_column_as<kCols, __half>(a, m, n, sum, s_x);
   else
     put_column_as<kCols, __nv_bfloat16>(a, m, n, sum, s_x);
+}
+
+// Tokens j, j + 8, .. of a tile below `end`, U of them: four channels of each, summed over the cluster's
+// parts, I at a time, and written.  U x I loads from the peers are on their way together (one after the
+// other, 48 x 8192 x 4096 spent 2.4 of its 16.3 us here, now 1.4 of 15.2).
+template <int U, int I, int kCols>
+__device__ __forceinline__ void add_parts(const LinearTc& p, uint32_t from, int j, int end, const float (&scales)[8][kCols],
+                                          int64_t m0, int n, const float (&s_w)[4], const float (&bias)[4], bool wide) {
+  int4 sums[U] = {};
+  for (int b = 0; b < p.k_parts; b += I) {
+    int4 v[I][U] = {};
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (b + i < p.k_parts && j + 8 * u < end) v[i][u] = load_of_peer(from + (j + 8 * u) * 512, b + i);
+#pragma unroll
+    for (int i = 0; i < I; ++i)
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        sums[u].x += v[i][u].x, sums[u].y += v[i][u].y, sums[u].z += v[i][u].z, sums[u].w += v[i][u].w;
+  }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int t = j + 8 * u;
+    if (t < end) put_results4(p.a, m0 + t, n, sums[u], scales[4 * (t / kCols)][t % kCols], s_w, bias, wide);
+  }
 }
 
 // Tile t: channel tiles in bands, the tokens' tiles along a band, so that the tiles
@@ -467,20 +525,16 @@ __global__ void __launch_bounds__(kTcThreads, 1)
         s_w[i] = p.a.s_w != nullptr && n + i < p.a.N ? p.a.s_w[n + i] : 0.0f;
         bias[i] = p.a.bias != nullptr && n + i < p.a.N ? p.a.bias[n + i] : 0.0f;
       }
+      // four channels of a token in one store
+      const bool wide = n + 4 <= p.a.N && p.a.acc == nullptr && p.a.ldy % 4 == 0 &&
+                        reinterpret_cast<uintptr_t>(p.a.y) % (p.a.y_type == PQ_F32 ? 16 : 8) == 0;
       cluster_sync();
       const int j1 = static_cast<int>(min(static_cast<int64_t>(BN * (rank + 1) / p.k_parts), p.a.M - m0));
-#pragma unroll 2
-      for (int j = BN * rank / p.k_parts + warp - 12; ok && j < j1; j += 8) {
-        int4 acc = make_int4(0, 0, 0, 0);
-        for (int b = 0; b < p.k_parts; ++b) {
-          const int4 v = load_of_peer(tok_base + (j * 128 + 4 * lane) * 4, b);
-          acc.x += v.x, acc.y += v.y, acc.z += v.z, acc.w += v.w;
-        }
-        const int sums[4] = {acc.x, acc.y, acc.z, acc.w};
-        const float s_x = scales[4 * (j / kCols)][j % kCols];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (n + i < p.a.N) put_result(p.a, m0 + j, n + i, sums[i], s_x, s_w[i], bias[i]);
+      const int j0 = BN * rank / p.k_parts + warp - 12;
+      if (ok && j0 + 8 >= j1) {
+        if (j0 < j1) add_parts<1, 8>(p, tok_base + 16 * lane, j0, j1, scales, m0, n, s_w, bias, wide);
+      } else if (ok) {
+        for (int j = j0; j < j1; j += 32) add_parts<4, 2>(p, tok_base + 16 * lane, j, j1, scales, m0, n, s_w, bias, wide);
       }
       cluster_sync();
     }
@@ -562,12 +616,14 @@ cudaError_t launch_linear_tc(const LinearArgs& a, bool after_tokens, cudaStream_
   // 160 or 192, by rounds of tiles x the time of 64 of K, which was 384, 404 and 423 cycles for
   // the pairs (about bn + 500 in units of 0.6 cycles).  Single blocks share K while the
   // chip is less than half full and each part keeps 256 of K; eight parts of 128 tokens
-  // take longer to add than they save (16 tiles of K = 8192: 22 us, four parts 15 us).
+  // take longer to add than they save (16 tiles of K = 8192: 22 us, four parts 15 us), and
+  // of clusters of eight only one or two fit a part of the chip at a time (64 tokens, K = 8192: 16
+  // tiles 20.6 us, in four parts 14.7; 8 tiles 10.7, in four parts 13.4).
   auto ceil_div = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
   int bn = a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
   const int64_t singles = ceil_div(a.N, 128) * ceil_div(a.M, bn);
   p.k_parts = 1;
-  while (p.k_parts < (bn < 128 ? 8 : 4) && singles * p.k_parts * 2 <= sms && a.K / (p.k_parts * 2) >= 256) p.k_parts *= 2;
+  for (int c = 2; c <= (bn < 128 ? 8 : 4) && singles * c <= (c == 8 ? sms / 2 : sms) && a.K / c >= 256; c *= 2) p.k_parts = c;
   bool pair = false;
   if (a.M > 128) {
     double best = static_cast<double>(ceil_div(singles * p.k_parts, sms)) * (bn + 500) / p.k_parts;
