@@ -6,7 +6,10 @@
 // Reading, a block takes several heads of a small page: the lookups (run, page) are three
 // dependent loads (16 tokens a page, 8 x 2000 tokens of 8 heads of 128: 28 us one head
 // a block, 21 us eight).
-// Bound by HBM: each new element is read once and each code written once.
+// Bound by HBM: each new element is read once and each code written once.  16 prompts of up to 4096
+// tokens, 8 heads of 128, bf16: append 71 us, read 53 us (4.0 and 5.3 TB/s); the rest is the
+// blocks' dependent lookups.  Vectors of all of a block's heads in one loop, four loads before their
+// stores, took 60 us to read.
 #include <cuda_runtime.h>
 
 #include <algorithm>
