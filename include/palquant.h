@@ -538,7 +538,8 @@ int32_t palquant_linear_code_format(const pq_linear_desc* d);
  * q_dev [M, ldq] in code_format; s_x_dev M floats, s_w_dev and bias_dev N floats;
  * acc_dev (int32 [M, N], contiguous) and y_dev may each be NULL, not both (s_x_dev
  * and s_w_dev may be NULL when y_dev is).  d->x_type and d->ldx are not read.
- * M = 0 does nothing. */
+ * M = 0 does nothing.  M above 16 * 65535 needs PQ_CODES_F16 and rows of codes and
+ * weights on 16-byte boundaries (PQ_EUNSUPPORTED else). */
 pq_status palquant_linear_i8(const void* q_dev, int32_t code_format, int64_t ldq, const float* s_x_dev,
                              const int8_t* w_dev, const float* s_w_dev, const float* bias_dev, int32_t* acc_dev,
                              void* y_dev, const pq_linear_desc* d, pq_stream_t stream);
@@ -559,9 +560,9 @@ pq_status palquant_linear_q8(const void* x_dev, const int8_t* w_dev, const float
  * scale for each page and head [num_pages][Hkv], for each side.  The token at
  * position p of sequence b sits in page page_table[b][p / page_tokens], slot
  * p % page_tokens.  page_tokens is 16, 32, 64 or 128; D a multiple of 16, 16 to 256;
- * codes 16-byte aligned; scales not negative, and 0, NaN or between 2^-100 and 2^100.  A page id outside [0, num_pages) that a call meets is
- * skipped (nothing is read or written there) and reported by palquant_sync_check as
- * PQ_EINVAL. */
+ * codes 16-byte aligned; scales not negative, and 0, NaN or between 2^-100 and 2^100.
+ * A page id outside [0, num_pages) that a call meets is skipped (nothing is read or
+ * written there) and reported by palquant_sync_check as PQ_EINVAL. */
 typedef struct {
     int32_t num_pages, page_tokens, Hkv, D;
     int8_t *k_dev, *v_dev;

@@ -151,6 +151,29 @@ def test_many_tokens_on_weight_rows_off_16_bytes(B, M, N, K, gap):
     assert bool((scratch[need:] == 171).all())
 
 
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("M,N,K,shift", [(1, 33, 16, 0), (1, 100, 500, 1), (2, 65, 513, 0), (3, 129, 1024, 3), (4, 260, 1030, 0),
+                                         (4, 64, 4096, 0), (1, 48, 16384, 0), (5, 48, 1100, 0), (2, 31, 8200, 1)])
+def test_few_tokens_on_padded_weight_rows(B, M, N, K, shift, kind):
+    """One to five tokens, weight rows padded to 16 bytes, token rows `shift` elements into a wider matrix."""
+    x = _x(M, K, kind, K + M)
+    xbig = torch.full((M, K + 8), 1e4, dtype=TYPES[kind], device="cuda")
+    xbig[:, shift:shift + K] = x
+    w, s_w = _weights(N, K, N + M)
+    wbig = torch.full((N, -(-K // 16) * 16), 77, dtype=torch.int8, device="cuda")
+    wbig[:, :K] = torch.from_numpy(w).cuda()
+    xs, wd, sd = xbig[:, shift:shift + K], wbig[:, :K], torch.from_numpy(s_w).cuda()
+    bias = np.random.default_rng(4).normal(size=N).astype(np.float32) if M % 2 else None
+    y = torch.full((M, N + 3), 7.0, dtype=TYPES[kind], device="cuda")
+    d = B.linear_desc(xs, wd, y[:, 1:1 + N])
+    scratch = torch.empty(B.palquant_linear_q8_scratch_bytes(d), dtype=torch.uint8, device="cuda")
+    B.palquant_linear_q8(xs, wd, sd, None if bias is None else torch.from_numpy(bias).cuda(), y[:, 1:1 + N], d, scratch,
+                         scratch.numel())
+    q, s_x = ref.quantize_tokens(_f32(x))
+    _check_y(y[:, 1:1 + N], ref.linear(q, w), s_x, s_w, bias, kind)
+    assert bool((y[:, 0] == 7).all()) and bool((y[:, 1 + N:] == 7).all())
+
+
 @pytest.mark.parametrize("M", [4, 160])
 def test_non_finite_tokens_poison_themselves_only(B, M):
     K, N = 256, 144
