@@ -7,7 +7,7 @@
 // dependent loads (16 tokens a page, 8 x 2000 tokens of 8 heads of 128: 28 us one head
 // a block, 21 us eight).
 // Bound by HBM: each new element is read once and each code written once.  16 prompts of up to 4096
-// tokens, 8 heads of 128, bf16: append 71 us, read 53 us (4.0 and 5.3 TB/s); the rest is the
+// tokens, 8 heads of 128, bf16: append 67 us, read 53 us (4.2 and 5.3 TB/s); the rest is the
 // blocks' dependent lookups.  Vectors of all of a block's heads in one loop, four loads before their
 // stores, took 60 us to read.
 #include <cuda_runtime.h>
@@ -39,7 +39,8 @@ struct KvUnit {
   int side, h, h_end;
   int64_t row;      // float row of the run's first token in the page
   int first, count; // slots [first, first + count) of the page belong to the run
-  int64_t page;     // -1: none (nothing to do)
+  int64_t page;     // as the table has it
+  bool there;       // false: nothing to do
 };
 
 __device__ __forceinline__ KvUnit kv_unit(const KvArgs& a) {
@@ -55,49 +56,69 @@ __device__ __forceinline__ KvUnit kv_unit(const KvArgs& a) {
   const int page = start / T + blk;
   const int64_t lo = max(static_cast<int64_t>(start), static_cast<int64_t>(page) * T);
   const int64_t hi = min(static_cast<int64_t>(start) + n, static_cast<int64_t>(page + 1) * T);
-  u.page = -1;
+  u.there = false;
   if (start < 0 || n <= 0 || lo >= hi) return u;
   u.row = cu + (lo - start);
   u.first = static_cast<int>(lo - static_cast<int64_t>(page) * T);
   u.count = static_cast<int>(hi - lo);
-  int id = -1;
-  if (page < a.t.table_pitch) id = a.t.page_table_dev[static_cast<int64_t>(b) * a.t.table_pitch + page];
-  if (id < 0 || id >= a.c.num_pages) {
-    if (threadIdx.x == 0) atomicOr(a.err, PQ_ERR_PAGE);
-    return u;
-  }
-  u.page = id;
+  u.page = page < a.t.table_pitch ? a.t.page_table_dev[static_cast<int64_t>(b) * a.t.table_pitch + page] : -2;
+  u.there = true;
   return u;
 }
 
+// False for a page that is not in the pool; reported.
+__device__ __forceinline__ bool page_ok(const KvArgs& a, const KvUnit& u) {
+  if (u.page >= 0 && u.page < a.c.num_pages) return true;
+  if (threadIdx.x == 0) atomicOr(a.err, PQ_ERR_PAGE);
+  return false;
+}
+
+// The vectors of a thread: v = threadIdx.x + i blockDim.x is piece `at` of row `row`, stepped
+// along without a division a vector (only for loads that are all in flight together: in the read's
+// loop the steps' chain cost 58 us instead of 53).
+struct Walk {
+  int D8, row, at, rows_on, pieces_on;
+  __device__ explicit Walk(int d8)
+      : D8(d8), row(threadIdx.x / d8), at(threadIdx.x % d8), rows_on(blockDim.x / d8), pieces_on(blockDim.x % d8) {}
+  __device__ void next() {
+    row += rows_on, at += pieces_on;
+    if (at >= D8) at -= D8, ++row;
+  }
+};
+
 // NV: vectors of 8 elements that a thread keeps; 0: the tokens are read twice.  Up to 64
 // bytes of them, six blocks fit an SM (42 registers; with the 47 that the compiler would
-// take five fit, and 16 prompts of up to 4096 tokens took 89 us instead of 71).
+// take five fit, and 16 prompts of up to 4096 tokens took 89 us instead of 71, now 67).
 template <typename T, int NV>
 __global__ void __launch_bounds__(kKvThreads, sizeof(T) * NV > 8 ? 1 : 6) pq_kv8_append(const __grid_constant__ KvArgs a) {
   __shared__ uint32_t red[8];
   const KvUnit u = kv_unit(a);
-  if (u.page < 0) return;
+  if (!u.there) return;
   const int D8 = a.c.D / 8;
   const int64_t ts = u.side ? a.t.v_token_stride : a.t.k_token_stride;
   const int64_t hs = u.side ? a.t.v_head_stride : a.t.k_head_stride;
   const T* x = static_cast<const T*>(a.in[u.side]) + u.row * ts + u.h * hs;
+  const bool wide = a.wide[u.side];
+  const int nvec = u.count * D8;
+  // the new tokens are on their way before the page's id is there
+  Vec8<T> keep[NV > 0 ? NV : 1];
+  if (NV > 0) {
+    Walk w(D8);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      if (w.row < u.count) keep[i] = load8(x + w.row * ts + w.at * 8, 8, wide);
+      w.next();
+    }
+  }
+  if (!page_ok(a, u)) return;
   const int64_t slot0 = (u.page * a.c.Hkv + u.h) * a.c.page_tokens;
   int8_t* q = (u.side ? a.c.v_dev : a.c.k_dev) + slot0 * a.c.D;
   float* sp = (u.side ? a.c.v_scale_dev : a.c.k_scale_dev) + u.page * a.c.Hkv + u.h;
-  const bool wide = a.wide[u.side];
-  const int nvec = u.count * D8;
   const float was = u.first > 0 ? *sp : 0.0f;
   auto get = [&](int v) { return load8(x + (v / D8) * ts + (v % D8) * 8, 8, wide); };
 
-  Vec8<T> keep[NV > 0 ? NV : 1];
   uint32_t top = 0;
   if (NV > 0) {
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int v = threadIdx.x + i * blockDim.x;
-      if (v < nvec) keep[i] = get(v);
-    }
 #pragma unroll
     for (int i = 0; i < NV; ++i)
       if (threadIdx.x + i * blockDim.x < nvec) top = max(top, amax8(keep[i]));
@@ -135,7 +156,7 @@ __global__ void __launch_bounds__(kKvThreads, sizeof(T) * NV > 8 ? 1 : 6) pq_kv8
 template <typename T>
 __global__ void __launch_bounds__(kKvThreads) pq_kv8_read(const __grid_constant__ KvArgs a) {
   const KvUnit u = kv_unit(a);
-  if (u.page < 0 || a.out[u.side] == nullptr) return;
+  if (!u.there || a.out[u.side] == nullptr || !page_ok(a, u)) return;
   const int D8 = a.c.D / 8;
   const int64_t ts = u.side ? a.t.v_token_stride : a.t.k_token_stride;
   const int64_t hs = u.side ? a.t.v_head_stride : a.t.k_head_stride;
