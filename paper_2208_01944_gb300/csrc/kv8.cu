@@ -5,11 +5,10 @@
 // stay in registers between the search for their largest magnitude and the rounding.
 // Reading, a block takes several heads of a small page: the lookups (run, page) are three
 // dependent loads (16 tokens a page, 8 x 2000 tokens of 8 heads of 128: 28 us one head
-// a block, 21 us eight).
+// a block, 18 us eight).
 // Bound by HBM: each new element is read once and each code written once.  16 prompts of up to 4096
-// tokens, 8 heads of 128, bf16: append 67 us, read 53 us (4.2 and 5.3 TB/s); the rest is the
-// blocks' dependent lookups.  Vectors of all of a block's heads in one loop, four loads before their
-// stores, took 60 us to read.
+// tokens, 8 heads of 128, bf16: append 67 us, read 46 us (4.2 and 6.1 TB/s); the rest is the
+// blocks' dependent lookups.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -153,8 +152,12 @@ __global__ void __launch_bounds__(kKvThreads, sizeof(T) * NV > 8 ? 1 : 6) pq_kv8
   }
 }
 
+// 16-bit values: four loads of a thread before their stores, eight blocks an SM (16 prompts of up to
+// 4096 tokens 53 -> 46 us, pages of 16 tokens 25 -> 18).  fp32 values: one (8 runs of 2000 tokens,
+// 2 heads of 256: 17 us, four at a time 23).
 template <typename T>
-__global__ void __launch_bounds__(kKvThreads) pq_kv8_read(const __grid_constant__ KvArgs a) {
+__global__ void __launch_bounds__(kKvThreads, sizeof(T) == 2 ? 8 : 1) pq_kv8_read(const __grid_constant__ KvArgs a) {
+  constexpr int kLoads = sizeof(T) == 2 ? 4 : 1;
   const KvUnit u = kv_unit(a);
   if (!u.there || a.out[u.side] == nullptr || !page_ok(a, u)) return;
   const int D8 = a.c.D / 8;
@@ -169,15 +172,24 @@ __global__ void __launch_bounds__(kKvThreads) pq_kv8_read(const __grid_constant_
     const uint2* q = reinterpret_cast<const uint2*>(codes + slot0 * a.c.D);
     const float scale = scales[h];
     T* x = rows + h * hs;
-    for (int v = threadIdx.x; v < u.count * D8; v += blockDim.x) {
-      const uint2 c = q[v];
-      float f[2][4];
-      floats_of_codes(c.x, f[0]);
-      floats_of_codes(c.y, f[1]);
-      Vec8<T> r;
+    const int nvec = u.count * D8, step = blockDim.x;
+    for (int v0 = threadIdx.x; v0 < nvec; v0 += kLoads * step) {
+      uint2 c[kLoads];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) r.v[i] = from_f32<T>(__fmul_rn(f[i >> 2][i & 3], scale));
-      store8(x + (v / D8) * ts + (v % D8) * 8, r, 8, wide);
+      for (int k = 0; k < kLoads; ++k)
+        if (v0 + k * step < nvec) c[k] = q[v0 + k * step];
+#pragma unroll
+      for (int k = 0; k < kLoads; ++k) {
+        const int v = v0 + k * step;
+        if (v >= nvec) break;
+        float f[2][4];
+        floats_of_codes(c[k].x, f[0]);
+        floats_of_codes(c[k].y, f[1]);
+        Vec8<T> r;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.v[i] = from_f32<T>(__fmul_rn(f[i >> 2][i & 3], scale));
+        store8(x + (v / D8) * ts + (v % D8) * 8, r, 8, wide);
+      }
     }
   }
 }
