@@ -202,31 +202,40 @@ lib = _load()
 # ----------------------------------------------------------------- marshalling
 def _ptr(obj):
     """Device or host address of a tensor / array / int (None -> NULL)."""
-    if obj is None:
-        return None
-    if isinstance(obj, int):
+    if obj is None or type(obj) is int:
         return obj
+    address = getattr(obj, "data_ptr", None)
+    if address is not None:
+        assert obj.is_contiguous(), "tensors passed to libpalquant must be contiguous"
+        return address()
     if isinstance(obj, np.ndarray):
         assert obj.flags["C_CONTIGUOUS"]
         return obj.ctypes.data
-    if hasattr(obj, "data_ptr"):
-        assert obj.is_contiguous(), "tensors passed to libpalquant must be contiguous"
-        return obj.data_ptr()
+    if isinstance(obj, int):
+        return obj
     raise TypeError(f"cannot pass {type(obj)} as a pointer")
 
 
 def _strided(obj):
     """As _ptr, for a tensor whose strides are in its descriptor."""
-    return obj.data_ptr() if hasattr(obj, "data_ptr") else _ptr(obj)
+    address = getattr(obj, "data_ptr", None)
+    return address() if address is not None else _ptr(obj)
+
+
+_current = None  # torch's functions for the current stream's handle and the current device, once CUDA is up
 
 
 def _stream(stream):
+    global _current
     if stream is None:
-        import torch
+        if _current is None:
+            import torch
 
-        if torch.cuda.is_initialized():  # the handle alone: a Stream object costs 3 us a call
-            return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
-        return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+            if not torch.cuda.is_initialized():
+                return torch.cuda.current_stream().cuda_stream if torch.cuda.is_available() else None
+            # the handle alone: a Stream object costs 3 us a call
+            _current = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+        return _current[0](_current[1]())
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
