@@ -560,7 +560,10 @@ pq_status palquant_linear_q8(const void* x_dev, const int8_t* w_dev, const float
  * scale for each page and head [num_pages][Hkv], for each side.  The token at
  * position p of sequence b sits in page page_table[b][p / page_tokens], slot
  * p % page_tokens.  page_tokens is 16, 32, 64 or 128; D a multiple of 16, 16 to 256;
- * codes 16-byte aligned; scales not negative, and 0, NaN or between 2^-100 and 2^100.
+ * codes 16-byte aligned.  Scales are not negative.  Attention takes scales of 0, NaN, of keys
+ * between 2^-100 and 2^100, and of values between 2^-40 and 2^40 (append stores what the
+ * values ask for: every scale of PQ_F16 lies in these ranges, those of PQ_F32 and PQ_BF16 while a page
+ * and head's largest |v| is 0 or between 2^-33 and 2^46).
  * A page id outside [0, num_pages) that a call meets is skipped (nothing is read or
  * written there) and reported by palquant_sync_check as PQ_EINVAL. */
 typedef struct {

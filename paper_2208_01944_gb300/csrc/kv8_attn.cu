@@ -7,7 +7,7 @@
 // m_i the running maximum of x_ij + log2 s_v(j), up to a factor of 2^8.  Folding the value scale into the exponent keeps
 // every w in the halves' range whatever the pages' scales are, so w can be a half value and the
 // products with the codes run without a scale inside the MMA.  (A page whose value
-// scale is 0 holds zeros only; it counts with scale 1.)
+// scale is 0 holds zeros only; it counts with kZeroPageScale.)
 //
 // Split.  Bound by the cache's bytes: each must be read once for all heads of a
 // group.  A block takes one cache head, up to 16 query rows and a part of the token
@@ -282,7 +282,7 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
         kr[c][i] = 64 * c + 16 * t < D ? lds_16(at + key_at<DP>(g + 8 * i, 4 * c + t)) : make_uint4(0, 0, 0, 0);
     const float sk = lds_f32(at + 32 * DP);
     const float sv0 = lds_f32(at + 32 * DP + 4);
-    const float sv = sv0 == 0.0f ? 1.0f : sv0;
+    const float sv = sv0 == 0.0f ? kZeroPageScale : sv0;
     const float lv = log2_approx(sv), inv_v = exp2_approx(-lv);  // of one another, whatever the rounding
 
     // ---- scores

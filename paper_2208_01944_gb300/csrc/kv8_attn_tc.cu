@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
             const int id = slot < p.a.table_pitch ? table[slot] : -1;
             if (id >= 0 && id < p.c.num_pages) {
               const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
-              const float sk = p.c.k_scale_dev[ph], sv0 = p.c.v_scale_dev[ph], sv = sv0 == 0.0f ? 1.0f : sv0;
+              const float sk = p.c.k_scale_dev[ph], sv0 = p.c.v_scale_dev[ph], sv = sv0 == 0.0f ? kZeroPageScale : sv0;
               page = {sk, log2f(sv), 1.0f / sv, (ph << p.page_shift) * D};
             } else {
               atomicOr(p.err, PQ_ERR_PAGE);

@@ -39,6 +39,12 @@ cudaError_t launch_attn_tc(const AttnArgs& p, unsigned grid, cudaStream_t stream
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNone = -INFINITY;
 
+// The value scale that a page of zero values (scale 0) counts with.  Its weights 2^(x + log2 s_v) add
+// nothing to the outputs, only to the sum, where s_v is divided out again; but they take part in the running
+// maximum, and whatever lies below 2^-30 of that is lost to the outputs.  So it has to lie below every
+// other page's (2^-40 and up), and within 2^100 of the largest (2^40), for the sum's own terms to stay in fp32's range.
+constexpr float kZeroPageScale = 0x1p-60f;
+
 __device__ __forceinline__ float exp2_approx(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
