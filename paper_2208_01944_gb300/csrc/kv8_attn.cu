@@ -4,7 +4,7 @@
 // Mathematics.  With codes kc, vc and one scale for each page and head,
 //   x_ij = scale log2(e) s_k(j) sum_d q_id kc_jd,   w_ij = 2^(x_ij + log2 s_v(j) - m_i),
 //   o_id = sum_j w_ij vc_jd / sum_j w_ij / s_v(j),
-// m_i the running maximum of x_ij + log2 s_v(j), up to a factor of 2^8.  Folding the value scale into the exponent keeps
+// m_i the running maximum of x_ij + log2 s_v(j), up to a factor of 2^8 (2^2 for fp32).  Folding the value scale into the exponent keeps
 // every w in the halves' range whatever the pages' scales are, so w can be a half value and the
 // products with the codes run without a scale inside the MMA.  (A page whose value
 // scale is 0 holds zeros only; it counts with kZeroPageScale.)
@@ -25,7 +25,7 @@
 //
 // Rounding.  Queries enter as halves scaled by a power of two for each row so that their largest
 // element lies in [2^7, 2^8) (exact for 16-bit queries down to 2^-22 of it), w as
-// halves (scaled by 2^6: small ones stay normal, and 2^8 more fit); fp32 queries and their w carry a
+// halves (scaled, see kWShift); fp32 queries and their w carry a
 // second half for the remainder (22 bits).  All sums are fp32.
 #include <cuda_runtime.h>
 
@@ -40,8 +40,6 @@ namespace pq {
 namespace {
 
 constexpr int kAttnWarps = 8;
-constexpr float kWShift = 6.0f;
-constexpr float kGrow = 8.0f;  // log2 by which a maximum may grow without a rescale
 
 // The block's share of the grid: the row tile changes fastest (its neighbours read
 // the same codes).
@@ -114,6 +112,7 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
   constexpr int kJ = DP / 16;        // 16-row tiles of the transposed output
   constexpr int kRows = 8 * NT;
   constexpr int kHalves = TWO ? 2 : 1;
+  constexpr float kGrowth = TWO ? kGrowF32 : kGrow, kShift = TWO ? kWShiftF32 : kWShift;
   constexpr int kSteps = ring_steps(DP);
   constexpr int kStep = step_bytes(DP);
   extern __shared__ __align__(16) uint8_t ring_raw[];
@@ -308,7 +307,7 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
       }
     }
     // ---- probabilities, of the running maximum as it was; only where a score has grown
-    // past it by more than 2^8 (w could leave the halves' range) is it brought up to date
+    // past it by more than 2^8 (2^2 for fp32: w could leave the halves' range) is it brought up to date
     uint32_t pf[kHalves][NT][2];
     float wv[NT][4], to_l[NT][2];
     bool grew = false;
@@ -335,7 +334,7 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
 #pragma unroll
     for (int j = 0; j < NT; ++j)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) grew |= wv[j][e] > m[j][e & 1] + kGrow;
+      for (int e = 0; e < 4; ++e) grew |= wv[j][e] > m[j][e & 1] + kGrowth;
     if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
@@ -360,7 +359,7 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const float base = m[j][e & 1] == kNone ? 0.0f : m[j][e & 1];
-        wv[j][e] = exp2_approx(wv[j][e] - base + kWShift);
+        wv[j][e] = exp2_approx(wv[j][e] - base + kShift);
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) l[j][i] += (wv[j][i] + wv[j][i + 2]) * to_l[j][i];

@@ -11,7 +11,7 @@
 // (with one buffer of 128 tokens the softmax waited for its own product and the next scores,
 // 4600 cycles a step).  One thread's MMAs run in order, so scores never overwrite
 // probabilities in use.  The outputs stay in tensor memory; they are rescaled only when
-// a row's maximum has grown by more than 2^8 (w stays below 2^8, a half holds 2^16).
+// a row's maximum has grown by more than 2^8 (w, scaled by 2^6, stays below 2^14; a half holds 2^16).
 // Bound by the softmax's instructions, then by the tensor rate (at D = 128 a step's
 // products take 2560 cycles: scores of 64 tokens wait for shared memory, 48 cycles an MMA
 // instead of 32).  Four prompts of 2048 over 4096, 32 / 8 heads of 128: 277 us (0.80 PFLOP/s); one of
@@ -33,7 +33,6 @@ constexpr int kTokens = kAttnTcTokens;  // of one step
 constexpr int kHalf = 64;               // of one round of the softmax
 constexpr int kThreads = 512;
 constexpr int kSub = 128 * 128;         // 128 rows of 64 halves
-constexpr float kGrow = 8.0f;           // log2 by which a maximum may grow without a rescale
 constexpr int kPageRing = 8;            // steps whose pages are looked up ahead
 
 __host__ __device__ constexpr int attn_smem(int DP) { return 6 * (DP / 64) * kSub + 1024 /* alignment */; }
@@ -453,7 +452,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
             }
           }
         }
-        const float base = m == kNone ? 0.0f : m;
+        const float base = m == kNone ? 0.0f : m - kWShift;
 #pragma unroll
         for (int c = 0; c < kHalf; c += 32) {
           uint32_t h[16];

@@ -45,6 +45,14 @@ constexpr float kNone = -INFINITY;
 // other page's (2^-40 and up), and within 2^100 of the largest (2^40), for the sum's own terms to stay in fp32's range.
 constexpr float kZeroPageScale = 0x1p-60f;
 
+// log2 by which a maximum may grow before the sums and outputs are rescaled, and by which
+// the weights are scaled before they become halves: those of the running maximum are 2^6, the
+// largest below 2^14, and a weight keeps a half's full 11 bits down to 2^-20 of the maximum (2^-14 if it were not
+// scaled).  fp32 carries the rest of a weight in a second half, which wants more room
+// below: 22 bits down to 2^-16 of the maximum (2^-9 with the others' scaling), and a maximum that may grow by 2^2.
+constexpr float kGrow = 8.0f, kWShift = 6.0f;
+constexpr float kGrowF32 = 2.0f, kWShiftF32 = 13.0f;
+
 __device__ __forceinline__ float exp2_approx(float x) {
   float r;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));

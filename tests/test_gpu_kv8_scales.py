@@ -85,3 +85,23 @@ def test_scales_at_the_ends_of_the_range(B, ends, n, kind):
     _upload(c)
     q, o, scale = _attend(B, c, [n], [length], 8, kind, True, 0, seed=n, loud=0.2)
     _compare(c, q, o, length, kind, scale)
+
+
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n", [1, 150])
+def test_quiet_pages_beside_a_loud_one(B, n, kind):
+    """One page 2^19 times as loud as the others, in the first eight columns alone.  The other columns hold what the quiet
+    pages add, whose weights are 2^-18 to 2^-20 of the largest: normal halves once they are scaled by 2^6, so the bound
+    there has no part of the loud page's values."""
+    T, length = 32, 320
+    c = Cache(B, [length], 2, 64, T, seed=7)
+    c.ks[:] = 1 / 60
+    c.vs[:] = np.float32(2.0 ** -10)
+    loud = c.table[0, 0]  # every query sees it
+    c.vs[loud] = np.float32(2.0 ** 9)
+    c.v[loud, :, :, 8:] = 0
+    _upload(c)
+    q, o, scale = _attend(B, c, [n], [length], 8, kind, True, 0, seed=n, loud=0.05)
+    quiet = np.ones(64, bool)
+    quiet[:8] = False
+    _compare(c, q, o, length, kind, scale, quiet, 0.0)
