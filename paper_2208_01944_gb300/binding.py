@@ -529,11 +529,23 @@ def _float_type(t) -> int:
     return types[t.dtype]
 
 
+class ArgumentError(ValueError, AssertionError):
+    """Tensors that a call cannot take: of other shapes, types or layouts than it was told."""
+
+
+def _need(ok, message):
+    if not ok:
+        raise ArgumentError(message)
+
+
 def _rows(t, name, columns=None):
-    """Row pitch of a matrix with contiguous rows (any pitch for a single row)."""
-    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{name}: a matrix with contiguous rows"
-    assert columns is None or t.shape[1] == columns, f"{name}: {columns} columns"
-    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+    """Row pitch of a matrix with contiguous rows that do not overlap (any pitch for a single row)."""
+    _need(t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] <= 1), f"{name}: a matrix with contiguous rows")
+    _need(columns is None or t.shape[1] == columns, f"{name}: {columns} columns")
+    if t.shape[0] <= 1:
+        return t.shape[1]
+    _need(t.stride(0) >= t.shape[1], f"{name}: rows that overlap (a pitch of {t.stride(0)} for {t.shape[1]} columns)")
+    return t.stride(0)
 
 
 def _heads(t, name):
@@ -553,9 +565,9 @@ def linear_desc(x, w, y) -> LinearDesc:
     """Descriptor of y [M, N] = x [M, K] w [N, K]^T from the tensors (w: int8 codes)."""
     import torch
 
-    assert w.dtype == torch.int8, "w: int8 codes"
+    _need(w.dtype == torch.int8, "w: int8 codes")
     (M, K), N = x.shape, w.shape[0]
-    assert y.shape == (M, N), "y: [M, N]"
+    _need(y.shape == (M, N), "y: [M, N]")
     return LinearDesc(M, N, K, _float_type(x), _float_type(y), _rows(x, "x"), _rows(w, "w", K), _rows(y, "y"))
 
 
