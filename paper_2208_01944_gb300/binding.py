@@ -548,17 +548,44 @@ def _rows(t, name, columns=None):
     return t.stride(0)
 
 
+def _layout(t):
+    return t.shape, t.stride(), t.dtype, t.get_device()
+
+
+_BY_HAND = object()  # a descriptor that no builder made says nothing about tensors
+
+
+def _as_described(t, described, name):
+    """A call's tensor against the layout that its descriptor was made for (an address is the caller's word)."""
+    if described is _BY_HAND or t is None or not hasattr(t, "data_ptr"):
+        return
+    if described is None:
+        raise ArgumentError(f"{name}: not in the descriptor")
+    shape, strides, dtype, device = described
+    if t.shape == shape and t.dtype is dtype and t.get_device() == device:
+        now = t.stride()
+        if now == strides or all(n <= 1 or a == b for n, a, b in zip(shape, now, strides)):  # one element has no stride
+            return
+    raise ArgumentError(f"{name}: not as the descriptor has it")
+
+
 def _heads(t, name):
     """(token stride, head stride) of [tokens, heads, D] with contiguous D."""
-    assert t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] <= 1), f"{name}: [tokens, heads, D] with contiguous D"
+    _need(t.dim() == 3 and (t.stride(2) == 1 or t.shape[2] <= 1), f"{name}: [tokens, heads, D] with contiguous D")
     return t.stride(0), t.stride(1)
 
 
-def _index(t, name):
+def _heads_apart(t):
+    """No element of [tokens, heads, D] lies where another does, as far as single strides tell."""
+    return all(t.shape[i] <= 1 or t.stride(i) >= t.shape[2] for i in (0, 1))
+
+
+def _index(t, name, count, device):
     import torch
 
-    assert t.dtype == torch.int32 and t.is_contiguous(), f"{name}: a contiguous int32 tensor"
-    return t
+    _need(t.dtype == torch.int32 and t.is_contiguous(), f"{name}: a contiguous int32 tensor")
+    _need(t.numel() == count and t.device == device, f"{name}: {count} values, on the device of the other tensors")
+    return _ptr(t)
 
 
 def linear_desc(x, w, y) -> LinearDesc:
@@ -576,12 +603,14 @@ def kv8_cache(k, v, k_scale, v_scale) -> KV8Cache:
     It keeps the tensors alive."""
     import torch
 
+    _need(k.dim() == 4 and k.dtype == v.dtype == torch.int8 and v.shape == k.shape, "codes: two int8 tensors of one shape")
     pages, H, T, D = k.shape
-    assert k.dtype == v.dtype == torch.int8 and v.shape == k.shape, "codes: two int8 tensors of one shape"
-    assert k_scale.dtype == v_scale.dtype == torch.float32 and k_scale.shape == v_scale.shape == (pages, H), \
-        "scales: two float32 tensors [pages, Hkv]"
+    _need(k_scale.dtype == v_scale.dtype == torch.float32 and k_scale.shape == v_scale.shape == (pages, H),
+          "scales: two float32 tensors [pages, Hkv]")
+    _need(k.device == v.device == k_scale.device == v_scale.device, "codes and scales: on one device")
     c = KV8Cache(pages, T, H, D, _ptr(k), _ptr(v), _ptr(k_scale), _ptr(v_scale))
     c._keep = (k, v, k_scale, v_scale)
+    c._heads, c._queries = (H, D, k.device), (D, k.device)
     return c
 
 
@@ -589,27 +618,44 @@ def kv8_tokens(k, v, cu, start, page_table, max_n) -> KV8Tokens:
     """Descriptor of the runs that k and v [tokens, Hkv, D] hold (any token and head strides; v or k may be None
     for palquant_kv8_read).  cu [B + 1], start [B], page_table [B, pages]: int32.  It keeps the index tensors alive."""
     some = k if k is not None else v
-    B = start.numel()
-    assert cu.numel() == B + 1 and page_table.shape[0] == B, "cu: B + 1 values, page_table: B rows"
-    assert k is None or v is None or k.dtype == v.dtype, "k and v have one type"
+    B, dev = start.numel(), some.device
     ks, vs = ((0, 0) if t is None else _heads(t, n) for t, n in ((k, "k"), (v, "v")))
-    t = KV8Tokens(_float_type(some), B, int(max_n), page_table.shape[1], *ks, *vs, _ptr(_index(cu, "cu")),
-                  _ptr(_index(start, "start")), _ptr(_index(page_table, "page_table")))
+    _need(k is None or v is None or (k.shape, k.dtype, k.device) == (v.shape, v.dtype, v.device),
+          "k and v: of one shape, type and device")
+    _need(page_table.dim() == 2 and page_table.shape[0] == B, "page_table: [B, pages]")
+    pages = page_table.shape[1]
+    t = KV8Tokens(_float_type(some), B, int(max_n), pages, *ks, *vs, _index(cu, "cu", B + 1, dev),
+                  _index(start, "start", B, dev), _index(page_table, "page_table", B * pages, dev))
     t._keep = (cu, start, page_table)
+    t._heads = (*some.shape[1:], dev)
+    t._k, t._v = (None if x is None else _layout(x) for x in (k, v))
+    t._apart = all(x is None or _heads_apart(x) for x in (k, v))
     return t
 
 
 def kv8_attn(q, o, cu_q, lens, page_table, max_q, max_len, scale, causal=True, window=0) -> KV8Attn:
     """Descriptor of one attention call: q and o [tokens, Hq, D] (any token and head strides), cu_q [B + 1], lens [B],
     page_table [B, pages]: int32.  It keeps the index tensors alive."""
-    B = lens.numel()
-    assert cu_q.numel() == B + 1 and page_table.shape[0] == B, "cu_q: B + 1 values, page_table: B rows"
-    assert o.shape == q.shape and o.dtype == q.dtype, "o: as q"
+    B, dev = lens.numel(), q.device
+    q_strides, o_strides = _heads(q, "q"), _heads(o, "o")
+    _need((o.shape, o.dtype, o.device) == (q.shape, q.dtype, dev), "o: as q")
+    _need(_heads_apart(o), "o: outputs that overlap")
+    _need(page_table.dim() == 2 and page_table.shape[0] == B, "page_table: [B, pages]")
+    pages = page_table.shape[1]
     a = KV8Attn(_float_type(q), B, q.shape[1], int(max_q), int(max_len), int(bool(causal)), int(window),
-                page_table.shape[1], float(scale), *_heads(q, "q"), *_heads(o, "o"), _ptr(_index(cu_q, "cu_q")),
-                _ptr(_index(lens, "lens")), _ptr(_index(page_table, "page_table")))
+                pages, float(scale), *q_strides, *o_strides, _index(cu_q, "cu_q", B + 1, dev),
+                _index(lens, "lens", B, dev), _index(page_table, "page_table", B * pages, dev))
     a._keep = (cu_q, lens, page_table)
+    a._queries = (q.shape[2], dev)
+    a._q, a._o = _layout(q), _layout(o)
     return a
+
+
+def _fits_cache(cache, d, of="_heads"):
+    """A descriptor's heads, D and device against the cache's (descriptors filled by hand are not looked at)."""
+    c, t = getattr(cache, of, None), getattr(d, of, None)
+    if c != t and c is not None and t is not None:
+        raise ArgumentError(f"{t} on a cache of {c}")
 
 
 def palquant_quantize_tokens(x_dev, x_type, ldx, M, K, code_format, q_dev, ldq, s_dev, stream=None):
@@ -643,12 +689,19 @@ def palquant_linear_q8(x_dev, w_dev, s_w_dev, bias_dev, y_dev, d: LinearDesc, sc
 
 def palquant_kv8_append(cache: KV8Cache, k_dev, v_dev, t: KV8Tokens, stream=None):
     """Quantise runs of tokens into the cache (one scale for each page and head)."""
+    _fits_cache(cache, t)
+    _as_described(k_dev, getattr(t, "_k", _BY_HAND), "k")
+    _as_described(v_dev, getattr(t, "_v", _BY_HAND), "v")
     _check(lib.palquant_kv8_append(ctypes.byref(cache), _strided(k_dev), _strided(v_dev), ctypes.byref(t),
                                    _stream(stream)), "palquant_kv8_append")
 
 
 def palquant_kv8_read(cache: KV8Cache, k_dev, v_dev, t: KV8Tokens, stream=None):
     """The values that runs of cached tokens stand for; k_dev or v_dev may be None."""
+    _fits_cache(cache, t)
+    _need(getattr(t, "_apart", True), "k, v: outputs that overlap")
+    _as_described(k_dev, getattr(t, "_k", _BY_HAND), "k")
+    _as_described(v_dev, getattr(t, "_v", _BY_HAND), "v")
     _check(lib.palquant_kv8_read(ctypes.byref(cache), _strided(k_dev), _strided(v_dev), ctypes.byref(t),
                                  _stream(stream)), "palquant_kv8_read")
 
@@ -659,5 +712,8 @@ def palquant_kv8_attention_scratch_bytes(cache: KV8Cache, a: KV8Attn) -> int:
 
 def palquant_kv8_attention(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, scratch_dev, scratch_bytes, stream=None):
     """Attention over the cache: single tokens, chunks and prompts, grouped heads."""
+    _fits_cache(cache, a, "_queries")
+    _as_described(q_dev, getattr(a, "_q", _BY_HAND), "q")
+    _as_described(o_dev, getattr(a, "_o", _BY_HAND), "o")
     _check(lib.palquant_kv8_attention(ctypes.byref(cache), _strided(q_dev), _strided(o_dev), ctypes.byref(a),
                                       _ptr(scratch_dev), scratch_bytes, _stream(stream)), "palquant_kv8_attention")

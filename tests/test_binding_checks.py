@@ -18,3 +18,85 @@ def test_rows_that_overlap_are_refused():
     assert (d.M, d.ldx, d.ldy) == (1, 8, 5)
     wide = torch.zeros(4, 11)
     assert B.linear_desc(wide[:, 2:10], w, y).ldx == 11
+
+
+def _i32(*shape):
+    return torch.zeros(*shape, dtype=torch.int32)
+
+
+def _cache(H=2, D=64, pages=4, T=16):
+    codes, scales = torch.zeros(pages, H, T, D, dtype=torch.int8), torch.zeros(pages, H)
+    return B.kv8_cache(codes, codes.clone(), scales, scales.clone())
+
+
+def _runs(k, v):
+    return B.kv8_tokens(k, v, _i32(3), _i32(2), _i32(2, 2), 0)  # max_n = 0: a call that passes does nothing
+
+
+def _queries(q, o):
+    return B.kv8_attn(q, o, _i32(3), _i32(2), _i32(2, 2), 0, 32, 0.1)  # max_q = 0: the same
+
+
+def test_runs_are_held_against_each_other_and_the_cache():
+    k = torch.zeros(6, 2, 64)
+    t = _runs(k, k.clone())
+    B.palquant_kv8_append(_cache(), k, k, t, stream=0)
+    B.palquant_kv8_read(_cache(), k, k, t, stream=0)
+    B.palquant_kv8_read(_cache(), None, k, t, stream=0)
+    for other in (torch.zeros(5, 2, 64), torch.zeros(6, 1, 64), torch.zeros(6, 2, 48), k.half()):
+        with pytest.raises(ValueError):  # v unlike k
+            _runs(k, other)
+        with pytest.raises(ValueError):  # tensors unlike the descriptor's
+            B.palquant_kv8_append(_cache(), k, other, t, stream=0)
+        with pytest.raises(ValueError):
+            B.palquant_kv8_read(_cache(), other, None, t, stream=0)
+    sliced = torch.zeros(6, 4, 64)[:, :2]
+    with pytest.raises(ValueError):  # strides unlike the descriptor's
+        B.palquant_kv8_append(_cache(), sliced, k, t, stream=0)
+    one = _runs(k[:1], k[:1])
+    B.palquant_kv8_append(_cache(), sliced[:1], k[:1], one, stream=0)  # (the pitch of one row does not count)
+    only_k = _runs(k, None)
+    B.palquant_kv8_read(_cache(), k, None, only_k, stream=0)
+    with pytest.raises(ValueError):
+        B.palquant_kv8_read(_cache(), k, k, only_k, stream=0)
+    for cache in (_cache(H=1), _cache(H=4), _cache(D=128)):
+        for call in (B.palquant_kv8_append, B.palquant_kv8_read):
+            with pytest.raises(ValueError):
+                call(cache, k, k, t, stream=0)
+    everywhere = torch.zeros(1, 2, 64).expand(6, 2, 64)  # one token, six times: may be appended, not read into
+    B.palquant_kv8_append(_cache(), everywhere, everywhere, _runs(everywhere, everywhere), stream=0)
+    with pytest.raises(ValueError):
+        B.palquant_kv8_read(_cache(), everywhere, everywhere, _runs(everywhere, everywhere), stream=0)
+
+
+def test_queries_are_held_against_the_cache():
+    q, o = torch.zeros(6, 4, 64), torch.zeros(6, 4, 64)
+    a = _queries(q, o)
+    B.palquant_kv8_attention(_cache(), q, o, a, None, 0, stream=0)
+    with pytest.raises(ValueError):
+        B.palquant_kv8_attention(_cache(D=48), q, o, a, None, 0, stream=0)
+    with pytest.raises(B.PalquantError):  # 4 query heads on 3 cache heads
+        B.palquant_kv8_attention(_cache(H=3), q, o, a, None, 0, stream=0)
+    for bad in (torch.zeros(6, 4, 48), torch.zeros(6, 3, 64), torch.zeros(5, 4, 64), q.half(), torch.zeros(4, 6, 64).transpose(0, 1)):
+        with pytest.raises(ValueError):
+            B.palquant_kv8_attention(_cache(), bad, o, a, None, 0, stream=0)
+        with pytest.raises(ValueError):
+            B.palquant_kv8_attention(_cache(), q, bad, a, None, 0, stream=0)
+    with pytest.raises(ValueError):
+        _queries(q, o[:1].expand(6, 4, 64))
+    with pytest.raises(ValueError):
+        _queries(q, o[:, :1].expand(6, 4, 64))
+    shared = q[:, :1].expand(6, 4, 64)  # one query head for all: read only
+    B.palquant_kv8_attention(_cache(), shared, o, _queries(shared, o), None, 0, stream=0)
+
+
+@pytest.mark.parametrize("i", range(3))
+def test_index_tensors_are_counted(i):
+    k = torch.zeros(6, 2, 64)
+    for change in (lambda t: t[:-1], lambda t: t.long(), lambda t: t.to("meta")):
+        index = [_i32(3), _i32(2), _i32(2, 2)]
+        index[i] = change(index[i])
+        with pytest.raises(ValueError):
+            B.kv8_tokens(k, k, *index, 1)
+        with pytest.raises(ValueError):
+            B.kv8_attn(k, k.clone(), *index, 1, 32, 0.1)
