@@ -10,6 +10,7 @@ not been built, importing this module raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 import numpy as np
@@ -520,13 +521,20 @@ def palquant_quantize_layer_fused_lu(x_dev, l, u, w_packed_dev, d: LayerDesc, m_
 
 
 # ---------------------------------------------------------------- 8-bit transformer layers
-def _float_type(t) -> int:
+@functools.lru_cache(None)
+def _dtypes():
+    """torch's types of pq_float_type, of the token codes by code format, and of int32 sums."""
     import torch
 
-    types = {torch.float32: PQ_F32, torch.float16: PQ_F16, torch.bfloat16: PQ_BF16}
-    if t.dtype not in types:
-        raise TypeError(f"activations are float32, float16 or bfloat16, not {t.dtype}")
-    return types[t.dtype]
+    return ({PQ_F32: torch.float32, PQ_F16: torch.float16, PQ_BF16: torch.bfloat16},
+            {PQ_CODES_INT8: torch.int8, PQ_CODES_F16: torch.float16}, torch.int32)
+
+
+def _float_type(t) -> int:
+    for number, dtype in _dtypes()[0].items():
+        if t.dtype == dtype:
+            return number
+    raise TypeError(f"activations are float32, float16 or bfloat16, not {t.dtype}")
 
 
 class ArgumentError(ValueError, AssertionError):
@@ -555,18 +563,37 @@ def _layout(t):
 _BY_HAND = object()  # a descriptor that no builder made says nothing about tensors
 
 
-def _as_described(t, described, name):
-    """A call's tensor against the layout that its descriptor was made for (an address is the caller's word)."""
-    if described is _BY_HAND or t is None or not hasattr(t, "data_ptr"):
-        return
+def _described(t, described, name):
+    """Address of a call's tensor, which has the layout that its descriptor was made for (an address is the caller's word)."""
+    if t is None or type(t) is int:
+        return t
+    if described is _BY_HAND:
+        return _strided(t)
     if described is None:
         raise ArgumentError(f"{name}: not in the descriptor")
     shape, strides, dtype, device = described
-    if t.shape == shape and t.dtype is dtype and t.get_device() == device:
-        now = t.stride()
-        if now == strides or all(n <= 1 or a == b for n, a, b in zip(shape, now, strides)):  # one element has no stride
-            return
+    if t.shape == shape and t.dtype is dtype and t.get_device() == device and (
+            t.stride() == strides or all(n <= 1 or a == b for n, a, b in zip(shape, t.stride(), strides))):
+        return t.data_ptr()  # (the stride of a dimension of one element does not count)
     raise ArgumentError(f"{name}: not as the descriptor has it")
+
+
+def _vector(t, dtype, count, name):
+    """Address of a contiguous tensor of this type with at least `count` elements (None and addresses as they are)."""
+    if t is None or type(t) is int:
+        return t
+    if t.dtype is dtype and t.numel() >= count and t.is_contiguous():
+        return t.data_ptr()
+    raise ArgumentError(f"{name}: {count} contiguous elements of {dtype}")
+
+
+def _span(t, dtype, count, name):
+    """Address of a tensor of this type (None: one that the library refuses) with `count` elements from its first to its last."""
+    if t is None or type(t) is int or dtype is None:
+        return _strided(t)
+    if t.dtype is dtype and 1 + sum((n - 1) * step for n, step in zip(t.shape, t.stride())) >= count:
+        return t.data_ptr()
+    raise ArgumentError(f"{name}: {count} elements of {dtype}")
 
 
 def _heads(t, name):
@@ -595,7 +622,10 @@ def linear_desc(x, w, y) -> LinearDesc:
     _need(w.dtype == torch.int8, "w: int8 codes")
     (M, K), N = x.shape, w.shape[0]
     _need(y.shape == (M, N), "y: [M, N]")
-    return LinearDesc(M, N, K, _float_type(x), _float_type(y), _rows(x, "x"), _rows(w, "w", K), _rows(y, "y"))
+    _need(x.device == w.device == y.device, "x, w and y: on one device")
+    d = LinearDesc(M, N, K, _float_type(x), _float_type(y), _rows(x, "x"), _rows(w, "w", K), _rows(y, "y"))
+    d._x, d._w, d._y = _layout(x), _layout(w), _layout(y)
+    return d
 
 
 def kv8_cache(k, v, k_scale, v_scale) -> KV8Cache:
@@ -660,8 +690,12 @@ def _fits_cache(cache, d, of="_heads"):
 
 def palquant_quantize_tokens(x_dev, x_type, ldx, M, K, code_format, q_dev, ldq, s_dev, stream=None):
     """Signed 8-bit codes and one scale for each token (row); code_format PQ_CODES_INT8 or PQ_CODES_F16."""
-    _check(lib.palquant_quantize_tokens(_strided(x_dev), x_type, ldx, M, K, code_format, _strided(q_dev), ldq,
-                                        _ptr(s_dev), _stream(stream)), "palquant_quantize_tokens")
+    floats, codes, _ = _dtypes()
+    x, q, s = (_span(x_dev, floats.get(x_type), (M - 1) * ldx + K if M > 0 else 0, "x"),
+               _span(q_dev, codes.get(code_format), (M - 1) * ldq + K if M > 0 else 0, "q"),
+               _vector(s_dev, floats[PQ_F32], M, "s"))
+    _check(lib.palquant_quantize_tokens(x, x_type, ldx, M, K, code_format, q, ldq, s, _stream(stream)),
+           "palquant_quantize_tokens")
 
 
 def palquant_linear_code_format(d: LinearDesc) -> int:
@@ -671,9 +705,13 @@ def palquant_linear_code_format(d: LinearDesc) -> int:
 def palquant_linear_i8(q_dev, code_format, ldq, s_x_dev, w_dev, s_w_dev, bias_dev, acc_dev, y_dev, d: LinearDesc,
                        stream=None):
     """Dense layer on token codes: exact int32 sums, scales for each token and output channel."""
-    _check(lib.palquant_linear_i8(_strided(q_dev), code_format, ldq, _ptr(s_x_dev), _strided(w_dev), _ptr(s_w_dev),
-                                  _ptr(bias_dev), _ptr(acc_dev), _strided(y_dev), ctypes.byref(d), _stream(stream)),
-           "palquant_linear_i8")
+    floats, codes, sums = _dtypes()
+    M, N, f32 = d.M, d.N, floats[PQ_F32]
+    q = _span(q_dev, codes.get(code_format), (M - 1) * ldq + d.K if M > 0 else 0, "q")
+    _check(lib.palquant_linear_i8(q, code_format, ldq, _vector(s_x_dev, f32, M, "s_x"), _described(w_dev, getattr(d, "_w", _BY_HAND), "w"),
+                                  _vector(s_w_dev, f32, N, "s_w"), _vector(bias_dev, f32, N, "bias"),
+                                  _vector(acc_dev, sums, M * N, "acc"), _described(y_dev, getattr(d, "_y", _BY_HAND), "y"),
+                                  ctypes.byref(d), _stream(stream)), "palquant_linear_i8")
 
 
 def palquant_linear_q8_scratch_bytes(d: LinearDesc) -> int:
@@ -682,28 +720,28 @@ def palquant_linear_q8_scratch_bytes(d: LinearDesc) -> int:
 
 def palquant_linear_q8(x_dev, w_dev, s_w_dev, bias_dev, y_dev, d: LinearDesc, scratch_dev, scratch_bytes, stream=None):
     """Token quantiser and dense layer: x to y."""
-    _check(lib.palquant_linear_q8(_strided(x_dev), _strided(w_dev), _ptr(s_w_dev), _ptr(bias_dev), _strided(y_dev),
-                                  ctypes.byref(d), _ptr(scratch_dev), scratch_bytes, _stream(stream)),
-           "palquant_linear_q8")
+    N, f32 = d.N, _dtypes()[0][PQ_F32]
+    _check(lib.palquant_linear_q8(_described(x_dev, getattr(d, "_x", _BY_HAND), "x"), _described(w_dev, getattr(d, "_w", _BY_HAND), "w"),
+                                  _vector(s_w_dev, f32, N, "s_w"), _vector(bias_dev, f32, N, "bias"),
+                                  _described(y_dev, getattr(d, "_y", _BY_HAND), "y"), ctypes.byref(d), _ptr(scratch_dev),
+                                  scratch_bytes, _stream(stream)), "palquant_linear_q8")
 
 
 def palquant_kv8_append(cache: KV8Cache, k_dev, v_dev, t: KV8Tokens, stream=None):
     """Quantise runs of tokens into the cache (one scale for each page and head)."""
     _fits_cache(cache, t)
-    _as_described(k_dev, getattr(t, "_k", _BY_HAND), "k")
-    _as_described(v_dev, getattr(t, "_v", _BY_HAND), "v")
-    _check(lib.palquant_kv8_append(ctypes.byref(cache), _strided(k_dev), _strided(v_dev), ctypes.byref(t),
-                                   _stream(stream)), "palquant_kv8_append")
+    _check(lib.palquant_kv8_append(ctypes.byref(cache), _described(k_dev, getattr(t, "_k", _BY_HAND), "k"),
+                                   _described(v_dev, getattr(t, "_v", _BY_HAND), "v"), ctypes.byref(t), _stream(stream)),
+           "palquant_kv8_append")
 
 
 def palquant_kv8_read(cache: KV8Cache, k_dev, v_dev, t: KV8Tokens, stream=None):
     """The values that runs of cached tokens stand for; k_dev or v_dev may be None."""
     _fits_cache(cache, t)
     _need(getattr(t, "_apart", True), "k, v: outputs that overlap")
-    _as_described(k_dev, getattr(t, "_k", _BY_HAND), "k")
-    _as_described(v_dev, getattr(t, "_v", _BY_HAND), "v")
-    _check(lib.palquant_kv8_read(ctypes.byref(cache), _strided(k_dev), _strided(v_dev), ctypes.byref(t),
-                                 _stream(stream)), "palquant_kv8_read")
+    _check(lib.palquant_kv8_read(ctypes.byref(cache), _described(k_dev, getattr(t, "_k", _BY_HAND), "k"),
+                                 _described(v_dev, getattr(t, "_v", _BY_HAND), "v"), ctypes.byref(t), _stream(stream)),
+           "palquant_kv8_read")
 
 
 def palquant_kv8_attention_scratch_bytes(cache: KV8Cache, a: KV8Attn) -> int:
@@ -713,7 +751,6 @@ def palquant_kv8_attention_scratch_bytes(cache: KV8Cache, a: KV8Attn) -> int:
 def palquant_kv8_attention(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, scratch_dev, scratch_bytes, stream=None):
     """Attention over the cache: single tokens, chunks and prompts, grouped heads."""
     _fits_cache(cache, a, "_queries")
-    _as_described(q_dev, getattr(a, "_q", _BY_HAND), "q")
-    _as_described(o_dev, getattr(a, "_o", _BY_HAND), "o")
-    _check(lib.palquant_kv8_attention(ctypes.byref(cache), _strided(q_dev), _strided(o_dev), ctypes.byref(a),
-                                      _ptr(scratch_dev), scratch_bytes, _stream(stream)), "palquant_kv8_attention")
+    _check(lib.palquant_kv8_attention(ctypes.byref(cache), _described(q_dev, getattr(a, "_q", _BY_HAND), "q"),
+                                      _described(o_dev, getattr(a, "_o", _BY_HAND), "o"), ctypes.byref(a), _ptr(scratch_dev),
+                                      scratch_bytes, _stream(stream)), "palquant_kv8_attention")

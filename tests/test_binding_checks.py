@@ -100,3 +100,49 @@ def test_index_tensors_are_counted(i):
             B.kv8_tokens(k, k, *index, 1)
         with pytest.raises(ValueError):
             B.kv8_attn(k, k.clone(), *index, 1, 32, 0.1)
+
+
+def test_scales_bias_and_codes_of_the_dense_layer_are_looked_at():
+    """Tensors too short or of another type are refused before the library is called; what passes gets as far as its status."""
+    x, w, y = torch.zeros(4, 64), torch.zeros(32, 64, dtype=torch.int8), torch.zeros(4, 32)
+    s_w, bias, s_x = torch.zeros(32), torch.zeros(32), torch.zeros(4)
+    d = B.linear_desc(x, w, y)
+    with pytest.raises(ValueError):
+        B.linear_desc(x, w, y.to("meta"))
+
+    def q8(**kw):
+        a = {"x": x, "w": w, "s_w": s_w, "bias": bias, "y": y} | kw
+        B.palquant_linear_q8(*a.values(), d, None, 0, stream=0)
+
+    def i8(**kw):
+        a = {"q": w[:4], "format": B.PQ_CODES_INT8, "ldq": 64, "s_x": s_x, "w": w, "s_w": s_w, "bias": bias, "acc": None, "y": None} | kw
+        B.palquant_linear_i8(*a.values(), d, stream=0)
+
+    def tokens(**kw):
+        a = {"x": x, "type": B.PQ_F32, "ldx": 64, "M": 4, "K": 64, "format": B.PQ_CODES_INT8, "q": w[:4], "ldq": 64, "s": s_x} | kw
+        B.palquant_quantize_tokens(*a.values(), stream=0)
+
+    for call in (q8, i8):  # (no scratch, no output)
+        with pytest.raises(B.PalquantError):
+            call()
+    with pytest.raises(B.PalquantError):
+        tokens(K=0)
+    long = {"s_w": torch.zeros(40), "bias": torch.zeros(40)}  # longer than the layer is wide: taken
+    with pytest.raises(B.PalquantError):
+        q8(**long)
+    for bad in ({"s_w": s_w[:31]}, {"s_w": s_w.half()}, {"bias": bias[:31]}, {"bias": bias.double()}, {"x": x[:3]}, {"x": x.half()},
+                {"x": torch.zeros(64, 4).t()}, {"w": w[:31]}, {"w": torch.zeros(32, 80, dtype=torch.int8)[:, :64]}, {"y": y[:, :31]}):
+        with pytest.raises(ValueError):
+            q8(**bad)
+    for bad in ({"q": w[:3]}, {"q": w[:4].half()}, {"format": B.PQ_CODES_F16}, {"ldq": 80}, {"s_x": s_x[:3]}, {"s_x": s_x.half()},
+                {"w": w[:31]}, {"s_w": s_w[:31]}, {"bias": bias[:31]}, {"acc": torch.zeros(4, 31, dtype=torch.int32)},
+                {"acc": torch.zeros(4, 32)}, {"y": y[:3]}):
+        with pytest.raises(ValueError):
+            i8(**bad)
+    for bad in ({"x": x[:3]}, {"x": x.half()}, {"type": B.PQ_F16}, {"ldx": 65}, {"M": 5}, {"K": 65}, {"q": w[:3]}, {"q": x},
+                {"format": B.PQ_CODES_F16}, {"ldq": 65}, {"s": s_x[:3]}, {"s": s_x.double()}):
+        with pytest.raises(ValueError):
+            tokens(**bad)
+    padded = torch.zeros(4, 80)[:, :64]
+    with pytest.raises(B.PalquantError):  # rows of a wider matrix: as far as its last element
+        tokens(x=padded, ldx=80, format=7)
