@@ -19,7 +19,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libpalquant.so")
 SOURCES = ["api.cu", "conv_tc.cu", "pointwise_tc.cu", "quantize.cu", "watchdog.cu", "act_steps_noalloc.cu", "net_f32.cu",
            "bitsplit.cu", "qat.cu", "linear_i8.cu", "linear_tc.cu", "kv8.cu", "kv8_attn.cu", "kv8_attn_tc.cu"]
-HEADERS = ["pq_device.cuh", "pq_internal.h", "pq_tokens.cuh", "pq_linear.h", "pq_kv8.cuh"]
+HEADERS = ["pq_device.cuh", "pq_internal.h", "pq_tokens.cuh", "pq_linear.h", "pq_kv8.cuh", "pq_words.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fno-strict-aliasing",
               "-I" + os.path.join(ROOT, "include")]

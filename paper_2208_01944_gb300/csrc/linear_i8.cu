@@ -26,6 +26,7 @@
 #include "pq_internal.h"
 #include "pq_linear.h"
 #include "pq_tokens.cuh"
+#include "pq_words.h"
 
 namespace pq {
 namespace {
@@ -120,8 +121,8 @@ template <bool WIDE>
 __device__ __forceinline__ uint4 codes16(const int8_t* row, int k, int K) {
   if (WIDE && k + 16 <= K) return *reinterpret_cast<const uint4*>(row + k);
   uint32_t w[4] = {0, 0, 0, 0};
-  if (!WIDE && k >= 3 && k + 19 <= K) {
-    const uintptr_t at = reinterpret_cast<uintptr_t>(row + k);
+  const uintptr_t at = reinterpret_cast<uintptr_t>(row + k);
+  if (!WIDE && words_lie_in_row(k, K, static_cast<int>(at & 3))) {
     const uint32_t* p = reinterpret_cast<const uint32_t*>(at & ~static_cast<uintptr_t>(3));
     const unsigned shift = 8 * static_cast<unsigned>(at & 3);
     const uint32_t a = p[0], b = p[1], c = p[2], d = p[3], e = p[4];
