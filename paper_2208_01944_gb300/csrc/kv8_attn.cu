@@ -572,6 +572,12 @@ bool valid_attn(const pq_kv8_cache* c, const pq_kv8_attn* a) {
   return !(a->scale != a->scale);
 }
 
+// Query rows, and with them tiles and blocks before the tokens are cut, are counted in 32 bits.
+// (The product of three 32-bit numbers may pass 64 bits; as doubles it is exact far beyond the limit.)
+bool countable(const pq_kv8_attn* a) {
+  return static_cast<double>(a->B) * a->max_q * a->Hq <= static_cast<double>(0x7FFFFFFF);
+}
+
 // Which kernel, its row tiles, and the parts of the token range.  Few query rows are
 // spread over the chip by cutting the tokens: two blocks an SM (as many as fit) of at
 // least 256 tokens (two steps of every warp), or, on the tensor cores, one block an SM of
@@ -653,7 +659,7 @@ size_t scratch_of(const AttnArgs& p) {
 extern "C" {
 
 size_t palquant_kv8_attention_scratch_bytes(const pq_kv8_cache* cache, const pq_kv8_attn* a) {
-  if (!pq::valid_attn(cache, a) || a->B == 0 || a->max_q == 0) return 0;
+  if (!pq::valid_attn(cache, a) || !pq::countable(a) || a->B == 0 || a->max_q == 0) return 0;
   pq::AttnArgs p = {};
   p.c = *cache;
   p.a = *a;
@@ -670,6 +676,7 @@ pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, v
       (a->page_table_dev == nullptr && a->max_len > 0) || !pq::is_aligned(q_dev, e) || !pq::is_aligned(o_dev, e) ||
       !pq::is_aligned(a->cu_q_dev, 4) || !pq::is_aligned(a->len_dev, 4) || !pq::is_aligned(a->page_table_dev, 4))
     return PQ_EINVAL;
+  if (!pq::countable(a)) return PQ_EUNSUPPORTED;
   pq::AttnArgs p = {};
   p.c = *cache;
   p.a = *a;
@@ -689,8 +696,7 @@ pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, v
     p.part = reinterpret_cast<float*>(p.ml + parts);
   }
   const int64_t units = static_cast<int64_t>(p.row_tiles) * p.splits * cache->Hkv;
-  if (units > 0x7FFFFFFFll / a->B || static_cast<int64_t>(a->max_q) * a->Hq > 0x7FFFFFFFll / a->B)
-    return PQ_EUNSUPPORTED;
+  if (units > 0x7FFFFFFFll / a->B) return PQ_EUNSUPPORTED;
   const unsigned grid = static_cast<unsigned>(units * a->B);
   p.err = pq::device_error_word();
   if (p.err == nullptr) return PQ_ECUDA;
