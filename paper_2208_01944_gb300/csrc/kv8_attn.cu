@@ -578,6 +578,14 @@ bool countable(const pq_kv8_attn* a) {
   return static_cast<double>(a->B) * a->max_q * a->Hq <= static_cast<double>(0x7FFFFFFF);
 }
 
+// The call with a window that no text is longer than taken as none: the same result, and the kernels'
+// position - window stays in 32 bits where queries outnumber the tokens (positions below 0).
+pq_kv8_attn without_idle_window(const pq_kv8_attn* a) {
+  pq_kv8_attn r = *a;
+  if (r.window >= r.max_len) r.window = 0;
+  return r;
+}
+
 // Which kernel, its row tiles, and the parts of the token range.  Few query rows are
 // spread over the chip by cutting the tokens: two blocks an SM (as many as fit) of at
 // least 256 tokens (two steps of every warp), or, on the tensor cores, one block an SM of
@@ -662,8 +670,8 @@ size_t palquant_kv8_attention_scratch_bytes(const pq_kv8_cache* cache, const pq_
   if (!pq::valid_attn(cache, a) || !pq::countable(a) || a->B == 0 || a->max_q == 0) return 0;
   pq::AttnArgs p = {};
   p.c = *cache;
-  p.a = *a;
-  pq::plan_attention(cache, a, &p);
+  p.a = pq::without_idle_window(a);
+  pq::plan_attention(cache, &p.a, &p);
   return pq::scratch_of(p);
 }
 
@@ -679,14 +687,14 @@ pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, v
   if (!pq::countable(a)) return PQ_EUNSUPPORTED;
   pq::AttnArgs p = {};
   p.c = *cache;
-  p.a = *a;
+  p.a = pq::without_idle_window(a);
   p.q = q_dev;
   p.o = o_dev;
   p.group = a->Hq / cache->Hkv;
   p.page_shift = cache->page_tokens == 16 ? 4 : cache->page_tokens == 32 ? 5 : cache->page_tokens == 64 ? 6 : 7;
   p.wide_q = pq::is_aligned(q_dev, 16) && a->q_token_stride * e % 16 == 0 && a->q_head_stride * e % 16 == 0;
   p.wide_o = pq::is_aligned(o_dev, 16) && a->o_token_stride * e % 16 == 0 && a->o_head_stride * e % 16 == 0;
-  const pq::Plan plan = pq::plan_attention(cache, a, &p);
+  const pq::Plan plan = pq::plan_attention(cache, &p.a, &p);
   p.wait_limit_ns = pq::wait_limit_ns();
   const size_t need = pq::scratch_of(p);
   if (need > 0 && (scratch_dev == nullptr || scratch_bytes < need || !pq::is_aligned(scratch_dev, 16))) return PQ_EINVAL;
