@@ -612,8 +612,8 @@ pq_status palquant_kv8_read(const pq_kv8_cache* cache, void* k_dev, void* v_dev,
  * enter the products as half values scaled by a power of two for each row, and
  * the probabilities as half values; PQ_F32 carries a second half value for the rest of
  * each.  max_len >= every len_dev[b], max_q >= every n (both on the host, so that
- * the call does not wait for the device); Hq / Hkv <= 64; B max_q Hq below 2^31
- * (PQ_EUNSUPPORTED else). */
+ * the call does not wait for the device); Hq / Hkv <= 64; max_len and max_q up to 2^30
+ * and B max_q Hq below 2^31 (PQ_EUNSUPPORTED else). */
 typedef struct {
     int32_t type; /* pq_float_type of q and o */
     int32_t B, Hq, max_q, max_len;

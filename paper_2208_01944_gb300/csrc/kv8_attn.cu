@@ -574,8 +574,9 @@ bool valid_attn(const pq_kv8_cache* c, const pq_kv8_attn* a) {
 
 // Query rows, and with them tiles and blocks before the tokens are cut, are counted in 32 bits.
 // (The product of three 32-bit numbers may pass 64 bits; as doubles it is exact far beyond the limit.)
+// Positions are too, and a part's end or a warp's next step lies up to a part beyond the last: up to 2^30 of them.
 bool countable(const pq_kv8_attn* a) {
-  return static_cast<double>(a->B) * a->max_q * a->Hq <= static_cast<double>(0x7FFFFFFF);
+  return a->max_len <= 1 << 30 && a->max_q <= 1 << 30 && static_cast<double>(a->B) * a->max_q * a->Hq <= static_cast<double>(0x7FFFFFFF);
 }
 
 // The call with a window that no text is longer than taken as none: the same result, and the kernels'

@@ -38,3 +38,9 @@ ROWS = [dict(type=0, Hq=128, max_q=1 << 30), dict(Hq=128, max_q=1 << 30), dict(m
 @pytest.mark.parametrize("changes", ROWS, ids=str)
 def test_too_many_query_rows(changes):
     _refused(**changes)
+
+
+@pytest.mark.parametrize("changes", [dict(max_len=(1 << 30) + 1), dict(max_len=0x7FFFFFFF), dict(type=0, max_len=0x7FFFFFFF, window=5),
+                                     dict(B=1, Hq=2, max_q=(1 << 30) - 1, max_len=0x7FFFFF80)], ids=str)
+def test_positions_past_the_parts_ends(changes):
+    _refused(**changes)
