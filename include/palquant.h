@@ -523,7 +523,7 @@ typedef struct {
  * from one row to the next.  code_format PQ_CODES_INT8 (signed bytes) or
  * PQ_CODES_F16 (the codes as IEEE half values), q_dev [M, ldq], s_dev M floats.
  * Any alignment of the type; rows on 16-byte boundaries are read and written 16
- * bytes at a time.  M = 0 does nothing. */
+ * bytes at a time.  M = 0 does nothing; M up to 2^31 - 1, K up to 2^31 - 8 (PQ_EUNSUPPORTED else). */
 pq_status palquant_quantize_tokens(const void* x_dev, int32_t x_type, int64_t ldx, int64_t M, int32_t K,
                                    int32_t code_format, void* q_dev, int64_t ldq, float* s_dev, pq_stream_t stream);
 

@@ -429,6 +429,8 @@ bool valid_linear(const pq_linear_desc* d) {
          valid_type(d->y_type) && d->ldx >= d->K && d->ldw >= d->K && d->ldy >= d->N;
 }
 
+constexpr int64_t kMostTokens = 0x7FFFFFFF;  // a block each in the quantiser
+
 bool aligned_rows(const pq_linear_desc* d) { return d->ldw % 16 == 0; }
 // Weight rows off 16-byte boundaries: the kernels for few tokens read them in place, again for
 // every 16 tokens; the tensor cores' loads want a copy.  With the copy against without (us):
@@ -492,7 +494,7 @@ pq_status palquant_quantize_tokens(const void* x_dev, int32_t x_type, int64_t ld
   if (!pq::valid_type(x_type) || M < 0 || K < 1 || ldx < K || ldq < K) return PQ_EINVAL;
   if (code_format != PQ_CODES_INT8 && code_format != PQ_CODES_F16) return PQ_EINVAL;
   if (M == 0) return PQ_OK;
-  if (M > 0x7FFFFFFF) return PQ_EUNSUPPORTED;
+  if (M > pq::kMostTokens || K > 0x7FFFFFF8) return PQ_EUNSUPPORTED;  // blocks, and K rounded up to vectors of 8
   const bool half = code_format == PQ_CODES_F16;
   if (x_dev == nullptr || q_dev == nullptr || s_dev == nullptr || !pq::is_aligned(x_dev, pq::bytes_of_type(x_type)) ||
       !pq::is_aligned(q_dev, half ? 2 : 1) || !pq::is_aligned(s_dev, 4))
@@ -522,7 +524,7 @@ pq_status palquant_linear_i8(const void* q_dev, int32_t code_format, int64_t ldq
 }
 
 size_t palquant_linear_q8_scratch_bytes(const pq_linear_desc* d) {
-  if (!pq::valid_linear(d)) return 0;
+  if (!pq::valid_linear(d) || d->M > pq::kMostTokens) return 0;
   if (!pq::copies_weights(d)) return pq::scales_at(d) + static_cast<size_t>(d->M) * sizeof(float);
   return pq::weights_at(d) + static_cast<size_t>(d->N) * static_cast<size_t>(pq::padded_k(d));
 }
@@ -532,6 +534,7 @@ pq_status palquant_linear_q8(const void* x_dev, const int8_t* w_dev, const float
                              pq_stream_t stream) {
   if (!pq::valid_linear(d)) return PQ_EINVAL;
   if (d->M == 0) return PQ_OK;
+  if (d->M > pq::kMostTokens) return PQ_EUNSUPPORTED;
   if (x_dev == nullptr || w_dev == nullptr || s_w_dev == nullptr || y_dev == nullptr || scratch_dev == nullptr ||
       !pq::is_aligned(scratch_dev, 16) || scratch_bytes < palquant_linear_q8_scratch_bytes(d) ||
       !pq::is_aligned(y_dev, pq::bytes_of_type(d->y_type)) || !pq::is_aligned(s_w_dev, 4) ||
