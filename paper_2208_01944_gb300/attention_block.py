@@ -24,6 +24,7 @@ import torch
 
 from . import binding as B
 
+_INDEX_BUFFERS = 16
 _TYPES = {torch.float32: B.PQ_F32, torch.float16: B.PQ_F16, torch.bfloat16: B.PQ_BF16}
 
 
@@ -67,7 +68,12 @@ class AttentionBlock8:
             self.cache = B.kv8_cache(self.k, self.v, self.k_scale, self.v_scale)
             self.table = torch.arange(n, dtype=torch.int32, device=self.dev).view(sequences, pages)
             self._work = torch.empty(0, dtype=torch.uint8, device=self.dev)
-        self.lens = [0] * sequences  # tokens cached, on the host: no call waits for the device
+            # a call's positions, page-locked: a copy from pageable memory would wait for the device.  Used in turn, each
+            # again once its last copy is over (the host waits only when it is that many calls ahead)
+            self._index = torch.empty((_INDEX_BUFFERS, 3 * sequences + 1), dtype=torch.int32, pin_memory=True)
+            self._copied = [torch.cuda.Event() for _ in range(_INDEX_BUFFERS)]
+            self._calls = 0
+        self.lens = [0] * sequences  # tokens cached, on the host: no call waits for the device to know them
 
     def _enter(self, *tensors) -> None:
         """The block's stream waits for what the caller's has been given, and holds the caller's tensors."""
@@ -81,6 +87,16 @@ class AttentionBlock8:
         if self._work.numel() < n:
             self._work = torch.empty(n, dtype=torch.uint8, device=self.dev)
         return self._work
+
+    def _to_device(self, values) -> torch.Tensor:
+        """Positions on the device, without waiting for it."""
+        i = self._calls % _INDEX_BUFFERS
+        self._calls += 1
+        self._copied[i].synchronize()  # (returns at once before the first record)
+        self._index[i] = torch.tensor(values, dtype=torch.int32)
+        index = self._index[i].to(self.dev, non_blocking=True)
+        self._copied[i].record()
+        return index
 
     def _linear(self, x, w, s_w, bias, y):
         d = B.linear_desc(x, w, y)
@@ -108,7 +124,7 @@ class AttentionBlock8:
             ends = [0]
             for c in counts:
                 ends.append(ends[-1] + c)
-            index = torch.tensor(ends + self.lens + after, dtype=torch.int32, device=self.dev)
+            index = self._to_device(ends + self.lens + after)
             cu, start, lens = index.split([self.sequences + 1, self.sequences, self.sequences])
             qkv = torch.empty((tokens, (Hq + 2 * Hkv) * D), dtype=self.dtype, device=self.dev)
             self._linear(x, self.w_qkv, self.s_qkv, self.b_qkv, qkv)
