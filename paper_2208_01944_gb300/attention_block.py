@@ -20,6 +20,8 @@ wrote them (columns of its output), so nothing is copied between the four calls.
 """
 from __future__ import annotations
 
+import contextlib
+
 import torch
 
 from . import binding as B
@@ -28,14 +30,39 @@ _INDEX_BUFFERS = 16
 _TYPES = {torch.float32: B.PQ_F32, torch.float16: B.PQ_F16, torch.bfloat16: B.PQ_BF16}
 
 
+@contextlib.contextmanager
+def _in_turn(device, stream: torch.cuda.Stream | None, *tensors):
+    """Inside, `stream` (None: the current one) is current: after what the caller's stream holds and before what it is given
+    next.  `tensors`, the caller's, are held until it is done with them."""
+    caller = torch.cuda.current_stream(device)
+    if stream is None or stream == caller:
+        yield caller
+        return
+    stream.wait_stream(caller)
+    for t in tensors:
+        t.record_stream(stream)
+    with torch.cuda.stream(stream):
+        yield stream
+    caller.wait_stream(stream)
+
+
+def _give(device, *tensors) -> None:
+    """Tensors made on another stream, held until the current one is done with them."""
+    for t in tensors:
+        t.record_stream(torch.cuda.current_stream(device))
+
+
 def weight_codes(w: torch.Tensor, stream: torch.cuda.Stream | None = None):
-    """Signed 8-bit codes [N, K] and one scale for each output channel (row) of w: the token quantiser on the rows."""
+    """Signed 8-bit codes [N, K] and one scale for each output channel (row) of w: the token quantiser on the rows.  It runs
+    on `stream` (None: the current one), after what the current stream holds and before what it is given next."""
     if w.dim() != 2 or w.dtype not in _TYPES or w.stride(1) != 1:
         raise ValueError("w: a float matrix with contiguous rows")
-    codes = torch.empty(w.shape, dtype=torch.int8, device=w.device)
-    scales = torch.empty(w.shape[0], device=w.device)
-    B.palquant_quantize_tokens(w, _TYPES[w.dtype], w.stride(0), w.shape[0], w.shape[1], B.PQ_CODES_INT8, codes,
-                               w.shape[1], scales, stream)
+    with _in_turn(w.device, stream, w) as run:
+        codes = torch.empty(w.shape, dtype=torch.int8, device=w.device)
+        scales = torch.empty(w.shape[0], device=w.device)
+        B.palquant_quantize_tokens(w, _TYPES[w.dtype], w.stride(0), w.shape[0], w.shape[1], B.PQ_CODES_INT8, codes,
+                                   w.shape[1], scales, run)
+    _give(w.device, codes, scales)
     return codes, scales
 
 
