@@ -48,8 +48,9 @@ def _in_turn(device, stream: torch.cuda.Stream | None, *tensors):
 
 def _give(device, *tensors) -> None:
     """Tensors made on another stream, held until the current one is done with them."""
+    current = torch.cuda.current_stream(device)
     for t in tensors:
-        t.record_stream(torch.cuda.current_stream(device))
+        t.record_stream(current)
 
 
 def weight_codes(w: torch.Tensor, stream: torch.cuda.Stream | None = None):
@@ -81,12 +82,12 @@ class AttentionBlock8:
             raise ValueError("w_out: [hidden, heads D], of w_qkv's type")
         self.dtype, self.dev, self.stream = w_qkv.dtype, w_qkv.device, stream
         self.sequences, self.max_len = sequences, max_len
-        self.b_qkv = None if b_qkv is None else b_qkv.to(self.dev, torch.float32).contiguous()
-        self._enter(w_qkv, w_out)
-        with torch.cuda.stream(self.stream):
+        given = [t for t in (w_qkv, w_out, b_qkv) if t is not None and t.is_cuda]
+        with _in_turn(self.dev, stream, *given) as run:
+            self.b_qkv = None if b_qkv is None else b_qkv.to(self.dev, torch.float32).contiguous()
             w_qkv, w_out = w_qkv.contiguous(), w_out.contiguous()
-            self.w_qkv, self.s_qkv = weight_codes(w_qkv, stream)
-            self.w_out, self.s_out = weight_codes(w_out, stream)
+            self.w_qkv, self.s_qkv = weight_codes(w_qkv, run)
+            self.w_out, self.s_out = weight_codes(w_out, run)
             pages = -(-max_len // page_tokens)
             n = sequences * pages
             self.k, self.v = (torch.zeros((n, kv_heads, page_tokens, self.D), dtype=torch.int8, device=self.dev)
@@ -94,41 +95,44 @@ class AttentionBlock8:
             self.k_scale, self.v_scale = (torch.zeros((n, kv_heads), device=self.dev) for _ in range(2))
             self.cache = B.kv8_cache(self.k, self.v, self.k_scale, self.v_scale)
             self.table = torch.arange(n, dtype=torch.int32, device=self.dev).view(sequences, pages)
-            self._work = torch.empty(0, dtype=torch.uint8, device=self.dev)
             # a call's positions, page-locked: a copy from pageable memory would wait for the device.  Used in turn, each
             # again once its last copy is over (the host waits only when it is that many calls ahead)
             self._index = torch.empty((_INDEX_BUFFERS, 3 * sequences + 1), dtype=torch.int32, pin_memory=True)
             self._copied = [torch.cuda.Event() for _ in range(_INDEX_BUFFERS)]
             self._calls = 0
+            self._own = [t for t in (self.b_qkv, self.w_qkv, self.s_qkv, self.w_out, self.s_out, self.k, self.v, self.k_scale,
+                                     self.v_scale, self.table) if t is not None]
+            self._ran, self._over = run, torch.cuda.Event()  # the last call's stream, and its end there
+            self._over.record(run)
         self.lens = [0] * sequences  # tokens cached, on the host: no call waits for the device to know them
 
-    def _enter(self, *tensors) -> None:
-        """The block's stream waits for what the caller's has been given, and holds the caller's tensors."""
-        if self.stream is not None:
-            self.stream.wait_stream(torch.cuda.current_stream(self.dev))
-            for t in tensors:
-                t.record_stream(self.stream)
+    def _follow(self, run: torch.cuda.Stream) -> None:
+        """With no stream of its own the block runs on its callers': after its last call, which held another stream, and
+        with its memory held for this one too."""
+        if run != self._ran:
+            run.wait_event(self._over)
+            for t in self._own:
+                t.record_stream(run)
+            self._ran = run
 
-    def _scratch(self, n: int) -> torch.Tensor:
-        """The workspace, grown when a call needs more; the calls of a forward() follow each other on one stream."""
-        if self._work.numel() < n:
-            self._work = torch.empty(n, dtype=torch.uint8, device=self.dev)
-        return self._work
-
-    def _to_device(self, values) -> torch.Tensor:
+    def _to_device(self, values, run) -> torch.Tensor:
         """Positions on the device, without waiting for it."""
         i = self._calls % _INDEX_BUFFERS
         self._calls += 1
         self._copied[i].synchronize()  # (returns at once before the first record)
         self._index[i] = torch.tensor(values, dtype=torch.int32)
         index = self._index[i].to(self.dev, non_blocking=True)
-        self._copied[i].record()
+        self._copied[i].record(run)
         return index
 
-    def _linear(self, x, w, s_w, bias, y):
+    def _scratch(self, n: int) -> torch.Tensor:
+        """A call's workspace, of its stream's pool."""
+        return torch.empty(n, dtype=torch.uint8, device=self.dev)
+
+    def _linear(self, x, w, s_w, bias, y, run):
         d = B.linear_desc(x, w, y)
         work = self._scratch(B.palquant_linear_q8_scratch_bytes(d))
-        B.palquant_linear_q8(x, w, s_w, bias, y, d, work, work.numel(), self.stream)
+        B.palquant_linear_q8(x, w, s_w, bias, y, d, work, work.numel(), run)
 
     def reset(self, sequence: int) -> None:
         self.lens[sequence] = 0
@@ -136,7 +140,7 @@ class AttentionBlock8:
     def forward(self, x: torch.Tensor, counts) -> torch.Tensor:
         """x [sum(counts), hidden]: counts[b] new tokens of every sequence b, one sequence after the other; returns y
         of x's shape.  It runs on the block's stream (None: the current one), after what the current stream holds and
-        before what it is given next."""
+        before what it is given next; with the current stream another than the last call's, after that call too."""
         counts = [int(c) for c in counts]
         if len(counts) != self.sequences or min(counts) < 0 or x.shape != (sum(counts), self.hidden) or x.dtype != self.dtype:
             raise ValueError("counts: one for each sequence; x: [sum(counts), hidden] of the weights' type")
@@ -146,26 +150,26 @@ class AttentionBlock8:
         if not sum(counts):
             return torch.empty_like(x)
         Hq, Hkv, D, tokens = self.heads, self.kv_heads, self.D, x.shape[0]
-        self._enter(x)
-        with torch.cuda.stream(self.stream):
+        with _in_turn(self.dev, self.stream, x) as run:
+            self._follow(run)
             ends = [0]
             for c in counts:
                 ends.append(ends[-1] + c)
-            index = self._to_device(ends + self.lens + after)
+            index = self._to_device(ends + self.lens + after, run)
             cu, start, lens = index.split([self.sequences + 1, self.sequences, self.sequences])
             qkv = torch.empty((tokens, (Hq + 2 * Hkv) * D), dtype=self.dtype, device=self.dev)
-            self._linear(x, self.w_qkv, self.s_qkv, self.b_qkv, qkv)
+            self._linear(x, self.w_qkv, self.s_qkv, self.b_qkv, qkv, run)
             q, k, v = qkv.view(tokens, Hq + 2 * Hkv, D).split([Hq, Hkv, Hkv], 1)
-            B.palquant_kv8_append(self.cache, k, v, B.kv8_tokens(k, v, cu, start, self.table, max(counts)), self.stream)
+            B.palquant_kv8_append(self.cache, k, v, B.kv8_tokens(k, v, cu, start, self.table, max(counts)), run)
             mixed = torch.empty((tokens, Hq, D), dtype=self.dtype, device=self.dev)
             a = B.kv8_attn(q, mixed, cu, lens, self.table, max(counts), max(after), D ** -0.5, True, self.window)
             work = self._scratch(B.palquant_kv8_attention_scratch_bytes(self.cache, a))
-            B.palquant_kv8_attention(self.cache, q, mixed, a, work, work.numel(), self.stream)
+            B.palquant_kv8_attention(self.cache, q, mixed, a, work, work.numel(), run)
             y = torch.empty((tokens, self.hidden), dtype=self.dtype, device=self.dev)
-            self._linear(mixed.view(tokens, Hq * D), self.w_out, self.s_out, None, y)
+            self._linear(mixed.view(tokens, Hq * D), self.w_out, self.s_out, None, y, run)
+            self._over.record(run)
         if self.stream is not None:
-            torch.cuda.current_stream(self.dev).wait_stream(self.stream)
-            y.record_stream(torch.cuda.current_stream(self.dev))
+            _give(self.dev, y, qkv, mixed)
         self.lens = after
         self.qkv, self.mixed = qkv, mixed  # the last call's, for inspection
         return y
