@@ -72,19 +72,25 @@ class AttentionBlock8:
                  b_qkv: torch.Tensor | None = None, page_tokens: int = 64, window: int = 0,
                  stream: torch.cuda.Stream | None = None):
         """w_qkv [(heads + 2 kv_heads) D, hidden] (the rows of q, then k, then v) and w_out [hidden, heads D] on the
-        GPU; their type is the activations'."""
-        if heads % kv_heads or w_qkv.shape[0] % (heads + 2 * kv_heads):
+        GPU; their type is the activations'.  b_qkv: a value for each row of w_qkv."""
+        if w_qkv.dim() != 2 or w_qkv.dtype not in _TYPES or sequences < 1 or max_len < 1 or window < 0 or page_tokens not in (16, 32, 64, 128):
+            raise ValueError("w_qkv: a float matrix; at least one sequence and token; window >= 0; page_tokens: 16, 32, 64 or 128")
+        if heads < 1 or kv_heads < 1 or heads % kv_heads or w_qkv.shape[0] % (heads + 2 * kv_heads):
             raise ValueError("heads: a multiple of kv_heads; w_qkv: heads + 2 kv_heads blocks of rows")
         self.heads, self.kv_heads, self.window = heads, kv_heads, window
         self.D = w_qkv.shape[0] // (heads + 2 * kv_heads)
         self.hidden = w_qkv.shape[1]
+        if self.D % 16 or not 16 <= self.D <= 256:
+            raise ValueError("w_qkv: heads of D, a multiple of 16 from 16 to 256")
+        if b_qkv is not None and b_qkv.numel() != w_qkv.shape[0]:
+            raise ValueError("b_qkv: a value for each row of w_qkv")
         if w_out.shape != (self.hidden, heads * self.D) or w_out.dtype != w_qkv.dtype:
             raise ValueError("w_out: [hidden, heads D], of w_qkv's type")
         self.dtype, self.dev, self.stream = w_qkv.dtype, w_qkv.device, stream
         self.sequences, self.max_len = sequences, max_len
         given = [t for t in (w_qkv, w_out, b_qkv) if t is not None and t.is_cuda]
         with _in_turn(self.dev, stream, *given) as run:
-            self.b_qkv = None if b_qkv is None else b_qkv.to(self.dev, torch.float32).contiguous()
+            self.b_qkv = None if b_qkv is None else b_qkv.to(self.dev, torch.float32).contiguous().view(-1)
             w_qkv, w_out = w_qkv.contiguous(), w_out.contiguous()
             self.w_qkv, self.s_qkv = weight_codes(w_qkv, run)
             self.w_out, self.s_out = weight_codes(w_out, run)
@@ -142,8 +148,9 @@ class AttentionBlock8:
         of x's shape.  It runs on the block's stream (None: the current one), after what the current stream holds and
         before what it is given next; with the current stream another than the last call's, after that call too."""
         counts = [int(c) for c in counts]
-        if len(counts) != self.sequences or min(counts) < 0 or x.shape != (sum(counts), self.hidden) or x.dtype != self.dtype:
-            raise ValueError("counts: one for each sequence; x: [sum(counts), hidden] of the weights' type")
+        if len(counts) != self.sequences or min(counts) < 0 or x.shape != (sum(counts), self.hidden) \
+                or x.dtype != self.dtype or x.device != self.dev:
+            raise ValueError("counts: one for each sequence; x: [sum(counts), hidden] of the weights' type, on their device")
         after = [n + c for n, c in zip(self.lens, counts)]
         if max(after) > self.max_len:
             raise ValueError(f"a sequence would pass max_len = {self.max_len}")
