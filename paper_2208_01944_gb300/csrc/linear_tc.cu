@@ -613,9 +613,10 @@ cudaError_t launch_linear_tc(const LinearArgs& a, bool after_tokens, cudaStream_
   p.wait_limit_ns = wait_limit_ns();
   if (p.err == nullptr) return cudaErrorInitializationError;
   // Tiles.  Up to 128 tokens: single blocks, one tile of tokens, the fewest columns
-  // that hold them.  More: the cheaper of single blocks of 128 tokens and pairs of 128,
-  // 160 or 192, by rounds of tiles x the time of 64 of K, which was 384, 404 and 423 cycles for
-  // the pairs (about bn + 500 in units of 0.6 cycles).  Single blocks share K while the
+  // that hold them.  More: the cheaper of single blocks of 128 tokens and pairs of 160
+  // or 192, by rounds of tiles x the time of 64 of K, which was 404 and 423 cycles for
+  // the pairs and 384 for pairs of 128 (about bn + 500 in units of 0.6 cycles), which never take
+  // fewer rounds than single blocks of 128.  Single blocks share K while the
   // chip is less than half full and each part keeps 256 of K; eight parts of 128 tokens
   // take longer to add than they save (16 tiles of K = 8192: 22 us, four parts 15 us), and
   // of clusters of eight only one or two fit a part of the chip at a time (64 tokens, K = 8192: 16
@@ -628,7 +629,7 @@ cudaError_t launch_linear_tc(const LinearArgs& a, bool after_tokens, cudaStream_
   bool pair = false;
   if (a.M > 128) {
     double best = static_cast<double>(ceil_div(singles * p.k_parts, sms)) * (bn + 500) / p.k_parts;
-    for (int c = 192; c >= 128; c -= 32) {
+    for (int c = 192; c >= 160; c -= 32) {
       const double cost =
           static_cast<double>(ceil_div(ceil_div(a.N, 256) * ceil_div(a.M, c), std::max(1, sms / 2))) * (c + 500);
       if (cost < best) best = cost, bn = c, pair = true;
@@ -647,8 +648,7 @@ cudaError_t launch_linear_tc(const LinearArgs& a, bool after_tokens, cudaStream_
                      CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorInvalidValue;
   if (pair && bn == 192) return launch<192, true>(p, w, q, sms, after_tokens, stream);
-  if (pair && bn == 160) return launch<160, true>(p, w, q, sms, after_tokens, stream);
-  if (pair) return launch<128, true>(p, w, q, sms, after_tokens, stream);
+  if (pair) return launch<160, true>(p, w, q, sms, after_tokens, stream);
   if (bn == 32) return launch<32, false>(p, w, q, sms, after_tokens, stream);
   if (bn == 64) return launch<64, false>(p, w, q, sms, after_tokens, stream);
   return launch<128, false>(p, w, q, sms, after_tokens, stream);
