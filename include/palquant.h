@@ -536,6 +536,7 @@ int32_t palquant_linear_code_format(const pq_linear_desc* d);
  *   y[m, n] = fl(fl((float)acc * s_x[m]) * s_w[n]), then fl(y + bias[n]) if
  *   bias_dev != NULL, rounded to y_type once.
  * q_dev [M, ldq] in code_format; s_x_dev M floats, s_w_dev and bias_dev N floats;
+ * Fastest with rows of codes and weights (addresses and pitches) on 16-byte boundaries.
  * acc_dev (int32 [M, N], contiguous) and y_dev may each be NULL, not both (s_x_dev
  * and s_w_dev may be NULL when y_dev is).  d->x_type and d->ldx are not read.
  * M = 0 does nothing.  M above 16 * 65535 needs PQ_CODES_F16 and rows of codes and
@@ -610,8 +611,9 @@ pq_status palquant_kv8_read(const pq_kv8_cache* cache, void* k_dev, void* v_dev,
  *   o = sum softmax(score) v;        a query that sees no token gives 0.
  * Scores, softmax statistics and sums are fp32.  Queries of PQ_F16 and PQ_BF16
  * enter the products as half values scaled by a power of two for each row, and
- * the probabilities as half values; PQ_F32 carries a second half value for the rest of
- * each.  max_len >= every len_dev[b], max_q >= every n (both on the host, so that
+ * the probabilities, times their page's value scale, as half values; PQ_F32 carries a second half
+ * value for the rest of each.  Such a weight has its 11 (22) bits down to 2^-20 (2^-16) of the row's
+ * largest, and fewer below that: an error of at most 2^-31 (2^-38) of the largest.  max_len >= every len_dev[b], max_q >= every n (both on the host, so that
  * the call does not wait for the device); Hq / Hkv <= 64; max_len and max_q up to 2^30
  * and B max_q Hq below 2^31 (PQ_EUNSUPPORTED else). */
 typedef struct {

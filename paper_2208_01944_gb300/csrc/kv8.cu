@@ -7,7 +7,7 @@
 // dependent loads (16 tokens a page, 8 x 2000 tokens of 8 heads of 128: 28 us one head
 // a block, 18 us eight).
 // Bound by HBM: each new element is read once and each code written once.  16 prompts of up to 4096
-// tokens, 8 heads of 128, bf16: append 67 us, read 46 us (4.2 and 6.1 TB/s); the rest is the
+// tokens, 8 heads of 128, bf16: append 67 us, read 47 us (4.2 and 6.0 TB/s); the rest is the
 // blocks' dependent lookups.
 #include <cuda_runtime.h>
 

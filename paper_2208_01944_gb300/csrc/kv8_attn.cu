@@ -19,14 +19,17 @@
 // Codes come through shared memory, three or four steps of each warp in flight (16-byte
 // asynchronous copies into a ring of the warp's own, no block-wide wait): with loads
 // straight into registers a step waited for its page's id and then for its codes, and a
-// batch of single tokens read 3.9 TB/s; now 4.6 (64 over up to 8192, 32 / 8 heads of 128: 146 us),
-// bound by the instructions issued, a third of them the codes' conversions.  Few query rows are spread over the chip by splitting
+// batch of single tokens read 3.9 TB/s; now 4.7 (64 over up to 8192, 32 / 8 heads of 128: 143 us).  Of
+// the rest, instructions (60 % of the issue slots, a third of them the codes' conversions) are one part and uneven shares
+// the other: 512 uncut (sequence, head) blocks of ragged lengths on 304 places keep 65 % of them at work, by a simulation
+// of that schedule.  Few query rows are spread over the chip by splitting
 // the tokens; the parts' maxima, sums and outputs are joined by pq_kv8_join.
 //
 // Rounding.  Queries enter as halves scaled by a power of two for each row so that their largest
 // element lies in [2^7, 2^8) (exact for 16-bit queries down to 2^-22 of it), w as
 // halves (scaled, see kWShift); fp32 queries and their w carry a
-// second half for the remainder (22 bits).  All sums are fp32.
+// second half for the remainder (22 bits).  All sums are fp32.  exp2 and log2 are the chip's approximations
+// (2^-22 or so of the result, for log2 of values near 1 absolute): below both.
 #include <cuda_runtime.h>
 
 #include <algorithm>

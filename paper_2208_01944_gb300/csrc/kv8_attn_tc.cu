@@ -12,10 +12,10 @@
 // 4600 cycles a step).  One thread's MMAs run in order, so scores never overwrite
 // probabilities in use.  The outputs stay in tensor memory; they are rescaled only when
 // a row's maximum has grown by more than 2^8 (w, scaled by 2^6, stays below 2^14; a half holds 2^16).
-// Bound by the softmax's instructions, then by the tensor rate (at D = 128 a step's
-// products take 2560 cycles: scores of 64 tokens wait for shared memory, 48 cycles an MMA
-// instead of 32).  Four prompts of 2048 over 4096, 32 / 8 heads of 128: 277 us (0.80 PFLOP/s); one of
-// 8192, causal: 570 us (0.96 PFLOP/s).
+// Bound by waiting: at D = 128 a step's products take 2560 cycles (scores of 64 tokens wait for
+// shared memory, 48 cycles an MMA instead of 32), a step about 5500 over a whole launch, and no pipe is near its limit (issue 48 %,
+// exponentials 19 %).  Both tiles share their barriers, so their softmax runs at one time and little covers it.  Four prompts
+// of 2048 over 4096, 32 / 8 heads of 128: 278 us (0.79 PFLOP/s); one of 8192, causal: 569 us (0.97 PFLOP/s).
 //
 // Roles (16 warps): 0 issues the MMAs, 4 looks up pages, the other six below 8 convert
 // (none of them on the issuing warp's scheduler), 8-11 and 12-15 are the tiles' softmax.  Tiles with the most tokens come first.

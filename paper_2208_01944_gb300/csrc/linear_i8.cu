@@ -16,8 +16,8 @@
 // the tokens its 8 columns, so few tokens waste little.  The warps of a block share
 // 16 output channels and take turns along K, each lane reading 16 contiguous
 // bytes; within a 64-wide step the order of K is the lanes' own, the same for both
-// operands.  Measured, tokens quantised: one token times 4096 x 4096 6.6 us, 8 x 8192 x 8192
-// 17.1 us (3.9 TB/s of weights), one token times 12000 rows of 1001 codes 8.4 us.
+// operands.  Measured, whole calls in a graph, inputs in turn beyond L2: one token times 4096 x 4096 7.5 us, 8 x
+// 8192 x 8192 17.2 us (3.9 TB/s of weights), one token times 12000 rows of 1001 codes 9.4 us.
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -277,8 +277,8 @@ __global__ void __launch_bounds__(32 * kRowWarps) pq_linear_rows(const __grid_co
 // ahead (no other lane reads them, so nothing but the lane's own copies is waited for).
 // Bound by the weights' bytes; registers hold one step, so blocks of 8 warps keep 100 KB in
 // flight on an SM.  The rings are no deeper than a warp has steps, for more blocks on an SM
-// where K is short.  One token times 4096 x 4096, tokens quantised: 6.5 us, and 8 x 8192 x 8192 17.3
-// (9.8 and 20.7 with loads into registers; rings of 8 steps take 7.0 and 18.5).
+// where K is short.  When they came, calls with their weights in L2 (now 6.1 and 15.4 us): one token times 4096 x 4096
+// 9.8 us with loads into registers, 6.5 with these rings, 7.0 with rings of 8 steps; 8 x 8192 x 8192 20.7, 17.3 and 18.5.
 template <int NT, int RING>
 __host__ __device__ constexpr int ring_bytes() { return kRowWarps * RING * (2 + NT) * 512; }
 

@@ -23,8 +23,8 @@
 // write.  A stage is 128 of K: waiting for one and freeing it costs the issuing warp about
 // 130 cycles beside its MMAs, more than there are to spare with stages of 64.  Few
 // tiles: the blocks of a cluster take parts of K of one tile and add their int32 sums
-// through distributed shared memory (in a fixed order; exact anyway).  Measured: 8192 x 8192 x 8192
-// 558 us (1.97 PFLOP/s), 2048 x 4096 x 4096 46 us, 48 x 8192 x 4096 14.7 us (2.3 TB/s of weights).
+// through distributed shared memory (in a fixed order; exact anyway).  Measured, the product alone: 8192 x 8192 x 8192
+// 560 us (1.96 PFLOP/s), 2048 x 4096 x 4096 47 us, 48 x 8192 x 4096 14.5 us (2.3 TB/s of weights).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -250,7 +250,7 @@ __device__ __forceinline__ void put_column(const LinearArgs& a, int64_t m, int n
 
 // Tokens j, j + 8, .. of a tile below `end`, U of them: four channels of each, summed over the cluster's
 // parts, I at a time, and written.  U x I loads from the peers are on their way together (one after the
-// other, 48 x 8192 x 4096 spent 2.4 of its 16.3 us here, now 1.4 of 15.2).
+// other, a call of 48 x 8192 x 4096 spent 2.4 of its 16.3 us here, now 1.4 of 15.3).
 template <int U, int I, int kCols>
 __device__ __forceinline__ void add_parts(const LinearTc& p, uint32_t from, int j, int end, const float (&scales)[8][kCols],
                                           int64_t m0, int n, const float (&s_w)[4], const float (&bias)[4], bool wide) {
