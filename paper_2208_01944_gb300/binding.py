@@ -4,7 +4,8 @@ Functions keep the C names and argument order.  They only marshal arguments:
 device buffers are passed as ``torch.Tensor`` (their ``data_ptr()``) or raw integer
 addresses, host arrays as numpy arrays or sequences, streams as ``torch.cuda.Stream``
 or raw handles (default: torch's current stream).  A non-OK status raises
-:class:`PalquantError`.  Every computation happens in the CUDA library; if it has
+:class:`PalquantError`.  The calls of the 8-bit transformer layers hold tensors against
+their descriptors first and raise :class:`ArgumentError`; addresses are the caller's word.  Every computation happens in the CUDA library; if it has
 not been built, importing this module raises.
 """
 from __future__ import annotations
