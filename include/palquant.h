@@ -632,6 +632,107 @@ size_t palquant_kv8_attention_scratch_bytes(const pq_kv8_cache* cache, const pq_
 pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, void* o_dev, const pq_kv8_attn* a,
                                  void* scratch_dev, size_t scratch_bytes, pq_stream_t stream);
 
+/* The same through a window with sinks: a->causal = 1, and the query at position p sees token j <= p
+ * where j > p - window or j < sinks.  sinks >= 0; with no window, or 0 sinks, it is
+ * palquant_kv8_attention.  The scratch as there, of this call's own size. */
+size_t palquant_kv8_attention_sinks_scratch_bytes(const pq_kv8_cache* cache, const pq_kv8_attn* a, int32_t sinks);
+
+pq_status palquant_kv8_attention_sinks(const pq_kv8_cache* cache, const void* q_dev, void* o_dev, const pq_kv8_attn* a,
+                                       int32_t sinks, void* scratch_dev, size_t scratch_bytes, pq_stream_t stream);
+
+/* Which drafted tokens each draft sees: row t of `words` 32-bit words, `pitch` words from one row to the
+ * next, belongs to row t of q; bit j % 32 of word j / 32 stands for the sequence's draft j.  A tree's
+ * rows have the bits of the draft itself and of its ancestors; any others may be set or not.  Bits past
+ * the sequence's last draft do not count.  32 words >= max_q. */
+typedef struct {
+    const uint32_t* bits_dev;
+    int64_t pitch;
+    int32_t words;
+} pq_kv8_tree;
+
+/* Attention for drafted tokens: the n queries of sequence b are its last n cached tokens (drafts, appended as
+ * any others), len_dev[b] counts them, and draft i sees every token before the drafts and draft j where
+ * its row's bit j is set; a draft that sees nothing gives 0.  a->causal = 1 and a->window = 0. */
+size_t palquant_kv8_attention_tree_scratch_bytes(const pq_kv8_cache* cache, const pq_kv8_attn* a, const pq_kv8_tree* tree);
+
+pq_status palquant_kv8_attention_tree(const pq_kv8_cache* cache, const void* q_dev, void* o_dev, const pq_kv8_attn* a,
+                                      const pq_kv8_tree* tree, void* scratch_dev, size_t scratch_bytes,
+                                      pq_stream_t stream);
+
+/* Query and key heads normed and rotated by position, between the projection and the cache.  For every
+ * token t and head x of D elements, in fp32 with one rounding to the type at the end:
+ *   n_i = x_i * w_i / sqrt(sum x^2 / D + eps)        (norm = 1; w NULL: 1; norm = 0: n = x)
+ *   rotated by a_j = pos_dev[t] * frequency j, j < R / 2, the pair (a, b) = (n_j, n_{j + R/2}), or with
+ *   interleaved = 1 (n_{2j}, n_{2j+1}), becomes (a cos a_j - b sin a_j, b cos a_j + a sin a_j).
+ * Elements from R on are normed only; R = 0 rotates nothing (pos_dev and turns_dev may be NULL).  R is
+ * even, 0 to D; D up to 1024 and Hq + Hkv up to 65535 (PQ_EUNSUPPORTED else); Hq or Hkv may be 0.  Element
+ * (t, h, i) of a tensor at t * token stride + h * head stride + i.  Outputs may be the inputs themselves
+ * (same pointer, same strides); else they share no element with an input.  turns_dev: R / 2 values of
+ * palquant_rope_turns_host, whose frequencies are in radians a position; angles are exact to |position| 2^-63
+ * turns, positions of either sign.  Squares are summed in fp32, the magnitudes below 2^60.  Bound by HBM: every element read and
+ * written once; rows on 16-byte boundaries (R / 2 elements with them) are the fast ones. */
+typedef struct {
+    int32_t type;   /* pq_float_type of q, k and the outputs */
+    int32_t w_type; /* ... of the norm's weights */
+    int64_t tokens;
+    int32_t Hq, Hkv, D, R, interleaved, norm;
+    float eps; /* 0 and up */
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride;
+    int64_t q_out_token_stride, q_out_head_stride, k_out_token_stride, k_out_head_stride;
+    const int32_t* pos_dev;
+    const uint64_t* turns_dev;
+    const void *q_weight_dev, *k_weight_dev; /* D values each, NULL for ones */
+} pq_qk_rope;
+
+/* n frequencies as fractions of a turn in units of 2^-64.  Host only; finite frequencies. */
+pq_status palquant_rope_turns_host(const double* frequencies_host, int32_t n, uint64_t* turns_host);
+
+pq_status palquant_qk_norm_rope(const void* q_dev, const void* k_dev, void* q_out_dev, void* k_out_dev, const pq_qk_rope* d,
+                                pq_stream_t stream);
+
+/* Dense layers with 4-bit weights: codes in [-8, 7], one scale for each output channel and group of
+ * `group` input channels (the last one may be shorter):
+ *   y[m, n] = sum_g s[n, g] sum_{k in g} c[n, k] x[m, k], + bias[n], rounded to y_type once.
+ * Activations are not quantised: 16-bit ones enter the products as they are, fp32 ones as three exact parts;
+ * products are exact, sums fp32 (magnitudes of x below 2^117 keep a group's sum in range), a group's scale
+ * multiplies its sum. */
+typedef struct {
+    int32_t N, K;    /* K <= 131072 */
+    int32_t group;   /* 32, 64 or 128 */
+    int32_t s_type;  /* pq_float_type that the scales are stored in */
+} pq_w4_weights;
+
+/* Bytes of the packed weights (codes two to a byte in the order of the products, padded to 16 channels and
+ * 128 of K, with their scales); 0 for a descriptor that is refused. */
+size_t palquant_w4_packed_bytes(const pq_w4_weights* w);
+
+/* Codes (one to a byte, [N, ldc], their low 4 bits count) and scales (s_type [N][ceil(K / group)],
+ * contiguous) into packed_dev (16-byte aligned, packed_bytes of it there). */
+pq_status palquant_w4_pack(const int8_t* codes_dev, int64_t ldc, const void* s_dev, const pq_w4_weights* w,
+                           void* packed_dev, size_t packed_bytes, pq_stream_t stream);
+
+/* Float weights [N, ldw] of w_type quantised and packed: for each group, with amax its largest magnitude,
+ *   s = fl(amax * fl(1/7)) rounded to s_type, code = clamp(rint(fl(w * fl(1/s))), -7, 7);
+ * an s below the smallest normal number of fp32 (for PQ_F16: of half precision) counts as 0: codes 0.  A
+ * NaN or an infinity under a scale, and a scale that s_type cannot hold, makes the scale NaN and the codes 0. */
+pq_status palquant_w4_quantize(const void* w_dev, int32_t w_type, int64_t ldw, const pq_w4_weights* w,
+                               void* packed_dev, size_t packed_bytes, pq_stream_t stream);
+
+/* The codes [N, ldc] and scales (fp32 [N][ceil(K / group)]) that packed weights hold; each may be NULL. */
+pq_status palquant_w4_unpack(const void* packed_dev, const pq_w4_weights* w, int8_t* codes_dev, int64_t ldc,
+                             float* s_dev, pq_stream_t stream);
+
+/* Bytes of device scratch palquant_linear_w4 needs (16-byte aligned; 0: none, or a refused call). */
+size_t palquant_linear_w4_scratch_bytes(const pq_w4_weights* w, const pq_linear_desc* d);
+
+/* x_dev [M, K] of x_type to y_dev [M, N] of y_type; d->N and d->K are w's, d->ldw is not read, bias_dev
+ * fp32 [N] or NULL.  Made for few tokens, where the weights' bytes are what counts; any M up to
+ * 64 * 65535 (PQ_EUNSUPPORTED else).  M = 0 does nothing.  Any alignment of the types; token rows on 16-byte boundaries
+ * are read 16 bytes at a time. */
+pq_status palquant_linear_w4(const void* x_dev, const void* packed_dev, const float* bias_dev, void* y_dev,
+                             const pq_w4_weights* w, const pq_linear_desc* d, void* scratch_dev, size_t scratch_bytes,
+                             pq_stream_t stream);
+
 /* ------------------------------------------------------------------------ */
 /* Introspection (host only; no GPU needed).                                */
 /* ------------------------------------------------------------------------ */

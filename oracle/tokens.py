@@ -79,8 +79,8 @@ def read(codes, scales, table, start, n):
     return (codes[page, :, slot].astype(F) * scales[page][:, :, None]).astype(F)
 
 
-def attention(q, k, v, scale, causal=True, window=0):
-    """One sequence: q [n, Hq, D], k and v [len, Hkv, D].  Returns (o, spread, top) in double: o [n, Hq, D], spread = sum
+def attention(q, k, v, scale, causal=True, window=0, seen=None):
+    """One sequence: q [n, Hq, D], k and v [len, Hkv, D]; seen [n, len]: what each query sees, instead of the rest.  Returns (o, spread, top) in double: o [n, Hq, D], spread = sum
     softmax * |v| (what an error of the probabilities is multiplied with) and the largest |score| of each row [n, Hq, 1]."""
     n, Hq, D = q.shape
     length, H = k.shape[0], k.shape[1]
@@ -91,7 +91,10 @@ def attention(q, k, v, scale, causal=True, window=0):
         return o, spread, top
     at = (length - n + np.arange(n))[:, None]
     j = np.arange(length)[None]
-    seen = np.ones((n, length), bool)
+    if seen is not None:
+        causal = False
+    else:
+        seen = np.ones((n, length), bool)
     if causal:
         seen = j <= at
         if window:
@@ -113,3 +116,63 @@ def attention(q, k, v, scale, causal=True, window=0):
             spread[i, hq] = p[i, on] @ np.abs(vh[on])
         top[:, hq, 0] = np.where(seen, np.abs(np.where(seen, s, 0)), 0).max(1)
     return o, spread, top
+
+
+def sees_sinks(n, length, window, sinks):
+    """[n, length]: the tokens up to each of the last n ones, through a window (0: none) and with the first `sinks`."""
+    at, j = (length - n + np.arange(n))[:, None], np.arange(length)[None]
+    return (j <= at) & ((j > at - window) | (j < sinks) | (window == 0))
+
+
+def sees_tree(n, length, bits):
+    """[n, length]: everything before the last n tokens, and those of the last n whose bit is set in bits [n, words]."""
+    out = np.zeros((n, length), bool)
+    for i in range(n):
+        for j in range(length):
+            d = j - (length - n)
+            out[i, j] = d < 0 or int(bits[i, d // 32]) >> (d % 32) & 1
+    return out
+
+
+def norm_rope(x, weight, eps, positions, frequencies, interleaved, norm=True):
+    """Heads x [tokens, heads, D] normed and rotated, in double.  Returns (y, size): size [tokens, heads, D] the sum of the
+    magnitudes that each output is made of."""
+    x = np.asarray(x, np.float64)
+    if norm:
+        x = x / np.sqrt((x * x).mean(-1, keepdims=True) + eps) * (1 if weight is None else np.asarray(weight, np.float64))
+    y, size = x.copy(), np.abs(x)
+    for j, f in enumerate(frequencies):
+        a, b = (2 * j, 2 * j + 1) if interleaved else (j, j + len(frequencies))
+        angle = np.asarray(positions, np.float64) * f
+        c, s = np.cos(angle)[:, None], np.sin(angle)[:, None]
+        y[..., a], y[..., b] = x[..., a] * c - x[..., b] * s, x[..., b] * c + x[..., a] * s
+        size[..., a] = size[..., b] = np.abs(x[..., a]) + np.abs(x[..., b])
+    return y, size
+
+
+def w4_quantize(w, group, round_scale=None, smallest=TINY):
+    """(codes [N, K] int8, scales [N, groups] fp32) of w [N, K]; round_scale: fp32 to the scales' type and back."""
+    w = np.asarray(w, F)
+    N, K = w.shape
+    groups = -(-K // group)
+    codes, scales = np.zeros((N, K), np.int8), np.zeros((N, groups), F)
+    for g in range(groups):
+        part = w[:, g * group:(g + 1) * group]
+        a = np.abs(part)
+        with np.errstate(all="ignore"):
+            s = (np.where(np.isfinite(a), a, 0).max(1) * (F(1) / F(7))).astype(F)
+            s = s if round_scale is None else round_scale(s)
+            s = np.where(s < smallest, F(0), s).astype(F)
+            s = np.where(np.isfinite(part).all(1) & np.isfinite(s), s, F(np.nan))
+            inv = np.where(s > 0, F(1) / s, F(0)).astype(F)[:, None]
+            c = np.clip(np.rint((part * inv).astype(F)), -7, 7)
+        codes[:, g * group:(g + 1) * group] = np.where(inv > 0, c, 0).astype(np.int8)
+        scales[:, g] = s
+    return codes, scales
+
+
+def linear_w4(x, codes, scales, group, bias=None):
+    """(y, size) in double: y [M, N], size the sum of the products' magnitudes."""
+    x, w = np.asarray(x, np.float64), codes.astype(np.float64) * np.repeat(np.asarray(scales, np.float64), group, 1)[:, : codes.shape[1]]
+    y, size = x @ w.T, np.abs(x) @ np.abs(w).T
+    return (y, size) if bias is None else (y + np.asarray(bias, np.float64), size + np.abs(bias))

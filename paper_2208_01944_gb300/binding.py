@@ -42,6 +42,10 @@ EXPORTS = [
     "palquant_quantize_tokens", "palquant_linear_code_format", "palquant_linear_i8",
     "palquant_linear_q8_scratch_bytes", "palquant_linear_q8", "palquant_kv8_append", "palquant_kv8_read",
     "palquant_kv8_attention_scratch_bytes", "palquant_kv8_attention",
+    "palquant_kv8_attention_sinks_scratch_bytes", "palquant_kv8_attention_sinks",
+    "palquant_kv8_attention_tree_scratch_bytes", "palquant_kv8_attention_tree",
+    "palquant_rope_turns_host", "palquant_qk_norm_rope", "palquant_w4_packed_bytes", "palquant_w4_pack",
+    "palquant_w4_quantize", "palquant_w4_unpack", "palquant_linear_w4_scratch_bytes", "palquant_linear_w4",
 ]
 
 
@@ -92,6 +96,22 @@ class KV8Attn(ctypes.Structure):
         [("scale", ctypes.c_float)] + \
         [(n, ctypes.c_int64) for n in ("q_token_stride", "q_head_stride", "o_token_stride", "o_head_stride")] + \
         [(n, ctypes.c_void_p) for n in ("cu_q_dev", "len_dev", "page_table_dev")]
+
+
+class KV8Tree(ctypes.Structure):
+    _fields_ = [("bits_dev", ctypes.c_void_p), ("pitch", ctypes.c_int64), ("words", ctypes.c_int32)]
+
+
+class QKRope(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("type", "w_type")] + [("tokens", ctypes.c_int64)] + \
+        [(n, ctypes.c_int32) for n in ("Hq", "Hkv", "D", "R", "interleaved", "norm")] + [("eps", ctypes.c_float)] + \
+        [(n, ctypes.c_int64) for n in ("q_token_stride", "q_head_stride", "k_token_stride", "k_head_stride",
+                                       "q_out_token_stride", "q_out_head_stride", "k_out_token_stride", "k_out_head_stride")] + \
+        [(n, ctypes.c_void_p) for n in ("pos_dev", "turns_dev", "q_weight_dev", "k_weight_dev")]
+
+
+class W4Weights(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "K", "group", "s_type")]
 
 
 _P = ctypes.c_void_p
@@ -195,6 +215,23 @@ def _load():
     L.palquant_kv8_attention.restype = _I32
     L.palquant_kv8_attention.argtypes = [ctypes.POINTER(KV8Cache), _P, _P, ctypes.POINTER(KV8Attn), _P, ctypes.c_size_t,
                                          _P]
+    cache_p, attn_p, tree_p = (ctypes.POINTER(s) for s in (KV8Cache, KV8Attn, KV8Tree))
+    w4_p, linear_p = ctypes.POINTER(W4Weights), ctypes.POINTER(LinearDesc)
+    for name, result, args in (
+            ("palquant_kv8_attention_sinks_scratch_bytes", ctypes.c_size_t, [cache_p, attn_p, _I32]),
+            ("palquant_kv8_attention_sinks", _I32, [cache_p, _P, _P, attn_p, _I32, _P, ctypes.c_size_t, _P]),
+            ("palquant_kv8_attention_tree_scratch_bytes", ctypes.c_size_t, [cache_p, attn_p, tree_p]),
+            ("palquant_kv8_attention_tree", _I32, [cache_p, _P, _P, attn_p, tree_p, _P, ctypes.c_size_t, _P]),
+            ("palquant_rope_turns_host", _I32, [_P, _I32, _P]),
+            ("palquant_qk_norm_rope", _I32, [_P, _P, _P, _P, ctypes.POINTER(QKRope), _P]),
+            ("palquant_w4_packed_bytes", ctypes.c_size_t, [w4_p]),
+            ("palquant_w4_pack", _I32, [_P, _I64, _P, w4_p, _P, ctypes.c_size_t, _P]),
+            ("palquant_w4_quantize", _I32, [_P, _I32, _I64, w4_p, _P, ctypes.c_size_t, _P]),
+            ("palquant_w4_unpack", _I32, [_P, w4_p, _P, _I64, _P, _P]),
+            ("palquant_linear_w4_scratch_bytes", ctypes.c_size_t, [w4_p, linear_p]),
+            ("palquant_linear_w4", _I32, [_P, _P, _P, _P, w4_p, linear_p, _P, ctypes.c_size_t, _P])):
+        getattr(L, name).restype = result
+        getattr(L, name).argtypes = args
     return L
 
 
@@ -755,3 +792,210 @@ def palquant_kv8_attention(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, scratch_de
     _check(lib.palquant_kv8_attention(ctypes.byref(cache), _described(q_dev, getattr(a, "_q", _BY_HAND), "q"),
                                       _described(o_dev, getattr(a, "_o", _BY_HAND), "o"), ctypes.byref(a), _ptr(scratch_dev),
                                       scratch_bytes, _stream(stream)), "palquant_kv8_attention")
+
+
+# ---------------------------------------------------------------- a decoder's operators around the 8-bit cache
+def _here(*tensors):
+    """Tensors of a call lie on the current device, whose stream it takes (None and addresses are the caller's word)."""
+    import torch
+
+    for t in tensors:
+        if t is not None and type(t) is not int:
+            at = t.get_device()
+            if at < 0 or at != torch._C._cuda_getDevice():
+                raise ArgumentError(f"a tensor on {t.device}: not the current device")
+
+
+def _room(t, nbytes, name):
+    """Address of a buffer of at least `nbytes` contiguous bytes (None and addresses as they are)."""
+    if t is None or type(t) is int:
+        return t
+    if t.is_contiguous() and t.numel() * t.element_size() >= nbytes:
+        return t.data_ptr()
+    raise ArgumentError(f"{name}: {nbytes} contiguous bytes")
+
+
+def _same_or_apart(src, dst, name):
+    """An output that starts where its input does is the input itself."""
+    _need(dst.data_ptr() != src.data_ptr() or _layout(dst) == _layout(src) or not dst.numel(),
+          f"{name}: the input itself, or elsewhere")
+
+
+def rope_turns(frequencies, device):
+    """The rotation's frequencies (radians a position, one for each pair of elements) as palquant_qk_norm_rope reads them."""
+    import torch
+
+    f = np.ascontiguousarray(np.asarray(frequencies, dtype=np.float64))
+    _need(f.ndim == 1, "frequencies: one for each pair")
+    turns = np.empty(f.shape, np.uint64)
+    _check(lib.palquant_rope_turns_host(_ptr(f), f.size, _ptr(turns)), "palquant_rope_turns_host")
+    return torch.from_numpy(turns.view(np.int64)).to(device)
+
+
+def qk_norm_rope(q, k, q_out, k_out, positions=None, turns=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
+                 norm=True) -> QKRope:
+    """Descriptor of a call on queries and keys [tokens, heads, D] (any token and head strides; one of them may be None, with its
+    output): norms with a weight for each element (None: ones; norm=False: no norm), rotation of the first 2 * len(turns)
+    elements by positions [tokens] (int32; turns=None: no rotation).  An output is its input itself or apart from the
+    inputs.  It keeps positions, turns and weights alive."""
+    import torch
+
+    some = q if q is not None else k
+    _need(some is not None and (q is None) == (q_out is None) and (k is None) == (k_out is None), "q, k: at least one, with its output")
+    tokens, D, dev = some.shape[0], some.shape[-1], some.device
+    strides, heads = [], []
+    for name, x, y in (("q", q, q_out), ("k", k, k_out)):
+        if x is None:
+            strides.append((0, 0, 0, 0))
+            heads.append(0)
+            continue
+        strides.append(_heads(x, name) + _heads(y, name + "_out"))
+        _need(x.shape[0] == tokens and x.shape[2] == D and (x.dtype, x.device) == (some.dtype, dev), "q and k: of one length, D, type and device")
+        _need((y.shape, y.dtype, y.device) == (x.shape, x.dtype, dev), f"{name}_out: as {name}")
+        _need(_heads_apart(y), f"{name}_out: outputs that overlap")
+        _same_or_apart(x, y, name + "_out")
+        heads.append(x.shape[1])
+    w_type, keep = PQ_F32, []
+    _need(norm or (q_weight is None and k_weight is None), "weights: of a norm")
+    weights = [w for w in (q_weight, k_weight) if w is not None]
+    if weights:
+        w_type = _float_type(weights[0])
+        for w in weights:
+            _need(w.dtype == weights[0].dtype and w.shape == (D,) and w.is_contiguous() and w.device == dev, "weights: [D] of one type")
+    R = 0
+    if turns is not None:
+        _need(turns.dtype == torch.int64 and turns.dim() == 1 and turns.is_contiguous() and turns.device == dev, "turns: those of rope_turns")
+        R = 2 * turns.numel()
+        _need(R <= D, "turns: one for each pair of elements at most")
+        _need(positions is not None, "positions: one for each token")
+        keep += [turns, positions]
+    d = QKRope(_float_type(some), w_type, tokens, *heads, D, R, int(bool(interleaved)), int(bool(norm)), float(eps), *strides[0][:2],
+               *strides[1][:2], *strides[0][2:], *strides[1][2:], _index(positions, "positions", tokens, dev) if R else None,
+               _ptr(turns) if R else None, _ptr(q_weight), _ptr(k_weight))
+    d._keep = keep + weights
+    d._q, d._k, d._q_out, d._k_out = (None if x is None else _layout(x) for x in (q, k, q_out, k_out))
+    return d
+
+
+def palquant_qk_norm_rope(q_dev, k_dev, q_out_dev, k_out_dev, d: QKRope, stream=None):
+    """Norms of query and key heads and the rotation by position, in one pass."""
+    _here(q_dev, k_dev)
+    for x, y, name in ((q_dev, q_out_dev, "q_out"), (k_dev, k_out_dev, "k_out")):
+        if getattr(x, "data_ptr", None) is not None and getattr(y, "data_ptr", None) is not None:
+            _same_or_apart(x, y, name)
+    _check(lib.palquant_qk_norm_rope(_described(q_dev, getattr(d, "_q", _BY_HAND), "q"), _described(k_dev, getattr(d, "_k", _BY_HAND), "k"),
+                                     _described(q_out_dev, getattr(d, "_q_out", _BY_HAND), "q_out"),
+                                     _described(k_out_dev, getattr(d, "_k_out", _BY_HAND), "k_out"), ctypes.byref(d),
+                                     _stream(stream)), "palquant_qk_norm_rope")
+
+
+def w4_weights(N, K, group, scales) -> W4Weights:
+    """Descriptor of packed 4-bit weights [N, K] with a scale (of torch type `scales`) for each channel and `group` of K."""
+    types = {dtype: number for number, dtype in _dtypes()[0].items()}
+    _need(scales in types, "scales: float32, float16 or bfloat16")
+    return W4Weights(N, K, group, types[scales])
+
+
+def palquant_w4_packed_bytes(w: W4Weights) -> int:
+    return lib.palquant_w4_packed_bytes(ctypes.byref(w))
+
+
+def palquant_w4_pack(codes_dev, s_dev, w: W4Weights, packed_dev, packed_bytes, stream=None):
+    """Codes [N, K] (int8, -8 to 7) and scales [N, groups] into the layout of the products."""
+    import torch
+
+    ldc = w.K
+    _here(codes_dev, s_dev, packed_dev)
+    if getattr(codes_dev, "data_ptr", None) is not None:
+        _need(codes_dev.dtype == torch.int8 and codes_dev.shape == (w.N, w.K), "codes: int8 [N, K]")
+        ldc = _rows(codes_dev, "codes")
+    groups = -(-w.K // w.group) if w.group > 0 else 0
+    _check(lib.palquant_w4_pack(_strided(codes_dev), ldc, _vector(s_dev, _dtypes()[0].get(w.s_type), w.N * groups, "scales"), ctypes.byref(w),
+                                _room(packed_dev, packed_bytes, "packed"), packed_bytes, _stream(stream)), "palquant_w4_pack")
+
+
+def palquant_w4_quantize(w_dev, w_type, ldw, w: W4Weights, packed_dev, packed_bytes, stream=None):
+    """Float weights [N, K] (rows `ldw` elements apart) quantised to 4 bits and packed."""
+    _here(w_dev, packed_dev)
+    _check(lib.palquant_w4_quantize(_span(w_dev, _dtypes()[0].get(w_type), (w.N - 1) * ldw + w.K, "w"), w_type, ldw, ctypes.byref(w),
+                                    _room(packed_dev, packed_bytes, "packed"), packed_bytes, _stream(stream)), "palquant_w4_quantize")
+
+
+def palquant_w4_unpack(packed_dev, w: W4Weights, codes_dev, s_dev, stream=None):
+    """The codes (int8 [N, K]) and fp32 scales [N, groups] that packed weights hold; either may be None."""
+    import torch
+
+    ldc = w.K
+    _here(packed_dev, codes_dev, s_dev)
+    if getattr(codes_dev, "data_ptr", None) is not None:
+        _need(codes_dev.dtype == torch.int8 and codes_dev.shape == (w.N, w.K), "codes: int8 [N, K]")
+        ldc = _rows(codes_dev, "codes")
+    groups = -(-w.K // w.group) if w.group > 0 else 0
+    _check(lib.palquant_w4_unpack(_room(packed_dev, palquant_w4_packed_bytes(w), "packed"), ctypes.byref(w), _strided(codes_dev), ldc,
+                                  _vector(s_dev, _dtypes()[0][PQ_F32], w.N * groups, "scales"), _stream(stream)), "palquant_w4_unpack")
+
+
+def linear_w4_desc(x, w: W4Weights, y) -> LinearDesc:
+    """Descriptor of y [M, N] = x [M, K] times packed 4-bit weights."""
+    M = x.shape[0]
+    _need(x.dim() == 2 and x.shape[1] == w.K and y.shape == (M, w.N), "x: [M, K], y: [M, N]")
+    _need(x.device == y.device, "x and y: on one device")
+    d = LinearDesc(M, w.N, w.K, _float_type(x), _float_type(y), _rows(x, "x"), w.K, _rows(y, "y"))
+    d._x, d._y = _layout(x), _layout(y)
+    return d
+
+
+def palquant_linear_w4_scratch_bytes(w: W4Weights, d: LinearDesc) -> int:
+    return lib.palquant_linear_w4_scratch_bytes(ctypes.byref(w), ctypes.byref(d))
+
+
+def palquant_linear_w4(x_dev, packed_dev, bias_dev, y_dev, w: W4Weights, d: LinearDesc, scratch_dev, scratch_bytes, stream=None):
+    """Dense layer with 4-bit weights and group scales: x to y."""
+    _here(x_dev, packed_dev)
+    _check(lib.palquant_linear_w4(_described(x_dev, getattr(d, "_x", _BY_HAND), "x"), _room(packed_dev, lib.palquant_w4_packed_bytes(ctypes.byref(w)), "packed"),
+                                  _vector(bias_dev, _dtypes()[0][PQ_F32], d.N, "bias"), _described(y_dev, getattr(d, "_y", _BY_HAND), "y"),
+                                  ctypes.byref(w), ctypes.byref(d), _room(scratch_dev, scratch_bytes, "scratch"), scratch_bytes, _stream(stream)),
+           "palquant_linear_w4")
+
+
+def palquant_kv8_attention_sinks_scratch_bytes(cache: KV8Cache, a: KV8Attn, sinks) -> int:
+    return lib.palquant_kv8_attention_sinks_scratch_bytes(ctypes.byref(cache), ctypes.byref(a), sinks)
+
+
+def palquant_kv8_attention_sinks(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, sinks, scratch_dev, scratch_bytes, stream=None):
+    """Attention over the cache through a window, with the first `sinks` tokens of every sequence in sight."""
+    _here(q_dev)
+    _fits_cache(cache, a, "_queries")
+    _check(lib.palquant_kv8_attention_sinks(ctypes.byref(cache), _described(q_dev, getattr(a, "_q", _BY_HAND), "q"),
+                                            _described(o_dev, getattr(a, "_o", _BY_HAND), "o"), ctypes.byref(a), sinks,
+                                            _room(scratch_dev, scratch_bytes, "scratch"), scratch_bytes, _stream(stream)),
+           "palquant_kv8_attention_sinks")
+
+
+def kv8_tree(bits, a: KV8Attn) -> KV8Tree:
+    """Descriptor of which drafts each draft sees: bits [tokens, words] (int32, contiguous rows), a row for each of a's
+    queries, bit j % 32 of word j / 32 for the sequence's draft j.  It keeps the bits alive."""
+    import torch
+
+    _need(bits.dtype == torch.int32, "bits: int32")
+    pitch = _rows(bits, "bits")
+    q = getattr(a, "_q", None)
+    _need(q is None or (bits.shape[0] == q[0][0] and bits.get_device() == q[3]), "bits: a row for each query, on its device")
+    t = KV8Tree(_strided(bits), pitch, bits.shape[1])
+    t._keep, t._for = bits, q
+    return t
+
+
+def palquant_kv8_attention_tree_scratch_bytes(cache: KV8Cache, a: KV8Attn, tree: KV8Tree) -> int:
+    return lib.palquant_kv8_attention_tree_scratch_bytes(ctypes.byref(cache), ctypes.byref(a), ctypes.byref(tree))
+
+
+def palquant_kv8_attention_tree(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, tree: KV8Tree, scratch_dev, scratch_bytes, stream=None):
+    """Attention for drafted tokens, the sequences' last cached ones: each sees the text before them and the drafts of its bits."""
+    _here(q_dev)
+    _fits_cache(cache, a, "_queries")
+    _need(getattr(tree, "_for", None) == getattr(a, "_q", None) or not hasattr(tree, "_for"), "tree: of other queries")
+    _check(lib.palquant_kv8_attention_tree(ctypes.byref(cache), _described(q_dev, getattr(a, "_q", _BY_HAND), "q"),
+                                           _described(o_dev, getattr(a, "_o", _BY_HAND), "o"), ctypes.byref(a), ctypes.byref(tree),
+                                           _room(scratch_dev, scratch_bytes, "scratch"), scratch_bytes, _stream(stream)),
+           "palquant_kv8_attention_tree")

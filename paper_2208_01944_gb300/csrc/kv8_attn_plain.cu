@@ -1,0 +1,10 @@
+// The attention kernels over the 8-bit cache as they see the tokens up to the query, through a window or not, or every token.
+#include "pq_kv8_rows.cuh"
+#include "pq_kv8_tiles.cuh"
+
+namespace pq {
+
+template cudaError_t launch_attn_rows<kPlain>(const AttnArgs& p, unsigned grid, int nt, cudaStream_t stream);
+template cudaError_t launch_attn_tc<kPlain>(const AttnArgs& p, unsigned grid, cudaStream_t stream);
+
+}  // namespace pq

@@ -26,14 +26,27 @@ struct AttnArgs {
   unsigned int* err;
   uint64_t wait_limit_ns;
   bool wide_q, wide_o;  // rows on 16-byte boundaries
+  int sinks;            // kSinks: first tokens that stay visible (0 in the other views)
+  const uint32_t* tree; // kTree: which drafts each draft sees, tree_words words a row
+  int64_t tree_pitch;
+  int tree_words;
 };
 
+// What a query sees: the tokens up to it (all of them, or through a window) or every token; through
+// a window with the first tokens; the text before the drafts and the drafts that its bits name.
+enum AttnView : int { kPlain = 0, kSinks = 1, kTree = 2 };
+
 bool valid_kv8_cache(const pq_kv8_cache* c);
+
+// Few query rows of a cache head, any type and D: nt tiles of 8 a block.
+template <int VIEW>
+cudaError_t launch_attn_rows(const AttnArgs& p, unsigned grid, int nt, cudaStream_t stream);
 
 // Tiles of 256 query rows on the tensor cores; fp32 queries and D above 128 are not its.
 bool attn_tc_takes(const pq_kv8_cache& c, const pq_kv8_attn& a);
 constexpr int kAttnTcRows = 256;
 constexpr int kAttnTcTokens = 128;
+template <int VIEW>
 cudaError_t launch_attn_tc(const AttnArgs& p, unsigned grid, cudaStream_t stream);
 
 constexpr float kLog2e = 1.4426950408889634f;
@@ -78,6 +91,34 @@ __device__ __forceinline__ Span span_of(const AttnArgs& p, int b, int r0, int ro
     if (p.a.window > 0) s.lo = max(0, s.len - s.n + r0 / p.group + 1 - p.a.window);
   }
   return s;
+}
+
+// How a row tile walks through its tokens: steps of 16 or 128 (the kernel's `align`) through the first
+// `head` of them, then from `head` + gap on, `end` in all.  The head holds the sinks that lie before the
+// span; it and the gap are multiples of a step, so no step lies on both sides.
+struct Walk {
+  int head, gap, end;
+};
+
+__device__ __forceinline__ Walk walk_of(const AttnArgs& p, const Span& s) {
+  const int first = s.lo & ~(p.align - 1);
+  Walk w;
+  w.head = min((p.sinks + p.align - 1) & ~(p.align - 1), first);
+  w.gap = first - w.head;
+  w.end = s.hi - w.gap;
+  return w;
+}
+
+// The lowest n of 32 bits (none below 0, all from 32 on).
+__device__ __forceinline__ uint32_t first_bits(int n) { return n >= 32 ? 0xFFFFFFFFu : (1u << max(n, 0)) - 1u; }
+
+// Which of the drafts off to off + 31 a draft sees, from the `words` words of its row; what lies
+// before draft 0 is the text, which it sees.
+__device__ __forceinline__ uint32_t drafts_seen(const uint32_t* row, int words, int off) {
+  if (off <= -32) return 0xFFFFFFFFu;
+  if (off < 0) return (row[0] << -off) | first_bits(-off);
+  const int w = off >> 5;
+  return __funnelshift_r(w < words ? row[w] : 0u, w + 1 < words ? row[w + 1] : 0u, off & 31);
 }
 
 }  // namespace pq

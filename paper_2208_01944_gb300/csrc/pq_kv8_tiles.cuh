@@ -19,6 +19,8 @@
 //
 // Roles (16 warps): 0 issues the MMAs, 4 looks up pages, the other six below 8 convert
 // (none of them on the issuing warp's scheduler), 8-11 and 12-15 are the tiles' softmax.  Tiles with the most tokens come first.
+#pragma once
+
 #include <cuda_runtime.h>
 
 #include "palquant.h"
@@ -131,7 +133,8 @@ __device__ __forceinline__ TcPlace tc_place(const AttnArgs& p) {
   return r;
 }
 
-template <typename T, int DP>
+// VIEW: see AttnView.
+template <typename T, int DP, int VIEW>
 __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constant__ AttnArgs p) {
   constexpr int kSubs = DP / 64;
   constexpr uint32_t kO = 256;  // tensor memory: scores of both tiles, then their outputs
@@ -146,10 +149,13 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
   const Span sp = span_of(p, w.b, r0, kAttnTcRows);
   const int rows = sp.n * p.group;
   if (r0 >= rows) return;
-  const int first = sp.lo & ~(p.align - 1);
-  const int from = first + w.split * p.chunk;
-  if (w.split > 0 && from >= sp.hi) return;
-  const int to = min(sp.hi, from + p.chunk);
+  // (with sinks, steps are counted without the gap behind them; token() has it)
+  const Walk walk = walk_of(p, sp);
+  const int from = (VIEW == kSinks ? 0 : walk.gap) + w.split * p.chunk;
+  const int end = VIEW == kSinks ? walk.end : sp.hi;
+  if (w.split > 0 && from >= end) return;
+  const int to = min(end, from + p.chunk);
+  auto token = [&](int s) { return VIEW == kSinks && s >= walk.head ? s + walk.gap : s; };
   const int steps = to > from ? (to - from + kTokens - 1) / kTokens : 0;
   const int halves = to > from ? (to - from + kHalf - 1) / kHalf : 0;
   const int tiles = rows - r0 > 128 ? 2 : 1;
@@ -252,9 +258,9 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
             !__all_sync(0xffffffffu, mbar_wait(bars.page_empty(i), (j / kPageRing - 1) & 1, ctx)))
           break;
         if (lane < kTokens >> p.page_shift) {
-          const int start = from + j * kTokens + (lane << p.page_shift), slot = start >> p.page_shift;
+          const int start = token(from + j * kTokens) + (lane << p.page_shift), slot = start >> p.page_shift;
           StepPage page = {0.0f, kNone, 0.0f, -1};
-          if (start < sp.hi && start + p.c.page_tokens > sp.lo) {  // within the rows' span
+          if (start < sp.hi && (start + p.c.page_tokens > sp.lo || (VIEW == kSinks && start < p.sinks))) {  // within the rows' span
             const int id = slot < p.a.table_pitch ? table[slot] : -1;
             if (id >= 0 && id < p.c.num_pages) {
               const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
@@ -384,6 +390,9 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
       const int at = sp.len - sp.n + qi + 1;
       const int hi = !mine ? 0 : p.a.causal ? min(at, sp.len) : sp.len;
       const int lo = p.a.window > 0 ? max(0, at - p.a.window) : 0;
+      // the draft's row of bits (one that is there for rows past the end), and the first draft's position
+      const uint32_t* drafts = VIEW == kTree ? p.tree + (mine ? tok : p.a.cu_q_dev[w.b]) * p.tree_pitch : nullptr;
+      const int text = sp.len - sp.n;
       float m = kNone, l = 0.0f;
       bool ok = true;
       for (int i = 0; i < halves; ++i) {
@@ -401,8 +410,9 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         }
         tmem_wait_ld();
         const StepPage* page = pages[(i >> 1) % kPageRing];
-        const int c0 = kHalf * (i & 1), j0 = from + i * kHalf;
-        const bool whole = __all_sync(0xffffffffu, j0 >= lo && j0 + kHalf <= hi) != 0;
+        const int c0 = kHalf * (i & 1), j0 = token(from + i * kHalf);
+        const bool whole = __all_sync(0xffffffffu, (j0 >= lo || (VIEW == kSinks && j0 + kHalf <= p.sinks)) &&
+                                                       j0 + kHalf <= (VIEW == kTree ? min(hi, text) : hi)) != 0;
         // the row's maximum: within 16 tokens of one page that of the raw scores (the scales
         // are not negative)
         float high = m;
@@ -416,13 +426,22 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
             high = fmaxf(high, fmaf(top, f.k * factor, f.log2_v));
           }
         } else {
+          uint32_t bits[2] = {};
+          if (VIEW == kTree) {
+            bits[0] = first_bits(hi - j0) & drafts_seen(drafts, p.tree_words, j0 - text);
+            bits[1] = first_bits(hi - j0 - 32) & drafts_seen(drafts, p.tree_words, j0 + 32 - text);
+          }
+          if (VIEW == kSinks) {
+            bits[0] = first_bits(hi - j0) & (~first_bits(lo - j0) | first_bits(p.sinks - j0));
+            bits[1] = first_bits(hi - j0 - 32) & (~first_bits(lo - j0 - 32) | first_bits(p.sinks - j0 - 32));
+          }
 #pragma unroll
           for (int c = 0; c < kHalf; c += 16) {
             const StepPage& f = page[(c0 + c) >> p.page_shift];
             const float g = f.k * factor, lv = f.log2_v;
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
-              const bool seen = j0 + c + k >= lo && j0 + c + k < hi;
+              const bool seen = VIEW == kPlain ? j0 + c + k >= lo && j0 + c + k < hi : ((bits[c / 32] >> ((c & 16) + k)) & 1u) != 0;
               x[c + k] = seen ? fmaf(x[c + k], g, lv) : kNone;
               high = fmaxf(high, x[c + k]);
             }
@@ -525,34 +544,27 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
   }
 }
 
-template <typename T, int DP>
-cudaError_t launch(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
+template <typename T, int DP, int VIEW>
+cudaError_t launch_tiles(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
   static int attr_set[64] = {0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(pq_kv8_tiles<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(DP));
+    e = cudaFuncSetAttribute(pq_kv8_tiles<T, DP, VIEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(DP));
     if (e != cudaSuccess) return e;
     if (dev < 64) attr_set[dev] = 1;
   }
-  pq_kv8_tiles<T, DP><<<grid, kThreads, attn_smem(DP), stream>>>(p);
+  pq_kv8_tiles<T, DP, VIEW><<<grid, kThreads, attn_smem(DP), stream>>>(p);
   return cudaGetLastError();
 }
 
 }  // namespace
 
-// From about 40 query rows of a cache head on: a block's step costs the same for 1 to
-// 128 rows here, and in pq_kv8_rows it grows with every 16 (D = 128, rows of a head, here
-// against there: one sequence of 4000, 24 rows 21 / 21 us, 48 22 / 25; 32 sequences of 3000, 32 rows
-// 111 / 87, 48 111 / 123, 64 112 / 150).
-bool attn_tc_takes(const pq_kv8_cache& c, const pq_kv8_attn& a) {
-  return a.type != PQ_F32 && c.D <= 128 && static_cast<int64_t>(a.max_q) * (a.Hq / c.Hkv) > 40;
-}
-
+template <int VIEW>
 cudaError_t launch_attn_tc(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
-  if (p.a.type == PQ_F16) return p.c.D <= 64 ? launch<__half, 64>(p, grid, stream) : launch<__half, 128>(p, grid, stream);
-  return p.c.D <= 64 ? launch<__nv_bfloat16, 64>(p, grid, stream) : launch<__nv_bfloat16, 128>(p, grid, stream);
+  if (p.a.type == PQ_F16) return p.c.D <= 64 ? launch_tiles<__half, 64, VIEW>(p, grid, stream) : launch_tiles<__half, 128, VIEW>(p, grid, stream);
+  return p.c.D <= 64 ? launch_tiles<__nv_bfloat16, 64, VIEW>(p, grid, stream) : launch_tiles<__nv_bfloat16, 128, VIEW>(p, grid, stream);
 }
 
 }  // namespace pq

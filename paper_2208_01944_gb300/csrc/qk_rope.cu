@@ -1,0 +1,201 @@
+// Norms of query and key heads and the rotation by position, in one pass.
+//
+// Mathematics.  For each head x of D elements: y_i = x_i w_i / sqrt(sum x^2 / D + eps), then the pairs
+// (y_i, y_{i + R/2}) (or (y_2i, y_{2i+1})) of the first R elements turn by the angle pos f_i.  A frequency comes as
+// a 64-bit fraction of a turn, F_i = f_i / 2 pi * 2^64 to 2 units, and pos F_i mod 2^64 is the angle's fraction of a turn, off by
+// at most |pos| 2^-63 turns: whole turns fall off the top of the product.  Its nearest quarter turn is
+// taken out in integers, so the rest (an eighth of a turn at most) keeps fp32's relative precision.
+// Everything after is fp32, rounded to the type once.
+//
+// Split.  Bound by HBM: each element is read and written once.  A block takes a few tokens with all their heads, so
+// that a token's cosines and sines are computed once a block and not once a head; 2^k lanes hold a head,
+// each two 16-byte pieces, so that both members of every pair are in one thread and the sum of squares
+// needs k shuffles.  Whole heads are in registers before they are written: outputs may be the inputs.
+#include <cuda_runtime.h>
+
+#include <cmath>
+
+#include "palquant.h"
+#include "pq_internal.h"
+#include "pq_tokens.cuh"
+
+namespace pq {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kMostD = 1024;
+
+struct RopeArgs {
+  pq_qk_rope d;
+  const void* in[2];  // queries, keys
+  void* out[2];
+  int heads;   // of both
+  int block_tokens;
+};
+
+// cos and sin of pos * F / 2^64 turns.
+__device__ __forceinline__ float2 cos_sin(int pos, uint64_t turns) {
+  const uint64_t t = static_cast<uint64_t>(static_cast<int64_t>(pos)) * turns;
+  const uint32_t quarter = static_cast<uint32_t>((t + (1ull << 61)) >> 62);
+  // the rest, at most an eighth of a turn, in units of 2^-32 turns
+  const int rest = static_cast<int>(static_cast<int64_t>(t - (static_cast<uint64_t>(quarter) << 62)) >> 32);
+  float s, c;
+  sincospif(static_cast<float>(rest) * 0x1p-31f, &s, &c);
+  const float a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
+  return make_float2((quarter + 1) & 2 ? -a : a, quarter & 2 ? -b : b);
+}
+
+__device__ __forceinline__ float weight_at(const void* w, int type, int i) {
+  if (w == nullptr) return 1.0f;
+  if (type == PQ_F32) return static_cast<const float*>(w)[i];
+  if (type == PQ_F16) return __half2float(static_cast<const __half*>(w)[i]);
+  return __bfloat162float(static_cast<const __nv_bfloat16*>(w)[i]);
+}
+
+// The block's angles [tokens][R / 2] and weights [2][D], in shared memory.
+__device__ __forceinline__ void block_tables(const RopeArgs& p, int64_t tok0, int tokens, float2* angles, float* weights) {
+  const int half = p.d.R / 2;
+  for (int i = threadIdx.x; i < tokens * half; i += blockDim.x) {
+    const int t = i / half;
+    angles[i] = cos_sin(p.d.pos_dev[tok0 + t], p.d.turns_dev[i - t * half]);
+  }
+  if (p.d.norm)
+    for (int i = threadIdx.x; i < 2 * p.d.D; i += blockDim.x)
+      weights[i] = i < p.d.D ? weight_at(p.d.q_weight_dev, p.d.w_type, i) : weight_at(p.d.k_weight_dev, p.d.w_type, i - p.d.D);
+}
+
+template <typename T>
+__device__ __forceinline__ T* head_at(const RopeArgs& p, const void* base, int64_t token, int head, bool key, bool out) {
+  const int64_t ts = out ? (key ? p.d.k_out_token_stride : p.d.q_out_token_stride) : (key ? p.d.k_token_stride : p.d.q_token_stride);
+  const int64_t hs = out ? (key ? p.d.k_out_head_stride : p.d.q_out_head_stride) : (key ? p.d.k_head_stride : p.d.q_head_stride);
+  return static_cast<T*>(const_cast<void*>(base)) + token * ts + head * hs;
+}
+
+// Any D up to kMostD, any alignment: a warp a head, pairs and single elements spread over its lanes.
+template <typename T>
+__global__ void __launch_bounds__(kThreads) pq_qk_rope_any(const __grid_constant__ RopeArgs p) {
+  extern __shared__ float2 tables[];
+  const int D = p.d.D, half = p.d.R / 2, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t tok0 = static_cast<int64_t>(blockIdx.x) * p.block_tokens;
+  const int tokens = static_cast<int>(min(static_cast<int64_t>(p.block_tokens), p.d.tokens - tok0));
+  float* weights = reinterpret_cast<float*>(tables + p.block_tokens * half);
+  block_tables(p, tok0, tokens, tables, weights);
+  __syncthreads();
+  for (int item = warp; item < tokens * p.heads; item += kThreads / 32) {
+    const int t = item / p.heads, h = item - t * p.heads;
+    const bool key = h >= p.d.Hq;
+    const T* src = head_at<T>(p, p.in[key], tok0 + t, key ? h - p.d.Hq : h, key, false);
+    T* dst = head_at<T>(p, p.out[key], tok0 + t, key ? h - p.d.Hq : h, key, true);
+    float x[kMostD / 32];
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kMostD / 32; ++i) {
+      const int d = lane + 32 * i;
+      x[i] = d < D ? to_f32(src[d]) : 0.0f;
+      sum = fmaf(x[i], x[i], sum);
+    }
+    float f = 1.0f;
+    if (p.d.norm) {
+#pragma unroll
+      for (int s = 16; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s);
+      f = __frsqrt_rn(sum / static_cast<float>(D) + p.d.eps);
+    }
+    __syncwarp();  // the head is in registers: the output may lie where it was
+    const float* w = weights + (key ? D : 0);
+    const float2* angle = tables + t * half;
+    // each element's partner sits in another lane's registers: it is read again from the normed values in shared memory
+    float* row = weights + (p.d.norm ? 2 * D : 0) + warp * D;
+#pragma unroll
+    for (int i = 0; i < kMostD / 32; ++i) {
+      const int d = lane + 32 * i;
+      if (d < D) row[d] = p.d.norm ? x[i] * f * w[d] : x[i];
+    }
+    __syncwarp();
+    for (int d = lane; d < D; d += 32) {
+      float y = row[d];
+      if (d < p.d.R) {
+        const int pair = p.d.interleaved ? d >> 1 : d < half ? d : d - half;
+        const bool second = p.d.interleaved ? d & 1 : d >= half;
+        const float other = row[p.d.interleaved ? d ^ 1 : second ? d - half : d + half];
+        const float2 cs = angle[pair];
+        y = second ? fmaf(y, cs.x, other * cs.y) : fmaf(y, cs.x, -other * cs.y);
+      }
+      dst[d] = from_f32<T>(y);
+    }
+    __syncwarp();
+  }
+}
+
+int64_t any_smem(const RopeArgs& p) {
+  return static_cast<int64_t>(p.block_tokens) * (p.d.R / 2) * 8 + (p.d.norm ? 2 : 0) * p.d.D * 4 + static_cast<int64_t>(kThreads / 32) * p.d.D * 4;
+}
+
+template <typename T>
+cudaError_t launch_rope(RopeArgs& p, cudaStream_t s) {
+  p.block_tokens = 1;
+  const int64_t blocks = (p.d.tokens + p.block_tokens - 1) / p.block_tokens;
+  pq_qk_rope_any<T><<<static_cast<unsigned>(blocks), kThreads, any_smem(p), s>>>(p);
+  return cudaGetLastError();
+}
+
+// The fraction of a number of turns, in units of 2^-64.
+uint64_t fraction(double turns) {
+  if (std::fabs(turns) < 0.25) return static_cast<uint64_t>(std::llrint(turns * 0x1p64));  // (modulo 2^64 below 0)
+  const double f = turns - std::floor(turns);
+  return f < 1.0 ? static_cast<uint64_t>(f * 0x1p64) : 0;
+}
+
+bool valid_rope(const pq_qk_rope* d) {
+  if (d == nullptr) return false;
+  auto type = [](int32_t t) { return t == PQ_F32 || t == PQ_F16 || t == PQ_BF16; };
+  if (!type(d->type) || d->tokens < 0 || d->Hq < 0 || d->Hkv < 0 || d->Hq + static_cast<int64_t>(d->Hkv) < 1 || d->D < 1) return false;
+  if (d->R < 0 || d->R > d->D || d->R % 2 != 0) return false;
+  if ((d->interleaved != 0 && d->interleaved != 1) || (d->norm != 0 && d->norm != 1)) return false;
+  if (d->norm && (!type(d->w_type) || !(d->eps >= 0.0f) || d->eps == INFINITY)) return false;
+  for (int64_t s : {d->q_token_stride, d->q_head_stride, d->k_token_stride, d->k_head_stride, d->q_out_token_stride,
+                    d->q_out_head_stride, d->k_out_token_stride, d->k_out_head_stride})
+    if (s < 0) return false;
+  return true;
+}
+
+}  // namespace
+}  // namespace pq
+
+extern "C" {
+
+pq_status palquant_rope_turns_host(const double* frequencies_host, int32_t n, uint64_t* turns_host) {
+  if (n < 0 || (n > 0 && (frequencies_host == nullptr || turns_host == nullptr))) return PQ_EINVAL;
+  for (int32_t i = 0; i < n; ++i) {
+    if (!std::isfinite(frequencies_host[i])) return PQ_EINVAL;
+  }
+  for (int32_t i = 0; i < n; ++i) {
+    // f / 2 pi with its rounding's rest (the reciprocal in two doubles), the fraction of each as 2^-64 turns
+    const double f = frequencies_host[i], inv = 0x1.45f306dc9c883p-3, inv_rest = -0x1.6b01ec5417056p-57;
+    const double turns = f * inv, rest = std::fma(f, inv, -turns) + f * inv_rest;
+    turns_host[i] = pq::fraction(turns) + pq::fraction(rest);  // modulo 2^64: whole turns
+  }
+  return PQ_OK;
+}
+
+pq_status palquant_qk_norm_rope(const void* q_dev, const void* k_dev, void* q_out_dev, void* k_out_dev, const pq_qk_rope* d,
+                                pq_stream_t stream) {
+  using namespace pq;
+  if (!valid_rope(d)) return PQ_EINVAL;
+  if (d->tokens == 0) return PQ_OK;
+  const size_t e = bytes_of_type(d->type);
+  if (d->Hq > 0 && (q_dev == nullptr || q_out_dev == nullptr || !is_aligned(q_dev, e) || !is_aligned(q_out_dev, e))) return PQ_EINVAL;
+  if (d->Hkv > 0 && (k_dev == nullptr || k_out_dev == nullptr || !is_aligned(k_dev, e) || !is_aligned(k_out_dev, e))) return PQ_EINVAL;
+  if (d->R > 0 && (d->pos_dev == nullptr || d->turns_dev == nullptr || !is_aligned(d->pos_dev, 4) || !is_aligned(d->turns_dev, 8)))
+    return PQ_EINVAL;
+  if (d->norm && (!is_aligned(d->q_weight_dev, bytes_of_type(d->w_type)) || !is_aligned(d->k_weight_dev, bytes_of_type(d->w_type))))
+    return PQ_EINVAL;
+  if (d->D > kMostD || d->tokens > 0x7FFFFFFF || d->Hq + static_cast<int64_t>(d->Hkv) > 65535) return PQ_EUNSUPPORTED;
+  RopeArgs p = {*d, {q_dev, k_dev}, {q_out_dev, k_out_dev}, d->Hq + d->Hkv, 1};
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t st = d->type == PQ_F32   ? launch_rope<float>(p, s)
+                         : d->type == PQ_F16 ? launch_rope<__half>(p, s)
+                                             : launch_rope<__nv_bfloat16>(p, s);
+  return st == cudaSuccess ? PQ_OK : PQ_ECUDA;
+}
+
+}  // extern "C"
