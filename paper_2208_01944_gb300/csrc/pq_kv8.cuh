@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "palquant.h"
 #include "pq_tokens.cuh"
@@ -35,6 +36,12 @@ struct AttnArgs {
 // What a query sees: the tokens up to it (all of them, or through a window) or every token; through
 // a window with the first tokens; the text before the drafts and the drafts that its bits name.
 enum AttnView : int { kPlain = 0, kSinks = 1, kTree = 2 };
+
+// With half-precision outputs an 11-bit weight is off by as much as the output's own rounding: together sqrt(2) of
+// it (measured against 64 bits: 3.1e-4 of the outputs' norm, the rounding alone 2.0e-4).  The views with sinks and drafts carry the
+// rest of a weight in a second half there, as fp32 does.  (bfloat16's rounding is eight times a half's.)
+template <typename T, int VIEW>
+constexpr bool kSecondHalf = VIEW != kPlain && sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value;
 
 bool valid_kv8_cache(const pq_kv8_cache* c);
 

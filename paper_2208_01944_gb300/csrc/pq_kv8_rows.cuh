@@ -114,7 +114,8 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
   constexpr int kC = DP / 64;        // 64-wide pieces of a key row
   constexpr int kJ = DP / 16;        // 16-row tiles of the transposed output
   constexpr int kRows = 8 * NT;
-  constexpr int kHalves = TWO ? 2 : 1;
+  constexpr int kHalves = TWO ? 2 : 1;                                  // of a query's element
+  constexpr int kWHalves = TWO || kSecondHalf<T, VIEW> ? 2 : 1;         // of a weight
   constexpr float kGrowth = TWO ? kGrowF32 : kGrow, kShift = TWO ? kWShiftF32 : kWShift;
   constexpr int kSteps = ring_steps(DP);
   constexpr int kStep = step_bytes(DP);
@@ -315,7 +316,7 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
     }
     // ---- probabilities, of the running maximum as it was; only where a score has grown
     // past it by more than 2^8 (2^2 for fp32: w could leave the halves' range) is it brought up to date
-    uint32_t pf[kHalves][NT][2];
+    uint32_t pf[kWHalves][NT][2];
     float wv[NT][4], to_l[NT][2];
     bool grew = false;
 #pragma unroll
@@ -385,9 +386,9 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
       for (int i = 0; i < 2; ++i) {
         const uint32_t h = pack_half2(wv[j][2 * i], wv[j][2 * i + 1]);
         pf[0][j][i] = transpose_8x8(h);
-        if (TWO) {
+        if (kWHalves == 2) {
           const __half2 hh = *reinterpret_cast<const __half2*>(&h);
-          pf[kHalves - 1][j][i] =
+          pf[kWHalves - 1][j][i] =
               transpose_8x8(pack_half2(wv[j][2 * i] - __low2float(hh), wv[j][2 * i + 1] - __high2float(hh)));
         }
       }
@@ -418,7 +419,7 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
 #pragma unroll
       for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int hf = 0; hf < kHalves; ++hf)
+        for (int hf = 0; hf < kWHalves; ++hf)
 #pragma unroll
           for (int j = 0; j < NT; ++j)
             mma_16x8x16(o[2 * c + i][j], a01[2 * i], a01[2 * i + 1], a23[2 * i], a23[2 * i + 1], pf[hf][j][0], pf[hf][j][1]);

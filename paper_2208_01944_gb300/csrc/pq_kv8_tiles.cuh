@@ -217,7 +217,10 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         const uint32_t v = desc_n(v_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128));
 #pragma unroll
         for (int t = 0; t < 2; ++t)
-          if (t < tiles) mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1), v, idesc_o, i > 0);
+          if (t < tiles) {
+            mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1), v, idesc_o, i > 0);
+            if (kSecondHalf<T, VIEW>) mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1) + kHalf / 2, v, idesc_o, 1);
+          }
         tc_commit_warp(bars.o_full());
       };
       bool ok = halves > 0 && wait(bars.q_full(), 0) && wait(bars.k_full(0), 0);
@@ -474,7 +477,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         const float base = m == kNone ? 0.0f : m - kWShift;
 #pragma unroll
         for (int c = 0; c < kHalf; c += 32) {
-          uint32_t h[16];
+          uint32_t h[16], rest[kSecondHalf<T, VIEW> ? 16 : 1];
 #pragma unroll
           for (int u = 0; u < 32; u += 16) {
             const StepPage& f = page[(c0 + c + u) >> p.page_shift];
@@ -488,6 +491,13 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
               a = exp2_approx(a);
               b = exp2_approx(b);
               add_pair(s0, s1, a, b);
+              if (kSecondHalf<T, VIEW>) {
+                // 11 bits by truncation: what is left is exact
+                const float a1 = __uint_as_float(__float_as_uint(a) & 0xFFFFE000u), b1 = __uint_as_float(__float_as_uint(b) & 0xFFFFE000u);
+                rest[kSecondHalf<T, VIEW> ? (u + k) / 2 : 0] = pack_half2(a - a1, b - b1);
+                a = a1;
+                b = b1;
+              }
               h[(u + k) / 2] = pack_half2(a, b);
             }
             // a page that the row does not see adds nothing, even with a NaN scale
@@ -495,6 +505,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
             l += whole || sum != 0.0f ? sum * f.inv_v : 0.0f;
           }
           tmem_st16(buffer + c / 2, h);
+          if constexpr (kSecondHalf<T, VIEW>) tmem_st16(buffer + kHalf / 2 + c / 2, rest);
         }
         tmem_wait_st();
         tc_fence_before();

@@ -31,6 +31,7 @@ struct RopeArgs {
   void* out[2];
   int heads;   // of both
   int block_tokens;
+  int token_groups;  // pq_qk_rope_wide: lane groups that share a token's heads
 };
 
 // cos and sin of pos * F / 2^64 turns.
@@ -126,12 +127,158 @@ __global__ void __launch_bounds__(kThreads) pq_qk_rope_any(const __grid_constant
   }
 }
 
+// Heads on 16-byte boundaries whose pairs fill 16-byte pieces: 2^LG lanes hold a head, lane u the pieces first(u) and
+// second(u).  A group of lanes keeps a token's cosines and sines in registers while it goes through heads of that token, the next
+// head on its way before the last one is written.
+template <typename T, int LG>
+__global__ void __launch_bounds__(kThreads) pq_qk_rope_wide(const __grid_constant__ RopeArgs p) {
+  constexpr int V = 16 / sizeof(T);  // elements of a piece
+  constexpr int kLanes = 1 << LG;
+  extern __shared__ float2 tables[];
+  const int D = p.d.D, R = p.d.R, half = R / 2;
+  const int u = threadIdx.x & (kLanes - 1), group = threadIdx.x >> LG;
+  const int64_t tok0 = static_cast<int64_t>(blockIdx.x) * p.block_tokens;
+  const int tokens = static_cast<int>(min(static_cast<int64_t>(p.block_tokens), p.d.tokens - tok0));
+  const int t = group / p.token_groups;
+  const bool there = u < D / (2 * V) && t < tokens;
+  const int rotated = R / (2 * V);  // lanes whose pieces are partners
+  const int first = p.d.interleaved ? 2 * u * V : u < rotated ? u * V : R + 2 * (u - rotated) * V;
+  const int second = p.d.interleaved || u >= rotated ? first + V : half + u * V;
+  auto at = [&](int h, bool out) {
+    const bool key = h >= p.d.Hq;
+    return head_at<T>(p, (out ? p.out : p.in)[key], tok0 + t, key ? h - p.d.Hq : h, key, out);
+  };
+  int h = group % p.token_groups;
+  uint4 next[2];
+  if (there && h < p.heads) {
+    const T* src = at(h, false);
+    next[0] = *reinterpret_cast<const uint4*>(src + first);
+    next[1] = *reinterpret_cast<const uint4*>(src + second);
+  }
+  float* weights = reinterpret_cast<float*>(tables + p.block_tokens * half);
+  block_tables(p, tok0, tokens, tables, weights);
+  __syncthreads();
+  // angles of this lane's pairs: V of two pieces, or V / 2 of each
+  float2 cs[V];
+#pragma unroll
+  for (int i = 0; i < V; ++i) {
+    const int pair = u * V + i;
+    cs[i] = there && pair < half && (p.d.interleaved || u < rotated) ? tables[t * half + pair] : make_float2(1.0f, 0.0f);
+  }
+  float w[2][V];
+  int weights_of = -1;
+  // (as often for every group of the warp: they sum together)
+  for (int turns = (p.heads + p.token_groups - 1) / p.token_groups; turns > 0; --turns, h += p.token_groups) {
+    const bool head = there && h < p.heads;
+    const uint4 now[2] = {next[0], next[1]};
+    if (there && h + p.token_groups < p.heads) {
+      const T* src = at(h + p.token_groups, false);
+      next[0] = *reinterpret_cast<const uint4*>(src + first);
+      next[1] = *reinterpret_cast<const uint4*>(src + second);
+    }
+    float x[2][V];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      T raw[V];
+      memcpy(raw, &now[j], 16);
+#pragma unroll
+      for (int i = 0; i < V; ++i) x[j][i] = head ? to_f32(raw[i]) : 0.0f;
+    }
+    if (p.d.norm) {
+      const int key = h >= p.d.Hq;
+      if (key != weights_of) {
+        weights_of = key;
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+          w[0][i] = there ? weights[key * D + first + i] : 0.0f;
+          w[1][i] = there ? weights[key * D + second + i] : 0.0f;
+        }
+      }
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < V; ++i) sum = fmaf(x[0][i], x[0][i], fmaf(x[1][i], x[1][i], sum));
+#pragma unroll
+      for (int s = kLanes / 2; s > 0; s >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, s, kLanes);
+      const float f = __frsqrt_rn(sum / static_cast<float>(D) + p.d.eps);
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < V; ++i) x[j][i] = x[j][i] * f * w[j][i];
+    }
+    T y[2][V];
+    if (p.d.interleaved) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < V; i += 2) {
+          const float2 c = cs[(j * V + i) / 2];
+          y[j][i] = from_f32<T>(fmaf(x[j][i], c.x, -x[j][i + 1] * c.y));
+          y[j][i + 1] = from_f32<T>(fmaf(x[j][i + 1], c.x, x[j][i] * c.y));
+        }
+    } else {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        y[0][i] = from_f32<T>(fmaf(x[0][i], cs[i].x, -x[1][i] * cs[i].y));
+        y[1][i] = from_f32<T>(fmaf(x[1][i], cs[i].x, x[0][i] * cs[i].y));
+      }
+    }
+    if (head) {
+      T* dst = at(h, true);
+      uint4 out[2];
+      memcpy(out, y, 32);
+      *reinterpret_cast<uint4*>(dst + first) = out[0];
+      *reinterpret_cast<uint4*>(dst + second) = out[1];
+    }
+  }
+}
+
 int64_t any_smem(const RopeArgs& p) {
   return static_cast<int64_t>(p.block_tokens) * (p.d.R / 2) * 8 + (p.d.norm ? 2 : 0) * p.d.D * 4 + static_cast<int64_t>(kThreads / 32) * p.d.D * 4;
 }
 
+// Rows of 16-byte pieces whose pairs share pieces or lie in two that one lane takes.
+template <typename T>
+bool takes_wide(const RopeArgs& p) {
+  constexpr int V = 16 / sizeof(T);
+  const pq_qk_rope& d = p.d;
+  if (d.D % (2 * V) != 0 || d.D > 64 * V || (!d.interleaved && d.R % (2 * V) != 0)) return false;
+  for (int key = 0; key < 2; ++key)
+    if ((key ? d.Hkv : d.Hq) > 0 && (!is_aligned(p.in[key], 16) || !is_aligned(p.out[key], 16))) return false;
+  for (int64_t s : {d.q_token_stride, d.q_head_stride, d.q_out_token_stride, d.q_out_head_stride})
+    if (d.Hq > 0 && s % V != 0) return false;
+  for (int64_t s : {d.k_token_stride, d.k_head_stride, d.k_out_token_stride, d.k_out_head_stride})
+    if (d.Hkv > 0 && s % V != 0) return false;
+  return true;
+}
+
+template <typename T>
+cudaError_t launch_wide(RopeArgs& p, cudaStream_t s) {
+  constexpr int V = 16 / sizeof(T);
+  int lg = 0;
+  while ((2 * V << lg) < p.d.D) ++lg;
+  const int groups = kThreads >> lg;
+  // about five heads a group; a group for each head where the tokens would not fill the chip
+  int share = 1;
+  while (share < groups && share * 5 < p.heads) share *= 2;
+  while (share < groups && share < p.heads && p.d.tokens * share < 304ll * groups) share *= 2;
+  p.token_groups = share;
+  p.block_tokens = groups / share;
+  const unsigned blocks = static_cast<unsigned>((p.d.tokens + p.block_tokens - 1) / p.block_tokens);
+  const size_t smem = static_cast<size_t>(p.block_tokens) * (p.d.R / 2) * 8 + (p.d.norm ? 2 * p.d.D * 4 : 0);
+  switch (lg) {
+    case 0: pq_qk_rope_wide<T, 0><<<blocks, kThreads, smem, s>>>(p); break;
+    case 1: pq_qk_rope_wide<T, 1><<<blocks, kThreads, smem, s>>>(p); break;
+    case 2: pq_qk_rope_wide<T, 2><<<blocks, kThreads, smem, s>>>(p); break;
+    case 3: pq_qk_rope_wide<T, 3><<<blocks, kThreads, smem, s>>>(p); break;
+    case 4: pq_qk_rope_wide<T, 4><<<blocks, kThreads, smem, s>>>(p); break;
+    default: pq_qk_rope_wide<T, 5><<<blocks, kThreads, smem, s>>>(p); break;
+  }
+  return cudaGetLastError();
+}
+
 template <typename T>
 cudaError_t launch_rope(RopeArgs& p, cudaStream_t s) {
+  if (takes_wide<T>(p)) return launch_wide<T>(p, s);
   p.block_tokens = 1;
   const int64_t blocks = (p.d.tokens + p.block_tokens - 1) / p.block_tokens;
   pq_qk_rope_any<T><<<static_cast<unsigned>(blocks), kThreads, any_smem(p), s>>>(p);
@@ -190,7 +337,7 @@ pq_status palquant_qk_norm_rope(const void* q_dev, const void* k_dev, void* q_ou
   if (d->norm && (!is_aligned(d->q_weight_dev, bytes_of_type(d->w_type)) || !is_aligned(d->k_weight_dev, bytes_of_type(d->w_type))))
     return PQ_EINVAL;
   if (d->D > kMostD || d->tokens > 0x7FFFFFFF || d->Hq + static_cast<int64_t>(d->Hkv) > 65535) return PQ_EUNSUPPORTED;
-  RopeArgs p = {*d, {q_dev, k_dev}, {q_out_dev, k_out_dev}, d->Hq + d->Hkv, 1};
+  RopeArgs p = {*d, {q_dev, k_dev}, {q_out_dev, k_out_dev}, d->Hq + d->Hkv, 1, 1};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t st = d->type == PQ_F32   ? launch_rope<float>(p, s)
                          : d->type == PQ_F16 ? launch_rope<__half>(p, s)
