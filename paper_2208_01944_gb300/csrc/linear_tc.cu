@@ -32,6 +32,7 @@
 #include "palquant.h"
 #include "pq_internal.h"
 #include "pq_linear.h"
+#include "pq_tc.cuh"
 #include "pq_tokens.cuh"
 
 namespace pq {
@@ -68,14 +69,6 @@ struct TcBars {
   __device__ uint32_t acc_empty(int i) const { return base + 8u * (4 * kTcMaxStages + 2 + i); }
   __device__ uint32_t done() const { return base + 8u * (4 * kTcMaxStages + 4); }
 };
-
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, int c0, int c1, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
-          dst),
-      "l"(reinterpret_cast<uint64_t>(tmap)), "r"(c0), "r"(c1), "r"(bar)
-      : "memory");
-}
 
 // Instruction descriptor of kind::f16: half operands, fp32 sums, K-major.
 __host__ __device__ constexpr uint32_t idesc_f16_f32(int M, int N) {
@@ -132,20 +125,6 @@ __device__ __forceinline__ void tmem_dealloc_group(uint32_t taddr, uint32_t ncol
     tmem_dealloc(taddr, ncols);
 }
 
-__device__ __forceinline__ uint4 lds128(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr));
-  return v;
-}
-
-__device__ __forceinline__ uint32_t cluster_rank() {
-  uint32_t r;
-  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-  return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-  asm volatile("barrier.cluster.arrive.release;\nbarrier.cluster.wait.acquire;" ::: "memory");
-}
 __device__ __forceinline__ int4 load_of_peer(uint32_t addr, uint32_t rank) {
   uint32_t a;
   int4 v;
@@ -165,15 +144,6 @@ __device__ __forceinline__ void arrive_at_first(uint32_t bar) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(a) : "r"(bar));
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(a) : "memory");
 }
-
-// Position in the ring.
-struct Ring {
-  int s = 0;
-  uint32_t phase = 0;
-  __device__ __forceinline__ void next(int stages) {
-    if (++s == stages) s = 0, phase ^= 1u;
-  }
-};
 
 // One channel's results of kCols tokens from m on: the warp's 32 lanes write 32
 // consecutive channels of one token at a time.  s_x: the tokens' scales in shared memory.

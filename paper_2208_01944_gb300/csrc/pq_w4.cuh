@@ -1,0 +1,96 @@
+// Packed 4-bit weights, and what the dense-layer kernels on them share.
+#pragma once
+
+#include <cuda_runtime.h>
+
+#include <cstdint>
+#include <type_traits>
+
+#include "palquant.h"
+#include "pq_tokens.cuh"
+
+namespace pq {
+
+constexpr int kBlockK = 128;  // of K between a strip's scales
+
+// A strip of 16 channels: for each 128 of K, 1024 bytes of codes (two steps of 64), then the scales of its groups.  Of a
+// step, lane 4 g + t holds 16 bytes: of rows g and g + 8, for each 32 of K a word of 8 codes: columns 4 t to 4 t + 3 and
+// 16 + 4 t to 16 + 4 t + 3.  That is an operand of two 16 x 16 MMAs, and in tensor memory a row's 64-bit piece.
+struct PackedW4 {
+  int strips, blocks;  // of 128 of K
+  int group_shift;     // log2(group): 5 to 7
+  int s_type, s_bytes;
+  int block_bytes;
+  __host__ __device__ int64_t strip_bytes() const { return static_cast<int64_t>(blocks) * block_bytes; }
+};
+
+inline PackedW4 packed_of(const pq_w4_weights* w) {
+  PackedW4 p;
+  p.strips = (w->N + 15) / 16;
+  p.blocks = (w->K + kBlockK - 1) / kBlockK;
+  p.group_shift = w->group == 32 ? 5 : w->group == 64 ? 6 : 7;
+  p.s_type = w->s_type;
+  p.s_bytes = static_cast<int>(bytes_of_type(w->s_type));
+  p.block_bytes = 1024 + (kBlockK >> p.group_shift) * 16 * p.s_bytes;
+  return p;
+}
+
+// Where word i of row r (words 4 b to 4 b + 3 hold columns 32 b to 32 b + 31) lies in a strip, and row r's scale of group g.
+__host__ __device__ inline int64_t word_at(const PackedW4& p, int r, int i) {
+  const int in = i & 15, step = in >> 3, half = (in >> 2) & 1, t = in & 3;
+  return static_cast<int64_t>(i >> 4) * p.block_bytes + step * 512 + ((r & 7) * 4 + t) * 16 + half * 8 + (r >> 3) * 4;
+}
+// Column of code j of word i, and its place in the word: pairs (j, j + 1) lie 16 bits apart.
+__host__ __device__ constexpr int column_of(int i, int j) { return 32 * (i >> 2) + 4 * (i & 3) + (j & 3) + 16 * (j >> 2); }
+__host__ __device__ inline int64_t scale_at(const PackedW4& p, int r, int g) {
+  const int per = kBlockK >> p.group_shift;
+  return static_cast<int64_t>(g / per) * p.block_bytes + 1024 + ((g % per) * 16 + (r & 7) * 2 + (r >> 3)) * p.s_bytes;
+}
+__host__ __device__ constexpr int nibble_shift(int j) { return 4 * ((j & 1) * 4 + (j >> 1)); }
+
+__device__ __forceinline__ float load_scale(const void* at, int type) {
+  if (type == PQ_F32) return *static_cast<const float*>(at);
+  if (type == PQ_F16) return __half2float(*static_cast<const __half*>(at));
+  return __bfloat162float(*static_cast<const __nv_bfloat16*>(at));
+}
+
+struct W4Args {
+  PackedW4 p;
+  const void* x;
+  const uint8_t* w;
+  const float* bias;
+  void* y;
+  int64_t ldx, ldy, M;
+  int N, K, y_type;
+  bool wide_x;  // four elements of a token row lie on a boundary of their size
+};
+
+// Up to 128 tokens a tile on the tensor cores; 16-bit activations in rows on 16-byte boundaries.
+bool w4_tc_takes(const W4Args& a, int x_type);
+cudaError_t launch_w4_tc(const W4Args& a, int x_type, cudaStream_t stream);
+
+// One output, in fp32 until here.
+__device__ __forceinline__ void put_w4(const W4Args& a, int64_t m, int n, float y) {
+  const int64_t at = m * a.ldy + n;
+  if (a.y_type == PQ_F32)
+    static_cast<float*>(a.y)[at] = y;
+  else if (a.y_type == PQ_F16)
+    static_cast<__half*>(a.y)[at] = __float2half_rn(y);
+  else
+    static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(y);
+}
+
+// Pair i (columns 2 i and 2 i + 1) of a word's codes in the products' type.  The code's sign bit is flipped under the
+// exponent of 1024 (128): 1032 + c (136 + c).
+template <typename T, int I>
+__device__ __forceinline__ uint32_t code_pair(uint32_t word) {
+  if constexpr (sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value) {
+    return sub_half2(((word >> (4 * I)) & 0x000F000Fu) ^ 0x64086408u, 0x64086408u);
+  } else {
+    uint32_t r;
+    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(((word >> (4 * I)) & 0x000F000Fu) ^ 0x43084308u), "r"(0x43084308u));
+    return r;
+  }
+}
+
+}  // namespace pq
