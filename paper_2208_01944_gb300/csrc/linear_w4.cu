@@ -21,8 +21,6 @@
 namespace pq {
 namespace {
 
-constexpr int kWarps = 8;
-
 __device__ __forceinline__ void store_scale(void* at, int type, float s) {
   if (type == PQ_F32)
     *static_cast<float*>(at) = s;
@@ -30,23 +28,6 @@ __device__ __forceinline__ void store_scale(void* at, int type, float s) {
     *static_cast<__half*>(at) = __float2half_rn(s);
   else
     *static_cast<__nv_bfloat16*>(at) = __float2bfloat16_rn(s);
-}
-
-// n of four consecutive elements (the others zero); `wide`: their address is a multiple of their size.
-template <typename T>
-__device__ __forceinline__ void load4(const T* p, int n, bool wide, T (&v)[4]) {
-  if (wide && n >= 4) {
-    if constexpr (sizeof(T) == 2) {
-      const uint2 q = *reinterpret_cast<const uint2*>(p);
-      memcpy(v, &q, 8);
-    } else {
-      const uint4 q = *reinterpret_cast<const uint4*>(p);
-      memcpy(v, &q, 16);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = i < n ? p[i] : from_f32<T>(0.0f);
-  }
 }
 
 // ------------------------------------------------------------------- packing
@@ -57,18 +38,17 @@ __global__ void __launch_bounds__(256) pq_w4_pack(const int8_t* __restrict__ cod
   const int groups = (K + (1 << p.group_shift) - 1) >> p.group_shift;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
     const int64_t n = i / words;
-    const int at = static_cast<int>(i - n * words), r = static_cast<int>(n & 15);
-    uint8_t* strip = out + (n >> 4) * p.strip_bytes();
+    const int at = static_cast<int>(i - n * words), row = static_cast<int>(n);
     uint32_t word = 0;
     if (n < N)
 #pragma unroll
       for (int j = 0; j < 8; ++j)
         if (column_of(at, j) < K) word |= static_cast<uint32_t>(codes[n * ldc + column_of(at, j)] & 15) << nibble_shift(j);
-    *reinterpret_cast<uint32_t*>(strip + word_at(p, r, at)) = word;
+    *reinterpret_cast<uint32_t*>(out + word_at(p, row, at)) = word;
     if ((at * 8 & ((1 << p.group_shift) - 1)) == 0) {
       const int g = at * 8 >> p.group_shift;
       const bool there = n < N && g < groups;
-      uint8_t* to = strip + scale_at(p, r, g);
+      uint8_t* to = out + scale_at(p, row, g);
       for (int b = 0; b < p.s_bytes; ++b) to[b] = there ? scales[(n * groups + g) * p.s_bytes + b] : 0;
     }
   }
@@ -80,9 +60,8 @@ __global__ void __launch_bounds__(256) pq_w4_unpack(const uint8_t* __restrict__ 
   const int groups = (K + (1 << p.group_shift) - 1) >> p.group_shift;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
     const int64_t n = i / words;
-    const int at = static_cast<int>(i - n * words), r = static_cast<int>(n & 15);
-    const uint8_t* strip = packed + (n >> 4) * p.strip_bytes();
-    const uint32_t word = *reinterpret_cast<const uint32_t*>(strip + word_at(p, r, at));
+    const int at = static_cast<int>(i - n * words), row = static_cast<int>(n);
+    const uint32_t word = *reinterpret_cast<const uint32_t*>(packed + word_at(p, row, at));
     if (codes != nullptr)
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -90,7 +69,7 @@ __global__ void __launch_bounds__(256) pq_w4_unpack(const uint8_t* __restrict__ 
           codes[n * ldc + column_of(at, j)] = static_cast<int8_t>(static_cast<int>((word >> nibble_shift(j) & 15u) ^ 8u) - 8);
     if (scales != nullptr && (at * 8 & ((1 << p.group_shift) - 1)) == 0) {
       const int g = at * 8 >> p.group_shift;
-      scales[n * groups + g] = load_scale(strip + scale_at(p, r, g), p.s_type);
+      scales[n * groups + g] = load_scale(packed + scale_at(p, row, g), p.s_type);
     }
   }
 }
@@ -113,7 +92,7 @@ __global__ void __launch_bounds__(256) pq_w4_quantize(const T* __restrict__ x, i
   const int members = 1 << (p.group_shift - 3);
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
     const int64_t n = i / words;
-    const int at = static_cast<int>(i - n * words), r = static_cast<int>(n & 15);
+    const int at = static_cast<int>(i - n * words), row = static_cast<int>(n);
     Vec8<T> v;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -133,233 +112,12 @@ __global__ void __launch_bounds__(256) pq_w4_quantize(const T* __restrict__ x, i
         const int c = min(7, max(-7, __float2int_rn(__fmul_rn(to_f32(v.v[j]), inv))));
         word |= static_cast<uint32_t>(c & 15) << nibble_shift(j);
       }
-    uint8_t* strip = out + (n >> 4) * p.strip_bytes();
-    *reinterpret_cast<uint32_t*>(strip + word_at(p, r, at)) = word;
-    if ((at * 8 & ((1 << p.group_shift) - 1)) == 0) store_scale(strip + scale_at(p, r, at * 8 >> p.group_shift), p.s_type, scale);
+    *reinterpret_cast<uint32_t*>(out + word_at(p, row, at)) = word;
+    if ((at * 8 & ((1 << p.group_shift) - 1)) == 0) store_scale(out + scale_at(p, row, at * 8 >> p.group_shift), p.s_type, scale);
   }
 }
 
 // ------------------------------------------------------------------ products
-// Rows g's and g + 8's scale of a group, neighbours in shared memory.
-__device__ __forceinline__ void scale_pair(uint32_t at, int type, float& s0, float& s1) {
-  if (type == PQ_F32) {
-    asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(s0), "=f"(s1) : "r"(at) : "memory");
-    return;
-  }
-  uint32_t w;
-  asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
-  if (type == PQ_F16) {
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    s0 = f.x, s1 = f.y;
-  } else {
-    s0 = __uint_as_float(w << 16), s1 = __uint_as_float(w & 0xFFFF0000u);
-  }
-}
-
-// How activations enter the products: halves, bfloat16, or fp32 as three bfloat16 parts.
-template <typename T>
-constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-
-template <typename T>
-__device__ __forceinline__ void mma_w4(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  if constexpr (sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value) {
-    mma_16x8x16(d, a0, a1, a2, a3, b0, b1);
-  } else {
-    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  }
-}
-
-// Four activations as two pairs, part by part.
-template <typename T>
-__device__ __forceinline__ void operand_pairs(const T (&v)[4], uint32_t (&r)[kParts<T>][2]) {
-  if constexpr (sizeof(T) == 2) {
-    memcpy(r[0], v, 8);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint32_t part[2][3];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        // 8 + 8 + 8 bits by truncation; an infinity or a NaN is its first part alone
-        const float x = v[2 * i + j];
-        const uint32_t hi = __float_as_uint(x) & 0xFFFF0000u;
-        const bool finite = (hi & 0x7F800000u) != 0x7F800000u;
-        const float rest = finite ? x - __uint_as_float(hi) : 0.0f;
-        const uint32_t mid = __float_as_uint(rest) & 0xFFFF0000u;
-        part[j][0] = finite || hi == __float_as_uint(x) ? hi : hi | 0x00400000u;
-        part[j][1] = mid;
-        part[j][2] = __float_as_uint(rest - __uint_as_float(mid));
-      }
-#pragma unroll
-      for (int h = 0; h < 3; ++h) r[h][i] = __byte_perm(part[0][h], part[1][h], 0x7632);
-    }
-  }
-}
-
-// A block: 16 channels x 8 NT tokens; its warps take the strip's blocks of 128 of K in turn.  The weights come through
-// rings of asynchronous copies, one for each warp (a block of 128 of K a stage, RING - 1 of them ahead, so that 32 warps keep
-// 100 KB in flight on an SM); each lane reads codes that it copied itself, and scales that its warp copied.  The tokens,
-// which every block reads, come from L1 and L2 into registers, a block of K ahead where they fit.
-constexpr int kMostBlock = 1024 + 256;  // bytes of 128 of K of a strip: four groups' fp32 scales
-
-template <typename T, int NT, int RING>
-__global__ void __launch_bounds__(32 * kWarps) pq_linear_w4_rows(const __grid_constant__ W4Args a) {
-  extern __shared__ __align__(16) uint8_t ring_raw[];
-  __shared__ float part[kWarps][NT][8][17];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int64_t m0 = static_cast<int64_t>(blockIdx.y) * (8 * NT);
-  const uint8_t* strip = a.w + static_cast<int64_t>(blockIdx.x) * a.p.strip_bytes();
-  const uint32_t ring = smem_u32(ring_raw) + warp * RING * a.p.block_bytes;
-  const int scale_pieces = (a.p.block_bytes - 1024) >> 4;
-  const int mine = a.p.blocks > warp ? (a.p.blocks - warp - 1) / kWarps + 1 : 0;
-  auto fetch = [&](int i, int stage) {
-    const uint8_t* from = strip + static_cast<int64_t>(warp + i * kWarps) * a.p.block_bytes + lane * 16;
-    const uint32_t to = ring + stage * a.p.block_bytes + lane * 16;
-    cp_async_16(to, from, 16);
-    cp_async_16(to + 512, from + 512, 16);
-    if (lane < scale_pieces) cp_async_16(to + 1024, from + 1024, 16);
-  };
-#pragma unroll
-  for (int i = 0; i < RING - 1; ++i) {
-    if (i < mine) fetch(i, i);
-    cp_async_commit();
-  }
-  const T* row[NT];
-  bool there[NT];
-#pragma unroll
-  for (int j = 0; j < NT; ++j) {
-    const int64_t m = m0 + 8 * j + g;
-    there[j] = m < a.M;
-    row[j] = static_cast<const T*>(a.x) + (there[j] ? m : 0) * a.ldx;
-  }
-  // 16 of K of a token: columns 128 b + 16 c + 4 t and up
-  auto tokens_at = [&](int j, int b, int c, T (&v)[4]) {
-    const int k = b * kBlockK + 16 * c + 4 * t;
-    load4(row[j] + min(k, a.K - 1), there[j] ? a.K - k : 0, a.wide_x, v);
-  };
-  constexpr bool kAhead = NT == 1 && sizeof(T) == 2;
-  T next[kAhead ? 8 : 1][4];
-  auto tokens_ahead = [&](int i) {
-    if constexpr (kAhead) {
-      if (i >= mine) return;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) tokens_at(0, warp + i * kWarps, c, next[c]);
-    }
-  };
-  tokens_ahead(0);
-  float sum[NT][4] = {};
-  int stage = 0;
-  for (int i = 0; i < mine; ++i) {
-    T now[kAhead ? 8 : 1][4];
-    if constexpr (kAhead) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) memcpy(now[c], next[c], sizeof(now[c]));
-      tokens_ahead(i + 1);
-    }
-    cp_async_wait<RING - 2>();
-    __syncwarp();  // the block's scales have arrived, and every lane is done with the stage before
-    const uint32_t at = ring + stage * a.p.block_bytes;
-    {
-      const int before = stage == 0 ? RING - 1 : stage - 1;
-      if (i + RING - 1 < mine) fetch(i + RING - 1, before);
-      cp_async_commit();
-      stage = stage + 1 == RING ? 0 : stage + 1;
-    }
-    float d[NT][4] = {};
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      uint4 u;
-      asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                   : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w)
-                   : "r"(at + s * 512 + lane * 16)
-                   : "memory");
-      const uint32_t words[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t p[4], q[4];
-        p[0] = code_pair<T, 0>(words[2 * h]), p[1] = code_pair<T, 1>(words[2 * h]);
-        p[2] = code_pair<T, 2>(words[2 * h]), p[3] = code_pair<T, 3>(words[2 * h]);
-        q[0] = code_pair<T, 0>(words[2 * h + 1]), q[1] = code_pair<T, 1>(words[2 * h + 1]);
-        q[2] = code_pair<T, 2>(words[2 * h + 1]), q[3] = code_pair<T, 3>(words[2 * h + 1]);
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const int in = 4 * s + 2 * h + c;  // 16 of K
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            uint32_t x[kParts<T>][2];
-            if constexpr (kAhead) {
-              operand_pairs(now[in], x);
-            } else {
-              T v[4];
-              tokens_at(j, warp + i * kWarps, in, v);
-              operand_pairs(v, x);
-            }
-#pragma unroll
-            for (int f = 0; f < kParts<T>; ++f) mma_w4<T>(d[j], p[2 * c], q[2 * c], p[2 * c + 1], q[2 * c + 1], x[f][0], x[f][1]);
-          }
-        }
-        // a group is over
-        const int end = 64 * s + 32 * h + 32;
-        if ((end & ((1 << a.p.group_shift) - 1)) == 0) {
-          const int group = (end - 32) >> a.p.group_shift;
-          float s0, s1;
-          scale_pair(at + 1024 + (group * 16 + g * 2) * a.p.s_bytes, a.p.s_type, s0, s1);
-#pragma unroll
-          for (int j = 0; j < NT; ++j) {
-            sum[j][0] = fmaf(s0, d[j][0], sum[j][0]);
-            sum[j][1] = fmaf(s0, d[j][1], sum[j][1]);
-            sum[j][2] = fmaf(s1, d[j][2], sum[j][2]);
-            sum[j][3] = fmaf(s1, d[j][3], sum[j][3]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) d[j][e] = 0.0f;
-          }
-        }
-      }
-    }
-  }
-#pragma unroll
-  for (int j = 0; j < NT; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) part[warp][j][2 * t + (e & 1)][g + 8 * (e >> 1)] = sum[j][e];
-  __syncthreads();
-  for (int e = threadIdx.x; e < NT * 128; e += 32 * kWarps) {
-    const int r = e & 15, c = (e >> 4) & 7, j = e >> 7;
-    const int n = blockIdx.x * 16 + r;
-    const int64_t m = m0 + 8 * j + c;
-    if (n >= a.N || m >= a.M) continue;
-    float y = 0.0f;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) y += part[w][j][c][r];
-    put_w4(a, m, n, a.bias != nullptr ? y + a.bias[n] : y);
-  }
-}
-
-template <typename T, int NT, int RING>
-cudaError_t launch_rows_as(const W4Args& a, cudaStream_t s) {
-  static int attr_set[64] = {0};
-  int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
-  if (dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(pq_linear_w4_rows<T, NT, RING>, cudaFuncAttributeMaxDynamicSharedMemorySize, kWarps * RING * kMostBlock);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) attr_set[dev] = 1;
-  }
-  const dim3 grid(static_cast<unsigned>(a.p.strips), static_cast<unsigned>((a.M + 8 * NT - 1) / (8 * NT)));
-  pq_linear_w4_rows<T, NT, RING><<<grid, 32 * kWarps, kWarps * RING * a.p.block_bytes, s>>>(a);
-  return cudaGetLastError();
-}
-
-template <typename T>
-cudaError_t launch_w4(const W4Args& a, cudaStream_t s) {
-  if (a.M <= 8) return launch_rows_as<T, 1, 4>(a, s);
-  if (a.M <= 16) return launch_rows_as<T, 2, 4>(a, s);
-  if (a.M <= 32) return launch_rows_as<T, 4, 4>(a, s);
-  return launch_rows_as<T, 8, 4>(a, s);
-}
-
 bool valid_w4_type(int32_t t) { return t == PQ_F32 || t == PQ_F16 || t == PQ_BF16; }
 
 bool valid_w4(const pq_w4_weights* w) {
@@ -385,7 +143,7 @@ extern "C" {
 size_t palquant_w4_packed_bytes(const pq_w4_weights* w) {
   if (!pq::valid_w4(w)) return 0;
   const pq::PackedW4 p = pq::packed_of(w);
-  return static_cast<size_t>(p.strips) * static_cast<size_t>(p.strip_bytes());
+  return static_cast<size_t>(p.strips) * static_cast<size_t>(p.blocks) * static_cast<size_t>(p.block_bytes);
 }
 
 pq_status palquant_w4_pack(const int8_t* codes_dev, int64_t ldc, const void* s_dev, const pq_w4_weights* w,
@@ -447,14 +205,14 @@ pq_status palquant_linear_w4(const void* x_dev, const void* packed_dev, const fl
   if (x_dev == nullptr || packed_dev == nullptr || y_dev == nullptr || !pq::is_aligned(x_dev, e) ||
       !pq::is_aligned(packed_dev, 16) || !pq::is_aligned(bias_dev, 4) || !pq::is_aligned(y_dev, pq::bytes_of_type(d->y_type)))
     return PQ_EINVAL;
-  if (d->M > 64ll * 65535) return PQ_EUNSUPPORTED;  // blocks along the grid's second axis
+  if (d->M > 32ll * 65535) return PQ_EUNSUPPORTED;  // blocks along the grid's second axis
   const pq::W4Args a = {pq::packed_of(w), x_dev, static_cast<const uint8_t*>(packed_dev), bias_dev, y_dev, d->ldx, d->ldy, d->M,
                         d->N, d->K, d->y_type, pq::is_aligned(x_dev, 4 * e) && d->ldx % 4 == 0};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t st = pq::w4_tc_takes(a, d->x_type) ? pq::launch_w4_tc(a, d->x_type, s)
-                         : d->x_type == PQ_F32   ? pq::launch_w4<float>(a, s)
-                         : d->x_type == PQ_F16 ? pq::launch_w4<__half>(a, s)
-                                               : pq::launch_w4<__nv_bfloat16>(a, s);
+                         : d->x_type == PQ_F32         ? pq::launch_w4_rows<float>(a, s)
+                         : d->x_type == PQ_F16         ? pq::launch_w4_rows<__half>(a, s)
+                                                       : pq::launch_w4_rows<__nv_bfloat16>(a, s);
   return st == cudaSuccess ? PQ_OK : PQ_ECUDA;
 }
 

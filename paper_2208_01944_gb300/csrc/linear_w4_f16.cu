@@ -1,0 +1,8 @@
+// The 4-bit dense layer for few tokens of this type.
+#include "pq_w4_rows.cuh"
+
+namespace pq {
+
+template cudaError_t launch_w4_rows<__half>(const W4Args& a, cudaStream_t stream);
+
+}  // namespace pq

@@ -11,8 +11,7 @@
 // The accumulators of groups take turns, so that one is read while others are written.  Few tiles: the blocks of a cluster take
 // parts of K of one tile and add their fp32 sums through distributed shared memory, in order.
 //
-// Roles (20 warps): 0 and 2 load (weights, tokens), 1 issues the MMAs, 4-7 and 8-11 unpack 64 of K each of every stage, 12-19 drain
-// and write.  A stage is 128 of K.
+// Roles (32 warps): 0 and 2 load (weights, tokens), 4-19 unpack, 20-27 drain and write, 28-31 issue the MMAs.  A stage is 128 of K.
 #include <cuda.h>
 #include <cuda_runtime.h>
 
@@ -28,16 +27,29 @@
 namespace pq {
 namespace {
 
-constexpr int kThreads = 640;
-constexpr int kStrips = 8;                            // of a tile
-constexpr int kWBytes = kStrips * (1024 + 256);       // of a stage's weights at most
+constexpr int kThreads = 1024;
+constexpr int kWBytes = kTileStrips * (1024 + 256);   // of a stage's weights at most
 constexpr int kMaxStages = 8;
-constexpr int kSlots = 8;                             // 64 of K of unpacked weights each, 32 columns of tensor memory
-constexpr uint32_t kAccColumns = 256;                 // of the accumulators
+constexpr int kMaxSlots = 8;
+constexpr uint32_t kAColumns = 256;                   // of tensor memory for unpacked weights; as many for accumulators
+constexpr int kJoin = 8;                              // tokens that a thread adds up at one time
+
+// A job: 128 (groups of 128) or 64 of K.  Its unpacked weights take a slot, its groups' accumulators a place.  Each is used again
+// every kSlots or kPlaces jobs, powers of two that the numbers of warps in turn divide: so a warp that waits for a use has
+// waited for the one before, and a wait by parity is never for the wrong one.
+__host__ __device__ constexpr int job_k(int GS) { return GS == 7 ? 128 : 64; }
+__host__ __device__ constexpr int slots(int GS) { return kAColumns / (job_k(GS) / 2); }
+__host__ __device__ constexpr int places(int BN, int GS) {
+  return 256 / ((job_k(GS) >> GS) * BN) < kMaxSlots ? 256 / ((job_k(GS) >> GS) * BN) : kMaxSlots;
+}
 
 __host__ __device__ constexpr int stage_bytes(int BN) { return kWBytes + BN * 256; }
-__host__ __device__ constexpr int stages(int BN) { return 204800 / stage_bytes(BN) < kMaxStages ? 204800 / stage_bytes(BN) : kMaxStages; }
-__host__ __device__ constexpr int smem_bytes(int BN) { return stages(BN) * stage_bytes(BN) + 1024 /* alignment */; }
+// What the two sides of draining warps hand to one another at a tile's end.
+__host__ __device__ constexpr int exchange_bytes(int BN) { return BN < 128 ? BN * 512 : 0; }
+__host__ __device__ constexpr int stages(int BN) {
+  return (204800 - exchange_bytes(BN)) / stage_bytes(BN) < kMaxStages ? (204800 - exchange_bytes(BN)) / stage_bytes(BN) : kMaxStages;
+}
+__host__ __device__ constexpr int smem_bytes(int BN) { return stages(BN) * stage_bytes(BN) + exchange_bytes(BN) + 1024 /* alignment */; }
 
 struct W4Tc {
   W4Args a;
@@ -47,19 +59,20 @@ struct W4Tc {
   uint64_t wait_limit_ns;
 };
 
-// Barriers: loaded (a stage's bytes), empty (its MMAs are over and its scales read), full (a slot is unpacked), slot_empty (its
-// MMAs are over), acc_full, acc_empty, done.
+// Barriers: loaded (a stage's bytes), full (a slot is unpacked), acc_full (a place's MMAs are over); stage_empty, slot_empty and
+// acc_empty (the job's sums are read, and with them everything that they came from), done.  A wait or a commit takes a warp
+// among these 32 some 50 to 200 cycles, more than an MMA of these tiles: so one commit a job, and the draining warps free all.
 struct Bars {
   uint32_t base;
   __device__ uint32_t loaded(int s) const { return base + 8u * s; }
-  __device__ uint32_t empty(int s) const { return base + 8u * (kMaxStages + s); }
+  __device__ uint32_t stage_empty(int s) const { return base + 8u * (kMaxStages + s); }
   __device__ uint32_t full(int s) const { return base + 8u * (2 * kMaxStages + s); }
-  __device__ uint32_t slot_empty(int s) const { return base + 8u * (2 * kMaxStages + kSlots + s); }
-  __device__ uint32_t acc_full(int i) const { return base + 8u * (2 * kMaxStages + 2 * kSlots + i); }
-  __device__ uint32_t acc_empty(int i) const { return base + 8u * (2 * kMaxStages + 2 * kSlots + 8 + i); }
-  __device__ uint32_t done() const { return base + 8u * (2 * kMaxStages + 2 * kSlots + 16); }
+  __device__ uint32_t slot_empty(int s) const { return base + 8u * (2 * kMaxStages + kMaxSlots + s); }
+  __device__ uint32_t acc_full(int s) const { return base + 8u * (2 * kMaxStages + 2 * kMaxSlots + s); }
+  __device__ uint32_t acc_empty(int s) const { return base + 8u * (2 * kMaxStages + 3 * kMaxSlots + s); }
+  __device__ uint32_t done() const { return base + 8u * (2 * kMaxStages + 4 * kMaxSlots); }
 };
-constexpr int kBars = 2 * kMaxStages + 2 * kSlots + 17;
+constexpr int kBars = 2 * kMaxStages + 4 * kMaxSlots + 1;
 
 // Instruction descriptor of kind::f16: halves or bfloat16, fp32 sums, K-major.
 template <typename T>
@@ -78,6 +91,18 @@ __device__ __forceinline__ void mma_ts_x2(uint32_t d, uint32_t a, uint64_t b, ui
       : "memory");
 }
 
+// Four MMAs (64 of K).
+__device__ __forceinline__ void mma_ts_x4(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p, q, e;\nelect.sync _|e, 0xffffffff;\nsetp.ne.b32 p, %10, 0;\nsetp.eq.b32 q, 0, 0;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %5, %9, p;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%2], %6, %9, q;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%3], %7, %9, q;\n"
+      "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%4], %8, %9, q;\n}" ::"r"(d),
+      "r"(a), "r"(a + 8), "r"(a + 16), "r"(a + 24), "l"(b), "l"(b + 2), "l"(b + 4), "l"(b + 6), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+
 // 16 lanes x 32 columns: lane 4 g + t holds of lanes g and g + 8, for each 8 columns, columns 2 t and 2 t + 1.
 __device__ __forceinline__ void tmem_st_16x256b_x4(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile(
@@ -85,6 +110,13 @@ __device__ __forceinline__ void tmem_st_16x256b_x4(uint32_t taddr, const uint32_
       "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
+}
+
+// (s0, s1) += m (a, b), packed.
+__device__ __forceinline__ void fma_pair(float& s0, float& s1, float a, float b, float m) {
+  asm("{\n.reg .b64 s, t, u;\nmov.b64 s, {%0, %1};\nmov.b64 t, {%2, %3};\nmov.b64 u, {%4, %4};\nfma.rn.f32x2 s, t, u, s;\nmov.b64 {%0, %1}, s;\n}"
+      : "+f"(s0), "+f"(s1)
+      : "f"(a), "f"(b), "f"(m));
 }
 
 __device__ __forceinline__ float load_of_peer_f32(uint32_t addr, uint32_t rank) {
@@ -114,13 +146,24 @@ __device__ __forceinline__ void tile_origin(const W4Tc& p, int t, int BN, int* n
   *m0 = static_cast<int64_t>(in / width) * BN;
 }
 
-template <typename T, int BN>
+// GS: log2(group).
+template <typename T, int BN, int GS>
 __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_constant__ W4Tc p, const __grid_constant__ CUtensorMap map_x) {
   constexpr int kStages = stages(BN);
-  constexpr int kAccs = kAccColumns / BN;
+  constexpr int kSlots = slots(GS), kPlaces = places(BN, GS);
+  constexpr int kSlotColumns = kAColumns / kSlots;
+  constexpr int kAccs = job_k(GS) >> GS;           // accumulators of a job
+  constexpr int kPerStage = kBlockK / job_k(GS);   // jobs of a stage
+  constexpr int kIssuers = kPlaces < 4 ? kPlaces : 4;  // warps that issue jobs in turn
+  constexpr int kTurns = 2 * kPerStage;            // sets of warps that unpack jobs in turn
+  constexpr int kUnpackers = 16 / kTurns;          // warps of a set: 32 channels of 64 of K each
+  static_assert(kSlots % kTurns == 0 && kSlots % kIssuers == 0 && kPlaces % kIssuers == 0 && kPlaces % 2 == 0, "turns");
   constexpr int kTok = BN * 128;   // bytes of 64 of K of the tokens
-  constexpr int kCols = BN / 2;    // columns of an accumulator that one of its two draining warps takes
-  constexpr int kStep = kCols % 32 == 0 ? 32 : 16;
+  // Two sides of draining warps: up to 64 tokens they take jobs in turn, each all of their columns (one side's way through a
+  // job, 550 cycles, was the longest of all roles'); 128 tokens' sums do not fit a thread, there each takes half of the columns.
+  constexpr bool kSplit = BN == 128;
+  constexpr int kCols = kSplit ? BN / 2 : BN;
+  constexpr int kDrainers = kSplit ? 8 : 4;        // warps that drain a job
   extern __shared__ uint8_t raw[];
   __shared__ alignas(8) uint64_t bar_words[kBars];
   __shared__ int abort_flag;
@@ -136,17 +179,17 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(bars.loaded(s), 2);
-      mbar_init(bars.empty(s), 1 + 8);
+      mbar_init(bars.stage_empty(s), kDrainers * kPerStage);
     }
     for (int s = 0; s < kSlots; ++s) {
-      mbar_init(bars.full(s), 4);
-      mbar_init(bars.slot_empty(s), 1);
+      mbar_init(bars.full(s), kUnpackers);
+      mbar_init(bars.slot_empty(s), kDrainers);
     }
-    for (int i = 0; i < kAccs; ++i) {
-      mbar_init(bars.acc_full(i), 1);
-      mbar_init(bars.acc_empty(i), 8);
+    for (int s = 0; s < kPlaces; ++s) {
+      mbar_init(bars.acc_full(s), 1);
+      mbar_init(bars.acc_empty(s), kDrainers);
     }
-    mbar_init(bars.done(), 1);
+    mbar_init(bars.done(), kIssuers);
     abort_flag = 0;
     fence_mbar_init();
   }
@@ -154,17 +197,19 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  const uint32_t tmem = tmem_base;
+  // all 512 columns are this block's: the base is 0 (a constant address costs the issuing warps no register moves)
+  constexpr uint32_t tmem = 0;
 
   // this block's part of K, in stages, and its tiles
   const int kb0 = static_cast<int>(static_cast<int64_t>(w.blocks) * rank / p.k_parts);
   const int kbs = static_cast<int>(static_cast<int64_t>(w.blocks) * (rank + 1) / p.k_parts) - kb0;
   const int first_tile = blockIdx.x / p.k_parts, tile_step = gridDim.x / p.k_parts;
   const int tiles = p.n_tiles * p.m_tiles;
+  const int total = first_tile < tiles ? ((tiles - first_tile - 1) / tile_step + 1) * kbs * kPerStage : 0;  // jobs
   WaitCtx ctx{&abort_flag, p.err, p.wait_limit_ns, PQ_ERR_PRODUCER};
 
   if (warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
     if ((warp == 0 || warp == 2) && lane == 0) {
       // ---- loads: a stage's strips (warp 0), its tokens (warp 2)
       const bool weights = warp == 0;
@@ -175,19 +220,18 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
         int n_tile;
         int64_t m0;
         tile_origin(p, t, BN, &n_tile, &m0);
-        const int strips = min(kStrips, w.strips - n_tile * kStrips);
-        const uint8_t* from = p.a.w + n_tile * kStrips * w.strip_bytes() + static_cast<int64_t>(kb0) * w.block_bytes;
+        const uint32_t bytes = w.pitch(n_tile * kTileStrips);
+        const uint8_t* from = p.a.w + w.strip_at(n_tile * kTileStrips) + static_cast<int64_t>(kb0) * bytes;
         for (int kb = 0; kb < kbs; ++kb, ++issued) {
-          if (issued >= kStages && !mbar_wait(bars.empty(r.s), r.phase ^ 1u, ctx)) {
+          if (issued >= kStages && !mbar_wait(bars.stage_empty(r.s), r.phase ^ 1u, ctx)) {
             ok = false;
             break;
           }
           const uint32_t bar = bars.loaded(r.s);
           if (weights) {
-            mbar_arrive_expect_tx(bar, strips * w.block_bytes);
-            for (int i = 0; i < strips; ++i)
-              bulk_load(w_base + r.s * kWBytes + i * w.block_bytes, from + i * w.strip_bytes(), w.block_bytes, bar);
-            from += w.block_bytes;
+            mbar_arrive_expect_tx(bar, bytes);
+            bulk_load(w_base + r.s * kWBytes, from, bytes, bar);
+            from += bytes;
           } else {
             const int k = (kb0 + kb) * kBlockK;
             mbar_arrive_expect_tx(bar, 2 * kTok);
@@ -200,155 +244,186 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
       // what was loaded last may still be on its way
       for (int k = max(0, issued - kStages); k < issued; ++k)
         mbar_wait_drain(bars.loaded(k % kStages), (k / kStages) & 1, p.wait_limit_ns, p.err);
-    } else if (warp == 1) {
-      // ---- MMAs
-      ctx.err_bits = PQ_ERR_MMA;
+    }
+  } else if (warp >= 28) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    // ---- MMAs: these warps issue jobs in turn (one warp alone, its scheduler shared with unpacking warps, took 1200 cycles for 128 of K)
+    ctx.err_bits = PQ_ERR_MMA;
+    if (warp - 28 < kIssuers) {
       constexpr uint32_t idesc = idesc_of<T>(BN);
-      auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)) != 0; };
-      const int per_group = 1 << (w.group_shift - 5);  // MMA pairs of a group
-      Ring r, slot, acc;
-      uint32_t accs = 0;  // accumulators begun so far
-      bool ok = true;
-      for (int t = first_tile; ok && t < tiles; t += tile_step)
-        for (int kb = 0; ok && kb < kbs; ++kb) {
-          int in = 0;  // MMA pairs of the current group
-          for (int h = 0; ok && h < 2; ++h) {
-            ok = wait(bars.full(slot.s), slot.phase);
-            if (!ok) break;
-            tc_fence_after();
-            for (int c = 0; c < 2; ++c) {
-              if (in == 0 && accs >= kAccs) {
-                ok = wait(bars.acc_empty(acc.s), acc.phase ^ 1u);
-                if (!ok) break;
-                tc_fence_after();
-              }
-              if (in == 0) ++accs;
-              mma_ts_x2(tmem + acc.s * BN, tmem + kAccColumns + 32 * slot.s + 16 * c,
-                        sw128_desc(tok_base + (2 * r.s + h) * kTok) + 4 * c, idesc, in > 0);
-              if (++in == per_group) {
-                tc_commit_warp(bars.acc_full(acc.s));
-                acc.next(kAccs);
-                in = 0;
-              }
-            }
-            if (!ok) break;
-            tc_commit_warp(bars.slot_empty(slot.s));
-            slot.next(kSlots);
-          }
-          if (!ok) break;
-          tc_commit_warp(bars.empty(r.s));
-          r.next(kStages);
+      const int turn = warp - 28;
+      // stage of job i: i / kPerStage modulo kStages
+      int stage = turn / kPerStage;
+      const int stage_step = kIssuers / kPerStage > 0 ? kIssuers / kPerStage : 1;
+      uint32_t slot = turn, slot_phase = 0, place = turn, place_phase = 1;
+      for (int i = turn; i < total; i += kIssuers) {
+        if (!__all_sync(0xffffffffu, mbar_wait(bars.full(slot), slot_phase, ctx))) break;
+        if (i >= kPlaces && !__all_sync(0xffffffffu, mbar_wait(bars.acc_empty(place), place_phase, ctx))) break;
+        tc_fence_after();
+        const uint32_t acc = tmem + kAColumns + place * (kAccs * BN), codes = tmem + slot * kSlotColumns;
+        const uint64_t tokens = sw128_desc(tok_base + (2 * stage + (kPerStage == 2 ? i & 1 : 0)) * kTok);
+        if (GS == 7) {
+          mma_ts_x4(acc, codes, tokens, idesc, 0);
+          mma_ts_x4(acc, codes + 32, tokens + (kTok >> 4), idesc, 1);
+        } else if (GS == 6) {
+          mma_ts_x4(acc, codes, tokens, idesc, 0);
+        } else {
+          mma_ts_x2(acc, codes, tokens, idesc, 0);
+          mma_ts_x2(acc + BN, codes + 16, tokens + 4, idesc, 0);
         }
+        tc_commit_warp(bars.acc_full(place));
+        slot += kIssuers;
+        if (slot >= kSlots) slot -= kSlots, slot_phase ^= 1u;
+        place += kIssuers;
+        if (place >= kPlaces) place -= kPlaces, place_phase ^= 1u;
+        stage += stage_step;
+        if (stage >= kStages) stage -= kStages;
+      }
       // every MMA issued must be over before the tensor memory is given back
       tc_commit_warp(bars.done());
       if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
       __syncwarp();
     }
-  } else if (warp < 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
-    // ---- codes to operands: this warp's 32 channels, 64 of K of every stage
+  } else if (warp < 20) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    // ---- codes to operands
     ctx.err_bits = PQ_ERR_EPILOGUE;
-    const int quarter = warp & 3, half = (warp - 4) >> 2;
-    const uint32_t to = tmem + kAccColumns + (static_cast<uint32_t>(32 * quarter) << 16);
-    const int total = first_tile < tiles ? ((tiles - first_tile - 1) / tile_step + 1) * kbs : 0;
-    Ring r;
-    int slot = half;
-    uint32_t round = 0;  // times that the slot was used before
-    for (int i = 0; i < total; ++i) {
+    const int quarter = warp & 3, set = (warp - 4) >> 2;
+    const int turn = kPerStage == 1 ? set >> 1 : set, half = set & 1;  // (job i of 64 of K is half i % 2 of its stage)
+    const uint32_t to = tmem + (kPerStage == 1 ? 32 * half : 0) + (static_cast<uint32_t>(32 * quarter) << 16);
+    const uint32_t src = w_base + 2 * quarter * w.block_bytes + half * 512 + lane * 16;
+    Ring r, slot;
+    for (int i = 0; i < turn; ++i) slot.next(kSlots);
+    for (int i = 0; i < turn / kPerStage; ++i) r.next(kStages);
+    for (int i = turn; i < total; i += kTurns) {
       if (!__all_sync(0xffffffffu, mbar_wait(bars.loaded(r.s), r.phase, ctx))) break;
       uint32_t h[2][16];
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        const uint4 v = lds128(w_base + r.s * kWBytes + (2 * quarter + j) * w.block_bytes + half * 512 + lane * 16);
+        const uint4 v = lds128(src + r.s * kWBytes + j * w.block_bytes);
         const uint32_t words[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          const uint32_t low = words[2 * (c >> 1)], high = words[2 * (c >> 1) + 1];  // rows g and g + 8
-          if (c & 1) {
-            h[j][4 * c] = code_pair<T, 2>(low), h[j][4 * c + 1] = code_pair<T, 3>(low);
-            h[j][4 * c + 2] = code_pair<T, 2>(high), h[j][4 * c + 3] = code_pair<T, 3>(high);
-          } else {
-            h[j][4 * c] = code_pair<T, 0>(low), h[j][4 * c + 1] = code_pair<T, 1>(low);
-            h[j][4 * c + 2] = code_pair<T, 0>(high), h[j][4 * c + 3] = code_pair<T, 1>(high);
+        for (int c = 0; c < 2; ++c) {
+          uint32_t low[4], high[4];  // rows g and g + 8, 32 of K
+          code_pairs<T>(words[2 * c], low);
+          code_pairs<T>(words[2 * c + 1], high);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            h[j][8 * c + 4 * k] = low[2 * k], h[j][8 * c + 4 * k + 1] = low[2 * k + 1];
+            h[j][8 * c + 4 * k + 2] = high[2 * k], h[j][8 * c + 4 * k + 3] = high[2 * k + 1];
           }
         }
       }
-      if (round > 0 && !__all_sync(0xffffffffu, mbar_wait(bars.slot_empty(slot), (round - 1) & 1, ctx))) break;
+      if (i >= kSlots && !__all_sync(0xffffffffu, mbar_wait(bars.slot_empty(slot.s), slot.phase ^ 1u, ctx))) break;
       tc_fence_after();
-      tmem_st_16x256b_x4(to + 32 * slot, h[0]);
-      tmem_st_16x256b_x4(to + 32 * slot + (16u << 16), h[1]);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) tmem_st_16x256b_x4(to + slot.s * kSlotColumns + (static_cast<uint32_t>(16 * j) << 16), h[j]);
       tmem_wait_st();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(bars.full(slot));
+      if (lane == 0) mbar_arrive(bars.full(slot.s));
       r.next(kStages);
-      slot += 2;
-      if (slot >= kSlots) slot = half, ++round;
+      r.next(kStages);
+      slot.s += kTurns;
+      if (slot.s >= kSlots) slot.s -= kSlots, slot.phase ^= 1u;
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 144;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
     // ---- sums and outputs: this thread's channel, half of each accumulator's tokens
     ctx.err_bits = PQ_ERR_EPILOGUE;
-    const int quarter = warp & 3, side = (warp - 12) >> 2;
+    const int quarter = warp & 3, side = (warp - 20) >> 2;
     const int channel = 32 * quarter + lane, in_strip = channel & 15;
-    const uint32_t from = tmem + (static_cast<uint32_t>(32 * quarter) << 16) + side * kCols;
-    const int per_block = kBlockK >> w.group_shift;  // groups of a stage
-    const uint32_t scale_in = (channel >> 4) * w.block_bytes + 1024 + ((in_strip & 7) * 2 + (in_strip >> 3)) * w.s_bytes;
+    const uint32_t from = tmem + kAColumns + (static_cast<uint32_t>(32 * quarter) << 16) + (kSplit ? side * kCols : 0);
+    const uint32_t scale_in = w_base + (channel >> 4) * w.block_bytes + 1024 + ((in_strip & 7) * 2 + (in_strip >> 3)) * w.s_bytes;
+    const uint32_t exchange = w_base + kStages * kWBytes;
+    const int jobs = kbs * kPerStage;  // of a tile
     float sum[kCols];
-    Ring r, acc;
+    Ring r, place;
+    int job = 0, slot = 0;  // over all tiles
+    if (!kSplit && side == 1) {
+      ++job, ++slot;
+      place.next(kPlaces);
+      if (kPerStage == 1) r.next(kStages);
+    }
     bool ok = true;
-    for (int t = first_tile; ok && t < tiles; t += tile_step) {
+    for (int t = first_tile, end = jobs; t < tiles; t += tile_step, end += jobs) {
+#pragma unroll
+      for (int j = 0; j < kCols; ++j) sum[j] = 0.0f;
+      for (; ok && job < end; job += kSplit ? 1 : 2) {
+        ok = __all_sync(0xffffffffu, mbar_wait(bars.acc_full(place.s), place.phase, ctx)) != 0;
+        if (!ok) break;
+        tc_fence_after();
+        const int h = kPerStage == 1 ? 0 : kSplit ? job & 1 : side;
+#pragma unroll
+        for (int g = 0; g < kAccs; ++g) {
+          // (channels past the last strip have no scale there; they are not written)
+          const float s = scale_in_smem(scale_in + r.s * kWBytes + (h * kAccs + g) * 16 * w.s_bytes, w.s_type);
+#pragma unroll
+          for (int j = 0; j < kCols; j += 32) {
+            uint32_t v[32];
+            tmem_ld32(from + (place.s * kAccs + g) * BN + j, v);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 32; i += 2) fma_pair(sum[j + i], sum[j + i + 1], __uint_as_float(v[i]), __uint_as_float(v[i + 1]), s);
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(bars.acc_empty(place.s));
+          mbar_arrive(bars.slot_empty(slot));
+          mbar_arrive(bars.stage_empty(r.s));
+        }
+        place.next(kPlaces);
+        if (kSplit) {
+          slot = (slot + 1) & (kSlots - 1);
+          if (kPerStage == 1 || (job & 1)) r.next(kStages);
+        } else {
+          place.next(kPlaces);
+          slot = (slot + 2) & (kSlots - 1);
+          r.next(kStages);
+          if (kPerStage == 1) r.next(kStages);
+        }
+      }
+      if (p.k_parts > 1) break;  // (its only tile)
       int n_tile;
       int64_t m0;
       tile_origin(p, t, BN, &n_tile, &m0);
       const int n = n_tile * 128 + channel;
+      if (!kSplit) {
+        // each side writes half of the tokens: the other half's sums go to the other side.  (Every warp comes here for every tile, even
+        // after a wait that ran out.)
 #pragma unroll
-      for (int j = 0; j < kCols; ++j) sum[j] = 0.0f;
-      for (int kb = 0; ok && kb < kbs; ++kb) {
-        for (int g = 0; g < per_block; ++g) {
-          ok = __all_sync(0xffffffffu, mbar_wait(bars.acc_full(acc.s), acc.phase, ctx)) != 0;
-          if (!ok) break;
-          tc_fence_after();
-          // (channels past the last strip have no scale there; they are not written)
-          const float s = scale_in_smem(w_base + r.s * kWBytes + scale_in + g * 16 * w.s_bytes, w.s_type);
+        for (int j = 0; j < BN / 2; ++j)
+          asm volatile("st.shared.f32 [%0], %1;" ::"r"(exchange + ((side * (BN / 2) + j) * 128 + channel) * 4),
+                       "f"(side == 0 ? sum[BN / 2 + j] : sum[j])
+                       : "memory");
+        asm volatile("bar.sync 1, 256;" ::: "memory");
 #pragma unroll
-          for (int j = 0; j < kCols; j += kStep) {
-            uint32_t v[kStep];
-            if constexpr (kStep == 32)
-              tmem_ld32(from + acc.s * BN + j, v);
-            else
-              tmem_ld16(from + acc.s * BN + j, v);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < kStep; ++i) sum[j + i] = fmaf(s, __uint_as_float(v[i]), sum[j + i]);
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(bars.acc_empty(acc.s));
-          acc.next(kAccs);
+        for (int j = 0; j < BN / 2; ++j) {
+          float other;
+          asm volatile("ld.shared.f32 %0, [%1];" : "=f"(other) : "r"(exchange + (((1 - side) * (BN / 2) + j) * 128 + channel) * 4) : "memory");
+          sum[j] = side == 0 ? sum[j] + other : other + sum[BN / 2 + j];
         }
-        if (!ok) break;
-        if (lane == 0) mbar_arrive(bars.empty(r.s));
-        r.next(kStages);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
       }
-      if (!ok) break;
-      if (p.k_parts > 1) {
-        // the ring is idle: this block's only tile is over (the last accumulator was full)
-#pragma unroll
-        for (int j = 0; j < kCols; ++j)
-          asm volatile("st.shared.f32 [%0], %1;" ::"r"(tok_base + ((side * kCols + j) * 128 + channel) * 4), "f"(sum[j]) : "memory");
-        break;
-      }
-      if (n < p.a.N) {
+      if (ok && n < p.a.N) {
         const float bias = p.a.bias != nullptr ? p.a.bias[n] : 0.0f;
-        const int left = static_cast<int>(min(static_cast<int64_t>(kCols), p.a.M - m0 - side * kCols));
+        const int64_t m = m0 + side * (BN / 2);
+        const int left = static_cast<int>(min(static_cast<int64_t>(BN / 2), p.a.M - m));
 #pragma unroll
-        for (int j = 0; j < kCols; ++j)
-          if (j < left) put_w4(p.a, m0 + side * kCols + j, n, p.a.bias != nullptr ? sum[j] + bias : sum[j]);
+        for (int j = 0; j < BN / 2; ++j)
+          if (j < left) put_w4(p.a, m + j, n, p.a.bias != nullptr ? sum[j] + bias : sum[j]);
       }
     }
     if (p.k_parts > 1) {
-      // add the cluster's parts: every block writes a share of the tokens, a warp 32 channels of one at a time
+      // Add the cluster's parts: every block writes a share of the tokens, a warp 32 channels of one at a time.  The ring is idle:
+      // this block's only tile is over, but for the other side's last slot, which reads no tokens.
+      asm volatile("bar.sync 1, 256;" ::: "memory");
+      constexpr int kSides = kSplit ? 1 : 2;
+#pragma unroll
+      for (int j = 0; j < kCols; ++j)
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(tok_base + ((side * kCols + j) * 128 + channel) * 4), "f"(sum[j]) : "memory");
       int n_tile;
       int64_t m0;
       tile_origin(p, first_tile, BN, &n_tile, &m0);
@@ -357,20 +432,30 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
       cluster_sync();
       const int j1 = static_cast<int>(min(static_cast<int64_t>(BN * (rank + 1) / p.k_parts), p.a.M - m0));
       if (ok)
-        for (int j = BN * rank / p.k_parts + side; j < j1; j += 2) {
-          float v[8];
+        for (int j0 = BN * rank / p.k_parts + side; j0 < j1; j0 += 2 * kJoin) {
+          // (kJoin tokens' loads from a peer on their way together)
+          float y[kJoin] = {};
+          for (int b = 0; b < p.k_parts; ++b) {
+            float v[kSides][kJoin];
 #pragma unroll
-          for (int b = 0; b < 8; ++b) v[b] = b < p.k_parts ? load_of_peer_f32(tok_base + (j * 128 + channel) * 4, b) : 0.0f;
-          float y = v[0];
+            for (int i = 0; i < kJoin; ++i)
 #pragma unroll
-          for (int b = 1; b < 8; ++b) y += v[b];
-          if (n < p.a.N) put_w4(p.a, m0 + j, n, p.a.bias != nullptr ? y + bias : y);
+              for (int s = 0; s < kSides; ++s)
+                v[s][i] = j0 + 2 * i < j1 ? load_of_peer_f32(tok_base + ((s * BN + j0 + 2 * i) * 128 + channel) * 4, b) : 0.0f;
+#pragma unroll
+            for (int i = 0; i < kJoin; ++i)
+#pragma unroll
+              for (int s = 0; s < kSides; ++s) y[i] += v[s][i];
+          }
+#pragma unroll
+          for (int i = 0; i < kJoin; ++i)
+            if (n < p.a.N && j0 + 2 * i < j1) put_w4(p.a, m0 + j0 + 2 * i, n, p.a.bias != nullptr ? y[i] + bias : y[i]);
         }
       cluster_sync();
     }
   }
   // the blocks of a cluster leave together: their sums are read by the others
-  if (p.k_parts > 1 && warp < 12) {
+  if (p.k_parts > 1 && (warp < 20 || warp >= 28)) {
     cluster_sync();
     cluster_sync();
   }
@@ -379,18 +464,18 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
   if (warp == 1) {
     __syncwarp();
     tc_fence_after();
-    tmem_dealloc(tmem, 512);
+    tmem_dealloc(tmem_base, 512);
   }
 }
 
-template <typename T, int BN>
+template <typename T, int BN, int GS>
 cudaError_t launch(const W4Tc& p, const CUtensorMap& x, int sms, cudaStream_t stream) {
   static int attr_set[64] = {0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(pq_linear_w4_tc<T, BN>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes(BN));
+    e = cudaFuncSetAttribute(pq_linear_w4_tc<T, BN, GS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes(BN));
     if (e != cudaSuccess) return e;
     if (dev < 64) attr_set[dev] = 1;
   }
@@ -408,18 +493,27 @@ cudaError_t launch(const W4Tc& p, const CUtensorMap& x, int sms, cudaStream_t st
   // a cluster that shares K has one tile; otherwise as many blocks as there are SMs take the tiles in turn
   const int64_t at_once = p.k_parts > 1 ? tiles : std::min<int64_t>(tiles, sms);
   cfg.gridDim = dim3(static_cast<unsigned>(at_once * p.k_parts));
-  return cudaLaunchKernelEx(&cfg, pq_linear_w4_tc<T, BN>, p, x);
+  return cudaLaunchKernelEx(&cfg, pq_linear_w4_tc<T, BN, GS>, p, x);
+}
+
+template <typename T, int BN>
+cudaError_t launch_group(const W4Tc& p, const CUtensorMap& x, int sms, cudaStream_t s) {
+  const int gs = p.a.p.group_shift;
+  if constexpr (BN < 128)
+    if (gs == 5) return launch<T, BN, 5>(p, x, sms, s);
+  return gs == 6 ? launch<T, BN, 6>(p, x, sms, s) : launch<T, BN, 7>(p, x, sms, s);
 }
 
 template <typename T>
 cudaError_t launch_bn(const W4Tc& p, int bn, const CUtensorMap& x, int sms, cudaStream_t s) {
-  return bn == 32 ? launch<T, 32>(p, x, sms, s) : bn == 64 ? launch<T, 64>(p, x, sms, s) : launch<T, 128>(p, x, sms, s);
+  return bn == 32 ? launch_group<T, 32>(p, x, sms, s) : bn == 64 ? launch_group<T, 64>(p, x, sms, s) : launch_group<T, 128>(p, x, sms, s);
 }
 
 }  // namespace
 
+// From 17 tokens on (us, here against the kernel for few tokens: 16 x 8192 x 4096 14.2 / 10.7, 24 x 4096 x 4096 11.1 / 28.6).
 bool w4_tc_takes(const W4Args& a, int x_type) {
-  return x_type != PQ_F32 && a.M > 8 && a.M <= (1 << 30) && is_aligned(a.x, 16) && a.ldx % 8 == 0;
+  return x_type != PQ_F32 && a.M > 16 && a.M <= (1 << 30) && is_aligned(a.x, 16) && a.ldx % 8 == 0;
 }
 
 cudaError_t launch_w4_tc(const W4Args& a, int x_type, cudaStream_t stream) {
@@ -432,8 +526,9 @@ cudaError_t launch_w4_tc(const W4Args& a, int x_type, cudaStream_t stream) {
   p.err = device_error_word();
   p.wait_limit_ns = wait_limit_ns();
   if (p.err == nullptr) return cudaErrorInitializationError;
-  const int bn = a.M <= 32 ? 32 : a.M <= 64 ? 64 : 128;
-  p.n_tiles = (a.p.strips + kStrips - 1) / kStrips;
+  // (groups of 32 have two accumulators for each 64 of K: the tensor memory holds those of two jobs of 64 tokens, not of 128)
+  const int bn = a.M <= 32 ? 32 : a.M <= 64 || a.p.group_shift == 5 ? 64 : 128;
+  p.n_tiles = (a.p.strips + kTileStrips - 1) / kTileStrips;
   const int64_t m_tiles = (a.M + bn - 1) / bn;
   if (p.n_tiles * m_tiles > 0x7FFFFFFF) return cudaErrorInvalidValue;
   p.m_tiles = static_cast<int>(m_tiles);

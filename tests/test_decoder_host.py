@@ -227,7 +227,7 @@ def test_w4_arguments_refused():
             args[i] = bad
             _refused(call, *args)
     _refused(B.palquant_w4_unpack, 64, w, None, None)
-    _refused(B.palquant_linear_w4, 64, 64, None, 64, w, _linear(M=64 * 65535 + 1), 64, 1 << 60, status=B.PQ_EUNSUPPORTED)
+    _refused(B.palquant_linear_w4, 64, 64, None, 64, w, _linear(M=32 * 65535 + 1), 64, 1 << 60, status=B.PQ_EUNSUPPORTED)
     B.palquant_linear_w4(None, None, None, None, w, _linear(M=0), None, 0, stream=0)
 
 

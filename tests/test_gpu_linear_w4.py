@@ -100,6 +100,11 @@ SIZES = [  # M, N, K, group
     (1, 1, 1, 32), (1, 16, 128, 128), (2, 17, 31, 32), (3, 100, 129, 64), (5, 1001, 777, 32), (7, 48, 2048, 128), (8, 64, 4096, 64),
     (9, 33, 1000, 128), (16, 80, 512, 32), (17, 40, 640, 64), (31, 130, 1111, 128), (33, 65, 384, 32), (48, 256, 1024, 64), (64, 31, 900, 128),
     (65, 20, 260, 64), (200, 37, 300, 32), (1, 5000, 256, 64), (4, 12, 20000, 128), (1, 300, 8192, 32),
+    # many stages and slots in a block, of every tile width and group; many tiles a block; parts of K in clusters
+    (20, 130, 9000, 32), (20, 260, 9001, 64), (25, 140, 9100, 128), (40, 300, 9000, 32), (64, 129, 8960, 64), (57, 140, 9100, 128), (100, 300, 9000, 32),
+    (128, 150, 8900, 64), (120, 140, 9100, 128), (300, 2600, 640, 64), (30, 21000, 512, 32), (260, 1300, 1536, 128), (24, 1024, 4096, 128),
+    # pairs of strips, the last one alone; few tokens
+    (1, 9760, 520, 128), (8, 9744, 300, 32), (16, 2064, 700, 64), (12, 2049, 513, 128), (3, 12000, 260, 64),
 ]
 
 
