@@ -795,24 +795,33 @@ def palquant_kv8_attention(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, scratch_de
 
 
 # ---------------------------------------------------------------- a decoder's operators around the 8-bit cache
-def _here(*tensors):
-    """Tensors of a call lie on the current device, whose stream it takes (None and addresses are the caller's word)."""
-    import torch
-
-    for t in tensors:
-        if t is not None and type(t) is not int:
-            at = t.get_device()
-            if at < 0 or at != torch._C._cuda_getDevice():
-                raise ArgumentError(f"a tensor on {t.device}: not the current device")
+_get_device = None  # torch's function for the current device
 
 
-def _room(t, nbytes, name):
-    """Address of a buffer of at least `nbytes` contiguous bytes (None and addresses as they are)."""
+def _here(device):
+    """A call's tensors lie on the current device (its index), whose stream the call takes."""
+    global _get_device
+    if device is None:
+        return  # a descriptor that no builder made, or addresses: the caller's word
+    if _get_device is None:
+        import torch
+
+        _get_device = torch._C._cuda_getDevice
+    if device < 0 or device != _get_device():
+        raise ArgumentError(f"tensors on {'the CPU' if device < 0 else f'cuda:{device}'}: not the current device")
+
+
+def _index_of(t):
+    return None if t is None or type(t) is int else t.get_device()
+
+
+def _room(t, nbytes, name, device=None):
+    """Address of a buffer of at least `nbytes` contiguous bytes, on the device if one is named (None and addresses as they are)."""
     if t is None or type(t) is int:
         return t
-    if t.is_contiguous() and t.numel() * t.element_size() >= nbytes:
+    if t.is_contiguous() and t.numel() * t.element_size() >= nbytes and (device is None or t.get_device() == device):
         return t.data_ptr()
-    raise ArgumentError(f"{name}: {nbytes} contiguous bytes")
+    raise ArgumentError(f"{name}: {nbytes} contiguous bytes on the device of the other tensors")
 
 
 def _same_or_apart(src, dst, name):
@@ -874,26 +883,29 @@ def qk_norm_rope(q, k, q_out, k_out, positions=None, turns=None, q_weight=None, 
                _ptr(turns) if R else None, _ptr(q_weight), _ptr(k_weight))
     d._keep = keep + weights
     d._q, d._k, d._q_out, d._k_out = (None if x is None else _layout(x) for x in (q, k, q_out, k_out))
+    d._device = some.get_device()
     return d
 
 
 def palquant_qk_norm_rope(q_dev, k_dev, q_out_dev, k_out_dev, d: QKRope, stream=None):
     """Norms of query and key heads and the rotation by position, in one pass."""
-    _here(q_dev, k_dev)
-    for x, y, name in ((q_dev, q_out_dev, "q_out"), (k_dev, k_out_dev, "k_out")):
-        if getattr(x, "data_ptr", None) is not None and getattr(y, "data_ptr", None) is not None:
-            _same_or_apart(x, y, name)
-    _check(lib.palquant_qk_norm_rope(_described(q_dev, getattr(d, "_q", _BY_HAND), "q"), _described(k_dev, getattr(d, "_k", _BY_HAND), "k"),
-                                     _described(q_out_dev, getattr(d, "_q_out", _BY_HAND), "q_out"),
-                                     _described(k_out_dev, getattr(d, "_k_out", _BY_HAND), "k_out"), ctypes.byref(d),
-                                     _stream(stream)), "palquant_qk_norm_rope")
+    _here(getattr(d, "_device", None))
+    layouts = [getattr(d, name, _BY_HAND) for name in ("_q", "_k", "_q_out", "_k_out")]
+    q, k = _described(q_dev, layouts[0], "q"), _described(k_dev, layouts[1], "k")
+    q_out, k_out = _described(q_out_dev, layouts[2], "q_out"), _described(k_out_dev, layouts[3], "k_out")
+    # an output that starts where its input does is the input itself
+    _need((q is None or q != q_out or layouts[0] == layouts[2]) and (k is None or k != k_out or layouts[1] == layouts[3]),
+          "q_out, k_out: the input itself, or elsewhere")
+    _check(lib.palquant_qk_norm_rope(q, k, q_out, k_out, ctypes.byref(d), _stream(stream)), "palquant_qk_norm_rope")
 
 
 def w4_weights(N, K, group, scales) -> W4Weights:
     """Descriptor of packed 4-bit weights [N, K] with a scale (of torch type `scales`) for each channel and `group` of K."""
     types = {dtype: number for number, dtype in _dtypes()[0].items()}
     _need(scales in types, "scales: float32, float16 or bfloat16")
-    return W4Weights(N, K, group, types[scales])
+    w = W4Weights(N, K, group, types[scales])
+    w._bytes = lib.palquant_w4_packed_bytes(ctypes.byref(w))
+    return w
 
 
 def palquant_w4_packed_bytes(w: W4Weights) -> int:
@@ -905,7 +917,9 @@ def palquant_w4_pack(codes_dev, s_dev, w: W4Weights, packed_dev, packed_bytes, s
     import torch
 
     ldc = w.K
-    _here(codes_dev, s_dev, packed_dev)
+    at = _index_of(packed_dev)
+    _here(at)
+    _need(at is None or all(_index_of(t) in (None, at) for t in (codes_dev, s_dev)), "codes and scales: on the device of packed")
     if getattr(codes_dev, "data_ptr", None) is not None:
         _need(codes_dev.dtype == torch.int8 and codes_dev.shape == (w.N, w.K), "codes: int8 [N, K]")
         ldc = _rows(codes_dev, "codes")
@@ -916,7 +930,9 @@ def palquant_w4_pack(codes_dev, s_dev, w: W4Weights, packed_dev, packed_bytes, s
 
 def palquant_w4_quantize(w_dev, w_type, ldw, w: W4Weights, packed_dev, packed_bytes, stream=None):
     """Float weights [N, K] (rows `ldw` elements apart) quantised to 4 bits and packed."""
-    _here(w_dev, packed_dev)
+    at = _index_of(packed_dev)
+    _here(at)
+    _need(at is None or _index_of(w_dev) in (None, at), "w: on the device of packed")
     _check(lib.palquant_w4_quantize(_span(w_dev, _dtypes()[0].get(w_type), (w.N - 1) * ldw + w.K, "w"), w_type, ldw, ctypes.byref(w),
                                     _room(packed_dev, packed_bytes, "packed"), packed_bytes, _stream(stream)), "palquant_w4_quantize")
 
@@ -926,7 +942,9 @@ def palquant_w4_unpack(packed_dev, w: W4Weights, codes_dev, s_dev, stream=None):
     import torch
 
     ldc = w.K
-    _here(packed_dev, codes_dev, s_dev)
+    at = _index_of(packed_dev)
+    _here(at)
+    _need(at is None or all(_index_of(t) in (None, at) for t in (codes_dev, s_dev)), "codes and scales: on the device of packed")
     if getattr(codes_dev, "data_ptr", None) is not None:
         _need(codes_dev.dtype == torch.int8 and codes_dev.shape == (w.N, w.K), "codes: int8 [N, K]")
         ldc = _rows(codes_dev, "codes")
@@ -941,7 +959,7 @@ def linear_w4_desc(x, w: W4Weights, y) -> LinearDesc:
     _need(x.dim() == 2 and x.shape[1] == w.K and y.shape == (M, w.N), "x: [M, K], y: [M, N]")
     _need(x.device == y.device, "x and y: on one device")
     d = LinearDesc(M, w.N, w.K, _float_type(x), _float_type(y), _rows(x, "x"), w.K, _rows(y, "y"))
-    d._x, d._y = _layout(x), _layout(y)
+    d._x, d._y, d._device = _layout(x), _layout(y), x.get_device()
     return d
 
 
@@ -951,11 +969,20 @@ def palquant_linear_w4_scratch_bytes(w: W4Weights, d: LinearDesc) -> int:
 
 def palquant_linear_w4(x_dev, packed_dev, bias_dev, y_dev, w: W4Weights, d: LinearDesc, scratch_dev, scratch_bytes, stream=None):
     """Dense layer with 4-bit weights and group scales: x to y."""
-    _here(x_dev, packed_dev)
-    _check(lib.palquant_linear_w4(_described(x_dev, getattr(d, "_x", _BY_HAND), "x"), _room(packed_dev, lib.palquant_w4_packed_bytes(ctypes.byref(w)), "packed"),
-                                  _vector(bias_dev, _dtypes()[0][PQ_F32], d.N, "bias"), _described(y_dev, getattr(d, "_y", _BY_HAND), "y"),
-                                  ctypes.byref(w), ctypes.byref(d), _room(scratch_dev, scratch_bytes, "scratch"), scratch_bytes, _stream(stream)),
-           "palquant_linear_w4")
+    at = getattr(d, "_device", None)
+    _here(at)
+    nbytes = getattr(w, "_bytes", None)
+    if nbytes is None:
+        nbytes = lib.palquant_w4_packed_bytes(ctypes.byref(w))
+    packed = _room(packed_dev, nbytes, "packed", at)
+    _check(lib.palquant_linear_w4(_described(x_dev, getattr(d, "_x", _BY_HAND), "x"), packed, _vector(bias_dev, _dtypes()[0][PQ_F32], d.N, "bias"),
+                                  _described(y_dev, getattr(d, "_y", _BY_HAND), "y"), ctypes.byref(w), ctypes.byref(d),
+                                  _room(scratch_dev, scratch_bytes, "scratch"), scratch_bytes, _stream(stream)), "palquant_linear_w4")
+
+
+def _queries_device(a):
+    q = getattr(a, "_q", None)
+    return None if q is None else q[3]
 
 
 def palquant_kv8_attention_sinks_scratch_bytes(cache: KV8Cache, a: KV8Attn, sinks) -> int:
@@ -964,7 +991,7 @@ def palquant_kv8_attention_sinks_scratch_bytes(cache: KV8Cache, a: KV8Attn, sink
 
 def palquant_kv8_attention_sinks(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, sinks, scratch_dev, scratch_bytes, stream=None):
     """Attention over the cache through a window, with the first `sinks` tokens of every sequence in sight."""
-    _here(q_dev)
+    _here(_queries_device(a))
     _fits_cache(cache, a, "_queries")
     _check(lib.palquant_kv8_attention_sinks(ctypes.byref(cache), _described(q_dev, getattr(a, "_q", _BY_HAND), "q"),
                                             _described(o_dev, getattr(a, "_o", _BY_HAND), "o"), ctypes.byref(a), sinks,
@@ -992,7 +1019,7 @@ def palquant_kv8_attention_tree_scratch_bytes(cache: KV8Cache, a: KV8Attn, tree:
 
 def palquant_kv8_attention_tree(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, tree: KV8Tree, scratch_dev, scratch_bytes, stream=None):
     """Attention for drafted tokens, the sequences' last cached ones: each sees the text before them and the drafts of its bits."""
-    _here(q_dev)
+    _here(_queries_device(a))
     _fits_cache(cache, a, "_queries")
     _need(getattr(tree, "_for", None) == getattr(a, "_q", None) or not hasattr(tree, "_for"), "tree: of other queries")
     _check(lib.palquant_kv8_attention_tree(ctypes.byref(cache), _described(q_dev, getattr(a, "_q", _BY_HAND), "q"),

@@ -201,14 +201,33 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
                    static_cast<int64_t>(w.h * p.group + (there ? r % p.group : 0)) * p.a.q_head_stride;
     Vec8<T> v[kC][2];
     uint32_t top = 0;
+    // (the loads on their way at one time, not each behind a branch; rows past the end read the sequence's first and count as zeros)
+    if (p.wide_q) {
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int d = 64 * c + 16 * t + 8 * i;
+          v[c][i] = load8(src + (d < D ? d : 0), 8, true);
+        }
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (!there || 64 * c + 16 * t + 8 * i >= D) v[c][i] = Vec8<T>{};
+    } else {
+#pragma unroll
+      for (int c = 0; c < kC; ++c)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int d = 64 * c + 16 * t + 8 * i;
+          v[c][i] = load8(src + d, there && d < D ? 8 : 0, false);
+        }
+    }
 #pragma unroll
     for (int c = 0; c < kC; ++c)
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const int d = 64 * c + 16 * t + 8 * i;
-        v[c][i] = load8(src + d, there && d < D ? 8 : 0, there && d < D && p.wide_q);
-        top = max(top, amax8(v[c][i]));
-      }
+      for (int i = 0; i < 2; ++i) top = max(top, amax8(v[c][i]));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     // 2^e <= largest magnitude < 2^(e+1); the row is scaled by 2^(7 - e)

@@ -18,7 +18,8 @@
 // of 2048 over 4096, 32 / 8 heads of 128: 278 us (0.79 PFLOP/s); one of 8192, causal: 569 us (0.97 PFLOP/s).
 //
 // Roles (16 warps): 0 issues the MMAs, 4 looks up pages, the other six below 8 convert
-// (none of them on the issuing warp's scheduler), 8-11 and 12-15 are the tiles' softmax.  Tiles with the most tokens come first.
+// (none of them on the issuing warp's scheduler), 8-11 and 12-15 are the tiles' softmax.  With one tile of rows the softmax waits for
+// the codes: then eight warps convert, four more warps in all (TcRoles).  Tiles with the most tokens come first.
 #pragma once
 
 #include <cuda_runtime.h>
@@ -33,11 +34,13 @@ namespace {
 
 constexpr int kTokens = kAttnTcTokens;  // of one step
 constexpr int kHalf = 64;               // of one round of the softmax
-constexpr int kThreads = 512;
 constexpr int kSub = 128 * 128;         // 128 rows of 64 halves
 constexpr int kPageRing = 8;            // steps whose pages are looked up ahead
 
-__host__ __device__ constexpr int attn_smem(int DP) { return 6 * (DP / 64) * kSub + 1024 /* alignment */; }
+// Queries of two tiles (wide: of one), two stages of keys and values as halves, wide: two steps' codes.
+__host__ __device__ constexpr int attn_smem(int DP, bool wide) {
+  return (wide ? 5 : 6) * (DP / 64) * kSub + (wide ? 2 * 2 * kTokens * DP : 0) + 1024 /* alignment */;
+}
 
 struct AttnBars {
   uint32_t base;
@@ -47,14 +50,14 @@ struct AttnBars {
   __device__ uint32_t k_empty(int s) const { return base + 32u + 8u * s; }
   __device__ uint32_t v_full(int s) const { return base + 48u + 8u * s; }
   __device__ uint32_t v_empty(int s) const { return base + 64u + 8u * s; }
-  // both tiles' scores and probabilities in buffer b; their outputs
+  // scores and probabilities in buffer b (of both tiles, 2; of the two streams, 4), outputs (of both tiles; of stream t)
   __device__ uint32_t s_full(int b) const { return base + 80u + 8u * b; }
-  __device__ uint32_t p_full(int b) const { return base + 96u + 8u * b; }
-  __device__ uint32_t o_full() const { return base + 112u; }
-  __device__ uint32_t page_full(int i) const { return base + 120u + 8u * i; }
-  __device__ uint32_t page_empty(int i) const { return base + 120u + 8u * kPageRing + 8u * i; }
+  __device__ uint32_t p_full(int b) const { return base + 112u + 8u * b; }
+  __device__ uint32_t o_full(int t) const { return base + 144u + 8u * t; }
+  __device__ uint32_t page_full(int i) const { return base + 160u + 8u * i; }
+  __device__ uint32_t page_empty(int i) const { return base + 160u + 8u * kPageRing + 8u * i; }
 };
-constexpr int kBars = 15 + 2 * kPageRing;
+constexpr int kBars = 20 + 2 * kPageRing;
 
 // A page of a step: scale of the keys, log2 and inverse of the values' scale, and where
 // the head's codes begin (absent pages: -1).
@@ -133,9 +136,26 @@ __device__ __forceinline__ TcPlace tc_place(const AttnArgs& p) {
   return r;
 }
 
+// How the warps share the work.  Two tiles of rows: six converting warps beside the issuing one and the pages', off the issuing
+// warp's scheduler, and four of softmax for each tile.  Wide, for one tile: eight converting warps, and the two groups of softmax are
+// streams of the same rows, one through the first half of every step and one through the second, with maxima, sums and outputs of
+// their own, joined at the end (one group had 1100 to 1900 cycles' work with each half, and everything else waited for it).
+template <bool WIDE>
+struct TcRoles {
+  static constexpr int kThreads = WIDE ? 640 : 512;
+  static constexpr int kConverters = WIDE ? 8 : 6;
+  static constexpr int kPageWarp = WIDE ? 1 : 4, kFirstConverter = WIDE ? 4 : 1, kFirstSoftmax = WIDE ? 12 : 8;
+  // this warp's number among the converting ones, or -1
+  static __device__ __forceinline__ int converter(int warp) {
+    if (WIDE) return warp >= 4 && warp < 12 ? warp - 4 : -1;
+    return warp < 8 && (warp & 3) != 0 ? (warp < 4 ? warp - 1 : warp - 2) : -1;
+  }
+};
+
 // VIEW: see AttnView.
-template <typename T, int DP, int VIEW>
-__global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constant__ AttnArgs p) {
+template <typename T, int DP, int VIEW, bool WIDE>
+__global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const __grid_constant__ AttnArgs p) {
+  using Roles = TcRoles<WIDE>;
   constexpr int kSubs = DP / 64;
   constexpr uint32_t kO = 256;  // tensor memory: scores of both tiles, then their outputs
   extern __shared__ uint8_t raw[];
@@ -161,21 +181,23 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
   const int tiles = rows - r0 > 128 ? 2 : 1;
   const int D = p.c.D;
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
-  const uint32_t q_base = smem, k_base = q_base + 2 * kSubs * kSub, v_base = k_base + 2 * kSubs * kSub;
+  const uint32_t q_base = smem, k_base = q_base + (WIDE ? 1 : 2) * kSubs * kSub, v_base = k_base + 2 * kSubs * kSub;
   const AttnBars bars{smem_u32(bar_words)};
 
   if (threadIdx.x == 0) {
-    mbar_init(bars.q_full(), 4 * tiles);
+    mbar_init(bars.q_full(), 4 * (WIDE ? 2 : tiles));
     mbar_init(bars.done(), 1);
     for (int s = 0; s < 2; ++s) {
-      mbar_init(bars.k_full(s), 6);
+      mbar_init(bars.k_full(s), Roles::kConverters);
       mbar_init(bars.k_empty(s), 1);
-      mbar_init(bars.v_full(s), 6);
+      mbar_init(bars.v_full(s), Roles::kConverters);
       mbar_init(bars.v_empty(s), 1);
-      mbar_init(bars.s_full(s), 1);
-      mbar_init(bars.p_full(s), 4 * tiles);
     }
-    mbar_init(bars.o_full(), 1);
+    for (int b = 0; b < 4; ++b) {
+      mbar_init(bars.s_full(b), 1);
+      mbar_init(bars.p_full(b), 4 * (WIDE ? 1 : tiles));
+    }
+    for (int b = 0; b < 2; ++b) mbar_init(bars.o_full(b), 1);
     for (int i = 0; i < kPageRing; ++i) {
       mbar_init(bars.page_full(i), 1);
       mbar_init(bars.page_empty(i), 1);
@@ -192,172 +214,289 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
   constexpr uint32_t tmem = 0;
   WaitCtx ctx{&abort_flag, p.err, p.wait_limit_ns, PQ_ERR_MMA};
 
-  if (warp < 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
-    if (warp == 0) {
-      // ---- MMAs
-      auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)) != 0; };
-      const uint32_t idesc_s = (1u << 4) | (8u << 17) | (8u << 24);                                        // N = 64 tokens
-      const uint32_t idesc_o = (1u << 4) | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (8u << 24);  // N = D
-      // Half i is half i % 2 of step i / 2, whose operands are in stage (i / 2) % 2.  Both
-      // tiles share barriers: a wait or a commit costs this warp about as much as two MMAs.
-      auto scores = [&](int i) {
+  auto issue = [&]() {
+    // ---- MMAs
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)) != 0; };
+    const uint32_t idesc_s = (1u << 4) | (8u << 17) | (8u << 24);                                        // N = 64 tokens
+    const uint32_t idesc_o = (1u << 4) | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (8u << 24);  // N = D
+    // Half i is half i % 2 of step i / 2, whose operands are in stage (i / 2) % 2.  Both
+    // tiles share barriers: a wait or a commit costs this warp about as much as two MMAs.
+    auto scores = [&](int i) {
+      const uint32_t k = k_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128);
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (t < tiles) {
+#pragma unroll
+          for (int c = 0; c < kSubs; ++c)
+            mma_ss_x4(tmem + 128 * t + kHalf * (i & 1), desc_k(q_base + (t * kSubs + c) * kSub), desc_k(k + c * kSub),
+                      idesc_s, c > 0);
+        }
+      tc_commit_warp(bars.s_full(i & 1));
+    };
+    auto outputs = [&](int i) {
+      const uint32_t v = desc_n(v_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128));
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+        if (t < tiles) {
+          mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1), v, idesc_o, i > 0);
+          if (kSecondHalf<T, VIEW>) mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1) + kHalf / 2, v, idesc_o, 1);
+        }
+      tc_commit_warp(bars.o_full(0));
+    };
+    bool ok = halves > 0 && wait(bars.q_full(), 0) && wait(bars.k_full(0), 0);
+    if constexpr (WIDE) {
+      // Stream i % 2 takes half i; its scores are in its buffer (i / 2) % 2, two halves ahead of its probabilities.
+      auto stream_scores = [&](int i) {
         const uint32_t k = k_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-          if (t < tiles) {
-#pragma unroll
-            for (int c = 0; c < kSubs; ++c)
-              mma_ss_x4(tmem + 128 * t + kHalf * (i & 1), desc_k(q_base + (t * kSubs + c) * kSub), desc_k(k + c * kSub),
-                        idesc_s, c > 0);
-          }
-        tc_commit_warp(bars.s_full(i & 1));
+        for (int c = 0; c < kSubs; ++c)
+          mma_ss_x4(tmem + 128 * (i & 1) + kHalf * ((i >> 1) & 1), desc_k(q_base + c * kSub), desc_k(k + c * kSub), idesc_s, c > 0);
+        tc_commit_warp(bars.s_full(2 * (i & 1) + ((i >> 1) & 1)));
+        if ((i & 1) || i + 1 == halves) tc_commit_warp(bars.k_empty((i >> 1) & 1));
       };
-      auto outputs = [&](int i) {
-        const uint32_t v = desc_n(v_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128));
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-          if (t < tiles) {
-            mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1), v, idesc_o, i > 0);
-            if (kSecondHalf<T, VIEW>) mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1) + kHalf / 2, v, idesc_o, 1);
-          }
-        tc_commit_warp(bars.o_full());
-      };
-      bool ok = halves > 0 && wait(bars.q_full(), 0) && wait(bars.k_full(0), 0);
       if (ok) {
         tc_fence_after();
-        scores(0);
+        stream_scores(0);
+        if (halves > 1) stream_scores(1);
       }
       for (int i = 0; ok && i < halves; ++i) {
-        const int j = i >> 1, n = i + 1;
+        const int j = i >> 1, n = i + 2;
         if (n < halves) {
           if (!(n & 1)) ok = wait(bars.k_full((n >> 1) & 1), (n >> 2) & 1);
           if (!ok) break;
           tc_fence_after();
-          scores(n);
+          stream_scores(n);
         }
-        if (!(i & 1)) {  // both halves of the step's keys have been issued
-          tc_commit_warp(bars.k_empty(j & 1));
-          ok = wait(bars.v_full(j & 1), (j >> 1) & 1);
-        }
-        ok = ok && wait(bars.p_full(i & 1), j & 1);
+        if (!(i & 1)) ok = wait(bars.v_full(j & 1), (j >> 1) & 1);
+        ok = ok && wait(bars.p_full(2 * (i & 1) + (j & 1)), (j >> 1) & 1);
         if (!ok) break;
         tc_fence_after();
-        outputs(i);
-        if ((i & 1) || n == halves) tc_commit_warp(bars.v_empty(j & 1));
-      }
-      // every MMA issued is over: the outputs are whole, the tensor memory may be given back
-      tc_commit_warp(bars.done());
-      if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
-      __syncwarp();
-    } else if (warp == 4) {
-      // ---- the steps' pages, a lane each, up to kPageRing steps ahead of the codes (two
-      // dependent loads that would otherwise stand in every step's way)
-      ctx.err_bits = PQ_ERR_PRODUCER;
-      const int* table = p.a.page_table_dev + static_cast<int64_t>(w.b) * p.a.table_pitch;
-      for (int j = 0; j < steps; ++j) {
-        const int i = j % kPageRing;
-        if (j >= kPageRing &&
-            !__all_sync(0xffffffffu, mbar_wait(bars.page_empty(i), (j / kPageRing - 1) & 1, ctx)))
-          break;
-        if (lane < kTokens >> p.page_shift) {
-          const int start = token(from + j * kTokens) + (lane << p.page_shift), slot = start >> p.page_shift;
-          StepPage page = {0.0f, kNone, 0.0f, -1};
-          if (start < sp.hi && (start + p.c.page_tokens > sp.lo || (VIEW == kSinks && start < p.sinks))) {  // within the rows' span
-            const int id = slot < p.a.table_pitch ? table[slot] : -1;
-            if (id >= 0 && id < p.c.num_pages) {
-              const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
-              const float sk = p.c.k_scale_dev[ph], sv0 = p.c.v_scale_dev[ph], sv = sv0 == 0.0f ? kZeroPageScale : sv0;
-              page = {sk, log2f(sv), 1.0f / sv, (ph << p.page_shift) * D};
-            } else {
-              atomicOr(p.err, PQ_ERR_PAGE);
-            }
-          }
-          pages[i][lane] = page;
-        }
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bars.page_full(i));
+        const uint32_t v = desc_n(v_base + (j & 1) * kSubs * kSub + (i & 1) * (kHalf * 128));
+        const uint32_t weights = tmem + 128 * (i & 1) + kHalf * (j & 1), o = tmem + kO + (i & 1) * DP;
+        mma_ts_x4(o, weights, v, idesc_o, i > 1);
+        if (kSecondHalf<T, VIEW>) mma_ts_x4(o, weights + kHalf / 2, v, idesc_o, 1);
+        tc_commit_warp(bars.o_full(i & 1));
+        if ((i & 1) || i + 1 == halves) tc_commit_warp(bars.v_empty(j & 1));
       }
     } else {
-      // ---- codes to halves, six warps
-      ctx.err_bits = PQ_ERR_PRODUCER;
-      const int tid = 32 * (warp < 4 ? warp - 1 : warp - 2) + lane;
-      const int C = D / 16;  // 16-byte pieces of a token
-      // A thread takes one 16-byte piece of every (192 / kP)th token.  Eight neighbours
-      // hold four pieces of two tokens, whose halves lie in different banks.
-      constexpr int kP = DP / 16, kTokStep = 192 / kP, kTurns = (kTokens + kTokStep - 1) / kTokStep;
-      const int piece = kP == 8 ? (tid & 3) | ((tid >> 1) & 4) : tid & 3;
-      const int token = kP == 8 ? ((tid >> 3) & ~1) | ((tid >> 2) & 1) : tid >> 2;
-      const bool there = piece < C;
-      const uint32_t row = (piece >> 2) * kSub + token * 128;
-      const uint32_t at0 = row + (((2 * (piece & 3)) ^ (token & 7)) << 4), at1 = row + (((2 * (piece & 3) + 1) ^ (token & 7)) << 4);
-      auto fetch = [&](const int8_t* codes, int j, uint4 (&r)[kTurns]) {
+    if (ok) {
+      tc_fence_after();
+      scores(0);
+    }
+    for (int i = 0; ok && i < halves; ++i) {
+      const int j = i >> 1, n = i + 1;
+      if (n < halves) {
+        if (!(n & 1)) ok = wait(bars.k_full((n >> 1) & 1), (n >> 2) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        scores(n);
+      }
+      if (!(i & 1)) {  // both halves of the step's keys have been issued
+        tc_commit_warp(bars.k_empty(j & 1));
+        ok = wait(bars.v_full(j & 1), (j >> 1) & 1);
+      }
+      ok = ok && wait(bars.p_full(i & 1), j & 1);
+      if (!ok) break;
+      tc_fence_after();
+      outputs(i);
+      if ((i & 1) || n == halves) tc_commit_warp(bars.v_empty(j & 1));
+    }
+    }
+    // every MMA issued is over: the outputs are whole, the tensor memory may be given back
+    tc_commit_warp(bars.done());
+    if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
+    __syncwarp();
+  };
+  auto look_up = [&]() {
+    // ---- the steps' pages, a lane each, up to kPageRing steps ahead of the codes (two
+    // dependent loads that would otherwise stand in every step's way)
+    ctx.err_bits = PQ_ERR_PRODUCER;
+    const int* table = p.a.page_table_dev + static_cast<int64_t>(w.b) * p.a.table_pitch;
+    for (int j = 0; j < steps; ++j) {
+      const int i = j % kPageRing;
+      if (j >= kPageRing &&
+          !__all_sync(0xffffffffu, mbar_wait(bars.page_empty(i), (j / kPageRing - 1) & 1, ctx)))
+        break;
+      if (lane < kTokens >> p.page_shift) {
+        const int start = token(from + j * kTokens) + (lane << p.page_shift), slot = start >> p.page_shift;
+        StepPage page = {0.0f, kNone, 0.0f, -1};
+        if (start < sp.hi && (start + p.c.page_tokens > sp.lo || (VIEW == kSinks && start < p.sinks))) {  // within the rows' span
+          const int id = slot < p.a.table_pitch ? table[slot] : -1;
+          if (id >= 0 && id < p.c.num_pages) {
+            const int64_t ph = static_cast<int64_t>(id) * p.c.Hkv + w.h;
+            const float sk = p.c.k_scale_dev[ph], sv0 = p.c.v_scale_dev[ph], sv = sv0 == 0.0f ? kZeroPageScale : sv0;
+            page = {sk, log2f(sv), 1.0f / sv, (ph << p.page_shift) * D};
+          } else {
+            atomicOr(p.err, PQ_ERR_PAGE);
+          }
+        }
+        pages[i][lane] = page;
+      }
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bars.page_full(i));
+    }
+  };
+  auto convert = [&]() {
+    // ---- codes to halves
+    ctx.err_bits = PQ_ERR_PRODUCER;
+    const int tid = 32 * Roles::converter(warp) + lane;
+    const int C = D / 16;  // 16-byte pieces of a token
+    // A thread takes one 16-byte piece of every kTokStep-th token.  Eight neighbours
+    // hold four pieces of two tokens, whose halves lie in different banks.
+    constexpr int kP = DP / 16, kTokStep = 32 * Roles::kConverters / kP, kTurns = (kTokens + kTokStep - 1) / kTokStep;
+    const int piece = kP == 8 ? (tid & 3) | ((tid >> 1) & 4) : tid & 3;
+    const int token = kP == 8 ? ((tid >> 3) & ~1) | ((tid >> 2) & 1) : tid >> 2;
+    const bool there = piece < C;
+    const uint32_t row = (piece >> 2) * kSub + token * 128;
+    const uint32_t at0 = row + (((2 * (piece & 3)) ^ (token & 7)) << 4), at1 = row + (((2 * (piece & 3) + 1) ^ (token & 7)) << 4);
+    // every step's pieces lie at the same places of its pages
+    int slot[kTurns], in_page[kTurns];
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+      const int k = token + i * kTokStep;
+      slot[i] = min(k, kTokens - 1) >> p.page_shift;
+      in_page[i] = there && k < kTokens ? (k & (p.c.page_tokens - 1)) * D + 16 * piece : -1;
+    }
+    // wide: a step's codes are on their way through shared memory two steps ahead (each thread copies what it will convert; one step ahead
+    // in registers, half of a step's time went by waiting for them); else through registers
+    const uint32_t staged = v_base + 2 * kSubs * kSub + tid * 16;
+    auto copy = [&](const int8_t* codes, int j, int side) {
+      if (j < steps) {
         const StepPage* page = pages[j % kPageRing];
 #pragma unroll
         for (int i = 0; i < kTurns; ++i) {
-          const int k = token + i * kTokStep;
-          r[i] = make_uint4(0, 0, 0, 0);
-          if (!there || k >= kTokens) continue;
-          const int64_t base = page[k >> p.page_shift].codes;
-          if (base >= 0)
-            r[i] = *reinterpret_cast<const uint4*>(codes + base + (k & (p.c.page_tokens - 1)) * D + 16 * piece);
+          const int64_t base = page[slot[i]].codes;
+          const bool have = base >= 0 && in_page[i] >= 0;
+          cp_async_16(staged + ((j & 1) * 2 + side) * (kTokens * DP) + i * (32 * Roles::kConverters * 16), have ? codes + base + in_page[i] : codes,
+                      have ? 16 : 0);
         }
-      };
-      // (columns past D are zeros: the scores' products run over whole blocks of 64)
-      auto store = [&](uint32_t base, const uint4 (&r)[kTurns]) {
+      }
+      cp_async_commit();
+    };
+    auto arrived = [&](int j, int side, uint4 (&r)[kTurns]) {
+      cp_async_wait<3>();
 #pragma unroll
-        for (int i = 0; i < kTurns; ++i) {
-          if (token + i * kTokStep >= kTokens) break;
-          uint32_t h[8];
-          half_of_codes(r[i].x, h[0], h[1]);
-          half_of_codes(r[i].y, h[2], h[3]);
-          half_of_codes(r[i].z, h[4], h[5]);
-          half_of_codes(r[i].w, h[6], h[7]);
-          sts128(base + at0 + i * kTokStep * 128, h[0], h[1], h[2], h[3]);
-          sts128(base + at1 + i * kTokStep * 128, h[4], h[5], h[6], h[7]);
-        }
-      };
-      auto publish = [&](uint32_t bar) {
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(bar);
-      };
-      auto look = [&](int j) {
-        return __all_sync(0xffffffffu, mbar_wait(bars.page_full(j % kPageRing), (j / kPageRing) & 1, ctx)) != 0;
-      };
-      uint4 kr[kTurns], vr[kTurns];
+      for (int i = 0; i < kTurns; ++i)
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                     : "=r"(r[i].x), "=r"(r[i].y), "=r"(r[i].z), "=r"(r[i].w)
+                     : "r"(staged + ((j & 1) * 2 + side) * (kTokens * DP) + i * (32 * Roles::kConverters * 16))
+                     : "memory");
+    };
+    auto fetch = [&](const int8_t* codes, int j, uint4 (&r)[kTurns]) {
+      const StepPage* page = pages[j % kPageRing];
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int64_t base = page[slot[i]].codes;
+        r[i] = make_uint4(0, 0, 0, 0);
+        if (base >= 0 && in_page[i] >= 0) r[i] = *reinterpret_cast<const uint4*>(codes + base + in_page[i]);
+      }
+    };
+    // (columns past D are zeros: the scores' products run over whole blocks of 64)
+    auto store = [&](uint32_t base, const uint4 (&r)[kTurns]) {
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        if (token + i * kTokStep >= kTokens) break;
+        uint32_t h[8];
+        half_of_codes(r[i].x, h[0], h[1]);
+        half_of_codes(r[i].y, h[2], h[3]);
+        half_of_codes(r[i].z, h[4], h[5]);
+        half_of_codes(r[i].w, h[6], h[7]);
+        sts128(base + at0 + i * kTokStep * 128, h[0], h[1], h[2], h[3]);
+        sts128(base + at1 + i * kTokStep * 128, h[4], h[5], h[6], h[7]);
+      }
+    };
+    auto publish = [&](uint32_t bar) {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    };
+    auto look = [&](int j) {
+      return __all_sync(0xffffffffu, mbar_wait(bars.page_full(j % kPageRing), (j / kPageRing) & 1, ctx)) != 0;
+    };
+    if constexpr (WIDE) {
       bool ok = steps > 0 && look(0);
-      if (ok) {
-        fetch(p.c.k_dev, 0, kr);
-        fetch(p.c.v_dev, 0, vr);
+      for (int j = 0; ok && j < 2; ++j) {
+        if (j < steps) ok = look(j);
+        copy(p.c.k_dev, j, 0);
+        copy(p.c.v_dev, j, 1);
       }
       for (int j = 0; ok && j < steps; ++j) {
         const int s = j & 1;
+        uint4 r[kTurns];
         if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.k_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
         if (!ok) break;
-        store(k_base + s * kSubs * kSub, kr);
+        arrived(j, 0, r);
+        store(k_base + s * kSubs * kSub, r);
         publish(bars.k_full(s));
-        if (j + 1 < steps) {
-          ok = look(j + 1);
-          if (!ok) break;
-          fetch(p.c.k_dev, j + 1, kr);
-        }
+        if (j + 2 < steps) ok = look(j + 2);
+        if (!ok) break;
+        copy(p.c.k_dev, j + 2, 0);
         if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.v_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
         if (!ok) break;
         // step j - 2 is over: so is every use of its pages
-        if (j > 1 && warp == 1 && lane == 0) mbar_arrive(bars.page_empty((j - 2) % kPageRing));
-        store(v_base + s * kSubs * kSub, vr);
+        if (j > 1 && tid == 0) mbar_arrive(bars.page_empty((j - 2) % kPageRing));
+        arrived(j, 1, r);
+        store(v_base + s * kSubs * kSub, r);
         publish(bars.v_full(s));
-        if (j + 1 < steps) fetch(p.c.v_dev, j + 1, vr);
+        copy(p.c.v_dev, j + 2, 1);
       }
+      cp_async_wait<0>();
+      return;
     }
+    uint4 kr[kTurns], vr[kTurns];
+    bool ok = steps > 0 && look(0);
+    if (ok) {
+      fetch(p.c.k_dev, 0, kr);
+      fetch(p.c.v_dev, 0, vr);
+    }
+    for (int j = 0; ok && j < steps; ++j) {
+      const int s = j & 1;
+      if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.k_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
+      if (!ok) break;
+      store(k_base + s * kSubs * kSub, kr);
+      publish(bars.k_full(s));
+      if (j + 1 < steps) {
+        ok = look(j + 1);
+        if (!ok) break;
+        fetch(p.c.k_dev, j + 1, kr);
+      }
+      if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.v_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
+      if (!ok) break;
+      // step j - 2 is over: so is every use of its pages
+      if (j > 1 && tid == 0) mbar_arrive(bars.page_empty((j - 2) % kPageRing));
+      store(v_base + s * kSubs * kSub, vr);
+      publish(bars.v_full(s));
+      if (j + 1 < steps) fetch(p.c.v_dev, j + 1, vr);
+    }
+  };
+
+  if (!WIDE && warp < 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
+    if (warp == 0)
+      issue();
+    else if (warp == Roles::kPageWarp)
+      look_up();
+    else
+      convert();
+  } else if (WIDE && warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    if (warp == 0)
+      issue();
+    else if (warp == Roles::kPageWarp)
+      look_up();
+  } else if (WIDE && warp < 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    convert();
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+    if (WIDE)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
+    else
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
     // ---- softmax: this thread's row
     ctx.err_bits = PQ_ERR_EPILOGUE;
-    const int t = (warp - 8) >> 2;
-    if (t < tiles) {
-      const int in = 32 * (warp & 3) + lane, r = r0 + 128 * t + in;
+    const int t = (warp - Roles::kFirstSoftmax) >> 2;
+    if (WIDE || t < tiles) {
+      const int in = 32 * (warp & 3) + lane, r = r0 + (WIDE ? 0 : 128 * t) + in;
       const bool mine = r < rows;
       const int qi = mine ? r / p.group : 0, hq = w.h * p.group + (mine ? r % p.group : 0);
       const int64_t tok = static_cast<int64_t>(p.a.cu_q_dev[w.b]) + qi;
@@ -369,40 +508,51 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         const T* src = static_cast<const T*>(p.q) + tok * p.a.q_token_stride + static_cast<int64_t>(hq) * p.a.q_head_stride;
         Vec8<T> v[DP / 8];
         uint32_t top = 0;
+        // (all of a row's loads on their way at one time: with a branch around each they took 9000 cycles, one after the other.  Rows past
+        // the end read the sequence's first and count as zeros.)
+        if (p.wide_q) {
 #pragma unroll
-        for (int i = 0; i < DP / 8; ++i) {
-          const bool there = mine && 8 * i < D;
-          v[i] = load8(src + 8 * i, there ? 8 : 0, there && p.wide_q);
-          top = max(top, amax8(v[i]));
+          for (int i = 0; i < DP / 8; ++i) v[i] = load8(src + (8 * i < D ? 8 * i : 0), 8, true);
+#pragma unroll
+          for (int i = 0; i < DP / 8; ++i)
+            if (!mine || 8 * i >= D) v[i] = Vec8<T>{};
+        } else {
+#pragma unroll
+          for (int i = 0; i < DP / 8; ++i) v[i] = load8(src + 8 * i, mine && 8 * i < D ? 8 : 0, false);
         }
+#pragma unroll
+        for (int i = 0; i < DP / 8; ++i) top = max(top, amax8(v[i]));
         const int e = top >= 0x7F800000u ? 0 : max(static_cast<int>(top >> 23) - 127, -100);
         // (negated where the call's scale is negative: the scores' factor is not)
         const float f = __int_as_float((127 + 7 - e) << 23) * (p.a.scale < 0.0f ? -1.0f : 1.0f);
         factor = fabsf(p.a.scale) * kLog2e * __int_as_float((127 - 7 + e) << 23);
 #pragma unroll
         for (int i = 0; i < DP / 8; ++i) {
+          if (WIDE && i / (DP / 16) != t) continue;  // (each stream's threads write half of the row)
           uint32_t h[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) h[k] = pack_half2(to_f32(v[i].v[2 * k]) * f, to_f32(v[i].v[2 * k + 1]) * f);
-          sts128(q_base + (t * kSubs + i / 8) * kSub + in * 128 + (((i & 7) ^ (in & 7)) << 4), h[0], h[1], h[2], h[3]);
+          sts128(q_base + ((WIDE ? 0 : t * kSubs) + i / 8) * kSub + in * 128 + (((i & 7) ^ (in & 7)) << 4), h[0], h[1], h[2], h[3]);
         }
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bars.q_full());
       }
       const int at = sp.len - sp.n + qi + 1;
-      const int hi = !mine ? 0 : p.a.causal ? min(at, sp.len) : sp.len;
-      const int lo = p.a.window > 0 ? max(0, at - p.a.window) : 0;
+      // (rows past the end see everything, so that their warp's others need no masks; nothing of theirs is written)
+      const int hi = !mine ? (VIEW == kPlain ? 0 : 0x7FFFFFFF) : p.a.causal ? min(at, sp.len) : sp.len;
+      const int lo = p.a.window > 0 && (mine || VIEW == kPlain) ? max(0, at - p.a.window) : 0;
       // the draft's row of bits (one that is there for rows past the end), and the first draft's position
       const uint32_t* drafts = VIEW == kTree ? p.tree + (mine ? tok : p.a.cu_q_dev[w.b]) * p.tree_pitch : nullptr;
       const int text = sp.len - sp.n;
       float m = kNone, l = 0.0f;
       bool ok = true;
-      for (int i = 0; i < halves; ++i) {
-        ok = __all_sync(0xffffffffu, mbar_wait(bars.s_full(i & 1), (i >> 1) & 1, ctx)) != 0;
+      for (int i = WIDE ? t : 0; i < halves; i += WIDE ? 2 : 1) {
+        const int turn = WIDE ? i >> 1 : i, place = WIDE ? 2 * t + (turn & 1) : turn & 1;  // of this group's halves; its buffer's barriers
+        ok = __all_sync(0xffffffffu, mbar_wait(bars.s_full(place), (turn >> 1) & 1, ctx)) != 0;
         if (!ok) break;
         tc_fence_after();
-        const uint32_t buffer = s_mem + kHalf * (i & 1);
+        const uint32_t buffer = s_mem + kHalf * (turn & 1);
         float x[kHalf];
 #pragma unroll
         for (int c = 0; c < kHalf; c += 32) {
@@ -415,7 +565,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         const StepPage* page = pages[(i >> 1) % kPageRing];
         const int c0 = kHalf * (i & 1), j0 = token(from + i * kHalf);
         const bool whole = __all_sync(0xffffffffu, (j0 >= lo || (VIEW == kSinks && j0 + kHalf <= p.sinks)) &&
-                                                       j0 + kHalf <= (VIEW == kTree ? min(hi, text) : hi)) != 0;
+                                                       j0 + kHalf <= (VIEW == kTree && mine ? min(hi, text) : hi)) != 0;
         // the row's maximum: within 16 tokens of one page that of the raw scores (the scales
         // are not negative)
         float high = m;
@@ -456,9 +606,9 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
           const float alpha = next == kNone ? 1.0f : exp2_approx(m - next);
           m = next;
           l *= alpha;
-          if (i > 0) {
+          if (turn > 0) {
             // once the product of the half before is over
-            ok = __all_sync(0xffffffffu, mbar_wait(bars.o_full(), (i - 1) & 1, ctx)) != 0;
+            ok = __all_sync(0xffffffffu, mbar_wait(bars.o_full(WIDE ? t : 0), (turn - 1) & 1, ctx)) != 0;
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
@@ -510,21 +660,47 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
         tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(bars.p_full(i & 1));
+        if (lane == 0) mbar_arrive(bars.p_full(place));
       }
       // ---- outputs
       if (ok && steps > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars.done(), 0, ctx)) != 0;
       tc_fence_after();
+      float weight[2] = {1.0f, 0.0f};  // wide: of each stream's outputs
+      if constexpr (WIDE) {
+        // the streams' maxima and sums, in the queries' place
+        float2 (*joined)[128] = reinterpret_cast<float2 (*)[128]>(raw + (q_base - smem_u32(raw)));
+        joined[t][in] = make_float2(m, l);
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        const float2 a = joined[0][in], b = joined[1][in];
+        m = fmaxf(a.x, b.x);
+        const float top = m == kNone ? 0.0f : m;
+        weight[0] = exp2_approx(a.x - top), weight[1] = exp2_approx(b.x - top);
+        l = a.y * weight[0] + b.y * weight[1];
+      }
       const float inv = p.splits > 1 ? 1.0f : l == 0.0f ? 0.0f : 1.0f / l;
       const int64_t part = ((static_cast<int64_t>(w.b) * p.a.max_q + qi) * p.a.Hq + hq) * p.splits + w.split;
-      if (p.splits > 1 && mine) p.ml[part] = make_float2(m, l);
+      if (p.splits > 1 && mine && (!WIDE || t == 0)) p.ml[part] = make_float2(m, l);
       T* dst = static_cast<T*>(p.o) + tok * p.a.o_token_stride + static_cast<int64_t>(hq) * p.a.o_head_stride;
 #pragma unroll
       for (int c = 0; c < DP; c += 16) {
+        if (WIDE && c / (DP / 2) != t) continue;  // (each stream's threads write half of the row)
         if (c < D) {
           uint32_t v[16];
-          tmem_ld16(o_mem + c, v);
-          tmem_wait_ld();
+          if constexpr (WIDE) {
+            uint32_t u[16];
+            tmem_ld16(tmem + lanes + kO + c, v);
+            tmem_ld16(tmem + lanes + kO + DP + c, u);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              // (the second stream has written nothing where there is one half)
+              const float second = halves > 1 ? __uint_as_float(u[i]) * weight[1] : 0.0f;
+              v[i] = __float_as_uint(fmaf(__uint_as_float(v[i]), weight[0], second));
+            }
+          } else {
+            tmem_ld16(o_mem + c, v);
+            tmem_wait_ld();
+          }
           if (!ok || !mine) continue;
           if (p.splits > 1) {
 #pragma unroll
@@ -555,19 +731,26 @@ __global__ void __launch_bounds__(kThreads, 1) pq_kv8_tiles(const __grid_constan
   }
 }
 
-template <typename T, int DP, int VIEW>
-cudaError_t launch_tiles(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
+template <typename T, int DP, int VIEW, bool WIDE>
+cudaError_t launch_tiles_as(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
   static int attr_set[64] = {0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(pq_kv8_tiles<T, DP, VIEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(DP));
+    e = cudaFuncSetAttribute(pq_kv8_tiles<T, DP, VIEW, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize, attn_smem(DP, WIDE));
     if (e != cudaSuccess) return e;
     if (dev < 64) attr_set[dev] = 1;
   }
-  pq_kv8_tiles<T, DP, VIEW><<<grid, kThreads, attn_smem(DP), stream>>>(p);
+  pq_kv8_tiles<T, DP, VIEW, WIDE><<<grid, TcRoles<WIDE>::kThreads, attn_smem(DP, WIDE), stream>>>(p);
   return cudaGetLastError();
+}
+
+template <typename T, int DP, int VIEW>
+cudaError_t launch_tiles(const AttnArgs& p, unsigned grid, cudaStream_t stream) {
+  if constexpr (VIEW != kPlain)  // (its order of sums is another than the one that plain attention has always had)
+    if (static_cast<int64_t>(p.a.max_q) * p.group <= 128) return launch_tiles_as<T, DP, VIEW, true>(p, grid, stream);
+  return launch_tiles_as<T, DP, VIEW, false>(p, grid, stream);
 }
 
 }  // namespace
