@@ -120,10 +120,24 @@ struct Plan {
   int rows;  // query rows of a tile
 };
 
-Plan plan_attention(const pq_kv8_cache* c, const pq_kv8_attn* a, AttnArgs* p) {
+//
+// The views with sinks and drafts (`fine`) go further where little is to be done (us in a graph): a range of up to 512 tokens stays in
+// one part, without the joining kernel (one token through a window of 256: 5.8, two parts 7.3); and where parts of 128 tokens find room
+// on the chip at one time, the rows kernel takes them, more than 40 rows too (12 drafts x 4 heads over 2000: 9.9, parts of 256 11.8; on
+// the tensor cores parts of 128 10.7, of 512 15.1).  Plain attention keeps the parts, and with them the bits, that it always had.
+Plan plan_attention(const pq_kv8_cache* c, const pq_kv8_attn* a, AttnArgs* p, bool fine) {
   Plan plan;
   plan.tc = attn_tc_takes(*c, *a);
   plan.rows = plan.tc ? kAttnTcRows : 8 * row_tiles_of_block(c, a);
+  const int64_t head16 = (static_cast<int64_t>(p->sinks) + 15) / 16 * 16;
+  const int64_t tokens = a->window > 0 ? std::min<int64_t>(a->max_len, head16 + a->window + a->max_q + 16) : a->max_len;
+  const int64_t small_rows = 8 * row_tiles_of_block(c, a);
+  const int64_t small_units = static_cast<int64_t>(a->B) * c->Hkv * ((static_cast<int64_t>(a->max_q) * (a->Hq / c->Hkv) + small_rows - 1) / small_rows);
+  const bool roomy = fine && small_units <= 2 * sm_count() && small_units * ((tokens + 127) / 128) <= 2 * sm_count();
+  if (roomy) {
+    plan.tc = false;
+    plan.rows = static_cast<int>(small_rows);
+  }
   p->align = plan.tc ? kAttnTcTokens : 16;
   p->row_tiles = static_cast<int>((static_cast<int64_t>(a->max_q) * (a->Hq / c->Hkv) + plan.rows - 1) / plan.rows);
   // tokens that one row tile can see, from a multiple of `align` on
@@ -133,7 +147,7 @@ Plan plan_attention(const pq_kv8_cache* c, const pq_kv8_attn* a, AttnArgs* p) {
   range = std::max<int64_t>(range, 1);
   const int64_t units = static_cast<int64_t>(a->B) * c->Hkv * p->row_tiles;
   const int64_t want = ((plan.tc ? 1 : 2) * static_cast<int64_t>(sm_count()) + units - 1) / units;
-  const int64_t least = plan.tc ? 512 : 256;
+  const int64_t least = fine && !plan.tc && range <= 512 ? 512 : plan.tc ? 512 : roomy ? 128 : 256;
   const int64_t splits = std::max<int64_t>(1, std::min(want, (range + least - 1) / least));
   const int64_t chunk = ((range + splits - 1) / splits + 127) / 128 * 128;
   p->chunk = static_cast<int>(std::min<int64_t>(chunk, 0x7FFFFF80));
@@ -191,7 +205,7 @@ Plan prepare_attention(const pq_kv8_cache* c, const pq_kv8_attn* a, View& v, Att
     p->tree_pitch = v.tree->pitch;
     p->tree_words = v.tree->words;
   }
-  return plan_attention(c, &p->a, p);
+  return plan_attention(c, &p->a, p, v.kind != kPlain);
 }
 
 size_t scratch_bytes(const pq_kv8_cache* cache, const pq_kv8_attn* a, View v) {

@@ -80,6 +80,18 @@ SINKS = [  # queries, tokens, Hq, H, D, T, window, sinks
 ]
 
 
+# More work than finds room at one time, so that 16-bit queries go to the tensor cores: one tile of rows (two streams of softmax) and
+# two, one half step and many, parts that are joined, odd sizes of heads, sequences of nothing.
+SINKS += [
+    ([21] * 20 + [1, 0, 9], [300, 77] * 10 + [500, 0, 9], 8, 4, 128, 64, 50, 4),
+    ([12] * 30, [64, 90, 130] * 10, 16, 4, 64, 16, 33, 20),
+    ([45] * 12, [45, 400, 200] * 4, 6, 3, 96, 32, 128, 130),
+    ([90] * 12, [90, 500, 333] * 4, 6, 3, 112, 128, 100, 7),
+    ([30], [9000], 4, 1, 128, 64, 5000, 100),
+    ([30, 25], [9000, 8000], 8, 2, 32, 16, 5000, 16),
+]
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("case", SINKS, ids=str)
 def test_sinks(B, case, kind):
@@ -104,8 +116,8 @@ def test_sinks_that_hide_nothing_are_plain_attention(B, n):
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
-@pytest.mark.parametrize("n", [1, 120])
-def test_pages_between_sinks_and_window_are_not_read(B, n, kind):
+@pytest.mark.parametrize("n,sequences", [(1, 1), (120, 1), (40, 14), (90, 9)])
+def test_pages_between_sinks_and_window_are_not_read(B, n, sequences, kind):
     """Page ids out of range, NaN scales and scales of zero where no query looks."""
     T, window, sinks, length = 16, 100, 20, 2000
     c = Cache(B, [length], 2, 64, T, seed=5)
@@ -118,11 +130,12 @@ def test_pages_between_sinks_and_window_are_not_read(B, n, kind):
     for d, h in zip(c.dev, (c.k, c.v, c.ks, c.vs)):
         d.copy_(torch.from_numpy(h))
     table[0, hidden[::2]] = -5
-    c.table_dev = table
-    q, o = _queries(n, 6, 64, kind, 2)
-    _sinks(B, c, q, o, [n], [length], window, sinks)
+    c.table_dev, c.table = table.expand(sequences, -1).contiguous(), np.repeat(c.table, sequences, 0)  # the same text for every sequence
+    ns, lens = [n] * sequences, [length] * sequences
+    q, o = _queries(n * sequences, 6, 64, kind, 2)
+    _sinks(B, c, q, o, ns, lens, window, sinks)
     assert B.palquant_sync_check() == B.PQ_OK
-    _check(c, q, o, [n], [length], kind, lambda b: ref.sees_sinks(n, length, window, sinks))
+    _check(c, q, o, ns, lens, kind, lambda b: ref.sees_sinks(n, length, window, sinks))
 
 
 def _masks(kind, n, rng):
@@ -161,6 +174,17 @@ TREES = [  # drafts, tokens with them, Hq, H, D, T, masks
 ]
 
 
+TREES += [  # (as with the sinks above)
+    ([21] * 20 + [1, 0, 9], [300, 77] * 10 + [500, 0, 9], 8, 4, 128, 64, "tree"),
+    ([12] * 30, [12, 64, 130] * 10, 16, 4, 64, 16, "any"),
+    ([33] * 12, [33, 400, 200] * 4, 9, 3, 96, 32, "any"),
+    ([70] * 12, [70, 500, 333] * 4, 6, 3, 112, 128, "tree"),
+    ([30], [7000], 4, 1, 128, 64, "tree"),
+    ([30, 25], [7000, 6001], 8, 2, 32, 16, "any"),
+    ([130], [5000], 2, 1, 128, 32, "any"),
+]
+
+
 @pytest.mark.parametrize("kind", list(TYPES))
 @pytest.mark.parametrize("case", TREES, ids=str)
 def test_tree(B, case, kind):
@@ -189,29 +213,30 @@ def test_chain_is_causal_attention_and_bits_past_the_drafts_do_not_count(B, n, k
 
 
 @pytest.mark.parametrize("kind", list(TYPES))
-@pytest.mark.parametrize("n", [6, 80])
-def test_drafts_that_see_nothing(B, n, kind):
+@pytest.mark.parametrize("n,sequences", [(6, 1), (80, 1), (24, 40), (72, 20)])
+def test_drafts_that_see_nothing(B, n, sequences, kind):
     """No text before the drafts, and rows of bits that are empty: zeros, beside rows that see only themselves."""
-    c = Cache(B, [n], 2, 64, 16, seed=n)
-    bits = _bits([[(1 << i) if i % 3 else 0 for i in range(n)]], -(-n // 32))
-    q, o = _queries(n, 4, 64, kind, 4)
-    _tree(B, c, q, o, [n], [n], torch.from_numpy(bits.view(np.int32)).cuda())
-    _check(c, q, o, [n], [n], kind, lambda b: ref.sees_tree(n, n, bits))
-    assert not o[::3].any()
+    ns = [n] * sequences
+    c = Cache(B, ns, 2, 64, 16, seed=n)
+    bits = _bits([[(1 << i) if i % 3 else 0 for i in range(n)]] * sequences, -(-n // 32))
+    q, o = _queries(n * sequences, 4, 64, kind, 4)
+    _tree(B, c, q, o, ns, ns, torch.from_numpy(bits.view(np.int32)).cuda())
+    _check(c, q, o, ns, ns, kind, lambda b: ref.sees_tree(n, n, bits[:n]))
+    assert not o.view(sequences, n, 4, 64)[:, ::3].any()
 
 
-@pytest.mark.parametrize("n", [6, 80])
-def test_drafts_that_a_draft_does_not_see_do_not_touch_it(B, n):
+@pytest.mark.parametrize("n,sequences", [(6, 1), (80, 1), (24, 40), (72, 20)])
+def test_drafts_that_a_draft_does_not_see_do_not_touch_it(B, n, sequences):
     """Siblings on a page with NaN scales: only the drafts that see it become NaN."""
     T = 16
-    c = Cache(B, [64 + n], 1, 64, T, seed=9)
-    page = c.table[0, 64 // T]  # drafts 0 to T - 1
-    c.ks[page] = np.nan
+    ns, lens = [n] * sequences, [64 + n] * sequences
+    c = Cache(B, lens, 2, 64, T, seed=9)
+    c.ks[c.table[:, 64 // T]] = np.nan  # drafts 0 to T - 1
     c.dev[2].copy_(torch.from_numpy(c.ks))
-    bits = _bits([[1 if i % 2 else 0 for i in range(n)]], -(-n // 32))
-    q, o = _queries(n, 4, 64, "f16", 5)
-    _tree(B, c, q, o, [n], [64 + n], torch.from_numpy(bits.view(np.int32)).cuda())
-    assert torch.isnan(o[1::2]).all() and torch.isfinite(o[::2]).all()
+    bits = _bits([[1 if i % 2 else 0 for i in range(n)]] * sequences, -(-n // 32))
+    q, o = _queries(n * sequences, 8, 64, "f16", 5)
+    _tree(B, c, q, o, ns, lens, torch.from_numpy(bits.view(np.int32)).cuda())
+    assert torch.isnan(o[1::2]).all() and torch.isfinite(o[::2]).all()  # (n is even)
 
 
 @pytest.mark.parametrize("view", ["sinks", "tree"])
