@@ -264,3 +264,36 @@ def test_w4_quantizer_by_hand():
     codes, s = ref.w4_quantize(np.array([[7.0, -3.5, 0.5, 1.49, 0, 0, 14, -13]]), 4)
     assert np.allclose(s, [[1.0, 2.0]])
     assert codes.tolist() == [[7, -4, 0, 1, 0, 0, 7, -6]]
+
+
+# ------------------------------------------------------------------ the attention block
+def test_block_options_refused():
+    from paper_2208_01944_gb300.attention_block import AttentionBlock8
+
+    v = dict(w_qkv=torch.zeros(8 * 64, 256), w_out=torch.zeros(256, 4 * 64), heads=4, kv_heads=2, sequences=2, max_len=100)
+    one = torch.ones(64)
+    for kw in (dict(sinks=-1, window=5), dict(sinks=4), dict(weight_bits=2), dict(weight_bits=4, weight_group=16), dict(rope=[1.0] * 33), dict(rope=[float("nan")]),
+               dict(q_norm=one), dict(k_norm=one), dict(q_norm=one, k_norm=one.half()), dict(q_norm=one[:63], k_norm=one[:63]),
+               dict(q_norm=one, k_norm=one, norm_eps=-1.0), dict(q_norm=one.double(), k_norm=one.double())):
+        with pytest.raises(ValueError):
+            AttentionBlock8(**(v | kw))
+
+
+def test_bits_of_trees():
+    from paper_2208_01944_gb300.attention_block import tree_bits
+
+    assert tree_bits([[-1, 0, 0, 2], [], [-1, -1]]).tolist() == [[1], [3], [5], [13], [1], [2]]
+    chain = tree_bits([list(range(-1, 40))])
+    assert chain.shape == (41, 2) and chain[31].tolist() == [-1, 0] and chain[40].tolist() == [-1, 511]
+    assert tree_bits([]).shape == (0, 1)
+    for bad in ([[0]], [[-1, 1]], [[-2]]):
+        with pytest.raises(ValueError):
+            tree_bits(bad)
+
+
+def test_weights_to_4_bits_refused():
+    from paper_2208_01944_gb300.attention_block import weight_codes4
+
+    for w, group in ((torch.zeros(4), 128), (torch.zeros(4, 8).double(), 128), (torch.zeros(4, 8).t(), 128), (torch.zeros(4, 8), 16)):
+        with pytest.raises(ValueError):
+            weight_codes4(w, group)
