@@ -722,7 +722,8 @@ pq_status palquant_w4_quantize(const void* w_dev, int32_t w_type, int64_t ldw, c
 pq_status palquant_w4_unpack(const void* packed_dev, const pq_w4_weights* w, int8_t* codes_dev, int64_t ldc,
                              float* s_dev, pq_stream_t stream);
 
-/* Bytes of device scratch palquant_linear_w4 needs (16-byte aligned; 0: none, or a refused call). */
+/* Bytes of device scratch palquant_linear_w4 needs (16-byte aligned; 0: none, or a refused call): a copy of the
+ * tokens, for more than 8 of fp32, and more than 16 of 16 bits whose ldx is not a multiple of 8. */
 size_t palquant_linear_w4_scratch_bytes(const pq_w4_weights* w, const pq_linear_desc* d);
 
 /* x_dev [M, K] of x_type to y_dev [M, N] of y_type; d->N and d->K are w's, d->ldw is not read, bias_dev

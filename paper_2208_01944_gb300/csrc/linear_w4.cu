@@ -190,15 +190,12 @@ pq_status palquant_w4_unpack(const void* packed_dev, const pq_w4_weights* w, int
 }
 
 size_t palquant_linear_w4_scratch_bytes(const pq_w4_weights* w, const pq_linear_desc* d) {
-  if (!pq::valid_w4_call(w, d)) return 0;
-  return 0;
+  return pq::valid_w4_call(w, d) ? pq::w4_tc_scratch(d->M, d->N, d->K, d->ldx, d->x_type) : 0;
 }
 
 pq_status palquant_linear_w4(const void* x_dev, const void* packed_dev, const float* bias_dev, void* y_dev,
                              const pq_w4_weights* w, const pq_linear_desc* d, void* scratch_dev, size_t scratch_bytes,
                              pq_stream_t stream) {
-  (void)scratch_dev;
-  (void)scratch_bytes;
   if (!pq::valid_w4_call(w, d)) return PQ_EINVAL;
   if (d->M == 0) return PQ_OK;
   const size_t e = pq::bytes_of_type(d->x_type);
@@ -206,10 +203,12 @@ pq_status palquant_linear_w4(const void* x_dev, const void* packed_dev, const fl
       !pq::is_aligned(packed_dev, 16) || !pq::is_aligned(bias_dev, 4) || !pq::is_aligned(y_dev, pq::bytes_of_type(d->y_type)))
     return PQ_EINVAL;
   if (d->M > 32ll * 65535) return PQ_EUNSUPPORTED;  // blocks along the grid's second axis
+  const size_t need = palquant_linear_w4_scratch_bytes(w, d);
+  if (need > 0 && (scratch_dev == nullptr || scratch_bytes < need || !pq::is_aligned(scratch_dev, 16))) return PQ_EINVAL;
   const pq::W4Args a = {pq::packed_of(w), x_dev, static_cast<const uint8_t*>(packed_dev), bias_dev, y_dev, d->ldx, d->ldy, d->M,
                         d->N, d->K, d->y_type, pq::is_aligned(x_dev, 4 * e) && d->ldx % 4 == 0};
   cudaStream_t s = static_cast<cudaStream_t>(stream);
-  const cudaError_t st = pq::w4_tc_takes(a, d->x_type) ? pq::launch_w4_tc(a, d->x_type, s)
+  const cudaError_t st = pq::w4_tc_takes(a, d->x_type) ? pq::launch_w4_tc(a, d->x_type, scratch_dev, s)
                          : d->x_type == PQ_F32         ? pq::launch_w4_rows<float>(a, s)
                          : d->x_type == PQ_F16         ? pq::launch_w4_rows<__half>(a, s)
                                                        : pq::launch_w4_rows<__nv_bfloat16>(a, s);

@@ -43,13 +43,15 @@ __host__ __device__ constexpr int places(int BN, int GS) {
   return 256 / ((job_k(GS) >> GS) * BN) < kMaxSlots ? 256 / ((job_k(GS) >> GS) * BN) : kMaxSlots;
 }
 
-__host__ __device__ constexpr int stage_bytes(int BN) { return kWBytes + BN * 256; }
+__host__ __device__ constexpr int stage_bytes(int BN, int PARTS) { return kWBytes + BN * 256 * PARTS; }
 // What the two sides of draining warps hand to one another at a tile's end.
 __host__ __device__ constexpr int exchange_bytes(int BN) { return BN < 128 ? BN * 512 : 0; }
-__host__ __device__ constexpr int stages(int BN) {
-  return (204800 - exchange_bytes(BN)) / stage_bytes(BN) < kMaxStages ? (204800 - exchange_bytes(BN)) / stage_bytes(BN) : kMaxStages;
+__host__ __device__ constexpr int stages(int BN, int PARTS) {
+  return (204800 - exchange_bytes(BN)) / stage_bytes(BN, PARTS) < kMaxStages ? (204800 - exchange_bytes(BN)) / stage_bytes(BN, PARTS) : kMaxStages;
 }
-__host__ __device__ constexpr int smem_bytes(int BN) { return stages(BN) * stage_bytes(BN) + exchange_bytes(BN) + 1024 /* alignment */; }
+__host__ __device__ constexpr int smem_bytes(int BN, int PARTS) {
+  return stages(BN, PARTS) * stage_bytes(BN, PARTS) + exchange_bytes(BN) + 1024 /* alignment */;
+}
 
 struct W4Tc {
   W4Args a;
@@ -146,10 +148,10 @@ __device__ __forceinline__ void tile_origin(const W4Tc& p, int t, int BN, int* n
   *m0 = static_cast<int64_t>(in / width) * BN;
 }
 
-// GS: log2(group).
-template <typename T, int BN, int GS>
+// GS: log2(group).  PARTS: matrices of tokens, one below the other in map_x, whose products are added (three for fp32).
+template <typename T, int BN, int GS, int PARTS>
 __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_constant__ W4Tc p, const __grid_constant__ CUtensorMap map_x) {
-  constexpr int kStages = stages(BN);
+  constexpr int kStages = stages(BN, PARTS);
   constexpr int kSlots = slots(GS), kPlaces = places(BN, GS);
   constexpr int kSlotColumns = kAColumns / kSlots;
   constexpr int kAccs = job_k(GS) >> GS;           // accumulators of a job
@@ -169,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
   __shared__ int abort_flag;
   __shared__ uint32_t tmem_base;
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
-  const uint32_t tok_base = smem, w_base = smem + kStages * 2 * kTok;
+  const uint32_t tok_base = smem, w_base = smem + kStages * PARTS * 2 * kTok;
   const Bars bars{smem_u32(bar_words)};
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = p.k_parts > 1 ? static_cast<int>(cluster_rank()) : 0;
@@ -216,6 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
       Ring r;
       bool ok = true;
       int issued = 0;
+      if (!weights) wait_previous_kernel();  // it may have written the tokens' copy
       for (int t = first_tile; ok && t < tiles; t += tile_step) {
         int n_tile;
         int64_t m0;
@@ -234,9 +237,14 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
             from += bytes;
           } else {
             const int k = (kb0 + kb) * kBlockK;
-            mbar_arrive_expect_tx(bar, 2 * kTok);
-            tma_load_2d(tok_base + r.s * 2 * kTok, &map_x, k, static_cast<int>(m0), bar);
-            tma_load_2d(tok_base + r.s * 2 * kTok + kTok, &map_x, k + 64, static_cast<int>(m0), bar);
+            mbar_arrive_expect_tx(bar, PARTS * 2 * kTok);
+#pragma unroll
+            for (int part = 0; part < PARTS; ++part) {
+              const uint32_t to = tok_base + (r.s * PARTS + part) * 2 * kTok;
+              const int row = static_cast<int>(part * p.a.M + m0);  // (rows past the part's end are the next one's: not stored)
+              tma_load_2d(to, &map_x, k, row, bar);
+              tma_load_2d(to + kTok, &map_x, k + 64, row, bar);
+            }
           }
           r.next(kStages);
         }
@@ -261,15 +269,18 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
         if (i >= kPlaces && !__all_sync(0xffffffffu, mbar_wait(bars.acc_empty(place), place_phase, ctx))) break;
         tc_fence_after();
         const uint32_t acc = tmem + kAColumns + place * (kAccs * BN), codes = tmem + slot * kSlotColumns;
-        const uint64_t tokens = sw128_desc(tok_base + (2 * stage + (kPerStage == 2 ? i & 1 : 0)) * kTok);
-        if (GS == 7) {
-          mma_ts_x4(acc, codes, tokens, idesc, 0);
-          mma_ts_x4(acc, codes + 32, tokens + (kTok >> 4), idesc, 1);
-        } else if (GS == 6) {
-          mma_ts_x4(acc, codes, tokens, idesc, 0);
-        } else {
-          mma_ts_x2(acc, codes, tokens, idesc, 0);
-          mma_ts_x2(acc + BN, codes + 16, tokens + 4, idesc, 0);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+          const uint64_t tokens = sw128_desc(tok_base + ((stage * PARTS + part) * 2 + (kPerStage == 2 ? i & 1 : 0)) * kTok);
+          if (GS == 7) {
+            mma_ts_x4(acc, codes, tokens, idesc, part > 0);
+            mma_ts_x4(acc, codes + 32, tokens + (kTok >> 4), idesc, 1);
+          } else if (GS == 6) {
+            mma_ts_x4(acc, codes, tokens, idesc, part > 0);
+          } else {
+            mma_ts_x2(acc, codes, tokens, idesc, part > 0);
+            mma_ts_x2(acc + BN, codes + 16, tokens + 4, idesc, part > 0);
+          }
         }
         tc_commit_warp(bars.acc_full(place));
         slot += kIssuers;
@@ -338,6 +349,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
     const uint32_t exchange = w_base + kStages * kWBytes;
     const int jobs = kbs * kPerStage;  // of a tile
     float sum[kCols];
+    wait_previous_kernel();  // before anything is written
     Ring r, place;
     int job = 0, slot = 0;  // over all tiles
     if (!kSplit && side == 1) {
@@ -468,66 +480,114 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
   }
 }
 
-template <typename T, int BN, int GS>
-cudaError_t launch(const W4Tc& p, const CUtensorMap& x, int sms, cudaStream_t stream) {
+template <typename T, int BN, int GS, int PARTS>
+cudaError_t launch(const W4Tc& p, const CUtensorMap& x, int sms, bool after_copy, cudaStream_t stream) {
   static int attr_set[64] = {0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   if (dev >= 64 || !attr_set[dev]) {
-    e = cudaFuncSetAttribute(pq_linear_w4_tc<T, BN, GS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes(BN));
+    e = cudaFuncSetAttribute(pq_linear_w4_tc<T, BN, GS, PARTS>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem_bytes(BN, PARTS));
     if (e != cudaSuccess) return e;
     if (dev < 64) attr_set[dev] = 1;
   }
   cudaLaunchConfig_t cfg = {};
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem_bytes(BN);
+  cfg.dynamicSmemBytes = smem_bytes(BN, PARTS);
   cfg.stream = stream;
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = static_cast<unsigned>(p.k_parts);
   attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = after_copy ? 2 : 1;
   const int64_t tiles = static_cast<int64_t>(p.n_tiles) * p.m_tiles;
   // a cluster that shares K has one tile; otherwise as many blocks as there are SMs take the tiles in turn
   const int64_t at_once = p.k_parts > 1 ? tiles : std::min<int64_t>(tiles, sms);
   cfg.gridDim = dim3(static_cast<unsigned>(at_once * p.k_parts));
-  return cudaLaunchKernelEx(&cfg, pq_linear_w4_tc<T, BN, GS>, p, x);
+  return cudaLaunchKernelEx(&cfg, pq_linear_w4_tc<T, BN, GS, PARTS>, p, x);
 }
 
-template <typename T, int BN>
-cudaError_t launch_group(const W4Tc& p, const CUtensorMap& x, int sms, cudaStream_t s) {
+template <typename T, int BN, int PARTS>
+cudaError_t launch_group(const W4Tc& p, const CUtensorMap& x, int sms, bool after_copy, cudaStream_t s) {
   const int gs = p.a.p.group_shift;
   if constexpr (BN < 128)
-    if (gs == 5) return launch<T, BN, 5>(p, x, sms, s);
-  return gs == 6 ? launch<T, BN, 6>(p, x, sms, s) : launch<T, BN, 7>(p, x, sms, s);
+    if (gs == 5) return launch<T, BN, 5, PARTS>(p, x, sms, after_copy, s);
+  return gs == 6 ? launch<T, BN, 6, PARTS>(p, x, sms, after_copy, s) : launch<T, BN, 7, PARTS>(p, x, sms, after_copy, s);
 }
 
 template <typename T>
-cudaError_t launch_bn(const W4Tc& p, int bn, const CUtensorMap& x, int sms, cudaStream_t s) {
-  return bn == 32 ? launch_group<T, 32>(p, x, sms, s) : bn == 64 ? launch_group<T, 64>(p, x, sms, s) : launch_group<T, 128>(p, x, sms, s);
+cudaError_t launch_bn(const W4Tc& p, int bn, const CUtensorMap& x, int sms, bool after_copy, cudaStream_t s) {
+  return bn == 32   ? launch_group<T, 32, 1>(p, x, sms, after_copy, s)
+         : bn == 64 ? launch_group<T, 64, 1>(p, x, sms, after_copy, s)
+                    : launch_group<T, 128, 1>(p, x, sms, after_copy, s);
+}
+
+// ------------------------------------------------------------------ the tokens' copy
+// Tokens that the tensor cores cannot load where they are: 16-bit ones in rows off 16-byte boundaries, and fp32 ones as three parts,
+// into rows of `pitch` elements (zeros past K), a part below the other.  Bound by the launch; a thread four elements.
+template <typename T>
+__global__ void __launch_bounds__(256) pq_w4_tokens(const T* __restrict__ x, int64_t ldx, int64_t M, int K, uint16_t* __restrict__ out, int64_t pitch, bool wide) {
+  let_next_kernel_start();
+  const int64_t pieces = pitch / 4, total = M * pieces;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; i < total; i += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t m = i / pieces;
+    const int k = static_cast<int>(i - m * pieces) * 4;
+    T v[4];
+    load4(x + m * ldx + min(k, K - 1), K - k, wide, v);
+    uint32_t y[kParts<T>][2];
+    operand_pairs(v, y);
+#pragma unroll
+    for (int part = 0; part < kParts<T>; ++part)
+      *reinterpret_cast<uint2*>(out + (part * M + m) * pitch + k) = make_uint2(y[part][0], y[part][1]);
+  }
+}
+
+template <typename T>
+cudaError_t launch_tokens(const W4Args& a, uint16_t* out, int64_t pitch, cudaStream_t s) {
+  const int64_t blocks = (a.M * (pitch / 4) + 255) / 256;
+  pq_w4_tokens<T><<<static_cast<unsigned>(std::min<int64_t>(blocks, 152 * 16)), 256, 0, s>>>(static_cast<const T*>(a.x), a.ldx, a.M, a.K, out, pitch, a.wide_x);
+  return cudaGetLastError();
 }
 
 }  // namespace
 
-// From 17 tokens on (us, here against the kernel for few tokens: 16 x 8192 x 4096 14.2 / 10.7, 24 x 4096 x 4096 11.1 / 28.6).
-bool w4_tc_takes(const W4Args& a, int x_type) {
-  return x_type != PQ_F32 && a.M > 16 && a.M <= (1 << 30) && is_aligned(a.x, 16) && a.ldx % 8 == 0;
+// From 17 tokens on, fp32 from 9; not where the kernel for few tokens is over in the 7 to 9 us that this one takes at least (us in a graph,
+// here against there, N x K: bf16, 20 tokens: 1024 x 1024 7.9 / 6.5, 1024 x 2048 8.5 / 11.3, 8192 x 512 7.1 / 11.8, 4096 x 4096 11.0 / 28.6;
+// 60 tokens: 1024 x 1024 9.7 / 8.0, 2048 x 2048 10.9 / 14.7; 16 tokens: 8192 x 4096 14.2 / 10.7; fp32, 12 tokens: 1024 x 1024 9.2 / 6.2,
+// 2048 x 2048 9.6 / 16.2; 60 tokens: 1024 x 1024 9.4 / 11.2).
+static bool worth(int64_t M, int N, int K, int x_type) {
+  const int64_t rows = x_type == PQ_F32 ? 16 : 32;  // that the other kernel takes at one time
+  return M > (x_type == PQ_F32 ? 8 : 16) && M <= (1 << 29) && (K > 1024 || (M + rows - 1) / rows * static_cast<double>(N) * K >= 4e6);
 }
 
-cudaError_t launch_w4_tc(const W4Args& a, int x_type, cudaStream_t stream) {
+size_t w4_tc_scratch(int64_t M, int N, int K, int64_t ldx, int x_type) {
+  if (!worth(M, N, K, x_type) || (x_type != PQ_F32 && ldx % 8 == 0)) return 0;
+  return static_cast<size_t>(M) * static_cast<size_t>((K + 7) / 8 * 8) * 2 * (x_type == PQ_F32 ? 3 : 1);
+}
+
+bool w4_tc_takes(const W4Args& a, int x_type) {
+  return worth(a.M, a.N, a.K, x_type) && (x_type == PQ_F32 || a.ldx % 8 != 0 || is_aligned(a.x, 16));
+}
+
+cudaError_t launch_w4_tc(const W4Args& given, int x_type, void* scratch, cudaStream_t stream) {
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   W4Tc p = {};
-  p.a = a;
+  p.a = given;
   p.err = device_error_word();
   p.wait_limit_ns = wait_limit_ns();
   if (p.err == nullptr) return cudaErrorInitializationError;
-  // (groups of 32 have two accumulators for each 64 of K: the tensor memory holds those of two jobs of 64 tokens, not of 128)
-  const int bn = a.M <= 32 ? 32 : a.M <= 64 || a.p.group_shift == 5 ? 64 : 128;
+  W4Args& a = p.a;
+  const bool copy = w4_tc_scratch(a.M, a.N, a.K, a.ldx, x_type) > 0;
+  const int parts = x_type == PQ_F32 ? 3 : 1;
+  // (groups of 32 have two accumulators for each 64 of K: the tensor memory holds those of two jobs of 64 tokens, not of 128; three
+  // parts of 32 tokens are as many bytes as 96)
+  const int bn = a.M <= 32 || parts == 3 ? 32 : a.M <= 64 || a.p.group_shift == 5 ? 64 : 128;
   p.n_tiles = (a.p.strips + kTileStrips - 1) / kTileStrips;
   const int64_t m_tiles = (a.M + bn - 1) / bn;
   if (p.n_tiles * m_tiles > 0x7FFFFFFF) return cudaErrorInvalidValue;
@@ -535,11 +595,22 @@ cudaError_t launch_w4_tc(const W4Args& a, int x_type, cudaStream_t stream) {
   // the blocks of a cluster share K while the chip has room for them and each keeps 512 of K
   p.k_parts = 1;
   for (int c = 2; c <= 8 && p.n_tiles * m_tiles * c <= (c == 8 ? sms / 2 : sms) && a.p.blocks / c >= 4; c *= 2) p.k_parts = c;
+  if (copy) {
+    const int64_t pitch = (a.K + 7) / 8 * 8;
+    uint16_t* out = static_cast<uint16_t*>(scratch);
+    e = x_type == PQ_F32   ? launch_tokens<float>(a, out, pitch, stream)
+        : x_type == PQ_F16 ? launch_tokens<__half>(a, out, pitch, stream)
+                           : launch_tokens<__nv_bfloat16>(a, out, pitch, stream);
+    if (e != cudaSuccess) return e;
+    a.x = scratch;
+    a.ldx = pitch;
+  }
   CUtensorMap x;
-  if (!encode_map_2d(&x, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a.x, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M),
+  if (!encode_map_2d(&x, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, a.x, static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M) * parts,
                      static_cast<uint64_t>(a.ldx) * 2, 64, static_cast<uint32_t>(bn), CU_TENSOR_MAP_SWIZZLE_128B))
     return cudaErrorInvalidValue;
-  return x_type == PQ_F16 ? launch_bn<__half>(p, bn, x, sms, stream) : launch_bn<__nv_bfloat16>(p, bn, x, sms, stream);
+  if (parts == 3) return launch_group<__nv_bfloat16, 32, 3>(p, x, sms, copy, stream);
+  return x_type == PQ_F16 ? launch_bn<__half>(p, bn, x, sms, copy, stream) : launch_bn<__nv_bfloat16>(p, bn, x, sms, copy, stream);
 }
 
 }  // namespace pq

@@ -78,9 +78,11 @@ struct W4Args {
 template <typename T>
 cudaError_t launch_w4_rows(const W4Args& a, cudaStream_t stream);
 
-// Up to 128 tokens a tile on the tensor cores; 16-bit activations in rows on 16-byte boundaries.
+// Up to 128 tokens a tile on the tensor cores.  Scratch: a copy of tokens that it cannot load where they are (16-bit ones whose rows
+// begin off 16-byte boundaries; without a pitch that shows it, the other kernel takes them).
+size_t w4_tc_scratch(int64_t M, int N, int K, int64_t ldx, int x_type);
 bool w4_tc_takes(const W4Args& a, int x_type);
-cudaError_t launch_w4_tc(const W4Args& a, int x_type, cudaStream_t stream);
+cudaError_t launch_w4_tc(const W4Args& a, int x_type, void* scratch, cudaStream_t stream);
 
 // One output, in fp32 until here.
 __device__ __forceinline__ void put_w4(const W4Args& a, int64_t m, int n, float y) {
@@ -91,6 +93,37 @@ __device__ __forceinline__ void put_w4(const W4Args& a, int64_t m, int n, float 
     static_cast<__half*>(a.y)[at] = __float2half_rn(y);
   else
     static_cast<__nv_bfloat16*>(a.y)[at] = __float2bfloat16_rn(y);
+}
+
+// How activations enter the products: halves, bfloat16, or fp32 as three bfloat16 parts.
+template <typename T>
+constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
+
+// Four activations as two pairs, part by part.
+template <typename T>
+__device__ __forceinline__ void operand_pairs(const T (&v)[4], uint32_t (&r)[kParts<T>][2]) {
+  if constexpr (sizeof(T) == 2) {
+    memcpy(r[0], v, 8);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint32_t part[2][3];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        // 8 + 8 + 8 bits by truncation; an infinity or a NaN is its first part alone
+        const float x = v[2 * i + j];
+        const uint32_t hi = __float_as_uint(x) & 0xFFFF0000u;
+        const bool finite = (hi & 0x7F800000u) != 0x7F800000u;
+        const float rest = finite ? x - __uint_as_float(hi) : 0.0f;
+        const uint32_t mid = __float_as_uint(rest) & 0xFFFF0000u;
+        part[j][0] = finite || hi == __float_as_uint(x) ? hi : hi | 0x00400000u;
+        part[j][1] = mid;
+        part[j][2] = __float_as_uint(rest - __uint_as_float(mid));
+      }
+#pragma unroll
+      for (int h = 0; h < 3; ++h) r[h][i] = __byte_perm(part[0][h], part[1][h], 0x7632);
+    }
+  }
 }
 
 // n of four consecutive elements (the others zero); `wide`: their address is a multiple of their size.

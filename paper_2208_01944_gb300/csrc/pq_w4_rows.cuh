@@ -25,10 +25,6 @@ __device__ __forceinline__ void scale_pair(uint32_t at, float& s0, float& s1) {
   }
 }
 
-// How activations enter the products: halves, bfloat16, or fp32 as three bfloat16 parts.
-template <typename T>
-constexpr int kParts = sizeof(T) == 4 ? 3 : 1;
-
 template <typename T>
 __device__ __forceinline__ void mma_w4(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if constexpr (sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value) {
@@ -37,33 +33,6 @@ __device__ __forceinline__ void mma_w4(float (&d)[4], uint32_t a0, uint32_t a1, 
     asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  }
-}
-
-// Four activations as two pairs, part by part.
-template <typename T>
-__device__ __forceinline__ void operand_pairs(const T (&v)[4], uint32_t (&r)[kParts<T>][2]) {
-  if constexpr (sizeof(T) == 2) {
-    memcpy(r[0], v, 8);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      uint32_t part[2][3];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        // 8 + 8 + 8 bits by truncation; an infinity or a NaN is its first part alone
-        const float x = v[2 * i + j];
-        const uint32_t hi = __float_as_uint(x) & 0xFFFF0000u;
-        const bool finite = (hi & 0x7F800000u) != 0x7F800000u;
-        const float rest = finite ? x - __uint_as_float(hi) : 0.0f;
-        const uint32_t mid = __float_as_uint(rest) & 0xFFFF0000u;
-        part[j][0] = finite || hi == __float_as_uint(x) ? hi : hi | 0x00400000u;
-        part[j][1] = mid;
-        part[j][2] = __float_as_uint(rest - __uint_as_float(mid));
-      }
-#pragma unroll
-      for (int h = 0; h < 3; ++h) r[h][i] = __byte_perm(part[0][h], part[1][h], 0x7632);
-    }
   }
 }
 

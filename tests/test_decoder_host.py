@@ -297,3 +297,13 @@ def test_weights_to_4_bits_refused():
     for w, group in ((torch.zeros(4), 128), (torch.zeros(4, 8).double(), 128), (torch.zeros(4, 8).t(), 128), (torch.zeros(4, 8), 16)):
         with pytest.raises(ValueError):
             weight_codes4(w, group)
+
+
+@pytest.mark.parametrize("M,K,ldx,x_type,nbytes", [(8, 4096, 4096, 0, 0), (9, 4095, 4095, 0, 9 * 4096 * 6), (9, 700, 700, 0, 0), (16, 4095, 4095, 1, 0),
+                                                   (17, 4095, 4095, 1, 17 * 4096 * 2), (17, 4095, 4096, 2, 0), (64, 8000, 8001, 2, 64 * 8000 * 2)])
+def test_w4_scratch_is_a_copy_of_the_tokens_that_need_one(M, K, ldx, x_type, nbytes):
+    w, d = _w(N=1000, K=K), _linear(M=M, N=1000, K=K, ldx=ldx, ldy=1000, x_type=x_type)
+    assert B.palquant_linear_w4_scratch_bytes(w, d) == nbytes
+    if nbytes:
+        for scratch, n in ((None, nbytes), (72, nbytes), (64, nbytes - 1)):
+            _refused(B.palquant_linear_w4, 64, 64, None, 64, w, d, scratch, n)

@@ -129,7 +129,7 @@ def test_pitches_odd_addresses_and_other_output_types(B, kind, M):
     N, K, group = 50, 333, 64
     codes, scales = _weights(N, K, group, "f16", 3)
     w, packed = _pack(B, codes, scales, group)
-    for pad, shift, out in ((5, 1, "f32"), (8 + 3, 8, "bf16"), (0, 0, "f16"), (K % 8 and 8 - K % 8, 0, "f32")):
+    for pad, shift, out in ((5, 1, "f32"), (8 + 3, 8, "bf16"), (0, 0, "f16"), (K % 8 and 8 - K % 8, 0, "f32"), (2, 1, "f32"), (2, 8, "f32")):
         store = torch.full((M, K + pad + 9), float("nan"), dtype=TYPES[kind], device="cuda")  # what lies beside the rows is not read
         x = store[:, shift:shift + K]
         x.copy_(torch.randn(M, K, device="cuda"))
