@@ -124,7 +124,8 @@ struct Plan {
 // The views with sinks and drafts (`fine`) go further where little is to be done (us in a graph): a range of up to 512 tokens stays in
 // one part, without the joining kernel (one token through a window of 256: 5.8, two parts 7.3); and where parts of 128 tokens find room
 // on the chip at one time, the rows kernel takes them, more than 40 rows too (12 drafts x 4 heads over 2000: 9.9, parts of 256 11.8; on
-// the tensor cores parts of 128 10.7, of 512 15.1).  Plain attention keeps the parts, and with them the bits, that it always had.
+// the tensor cores parts of 128 10.7, of 512 15.1).  Up to 8 parts of at most 512 tokens are the blocks of a cluster, which join them
+// themselves (the same drafts 9.2).  Plain attention keeps the parts, and with them the bits, that it always had.
 Plan plan_attention(const pq_kv8_cache* c, const pq_kv8_attn* a, AttnArgs* p, bool fine) {
   Plan plan;
   plan.tc = attn_tc_takes(*c, *a);
@@ -152,6 +153,11 @@ Plan plan_attention(const pq_kv8_cache* c, const pq_kv8_attn* a, AttnArgs* p, bo
   const int64_t chunk = ((range + splits - 1) / splits + 127) / 128 * 128;
   p->chunk = static_cast<int>(std::min<int64_t>(chunk, 0x7FFFFF80));
   p->splits = static_cast<int>((range + chunk - 1) / chunk);
+  if (roomy && range > 512 && range <= 512 * kMostCluster) {
+    p->chunk = static_cast<int>(((range + kMostCluster - 1) / kMostCluster + 127) / 128 * 128);
+    p->splits = static_cast<int>((range + p->chunk - 1) / p->chunk);
+    p->cluster = p->splits > 1;
+  }
   return plan;
 }
 
@@ -172,7 +178,7 @@ cudaError_t launch_join(const AttnArgs& p, int tile_rows, cudaStream_t s) {
 }
 
 size_t scratch_of(const AttnArgs& p) {
-  if (p.splits <= 1) return 0;
+  if (p.splits <= 1 || p.cluster) return 0;
   const size_t parts = static_cast<size_t>(p.a.B) * p.a.max_q * p.a.Hq * p.splits;
   return parts * sizeof(float2) + parts * p.c.D * sizeof(float);
 }
@@ -237,7 +243,7 @@ pq_status attend(const pq_kv8_cache* cache, const void* q_dev, void* o_dev, cons
   p.wait_limit_ns = wait_limit_ns();
   const size_t need = scratch_of(p);
   if (need > 0 && (scratch_dev == nullptr || scratch_bytes < need || !is_aligned(scratch_dev, 16))) return PQ_EINVAL;
-  if (p.splits > 1) {
+  if (p.splits > 1 && !p.cluster) {
     const size_t parts = static_cast<size_t>(a->B) * a->max_q * a->Hq * p.splits;
     p.ml = static_cast<float2*>(scratch_dev);
     p.part = reinterpret_cast<float*>(p.ml + parts);
@@ -257,7 +263,7 @@ pq_status attend(const pq_kv8_cache* cache, const void* q_dev, void* o_dev, cons
     st = v.kind == kSinks  ? launch_attn_rows<kSinks>(p, grid, plan.rows / 8, s)
          : v.kind == kTree ? launch_attn_rows<kTree>(p, grid, plan.rows / 8, s)
                            : launch_attn_rows<kPlain>(p, grid, plan.rows / 8, s);
-  if (st == cudaSuccess && p.splits > 1) {
+  if (st == cudaSuccess && p.splits > 1 && !p.cluster) {
     if (a->type == PQ_F32)
       st = launch_join<float>(p, plan.rows, s);
     else if (a->type == PQ_F16)

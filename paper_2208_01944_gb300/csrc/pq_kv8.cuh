@@ -27,6 +27,7 @@ struct AttnArgs {
   unsigned int* err;
   uint64_t wait_limit_ns;
   bool wide_q, wide_o;  // rows on 16-byte boundaries
+  bool cluster;         // a row tile's parts are a cluster of blocks, which join them: no scratch, no second kernel
   int sinks;            // kSinks: first tokens that stay visible (0 in the other views)
   const uint32_t* tree; // kTree: which drafts each draft sees, tree_words words a row
   int64_t tree_pitch;
@@ -42,6 +43,8 @@ enum AttnView : int { kPlain = 0, kSinks = 1, kTree = 2 };
 // rest of a weight in a second half there, as fp32 does.  (bfloat16's rounding is eight times a half's.)
 template <typename T, int VIEW>
 constexpr bool kSecondHalf = VIEW != kPlain && sizeof(T) == 2 && !std::is_same<T, __nv_bfloat16>::value;
+
+constexpr int kMostCluster = 8;
 
 bool valid_kv8_cache(const pq_kv8_cache* c);
 

@@ -37,6 +37,7 @@
 #include "palquant.h"
 #include "pq_internal.h"
 #include "pq_kv8.cuh"
+#include "pq_tc.cuh"
 #include "pq_tokens.cuh"
 
 namespace pq {
@@ -53,6 +54,15 @@ struct Place {
 __device__ __forceinline__ Place place_of(const AttnArgs& p) {
   Place r;
   unsigned i = blockIdx.x;
+  if (p.cluster) {  // the parts of a row tile are one cluster
+    r.split = i % p.splits;
+    i /= p.splits;
+    r.tile = i % p.row_tiles;
+    i /= p.row_tiles;
+    r.h = i % p.c.Hkv;
+    r.b = i / p.c.Hkv;
+    return r;
+  }
   r.tile = i % p.row_tiles;
   i /= p.row_tiles;
   r.split = i % p.splits;
@@ -79,6 +89,21 @@ __device__ __forceinline__ uint4 lds_16(uint32_t addr) {
 __device__ __forceinline__ uint2 lds_8(uint32_t addr) {
   uint2 v;
   asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+// From a block of the cluster.
+__device__ __forceinline__ float peer_f32(uint32_t addr, uint32_t rank) {
+  uint32_t a;
+  float v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 peer_f32x4(uint32_t addr, uint32_t rank) {
+  uint32_t a;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
   return v;
 }
 __device__ __forceinline__ float lds_f32(uint32_t addr) {
@@ -136,7 +161,8 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
   const int from = (VIEW == kSinks ? 0 : walk.gap) + w.split * p.chunk;
   const int end = VIEW == kSinks ? walk.end : sp.hi;
   const int to = min(end, from + p.chunk);
-  if (w.split > 0 && from >= end) return;
+  const bool cluster = VIEW != kPlain && p.cluster;  // (a part without tokens takes part in the joining)
+  if (w.split > 0 && from >= end && !cluster) return;
   auto token = [&](int s) { return VIEW == kSinks && s >= walk.head ? s + walk.gap : s; };
   const int D = p.c.D, C = D / 16;
 
@@ -491,6 +517,59 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
     }
     __syncthreads();
   }
+  if constexpr (VIEW != kPlain) {
+    if (cluster) {
+      // The parts' maxima, sums and outputs in every block's shared memory, joined in order: each block writes a share.
+      float* mine_o = reinterpret_cast<float*>(ring_raw);
+      if (warp == 0) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int row = 8 * j + 2 * t + i;
+            if (g == 0) join_m[0][row] = m[j][i], join_l[0][row] = l[j][i];
+#pragma unroll
+            for (int k = 0; k < kJ; ++k)
+              *reinterpret_cast<float2*>(mine_o + row * DP + g * (DP / 8) + 2 * k) = make_float2(o[k][j][i], o[k][j][i + 2]);
+          }
+      }
+      cluster_sync();
+      const uint32_t at_o = smem_u32(ring_raw), at_m = smem_u32(join_m[0]), at_l = smem_u32(join_l[0]);
+      const int quads = D / 4, total = min(kRows, rows - r0) * quads;
+      for (int e = w.split * (32 * kAttnWarps) + threadIdx.x; e < total; e += p.splits * (32 * kAttnWarps)) {
+        const int row = e / quads, d = 4 * (e - row * quads);
+        float top = kNone, pm[kMostCluster], pl[kMostCluster];
+        float4 po[kMostCluster];
+#pragma unroll
+        for (int s = 0; s < kMostCluster; ++s)
+          if (s < p.splits) {
+            pm[s] = peer_f32(at_m + 4 * row, s);
+            pl[s] = peer_f32(at_l + 4 * row, s);
+            po[s] = peer_f32x4(at_o + 4 * (row * DP + d), s);
+          }
+#pragma unroll
+        for (int s = 0; s < kMostCluster; ++s)
+          if (s < p.splits) top = fmaxf(top, pm[s]);
+        const float base = top == kNone ? 0.0f : top;
+        float sum = 0.0f, y[4] = {};
+#pragma unroll
+        for (int s = 0; s < kMostCluster; ++s)
+          if (s < p.splits) {
+            const float f = exp2_approx(pm[s] - base);
+            sum += pl[s] * f;
+            y[0] += po[s].x * f, y[1] += po[s].y * f, y[2] += po[s].z * f, y[3] += po[s].w * f;
+          }
+        const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+        const int r = r0 + row, qi = r / p.group, hq = w.h * p.group + r % p.group;
+        T* dst = static_cast<T*>(p.o) + (static_cast<int64_t>(p.a.cu_q_dev[w.b]) + qi) * p.a.o_token_stride +
+                 static_cast<int64_t>(hq) * p.a.o_head_stride + d;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dst[i] = from_f32<T>(y[i] * inv);
+      }
+      cluster_sync();  // the others have read this block's part
+      return;
+    }
+  }
   if (warp != 0) return;
 #pragma unroll
   for (int j = 0; j < NT; ++j)
@@ -537,6 +616,20 @@ cudaError_t launch_rows_as(const AttnArgs& p, unsigned grid, cudaStream_t s) {
     e = cudaFuncSetAttribute(pq_kv8_rows<T, DP, NT, TWO, VIEW>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes(DP));
     if (e != cudaSuccess) return e;
     if (dev < 64) attr_set[dev] = 1;
+  }
+  if (VIEW != kPlain && p.cluster) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(grid);
+    cfg.blockDim = dim3(32 * kAttnWarps);
+    cfg.dynamicSmemBytes = ring_bytes(DP);
+    cfg.stream = s;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = static_cast<unsigned>(p.splits);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, pq_kv8_rows<T, DP, NT, TWO, VIEW>, p);
   }
   pq_kv8_rows<T, DP, NT, TWO, VIEW><<<grid, 32 * kAttnWarps, ring_bytes(DP), s>>>(p);
   return cudaGetLastError();

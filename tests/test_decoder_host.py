@@ -55,8 +55,8 @@ def test_no_tree_is_refused():
 
 def test_views_check_their_scratch_and_pointers():
     t = B.KV8Tree(64, 1, 1)
-    for call, size, a, extra in ((B.palquant_kv8_attention_sinks, B.palquant_kv8_attention_sinks_scratch_bytes, _attn(), 4),
-                                 (B.palquant_kv8_attention_tree, B.palquant_kv8_attention_tree_scratch_bytes, _attn(window=0), t)):
+    for call, size, a, extra in ((B.palquant_kv8_attention_sinks, B.palquant_kv8_attention_sinks_scratch_bytes, _attn(max_len=90000, window=30000), 4),
+                                 (B.palquant_kv8_attention_tree, B.palquant_kv8_attention_tree_scratch_bytes, _attn(max_len=90000, window=0), t)):
         need = size(_cache(), a, extra)
         assert need > 0
         for q, o, scratch, n in ((None, 64, 64, need), (64, None, 64, need), (65, 64, 64, need), (64, 64, None, need), (64, 64, 72, need), (64, 64, 64, need - 1)):
@@ -72,8 +72,11 @@ def test_views_check_their_scratch_and_pointers():
 @pytest.mark.parametrize("max_q", [1, 30])
 def test_sinks_cut_the_visible_tokens_alone(max_q):
     """The scratch follows the window and the sinks, not the text; sinks without a window are plain attention."""
-    small = B.palquant_kv8_attention_sinks_scratch_bytes(_cache(), _attn(max_q=max_q, max_len=100000), 4)
-    assert small == B.palquant_kv8_attention_sinks_scratch_bytes(_cache(), _attn(max_q=max_q, max_len=900000), 4)
+    small = B.palquant_kv8_attention_sinks_scratch_bytes(_cache(), _attn(max_q=max_q, max_len=100000, window=30000), 4)
+    assert small == B.palquant_kv8_attention_sinks_scratch_bytes(_cache(), _attn(max_q=max_q, max_len=900000, window=30000), 4) > 0
+    # a few rows over a few thousand tokens, or over a few hundred, are joined without it
+    assert B.palquant_kv8_attention_sinks_scratch_bytes(_cache(), _attn(max_q=1, max_len=100000), 4) == 0
+    assert B.palquant_kv8_attention_sinks_scratch_bytes(_cache(), _attn(max_q=1, max_len=100000, window=200), 4) == 0
     assert B.palquant_kv8_attention_sinks_scratch_bytes(_cache(), _attn(max_q=max_q, max_len=100000), 0x7FFFFFFF) == \
         B.palquant_kv8_attention_scratch_bytes(_cache(), _attn(max_q=max_q, max_len=100000, window=0))
     for a, sinks in ((_attn(window=0), 4), (_attn(window=3000), 4), (_attn(), 0)):
