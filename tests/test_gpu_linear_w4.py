@@ -105,6 +105,8 @@ SIZES = [  # M, N, K, group
     (128, 150, 8900, 64), (120, 140, 9100, 128), (300, 2600, 640, 64), (30, 21000, 512, 32), (260, 1300, 1536, 128), (24, 1024, 4096, 128),
     # pairs of strips, the last one alone; few tokens
     (1, 9760, 520, 128), (8, 9744, 300, 32), (16, 2064, 700, 64), (12, 2049, 513, 128), (3, 12000, 260, 64),
+    # fewer columns than a load of the tensor cores takes; a last tile of one strip
+    (20, 130007, 33, 32), (33, 66000, 70, 64),
 ]
 
 
