@@ -28,6 +28,7 @@ struct AttnArgs {
   uint64_t wait_limit_ns;
   bool wide_q, wide_o;  // rows on 16-byte boundaries
   bool cluster;         // a row tile's parts are a cluster of blocks, which join them: no scratch, no second kernel
+  bool in_order;        // sequences are taken the longest first
   int sinks;            // kSinks: first tokens that stay visible (0 in the other views)
   const uint32_t* tree; // kTree: which drafts each draft sees, tree_words words a row
   int64_t tree_pitch;
@@ -101,6 +102,32 @@ __device__ __forceinline__ Span span_of(const AttnArgs& p, int b, int r0, int ro
     if (p.a.window > 0) s.lo = max(0, s.len - s.n + r0 / p.group + 1 - p.a.window);
   }
   return s;
+}
+
+// The i-th sequence, the longest first (of equals the first; those without queries last).  Every thread of a block of 256 or
+// more calls; `room`, B + 1 numbers of shared memory, is free again afterwards.  Up to 8 neighbours count for one sequence.
+constexpr int kMostInOrder = 128;
+__device__ __forceinline__ int longest_first(const AttnArgs& p, int i, int* room) {
+  const int B = p.a.B, shift = B <= 32 ? 3 : B <= 64 ? 2 : 1;
+  const int b = threadIdx.x >> shift, part = threadIdx.x & ((1 << shift) - 1);
+  int mine = -1;
+  if (b < B && p.a.cu_q_dev[b + 1] > p.a.cu_q_dev[b]) mine = max(0, p.a.len_dev[b]);
+  if (b < B && part == 0) room[b] = mine;
+  __syncthreads();
+  int before = 0;
+  if (b < B) {
+#pragma unroll 4
+    for (int j = part; j < B; j += 1 << shift) {
+      const int other = room[j];
+      before += other > mine || (other == mine && j < b);
+    }
+  }
+  for (int k = 1; k < 1 << shift; k *= 2) before += __shfl_xor_sync(0xffffffffu, before, k);
+  if (b < B && part == 0 && before == i) room[B] = b;
+  __syncthreads();
+  const int r = room[B];
+  __syncthreads();
+  return r;
 }
 
 // How a row tile walks through its tokens: steps of 16 or 128 (the kernel's `align`) through the first

@@ -19,10 +19,10 @@
 // Codes come through shared memory, three or four steps of each warp in flight (16-byte
 // asynchronous copies into a ring of the warp's own, no block-wide wait): with loads
 // straight into registers a step waited for its page's id and then for its codes, and a
-// batch of single tokens read 3.9 TB/s; now 4.7 (64 over up to 8192, 32 / 8 heads of 128: 143 us).  Of
+// batch of single tokens read 3.9 TB/s; now 5.5 (64 over up to 8192, 32 / 8 heads of 128: 122 us).  Of
 // the rest, instructions (60 % of the issue slots, a third of them the codes' conversions) are one part and uneven shares
-// the other: 512 uncut (sequence, head) blocks of ragged lengths on 304 places keep 65 % of them at work, by a simulation
-// of that schedule.  Few query rows are spread over the chip by splitting
+// were the other: 512 uncut (sequence, head) blocks of ragged lengths on 304 places keep 65 % of them at work as they come, the longest
+// first 94 %, by a simulation of that schedule (143 us became 122).  Few query rows are spread over the chip by splitting
 // the tokens; the parts' maxima, sums and outputs are joined by pq_kv8_join.
 //
 // Rounding.  Queries enter as halves scaled by a power of two for each row so that their largest
@@ -150,7 +150,8 @@ __global__ void __launch_bounds__(32 * kAttnWarps, DP <= 128 && NT == 1 && !TWO 
   // the warps' outputs are joined in the ring's place
   static_assert(kAttnWarps / 2 * kJ * NT * 4 * 32 * 4 <= ring_bytes(DP), "join buffer");
   float (*join_o)[kJ * NT * 4][32] = reinterpret_cast<float (*)[kJ * NT * 4][32]>(ring_raw);
-  const Place w = place_of(p);
+  Place w = place_of(p);
+  if (p.in_order) w.b = longest_first(p, w.b, reinterpret_cast<int*>(ring_raw));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int r0 = w.tile * kRows;
   const Span sp = span_of(p, w.b, r0, kRows);

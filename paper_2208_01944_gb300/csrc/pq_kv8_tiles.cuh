@@ -13,16 +13,19 @@
 // probabilities in use.  The outputs stay in tensor memory; they are rescaled only when
 // a row's maximum has grown by more than 2^8 (w, scaled by 2^6, stays below 2^14; a half holds 2^16).
 // Bound by waiting: at D = 128 a step's products take 2560 cycles (scores of 64 tokens wait for
-// shared memory, 48 cycles an MMA instead of 32), a step about 5500 over a whole launch, and no pipe is near its limit (issue 48 %,
-// exponentials 19 %).  Both tiles share their barriers, so their softmax runs at one time and little covers it.  Four prompts
-// of 2048 over 4096, 32 / 8 heads of 128: 278 us (0.79 PFLOP/s); one of 8192, causal: 569 us (0.97 PFLOP/s).
+// shared memory, 48 cycles an MMA instead of 32), a step about 4900 over a whole launch, and no pipe is near its limit (issue 53 %,
+// tensor 40 %, exponentials 20 %).  Both tiles share their barriers, so their softmax runs at one time and little covers it; a warp and
+// barriers for each tile, with eight or six converting warps, cost more (a window of 2048 and 16 sinks, two prompts of 4096 over 10000: 284 us, so
+// 340 and 393).  Four prompts of 2048 over 4096, 32 / 8 heads of 128: 249 us.
 //
 // Roles (16 warps): 0 issues the MMAs, 4 looks up pages, the other six below 8 convert
-// (none of them on the issuing warp's scheduler), 8-11 and 12-15 are the tiles' softmax.  With one tile of rows the softmax waits for
-// the codes: then eight warps convert, four more warps in all (TcRoles).  Tiles with the most tokens come first.
+// (none of them on the issuing warp's scheduler), 8-11 and 12-15 are the tiles' softmax.  One tile of rows has other roles, and 20 warps
+// (TcRoles).  Tiles with the most tokens come first.
 #pragma once
 
 #include <cuda_runtime.h>
+
+#include <type_traits>
 
 #include "palquant.h"
 #include "pq_internal.h"
@@ -137,19 +140,20 @@ __device__ __forceinline__ TcPlace tc_place(const AttnArgs& p) {
 }
 
 // How the warps share the work.  Two tiles of rows: six converting warps beside the issuing one and the pages', off the issuing
-// warp's scheduler, and four of softmax for each tile.  Wide, for one tile: eight converting warps, and the two groups of softmax are
-// streams of the same rows, one through the first half of every step and one through the second, with maxima, sums and outputs of
-// their own, joined at the end (one group had 1100 to 1900 cycles' work with each half, and everything else waited for it).
+// warp's scheduler, and four of softmax for each tile.  Wide, for one tile of rows: the two groups of softmax are streams of the same
+// rows, one through the first half of every step and one through the second, with maxima, sums and outputs of their own, joined at
+// the end (one group had 1100 to 1900 cycles' work with each half, and everything else waited for it); each stream has a warp of
+// its own that issues its MMAs (`own`: one warp needed 3600 cycles for both streams' 24 MMAs, 6 waits and 7 commits of a step, and
+// everything else waited for it: 32 sequences of up to 24 drafts over up to 6000 103.9 us, so 94.8); four warps convert the keys and
+// four the values.
 template <bool WIDE>
 struct TcRoles {
+  static constexpr bool kOwn = WIDE;
   static constexpr int kThreads = WIDE ? 640 : 512;
-  static constexpr int kConverters = WIDE ? 8 : 6;
-  static constexpr int kPageWarp = WIDE ? 1 : 4, kFirstConverter = WIDE ? 4 : 1, kFirstSoftmax = WIDE ? 12 : 8;
-  // this warp's number among the converting ones, or -1
-  static __device__ __forceinline__ int converter(int warp) {
-    if (WIDE) return warp >= 4 && warp < 12 ? warp - 4 : -1;
-    return warp < 8 && (warp & 3) != 0 ? (warp < 4 ? warp - 1 : warp - 2) : -1;
-  }
+  static constexpr int kOneSide = WIDE ? 4 : 6;  // converting warps of the keys (and of the values)
+  static constexpr int kPageWarp = WIDE ? 1 : 4, kSecondIssuer = 2, kFirstConverter = 4, kFirstSoftmax = WIDE ? 12 : 8;
+  // this warp's number among the converting ones
+  static __device__ __forceinline__ int converter(int warp) { return WIDE ? warp - kFirstConverter : warp < 4 ? warp - 1 : warp - 2; }
 };
 
 // VIEW: see AttnView.
@@ -163,7 +167,8 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
   __shared__ StepPage pages[kPageRing][8];
   __shared__ int abort_flag;
   __shared__ uint32_t tmem_base;
-  const TcPlace w = tc_place(p);
+  TcPlace w = tc_place(p);
+  if (WIDE && p.in_order) w.b = longest_first(p, w.b, reinterpret_cast<int*>(raw));
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int r0 = w.tile * kAttnTcRows;
   const Span sp = span_of(p, w.b, r0, kAttnTcRows);
@@ -178,24 +183,24 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
   auto token = [&](int s) { return VIEW == kSinks && s >= walk.head ? s + walk.gap : s; };
   const int steps = to > from ? (to - from + kTokens - 1) / kTokens : 0;
   const int halves = to > from ? (to - from + kHalf - 1) / kHalf : 0;
-  const int tiles = rows - r0 > 128 ? 2 : 1;
+  const int streams = WIDE || rows - r0 > 128 ? 2 : 1;  // of MMAs and softmax: the tiles with rows, wide: both halves of a step
   const int D = p.c.D;
   const uint32_t smem = (smem_u32(raw) + 1023u) & ~1023u;
   const uint32_t q_base = smem, k_base = q_base + (WIDE ? 1 : 2) * kSubs * kSub, v_base = k_base + 2 * kSubs * kSub;
   const AttnBars bars{smem_u32(bar_words)};
 
   if (threadIdx.x == 0) {
-    mbar_init(bars.q_full(), 4 * (WIDE ? 2 : tiles));
-    mbar_init(bars.done(), 1);
+    mbar_init(bars.q_full(), 4 * streams);
+    mbar_init(bars.done(), Roles::kOwn ? streams : 1);
     for (int s = 0; s < 2; ++s) {
-      mbar_init(bars.k_full(s), Roles::kConverters);
-      mbar_init(bars.k_empty(s), 1);
-      mbar_init(bars.v_full(s), Roles::kConverters);
-      mbar_init(bars.v_empty(s), 1);
+      mbar_init(bars.k_full(s), Roles::kOneSide);
+      mbar_init(bars.k_empty(s), Roles::kOwn ? streams : 1);
+      mbar_init(bars.v_full(s), Roles::kOneSide);
+      mbar_init(bars.v_empty(s), Roles::kOwn ? streams : 1);
     }
     for (int b = 0; b < 4; ++b) {
       mbar_init(bars.s_full(b), 1);
-      mbar_init(bars.p_full(b), 4 * (WIDE ? 1 : tiles));
+      mbar_init(bars.p_full(b), 4 * (Roles::kOwn ? 1 : streams));
     }
     for (int b = 0; b < 2; ++b) mbar_init(bars.o_full(b), 1);
     for (int i = 0; i < kPageRing; ++i) {
@@ -214,8 +219,14 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
   constexpr uint32_t tmem = 0;
   WaitCtx ctx{&abort_flag, p.err, p.wait_limit_ns, PQ_ERR_MMA};
 
-  auto issue = [&]() {
-    // ---- MMAs
+  auto finish = [&]() {
+    // every MMA issued is over: the outputs are whole, the tensor memory may be given back
+    tc_commit_warp(bars.done());
+    if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
+    __syncwarp();
+  };
+  auto issue_both = [&]() {
+    // ---- MMAs of both tiles
     auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)) != 0; };
     const uint32_t idesc_s = (1u << 4) | (8u << 17) | (8u << 24);                                        // N = 64 tokens
     const uint32_t idesc_o = (1u << 4) | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (8u << 24);  // N = D
@@ -225,7 +236,7 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
       const uint32_t k = k_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128);
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        if (t < tiles) {
+        if (t < streams) {
 #pragma unroll
           for (int c = 0; c < kSubs; ++c)
             mma_ss_x4(tmem + 128 * t + kHalf * (i & 1), desc_k(q_base + (t * kSubs + c) * kSub), desc_k(k + c * kSub),
@@ -237,48 +248,13 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
       const uint32_t v = desc_n(v_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128));
 #pragma unroll
       for (int t = 0; t < 2; ++t)
-        if (t < tiles) {
+        if (t < streams) {
           mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1), v, idesc_o, i > 0);
           if (kSecondHalf<T, VIEW>) mma_ts_x4(tmem + kO + t * DP, tmem + 128 * t + kHalf * (i & 1) + kHalf / 2, v, idesc_o, 1);
         }
       tc_commit_warp(bars.o_full(0));
     };
     bool ok = halves > 0 && wait(bars.q_full(), 0) && wait(bars.k_full(0), 0);
-    if constexpr (WIDE) {
-      // Stream i % 2 takes half i; its scores are in its buffer (i / 2) % 2, two halves ahead of its probabilities.
-      auto stream_scores = [&](int i) {
-        const uint32_t k = k_base + ((i >> 1) & 1) * kSubs * kSub + (i & 1) * (kHalf * 128);
-#pragma unroll
-        for (int c = 0; c < kSubs; ++c)
-          mma_ss_x4(tmem + 128 * (i & 1) + kHalf * ((i >> 1) & 1), desc_k(q_base + c * kSub), desc_k(k + c * kSub), idesc_s, c > 0);
-        tc_commit_warp(bars.s_full(2 * (i & 1) + ((i >> 1) & 1)));
-        if ((i & 1) || i + 1 == halves) tc_commit_warp(bars.k_empty((i >> 1) & 1));
-      };
-      if (ok) {
-        tc_fence_after();
-        stream_scores(0);
-        if (halves > 1) stream_scores(1);
-      }
-      for (int i = 0; ok && i < halves; ++i) {
-        const int j = i >> 1, n = i + 2;
-        if (n < halves) {
-          if (!(n & 1)) ok = wait(bars.k_full((n >> 1) & 1), (n >> 2) & 1);
-          if (!ok) break;
-          tc_fence_after();
-          stream_scores(n);
-        }
-        if (!(i & 1)) ok = wait(bars.v_full(j & 1), (j >> 1) & 1);
-        ok = ok && wait(bars.p_full(2 * (i & 1) + (j & 1)), (j >> 1) & 1);
-        if (!ok) break;
-        tc_fence_after();
-        const uint32_t v = desc_n(v_base + (j & 1) * kSubs * kSub + (i & 1) * (kHalf * 128));
-        const uint32_t weights = tmem + 128 * (i & 1) + kHalf * (j & 1), o = tmem + kO + (i & 1) * DP;
-        mma_ts_x4(o, weights, v, idesc_o, i > 1);
-        if (kSecondHalf<T, VIEW>) mma_ts_x4(o, weights + kHalf / 2, v, idesc_o, 1);
-        tc_commit_warp(bars.o_full(i & 1));
-        if ((i & 1) || i + 1 == halves) tc_commit_warp(bars.v_empty(j & 1));
-      }
-    } else {
     if (ok) {
       tc_fence_after();
       scores(0);
@@ -301,11 +277,51 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
       outputs(i);
       if ((i & 1) || n == halves) tc_commit_warp(bars.v_empty(j & 1));
     }
+    finish();
+  };
+  // ---- wide: MMAs of stream t, which takes half t of every step (its `turn`)
+  auto issue = [&](auto which) {
+    constexpr int t = decltype(which)::value;
+    const int turns = (halves + 1 - t) >> 1;
+    auto wait = [&](uint32_t bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, ctx)) != 0; };
+    const uint32_t idesc_s = (1u << 4) | (8u << 17) | (8u << 24);                                        // N = 64 tokens
+    const uint32_t idesc_o = (1u << 4) | (1u << 16) | (static_cast<uint32_t>(D >> 3) << 17) | (8u << 24);  // N = D
+    auto scores = [&](int turn) {
+      const int s = turn & 1;
+      const uint32_t k = k_base + s * kSubs * kSub + t * (kHalf * 128);
+#pragma unroll
+      for (int c = 0; c < kSubs; ++c)
+        mma_ss_x4(tmem + 128 * t + kHalf * s, desc_k(q_base + c * kSub), desc_k(k + c * kSub), idesc_s, c > 0);
+      tc_commit_warp(bars.s_full(2 * t + s));
+      tc_commit_warp(bars.k_empty(s));
+    };
+    auto outputs = [&](int turn) {
+      const int s = turn & 1;
+      const uint32_t v = desc_n(v_base + s * kSubs * kSub + t * (kHalf * 128)), weights = tmem + 128 * t + kHalf * s;
+      mma_ts_x4(tmem + kO + t * DP, weights, v, idesc_o, turn > 0);
+      if (kSecondHalf<T, VIEW>) mma_ts_x4(tmem + kO + t * DP, weights + kHalf / 2, v, idesc_o, 1);
+      tc_commit_warp(bars.o_full(t));
+      tc_commit_warp(bars.v_empty(s));
+    };
+    bool ok = turns > 0 && wait(bars.q_full(), 0) && wait(bars.k_full(0), 0);
+    if (ok) {
+      tc_fence_after();
+      scores(0);
     }
-    // every MMA issued is over: the outputs are whole, the tensor memory may be given back
-    tc_commit_warp(bars.done());
-    if (lane == 0) mbar_wait_drain(bars.done(), 0, p.wait_limit_ns, p.err);
-    __syncwarp();
+    for (int turn = 0; ok && turn < turns; ++turn) {
+      const int next = turn + 1;
+      if (next < turns) {
+        ok = wait(bars.k_full(next & 1), (next >> 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        scores(next);
+      }
+      ok = wait(bars.v_full(turn & 1), (turn >> 1) & 1) && wait(bars.p_full(2 * t + (turn & 1)), (turn >> 1) & 1);
+      if (!ok) break;
+      tc_fence_after();
+      outputs(turn);
+    }
+    finish();
   };
   auto look_up = [&]() {
     // ---- the steps' pages, a lane each, up to kPageRing steps ahead of the codes (two
@@ -339,63 +355,60 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
   auto convert = [&]() {
     // ---- codes to halves
     ctx.err_bits = PQ_ERR_PRODUCER;
-    const int tid = 32 * Roles::converter(warp) + lane;
+    const int side = WIDE && Roles::converter(warp) >= Roles::kOneSide;  // wide: keys or values
+    const int tid = 32 * (Roles::converter(warp) - side * Roles::kOneSide) + lane;
     const int C = D / 16;  // 16-byte pieces of a token
     // A thread takes one 16-byte piece of every kTokStep-th token.  Eight neighbours
     // hold four pieces of two tokens, whose halves lie in different banks.
-    constexpr int kP = DP / 16, kTokStep = 32 * Roles::kConverters / kP, kTurns = (kTokens + kTokStep - 1) / kTokStep;
+    constexpr int kP = DP / 16, kTokStep = 32 * Roles::kOneSide / kP, kTurns = (kTokens + kTokStep - 1) / kTokStep;
     const int piece = kP == 8 ? (tid & 3) | ((tid >> 1) & 4) : tid & 3;
     const int token = kP == 8 ? ((tid >> 3) & ~1) | ((tid >> 2) & 1) : tid >> 2;
     const bool there = piece < C;
     const uint32_t row = (piece >> 2) * kSub + token * 128;
     const uint32_t at0 = row + (((2 * (piece & 3)) ^ (token & 7)) << 4), at1 = row + (((2 * (piece & 3) + 1) ^ (token & 7)) << 4);
     // every step's pieces lie at the same places of its pages
-    int slot[kTurns], in_page[kTurns];
-#pragma unroll
-    for (int i = 0; i < kTurns; ++i) {
-      const int k = token + i * kTokStep;
-      slot[i] = min(k, kTokens - 1) >> p.page_shift;
-      in_page[i] = there && k < kTokens ? (k & (p.c.page_tokens - 1)) * D + 16 * piece : -1;
-    }
+    auto slot = [&](int i) { return (WIDE ? token + i * kTokStep : min(token + i * kTokStep, kTokens - 1)) >> p.page_shift; };
+    auto in_page = [&](int i) { return ((token + i * kTokStep) & (p.c.page_tokens - 1)) * D + 16 * piece; };
     // wide: a step's codes are on their way through shared memory two steps ahead (each thread copies what it will convert; one step ahead
     // in registers, half of a step's time went by waiting for them); else through registers
     const uint32_t staged = v_base + 2 * kSubs * kSub + tid * 16;
-    auto copy = [&](const int8_t* codes, int j, int side) {
+    auto copy = [&](const int8_t* codes, int j) {
       if (j < steps) {
         const StepPage* page = pages[j % kPageRing];
 #pragma unroll
         for (int i = 0; i < kTurns; ++i) {
-          const int64_t base = page[slot[i]].codes;
-          const bool have = base >= 0 && in_page[i] >= 0;
-          cp_async_16(staged + ((j & 1) * 2 + side) * (kTokens * DP) + i * (32 * Roles::kConverters * 16), have ? codes + base + in_page[i] : codes,
+          const int64_t base = page[slot(i)].codes;
+          const bool have = base >= 0 && there;
+          cp_async_16(staged + ((j & 1) * 2 + side) * (kTokens * DP) + i * (32 * Roles::kOneSide * 16), have ? codes + base + in_page(i) : codes,
                       have ? 16 : 0);
         }
       }
       cp_async_commit();
     };
-    auto arrived = [&](int j, int side, uint4 (&r)[kTurns]) {
-      cp_async_wait<3>();
+    static_assert(!WIDE || kTurns * kTokStep == kTokens, "every turn is whole");
+    constexpr int kBatch = kTurns < 4 ? kTurns : 4;  // turns at a time
+    auto arrived = [&](int j, int i0, uint4 (&r)[kBatch]) {
 #pragma unroll
-      for (int i = 0; i < kTurns; ++i)
+      for (int i = 0; i < kBatch; ++i)
         asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
                      : "=r"(r[i].x), "=r"(r[i].y), "=r"(r[i].z), "=r"(r[i].w)
-                     : "r"(staged + ((j & 1) * 2 + side) * (kTokens * DP) + i * (32 * Roles::kConverters * 16))
+                     : "r"(staged + ((j & 1) * 2 + side) * (kTokens * DP) + (i0 + i) * (32 * Roles::kOneSide * 16))
                      : "memory");
     };
     auto fetch = [&](const int8_t* codes, int j, uint4 (&r)[kTurns]) {
       const StepPage* page = pages[j % kPageRing];
 #pragma unroll
       for (int i = 0; i < kTurns; ++i) {
-        const int64_t base = page[slot[i]].codes;
+        const int64_t base = page[slot(i)].codes;
         r[i] = make_uint4(0, 0, 0, 0);
-        if (base >= 0 && in_page[i] >= 0) r[i] = *reinterpret_cast<const uint4*>(codes + base + in_page[i]);
+        if (base >= 0 && there && token + i * kTokStep < kTokens) r[i] = *reinterpret_cast<const uint4*>(codes + base + in_page(i));
       }
     };
     // (columns past D are zeros: the scores' products run over whole blocks of 64)
-    auto store = [&](uint32_t base, const uint4 (&r)[kTurns]) {
+    auto store = [&](uint32_t base, const uint4* r, int n) {
 #pragma unroll
-      for (int i = 0; i < kTurns; ++i) {
-        if (token + i * kTokStep >= kTokens) break;
+      for (int i = 0; i < n; ++i) {
+        if (!WIDE && token + i * kTokStep >= kTokens) break;
         uint32_t h[8];
         half_of_codes(r[i].x, h[0], h[1]);
         half_of_codes(r[i].y, h[2], h[3]);
@@ -414,31 +427,29 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
       return __all_sync(0xffffffffu, mbar_wait(bars.page_full(j % kPageRing), (j / kPageRing) & 1, ctx)) != 0;
     };
     if constexpr (WIDE) {
-      bool ok = steps > 0 && look(0);
+      const int8_t* codes = side ? p.c.v_dev : p.c.k_dev;
+      const uint32_t base = side ? v_base : k_base, full = side ? bars.v_full(0) : bars.k_full(0), empty = side ? bars.v_empty(0) : bars.k_empty(0);
+      bool ok = true;
       for (int j = 0; ok && j < 2; ++j) {
         if (j < steps) ok = look(j);
-        copy(p.c.k_dev, j, 0);
-        copy(p.c.v_dev, j, 1);
+        if (ok) copy(codes, j);
       }
       for (int j = 0; ok && j < steps; ++j) {
         const int s = j & 1;
-        uint4 r[kTurns];
-        if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.k_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
+        if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(empty + 8u * s, ((j >> 1) - 1) & 1, ctx)) != 0;
         if (!ok) break;
-        arrived(j, 0, r);
-        store(k_base + s * kSubs * kSub, r);
-        publish(bars.k_full(s));
+        // values: step j - 2 is over, and so is every use of its pages
+        if (j > 1 && side && tid == 0) mbar_arrive(bars.page_empty((j - 2) % kPageRing));
+        cp_async_wait<1>();
+#pragma unroll
+        for (int i = 0; i < kTurns; i += kBatch) {
+          uint4 r[kBatch];
+          arrived(j, i, r);
+          store(base + s * kSubs * kSub + i * kTokStep * 128, r, kBatch);
+        }
+        publish(full + 8u * s);
         if (j + 2 < steps) ok = look(j + 2);
-        if (!ok) break;
-        copy(p.c.k_dev, j + 2, 0);
-        if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.v_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
-        if (!ok) break;
-        // step j - 2 is over: so is every use of its pages
-        if (j > 1 && tid == 0) mbar_arrive(bars.page_empty((j - 2) % kPageRing));
-        arrived(j, 1, r);
-        store(v_base + s * kSubs * kSub, r);
-        publish(bars.v_full(s));
-        copy(p.c.v_dev, j + 2, 1);
+        if (ok) copy(codes, j + 2);
       }
       cp_async_wait<0>();
       return;
@@ -453,7 +464,7 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
       const int s = j & 1;
       if (j > 1) ok = __all_sync(0xffffffffu, mbar_wait(bars.k_empty(s), ((j >> 1) - 1) & 1, ctx)) != 0;
       if (!ok) break;
-      store(k_base + s * kSubs * kSub, kr);
+      store(k_base + s * kSubs * kSub, kr, kTurns);
       publish(bars.k_full(s));
       if (j + 1 < steps) {
         ok = look(j + 1);
@@ -464,38 +475,38 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
       if (!ok) break;
       // step j - 2 is over: so is every use of its pages
       if (j > 1 && tid == 0) mbar_arrive(bars.page_empty((j - 2) % kPageRing));
-      store(v_base + s * kSubs * kSub, vr);
+      store(v_base + s * kSubs * kSub, vr, kTurns);
       publish(bars.v_full(s));
       if (j + 1 < steps) fetch(p.c.v_dev, j + 1, vr);
     }
   };
 
+  // (the registers of all together are what the threads had at launch: 512 of 128, 640 of 96)
   if (!WIDE && warp < 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
     if (warp == 0)
-      issue();
+      issue_both();
     else if (warp == Roles::kPageWarp)
       look_up();
     else
       convert();
   } else if (WIDE && warp < 4) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 48;");
     if (warp == 0)
-      issue();
+      issue(std::integral_constant<int, 0>{});
     else if (warp == Roles::kPageWarp)
       look_up();
+    else if (warp == Roles::kSecondIssuer)
+      issue(std::integral_constant<int, 1>{});
   } else if (WIDE && warp < 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
     convert();
   } else {
-    if (WIDE)
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
-    else
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
     // ---- softmax: this thread's row
     ctx.err_bits = PQ_ERR_EPILOGUE;
     const int t = (warp - Roles::kFirstSoftmax) >> 2;
-    if (WIDE || t < tiles) {
+    if (t < streams) {
       const int in = 32 * (warp & 3) + lane, r = r0 + (WIDE ? 0 : 128 * t) + in;
       const bool mine = r < rows;
       const int qi = mine ? r / p.group : 0, hq = w.h * p.group + (mine ? r % p.group : 0);
@@ -547,8 +558,16 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
       const int text = sp.len - sp.n;
       float m = kNone, l = 0.0f;
       bool ok = true;
-      for (int i = WIDE ? t : 0; i < halves; i += WIDE ? 2 : 1) {
-        const int turn = WIDE ? i >> 1 : i, place = WIDE ? 2 * t + (turn & 1) : turn & 1;  // of this group's halves; its buffer's barriers
+      int i = WIDE ? t : 0;
+      if (WIDE && __all_sync(0xffffffffu, !mine)) {  // a warp whose rows are all past the end only keeps the barriers' count
+        for (; ok && i < halves; i += 2) {
+          const int turn = i >> 1, place = 2 * t + (turn & 1);
+          ok = __all_sync(0xffffffffu, mbar_wait(bars.s_full(place), (turn >> 1) & 1, ctx)) != 0;
+          if (lane == 0 && ok) mbar_arrive(bars.p_full(place));
+        }
+      }
+      for (; i < halves; i += WIDE ? 2 : 1) {
+        const int turn = WIDE ? i >> 1 : i, place = Roles::kOwn ? 2 * t + (turn & 1) : turn & 1;  // of this group's halves; its buffer's barriers
         ok = __all_sync(0xffffffffu, mbar_wait(bars.s_full(place), (turn >> 1) & 1, ctx)) != 0;
         if (!ok) break;
         tc_fence_after();
@@ -608,7 +627,7 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
           l *= alpha;
           if (turn > 0) {
             // once the product of the half before is over
-            ok = __all_sync(0xffffffffu, mbar_wait(bars.o_full(WIDE ? t : 0), (turn - 1) & 1, ctx)) != 0;
+            ok = __all_sync(0xffffffffu, mbar_wait(bars.o_full(Roles::kOwn ? t : 0), (turn - 1) & 1, ctx)) != 0;
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
