@@ -11,6 +11,10 @@
 // The accumulators of groups take turns, so that one is read while others are written.  Few tiles: the blocks of a cluster take
 // parts of K of one tile and add their fp32 sums through distributed shared memory, in order.
 //
+// Bound by hand-overs between the roles where tokens are few (no pipe above 40 %), by reading groups' accumulators where they are many.
+// Measured, bf16: 48 x 8192 x 4096 with groups of 64 17 us (1.1 TB/s of weights), 2048 x 4096 x 4096 with groups of 128 86 us (0.80
+// PFLOP/s), of 64 111, of 32 183.
+//
 // Roles (32 warps): 0 and 2 load (weights, tokens), 4-19 unpack, 20-27 drain and write, 28-31 issue the MMAs.  A stage is 128 of K.
 #include <cuda.h>
 #include <cuda_runtime.h>

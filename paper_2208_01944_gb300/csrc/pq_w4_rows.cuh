@@ -39,7 +39,7 @@ __device__ __forceinline__ void mma_w4(float (&d)[4], uint32_t a0, uint32_t a1, 
 // A block: NS strips of 16 channels x 8 NT tokens; its warps take the strips' blocks of 128 of K in turn.  Bound by the weights'
 // bytes and, close to it, by the instructions of unpacking.  The weights come through rings of asynchronous copies, one for each
 // warp (a block of 128 of K a stage, kRing - 1 of them ahead); each lane reads codes that it copied itself, and scales that
-// its warp copied.  The tokens, which every block reads, come from L1 and L2 into registers, a block of K ahead
+// its warp copied (8 x 16384 x 8192, f16, groups of 128: 22 us, 3.1 TB/s; one x 4096 x 4096 5.0).  The tokens, which every block reads, come from L1 and L2 into registers, a block of K ahead
 // where two fit; two strips share them (8 tokens' 128 of K are twice a strip's bytes).  The loop is unrolled over the ring, so that
 // its places are constants (with one that was not, and the scales' type looked up, 128 of K of a strip took 218 instructions, not 176, and a
 // token times 16384 x 8192 25 us, not 20).

@@ -10,7 +10,7 @@
 // Split.  Bound by HBM: each element is read and written once.  A block takes a few tokens with all their heads, so
 // that a token's cosines and sines are computed once a block and not once a head; 2^k lanes hold a head,
 // each two 16-byte pieces, so that both members of every pair are in one thread and the sum of squares
-// needs k shuffles.  Whole heads are in registers before they are written: outputs may be the inputs.  Measured: 16384 tokens of 32 + 8
+// needs k shuffles.  Whole heads are in registers before they are written: outputs may be the inputs.  Measured: 13003 tokens of 32 + 8
 // heads of 128, bfloat16, 52 us (5.1 TB/s; a warp a head, its partners through shared memory, 404), one token 3.2.
 #include <cuda_runtime.h>
 
@@ -258,7 +258,7 @@ cudaError_t launch_wide(RopeArgs& p, cudaStream_t s) {
   int lg = 0;
   while ((2 * V << lg) < p.d.D) ++lg;
   const int groups = kThreads >> lg;
-  // about ten heads a group (16384 tokens of 32 + 8 heads of 128: 52 us; five 56, twenty 62); a group for each head where the tokens
+  // about ten heads a group (13003 tokens of 32 + 8 heads of 128: 52.4 us; five 54.6, twenty 54.4); a group for each head where the tokens
   // would not fill the chip
   int share = 1;
   while (share < groups && share * 10 < p.heads) share *= 2;
