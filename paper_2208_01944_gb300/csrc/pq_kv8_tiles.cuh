@@ -145,7 +145,7 @@ __device__ __forceinline__ TcPlace tc_place(const AttnArgs& p) {
 // the end (one group had 1100 to 1900 cycles' work with each half, and everything else waited for it); each stream has a warp of
 // its own that issues its MMAs (`own`: one warp needed 3600 cycles for both streams' 24 MMAs, 6 waits and 7 commits of a step, and
 // everything else waited for it: 32 sequences of up to 24 drafts over up to 6000 103.9 us, so 94.8); four warps convert the keys and
-// four the values.
+// four the values.  Bound by the softmax now: 2000 to 2200 of a step's 2800 cycles for 64 tokens of a row, and about 400 of hand-over.
 template <bool WIDE>
 struct TcRoles {
   static constexpr bool kOwn = WIDE;
@@ -375,9 +375,13 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
     auto copy = [&](const int8_t* codes, int j) {
       if (j < steps) {
         const StepPage* page = pages[j % kPageRing];
+        // (all looked up before the first copy: in turn, eight of them took 1900 cycles)
+        int64_t bases[kTurns];
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) bases[i] = page[slot(i)].codes;
 #pragma unroll
         for (int i = 0; i < kTurns; ++i) {
-          const int64_t base = page[slot(i)].codes;
+          const int64_t base = bases[i];
           const bool have = base >= 0 && there;
           cp_async_16(staged + ((j & 1) * 2 + side) * (kTokens * DP) + i * (32 * Roles::kOneSide * 16), have ? codes + base + in_page(i) : codes,
                       have ? 16 : 0);
@@ -499,10 +503,13 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
     else if (warp == Roles::kSecondIssuer)
       issue(std::integral_constant<int, 1>{});
   } else if (WIDE && warp < 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     convert();
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
+    if (WIDE)
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 136;");
+    else
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 152;");
     // ---- softmax: this thread's row
     ctx.err_bits = PQ_ERR_EPILOGUE;
     const int t = (warp - Roles::kFirstSoftmax) >> 2;
