@@ -143,12 +143,11 @@ __device__ __forceinline__ TcPlace tc_place(const AttnArgs& p) {
 // warp's scheduler, and four of softmax for each tile.  Wide, for one tile of rows: the two groups of softmax are streams of the same
 // rows, one through the first half of every step and one through the second, with maxima, sums and outputs of their own, joined at
 // the end (one group had 1100 to 1900 cycles' work with each half, and everything else waited for it); each stream has a warp of
-// its own that issues its MMAs (`own`: one warp needed 3600 cycles for both streams' 24 MMAs, 6 waits and 7 commits of a step, and
+// its own that issues its MMAs (one warp needed 3600 cycles for both streams' 24 MMAs, 6 waits and 7 commits of a step, and
 // everything else waited for it: 32 sequences of up to 24 drafts over up to 6000 103.9 us, so 94.8); four warps convert the keys and
 // four the values.  Bound by the softmax now: 2000 to 2200 of a step's 2800 cycles for 64 tokens of a row, and about 400 of hand-over.
 template <bool WIDE>
 struct TcRoles {
-  static constexpr bool kOwn = WIDE;
   static constexpr int kThreads = WIDE ? 640 : 512;
   static constexpr int kOneSide = WIDE ? 4 : 6;  // converting warps of the keys (and of the values)
   static constexpr int kPageWarp = WIDE ? 1 : 4, kSecondIssuer = 2, kFirstConverter = 4, kFirstSoftmax = WIDE ? 12 : 8;
@@ -191,16 +190,16 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
 
   if (threadIdx.x == 0) {
     mbar_init(bars.q_full(), 4 * streams);
-    mbar_init(bars.done(), Roles::kOwn ? streams : 1);
+    mbar_init(bars.done(), WIDE ? streams : 1);
     for (int s = 0; s < 2; ++s) {
       mbar_init(bars.k_full(s), Roles::kOneSide);
-      mbar_init(bars.k_empty(s), Roles::kOwn ? streams : 1);
+      mbar_init(bars.k_empty(s), WIDE ? streams : 1);
       mbar_init(bars.v_full(s), Roles::kOneSide);
-      mbar_init(bars.v_empty(s), Roles::kOwn ? streams : 1);
+      mbar_init(bars.v_empty(s), WIDE ? streams : 1);
     }
     for (int b = 0; b < 4; ++b) {
       mbar_init(bars.s_full(b), 1);
-      mbar_init(bars.p_full(b), 4 * (Roles::kOwn ? 1 : streams));
+      mbar_init(bars.p_full(b), 4 * (WIDE ? 1 : streams));
     }
     for (int b = 0; b < 2; ++b) mbar_init(bars.o_full(b), 1);
     for (int i = 0; i < kPageRing; ++i) {
@@ -574,7 +573,7 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
         }
       }
       for (; i < halves; i += WIDE ? 2 : 1) {
-        const int turn = WIDE ? i >> 1 : i, place = Roles::kOwn ? 2 * t + (turn & 1) : turn & 1;  // of this group's halves; its buffer's barriers
+        const int turn = WIDE ? i >> 1 : i, place = WIDE ? 2 * t + (turn & 1) : turn & 1;  // of this group's halves; its buffer's barriers
         ok = __all_sync(0xffffffffu, mbar_wait(bars.s_full(place), (turn >> 1) & 1, ctx)) != 0;
         if (!ok) break;
         tc_fence_after();
@@ -634,7 +633,7 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
           l *= alpha;
           if (turn > 0) {
             // once the product of the half before is over
-            ok = __all_sync(0xffffffffu, mbar_wait(bars.o_full(Roles::kOwn ? t : 0), (turn - 1) & 1, ctx)) != 0;
+            ok = __all_sync(0xffffffffu, mbar_wait(bars.o_full(WIDE ? t : 0), (turn - 1) & 1, ctx)) != 0;
             if (!ok) break;
             tc_fence_after();
 #pragma unroll
