@@ -729,7 +729,8 @@ size_t palquant_linear_w4_scratch_bytes(const pq_w4_weights* w, const pq_linear_
 /* x_dev [M, K] of x_type to y_dev [M, N] of y_type; d->N and d->K are w's, d->ldw is not read, bias_dev
  * fp32 [N] or NULL.  Made for few tokens, where the weights' bytes are what counts; any M up to
  * 32 * 65535 (PQ_EUNSUPPORTED else).  M = 0 does nothing.  Any alignment of the types; token rows on 16-byte boundaries
- * are read 16 bytes at a time. */
+ * are read 16 bytes at a time.  y shares no element with x: it lies apart, or in columns of its own in rows of one
+ * pitch (PQ_EINVAL else). */
 pq_status palquant_linear_w4(const void* x_dev, const void* packed_dev, const float* bias_dev, void* y_dev,
                              const pq_w4_weights* w, const pq_linear_desc* d, void* scratch_dev, size_t scratch_bytes,
                              pq_stream_t stream);

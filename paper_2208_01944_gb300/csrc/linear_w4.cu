@@ -130,6 +130,17 @@ bool valid_w4_call(const pq_w4_weights* w, const pq_linear_desc* d) {
          valid_w4_type(d->y_type) && d->ldx >= d->K && d->ldy >= d->N;
 }
 
+// Whether no output lies on a token's element: apart as a whole, or columns of their own in rows of one pitch (bytes).
+// (Blocks read tokens while others write outputs.)
+bool rows_apart(const void* x_dev, const void* y_dev, const pq_linear_desc* d) {
+  const __int128 x = static_cast<__int128>(reinterpret_cast<uintptr_t>(x_dev)), y = static_cast<__int128>(reinterpret_cast<uintptr_t>(y_dev));
+  const __int128 ex = bytes_of_type(d->x_type), ey = bytes_of_type(d->y_type), px = d->ldx * ex, py = d->ldy * ey;
+  if (x + (d->M - 1) * px + d->K * ex <= y || y + (d->M - 1) * py + d->N * ey <= x) return true;
+  if (d->M == 1 || px != py) return false;
+  const __int128 off = ((y - x) % px + px) % px;  // of y's row in x's
+  return off >= d->K * ex && off + d->N * ey <= px;
+}
+
 // Blocks of 256 threads for a loop over `items` of them.
 unsigned loop_grid(int64_t items) { return static_cast<unsigned>(std::max<int64_t>(1, std::min<int64_t>((items + 255) / 256, 152 * 16))); }
 
@@ -203,6 +214,7 @@ pq_status palquant_linear_w4(const void* x_dev, const void* packed_dev, const fl
       !pq::is_aligned(packed_dev, 16) || !pq::is_aligned(bias_dev, 4) || !pq::is_aligned(y_dev, pq::bytes_of_type(d->y_type)))
     return PQ_EINVAL;
   if (d->M > 32ll * 65535) return PQ_EUNSUPPORTED;  // blocks along the grid's second axis
+  if (!pq::rows_apart(x_dev, y_dev, d)) return PQ_EINVAL;
   const size_t need = palquant_linear_w4_scratch_bytes(w, d);
   if (need > 0 && (scratch_dev == nullptr || scratch_bytes < need || !pq::is_aligned(scratch_dev, 16))) return PQ_EINVAL;
   const pq::W4Args a = {pq::packed_of(w), x_dev, static_cast<const uint8_t*>(packed_dev), bias_dev, y_dev, d->ldx, d->ldy, d->M,

@@ -234,6 +234,18 @@ def test_w4_arguments_refused():
     B.palquant_linear_w4(None, None, None, None, w, _linear(M=0), None, 0, stream=0)
 
 
+def test_w4_outputs_over_the_tokens_are_refused():
+    """Where it is refused for nothing else: large scratch, aligned addresses."""
+    w = _w(N=64)
+    at = 1 << 20
+    for y, kw in ((at, {}),                                            # in place
+                  (at + 64, dict(M=1)), (at - 128, dict(M=1)),         # one row, over a part of it
+                  (at + 256, dict(ldx=128, ldy=96)),                   # rows of different pitch, one between the others
+                  (at + 128, dict(ldx=96, ldy=96)),                    # columns that reach into the other's
+                  (at + 768 + 576, dict(ldx=192, ldy=192))):           # and so from a row's end into the next one's
+        _refused(B.palquant_linear_w4, at, 64, None, y, w, _linear(**{**dict(N=64, ldy=64), **kw}), 64, 1 << 30)
+
+
 def test_w4_tensors_are_held_against_the_descriptor():
     w = B.w4_weights(32, 64, 32, torch.float16)
     x, y = torch.zeros(4, 64), torch.zeros(4, 32)

@@ -195,3 +195,21 @@ def test_captured_on_two_streams(B):
         torch.cuda.synchronize()
         for x, y, want, *_ in calls:
             assert torch.equal(y, want)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("M", [1, 5, 40, 300])
+def test_outputs_beside_the_tokens(B, M, kind):
+    """Columns of their own in the tokens' rows, before and behind them; the rest of the rows stays."""
+    N, K, group = 96, 256, 64
+    codes, scales = _weights(N, K, group, "f32", M)
+    w, packed = _pack(B, codes, scales, group)
+    rng = np.random.default_rng(M)
+    rows = torch.from_numpy(rng.normal(size=(M, 100 + K + 100)).astype(np.float32)).to(TYPES[kind]).cuda()
+    x = rows[:, 100:100 + K].clone()
+    for at in (0, 100 + K):
+        before = rows.clone()
+        _run(B, w, packed, rows[:, 100:100 + K], rows[:, at:at + N])
+        _check(x, rows[:, at:at + N], codes, scales, group, kind)
+        before[:, at:at + N] = rows[:, at:at + N]
+        assert torch.equal(rows, before)
