@@ -27,35 +27,23 @@
 #include "pq_tc.cuh"
 #include "pq_tokens.cuh"
 #include "pq_w4.cuh"
+#include "pq_w4_turns.h"
 
 namespace pq {
 namespace {
 
 constexpr int kThreads = 1024;
-constexpr int kWBytes = kTileStrips * (1024 + 256);   // of a stage's weights at most
-constexpr int kMaxStages = 8;
-constexpr int kMaxSlots = 8;
-constexpr uint32_t kAColumns = 256;                   // of tensor memory for unpacked weights; as many for accumulators
-constexpr int kJoin = 8;                              // tokens that a thread adds up at one time
-
-// A job: 128 (groups of 128) or 64 of K.  Its unpacked weights take a slot, its groups' accumulators a place.  Each is used again
-// every kSlots or kPlaces jobs, powers of two that the numbers of warps in turn divide: so a warp that waits for a use has
-// waited for the one before, and a wait by parity is never for the wrong one.
-__host__ __device__ constexpr int job_k(int GS) { return GS == 7 ? 128 : 64; }
-__host__ __device__ constexpr int slots(int GS) { return kAColumns / (job_k(GS) / 2); }
-__host__ __device__ constexpr int places(int BN, int GS) {
-  return 256 / ((job_k(GS) >> GS) * BN) < kMaxSlots ? 256 / ((job_k(GS) >> GS) * BN) : kMaxSlots;
-}
-
-__host__ __device__ constexpr int stage_bytes(int BN, int PARTS) { return kWBytes + BN * 256 * PARTS; }
-// What the two sides of draining warps hand to one another at a tile's end.
-__host__ __device__ constexpr int exchange_bytes(int BN) { return BN < 128 ? BN * 512 : 0; }
-__host__ __device__ constexpr int stages(int BN, int PARTS) {
-  return (204800 - exchange_bytes(BN)) / stage_bytes(BN, PARTS) < kMaxStages ? (204800 - exchange_bytes(BN)) / stage_bytes(BN, PARTS) : kMaxStages;
-}
-__host__ __device__ constexpr int smem_bytes(int BN, int PARTS) {
-  return stages(BN, PARTS) * stage_bytes(BN, PARTS) + exchange_bytes(BN) + 1024 /* alignment */;
-}
+constexpr int kJoin = 8;  // tokens that a thread adds up at one time
+using w4::job_k;
+using w4::kAColumns;
+using w4::kMaxSlots;
+using w4::kMaxStages;
+using w4::kWBytes;
+using w4::places;
+using w4::slots;
+using w4::smem_bytes;
+using w4::stages;
+static_assert(w4::kBlockK == kBlockK && kWBytes == kTileStrips * (1024 + 256), "a stage");
 
 struct W4Tc {
   W4Args a;
@@ -160,10 +148,10 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
   constexpr int kSlotColumns = kAColumns / kSlots;
   constexpr int kAccs = job_k(GS) >> GS;           // accumulators of a job
   constexpr int kPerStage = kBlockK / job_k(GS);   // jobs of a stage
-  constexpr int kIssuers = kPlaces < 4 ? kPlaces : 4;  // warps that issue jobs in turn
-  constexpr int kTurns = 2 * kPerStage;            // sets of warps that unpack jobs in turn
+  constexpr int kIssuers = w4::issuers(BN, GS);    // warps that issue jobs in turn
+  constexpr int kTurns = w4::unpacking_sets(GS);   // sets of warps that unpack jobs in turn
   constexpr int kUnpackers = 16 / kTurns;          // warps of a set: 32 channels of 64 of K each
-  static_assert(kSlots % kTurns == 0 && kSlots % kIssuers == 0 && kPlaces % kIssuers == 0 && kPlaces % 2 == 0, "turns");
+  static_assert(kSlots % kTurns == 0 && kSlots % kIssuers == 0 && kPlaces % kIssuers == 0 && kPlaces % 2 == 0 && kStages % 2 == 0, "turns");
   constexpr int kTok = BN * 128;   // bytes of 64 of K of the tokens
   // Two sides of draining warps: up to 64 tokens they take jobs in turn, each all of their columns (one side's way through a
   // job, 550 cycles, was the longest of all roles'); 128 tokens' sums do not fit a thread, there each takes half of the columns.

@@ -213,3 +213,15 @@ def test_outputs_beside_the_tokens(B, M, kind):
         _check(x, rows[:, at:at + N], codes, scales, group, kind)
         before[:, at:at + N] = rows[:, at:at + N]
         assert torch.equal(rows, before)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,N,K", [(9, 150, 20000), (32, 40, 20001), (33, 20000, 1100), (64, 260, 9000)])
+def test_three_parts_of_a_token_through_many_stages(B, M, N, K, group):
+    """fp32 tokens on the tensor cores: rings of stages that go round many times, in one tile, in several and in parts of K."""
+    codes, scales = _weights(N, K, group, "f32", M + group)
+    w, packed = _pack(B, codes, scales, group)
+    x = torch.randn(M, K, device="cuda", generator=torch.Generator(device="cuda").manual_seed(M))
+    y = torch.full((M, N), 7.0, device="cuda")
+    for _ in range(3):
+        _check(x, _run(B, w, packed, x, y), codes, scales, group, "f32")
