@@ -691,7 +691,8 @@ __global__ void __launch_bounds__(TcRoles<WIDE>::kThreads, 1) pq_kv8_tiles(const
       if (ok && steps > 0) ok = __all_sync(0xffffffffu, mbar_wait(bars.done(), 0, ctx)) != 0;
       tc_fence_after();
       float weight[2] = {1.0f, 0.0f};  // wide: of each stream's outputs
-      if constexpr (WIDE) {
+      // (without a step nothing has waited for the other warps' queries to be written, and there is nothing to join: every row has none)
+      if (WIDE && steps > 0) {
         // the streams' maxima and sums, in the queries' place
         float2 (*joined)[128] = reinterpret_cast<float2 (*)[128]>(raw + (q_base - smem_u32(raw)));
         joined[t][in] = make_float2(m, l);

@@ -304,3 +304,32 @@ def test_sinks_of_a_long_cache_past_32_bits(B, n):
     want, spread, top = ref.attention(q.float().cpu().numpy(), kf, vf, float(np.float32(D ** -0.5)), seen=ref.sees_sinks(n, length, 150, 9))
     tol = 2.0 ** -11 * np.abs(want) + (2.0 ** -11 + 2.0 ** -20 * (2 + top)) * spread + 2.0 ** -18
     assert np.all(np.abs(o.float().cpu().numpy() - want) <= tol)
+
+
+@pytest.mark.parametrize("view", ["sinks", "tree"])
+@pytest.mark.parametrize("kind", ["bf16", "f16"])
+@pytest.mark.parametrize("n,lens,Hq,H,D,T", [([30, 30], [9000, 0], 4, 1, 128, 64), ([25, 30, 12], [0, 8000, 0], 8, 2, 64, 16)])
+def test_queries_without_tokens_beside_long_texts(B, n, lens, Hq, H, D, T, kind, view):
+    """One tile of rows cut into parts: the empty texts' rows are joined from a part without a step.  They give 0, whatever their
+    queries hold (a NaN in one, the largest numbers in another)."""
+    c = Cache(B, [max(1, v) for v in lens], H, D, T, seed=13)
+    q, o = _queries(sum(n), Hq, D, kind, 6)
+    at = np.concatenate([[0], np.cumsum(n)])
+    for b in range(len(n)):
+        if lens[b] == 0:
+            q[at[b]:at[b] + 2], q[at[b] + 3] = float("nan"), 60000.0
+    bits = np.full((sum(n), 1), 0xFFFFFFFF, np.uint32)
+    for _ in range(10):
+        if view == "sinks":
+            _, scratch = _sinks(B, c, q, o, n, lens, 5000, 100)
+        else:
+            scratch = _tree(B, c, q, o, n, lens, torch.from_numpy(bits.view(np.int32)).cuda())[2]
+        assert scratch.numel() > 1
+        for b in range(len(n)):
+            if lens[b] == 0:
+                assert not o[at[b]:at[b + 1]].any()  # (a NaN counts as something)
+    full = [b for b in range(len(n)) if lens[b]]
+    rows = np.concatenate([np.arange(at[b], at[b + 1]) for b in full])
+    c.table = c.table[full]
+    _check(c, q[rows], o[rows], [n[b] for b in full], [lens[b] for b in full], kind,
+           lambda i: ref.sees_sinks(n[full[i]], lens[full[i]], 5000, 100) if view == "sinks" else ref.sees_tree(n[full[i]], lens[full[i]], bits))
