@@ -4,7 +4,8 @@
 // (y_i, y_{i + R/2}) (or (y_2i, y_{2i+1})) of the first R elements turn by the angle pos f_i.  A frequency comes as
 // a 64-bit fraction of a turn, F_i = f_i / 2 pi * 2^64 to 2 units, and pos F_i mod 2^64 is the angle's fraction of a turn, off by
 // at most |pos| 2^-63 turns: whole turns fall off the top of the product.  Its nearest quarter turn is
-// taken out in integers, so the rest (an eighth of a turn at most) keeps fp32's relative precision.
+// taken out in integers, and all 64 bits of the rest (an eighth of a turn at most) are rounded to fp32 at once: a small angle's sine
+// is as exact relative to itself as a large one's.
 // Everything after is fp32, rounded to the type once.
 //
 // Split.  Bound by HBM: each element is read and written once.  A block takes a few tokens with all their heads, so
@@ -39,10 +40,10 @@ struct RopeArgs {
 __device__ __forceinline__ float2 cos_sin(int pos, uint64_t turns) {
   const uint64_t t = static_cast<uint64_t>(static_cast<int64_t>(pos)) * turns;
   const uint32_t quarter = static_cast<uint32_t>((t + (1ull << 61)) >> 62);
-  // the rest, at most an eighth of a turn, in units of 2^-32 turns
-  const int rest = static_cast<int>(static_cast<int64_t>(t - (static_cast<uint64_t>(quarter) << 62)) >> 32);
+  // the rest, at most an eighth of a turn of either sign, rounded to fp32 once (the sine of a small angle is as exact as the angle)
+  const int64_t rest = static_cast<int64_t>(t - (static_cast<uint64_t>(quarter) << 62));
   float s, c;
-  sincospif(static_cast<float>(rest) * 0x1p-31f, &s, &c);
+  sincospif(__ll2float_rn(rest) * 0x1p-63f, &s, &c);
   const float a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
   return make_float2((quarter + 1) & 2 ? -a : a, quarter & 2 ? -b : b);
 }

@@ -185,3 +185,30 @@ def test_captured_calls_read_their_positions_anew(B):
         positions += step
         graph.replay()
         _check(x, y, None, 1e-6, positions, f, False, "bf16")
+
+
+@pytest.mark.parametrize("D", [24, 27])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_small_angles_keep_their_sine(B, interleaved, D):
+    """Heads of (1, 0) pairs come out as cosines and sines: each right relative to itself, near whole and quarter turns too.
+
+    Bound: frequencies are off by up to 2 units of 2^-64 turns a position (|p| 2^-60 in radians); the angle's remainder is rounded to fp32 (2^-24
+    of it, and of its sine); sine and cosine have an error of 2 units at most (2^-22)."""
+    from fractions import Fraction
+    pi = Fraction(31415926535897932384626433832795028841971693993751058209749445923078164062862090, 10 ** 79)
+    f = [1e-6, 1e-7, 3.3e-9, np.pi * (1 + 1e-6), np.pi / 2 * (1 - 1e-7), 2 * np.pi * (1 + 1e-8), -4e-7, 1e-3]
+    positions = torch.tensor([1, 2, 3, -1, 77, -1000], dtype=torch.int32, device="cuda")
+    x = torch.zeros(len(positions), 1, D, device="cuda")
+    a, b = (slice(0, 16, 2), slice(1, 16, 2)) if interleaved else (slice(0, 8), slice(8, 16))
+    x[..., a] = 1
+    y = torch.empty_like(x)
+    B.palquant_qk_norm_rope(x, None, y, None, B.qk_norm_rope(x, None, y, None, positions, B.rope_turns(f, "cuda"), norm=False, interleaved=interleaved))
+    got = y.double().cpu().numpy()[:, 0]
+    for t, p in enumerate(positions.tolist()):
+        for j, freq in enumerate(f):
+            angle = Fraction(freq) * p
+            quarter = round(angle / (pi / 2))
+            rest = float(angle - quarter * pi / 2)
+            c, s = [(np.cos(rest), np.sin(rest)), (-np.sin(rest), np.cos(rest)), (-np.cos(rest), -np.sin(rest)), (np.sin(rest), -np.cos(rest))][quarter % 4]
+            for value, want in ((got[t, a][j], c), (got[t, b][j], s)):
+                assert abs(value - want) <= (2.0 ** -22 + 2.0 ** -24) * abs(want) + abs(p) * 2.0 ** -60, (p, freq, value, want)
