@@ -208,20 +208,23 @@ __global__ void __launch_bounds__(kThreads) pq_qk_rope_wide(const __grid_constan
         for (int i = 0; i < V; ++i) x[j][i] = x[j][i] * f * w[j][i];
     }
     T y[2][V];
+    // (elements behind the rotated part are taken as they are: times (1, 0) an infinity would make its neighbour NaN)
     if (p.d.interleaved) {
 #pragma unroll
       for (int j = 0; j < 2; ++j)
 #pragma unroll
         for (int i = 0; i < V; i += 2) {
           const float2 c = cs[(j * V + i) / 2];
-          y[j][i] = from_f32<T>(fmaf(x[j][i], c.x, -x[j][i + 1] * c.y));
-          y[j][i + 1] = from_f32<T>(fmaf(x[j][i + 1], c.x, x[j][i] * c.y));
+          const bool turned = u * V + (j * V + i) / 2 < half;
+          y[j][i] = from_f32<T>(turned ? fmaf(x[j][i], c.x, -x[j][i + 1] * c.y) : x[j][i]);
+          y[j][i + 1] = from_f32<T>(turned ? fmaf(x[j][i + 1], c.x, x[j][i] * c.y) : x[j][i + 1]);
         }
     } else {
+      const bool turned = u < rotated;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        y[0][i] = from_f32<T>(fmaf(x[0][i], cs[i].x, -x[1][i] * cs[i].y));
-        y[1][i] = from_f32<T>(fmaf(x[1][i], cs[i].x, x[0][i] * cs[i].y));
+        y[0][i] = from_f32<T>(turned ? fmaf(x[0][i], cs[i].x, -x[1][i] * cs[i].y) : x[0][i]);
+        y[1][i] = from_f32<T>(turned ? fmaf(x[1][i], cs[i].x, x[0][i] * cs[i].y) : x[1][i]);
       }
     }
     if (head) {

@@ -212,3 +212,35 @@ def test_small_angles_keep_their_sine(B, interleaved, D):
             c, s = [(np.cos(rest), np.sin(rest)), (-np.sin(rest), np.cos(rest)), (-np.cos(rest), -np.sin(rest)), (np.sin(rest), -np.cos(rest))][quarter % 4]
             for value, want in ((got[t, a][j], c), (got[t, b][j], s)):
                 assert abs(value - want) <= (2.0 ** -22 + 2.0 ** -24) * abs(want) + abs(p) * 2.0 ** -60, (p, freq, value, want)
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("D,R,interleaved", [(64, 32, False), (64, 32, True), (64, 6, True), (128, 0, False), (128, 96, False), (37, 10, False), (37, 10, True), (80, 40, False)])
+def test_elements_behind_the_rotated_part_stay_as_they_are(B, D, R, interleaved, kind):
+    """Without a norm they are copied: infinities, NaN and zeros of either sign do not meet their neighbours."""
+    x = torch.randn(9, 3, D, device="cuda").to(TYPES[kind])
+    x[0, 0, R], x[1, 1, D - 1], x[2, 2, R + 3], x[3, 0, R::2] = float("inf"), float("-inf"), float("nan"), -0.0
+    y = torch.empty_like(x)
+    positions = torch.arange(9, dtype=torch.int32, device="cuda") * 1001
+    turns = B.rope_turns(_frequencies(R), "cuda") if R else None
+    B.palquant_qk_norm_rope(x, None, y, None, B.qk_norm_rope(x, None, y, None, positions, turns, norm=False, interleaved=interleaved))
+    same = lambda t: torch.where(torch.isnan(t), 0, t.view(torch.int32 if kind == "f32" else torch.int16))  # noqa: E731  (bits, but for those of a NaN)
+    assert torch.equal(torch.isnan(y[..., R:]), torch.isnan(x[..., R:]))
+    assert torch.equal(same(y[..., R:].contiguous()), same(x[..., R:].contiguous()))
+    assert torch.isfinite(y[..., :R]).all()
+
+
+@pytest.mark.parametrize("D,R,interleaved", [(64, 32, False), (64, 32, True), (37, 10, False)])
+def test_a_product_past_the_type_stays_its_own(B, D, R, interleaved):
+    """A weight that takes one normed element behind the rotated part to infinity."""
+    x = torch.randn(5, 2, D, device="cuda")
+    x[:, :, R + 1] = x.abs().amax(2) + 2
+    w = torch.ones(D, device="cuda")
+    w[R + 1] = 3e38
+    y = torch.empty_like(x)
+    positions = torch.arange(5, dtype=torch.int32, device="cuda")
+    B.palquant_qk_norm_rope(x, None, y, None, B.qk_norm_rope(x, None, y, None, positions, B.rope_turns(_frequencies(R), "cuda"), w, interleaved=interleaved))
+    assert torch.isinf(y[:, :, R + 1]).all()
+    keep = [d for d in range(D) if d != R + 1]
+    want, size = ref.norm_rope(x.cpu().numpy(), w.cpu().numpy(), 1e-6, positions.cpu().numpy(), _frequencies(R), interleaved)
+    assert np.all(np.abs(y.cpu().numpy().astype(np.float64) - want)[..., keep] <= ((2.0 ** -24 * np.abs(want) + 14 * 2.0 ** -23 * size))[..., keep])
