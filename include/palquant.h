@@ -666,8 +666,9 @@ pq_status palquant_kv8_attention_tree(const pq_kv8_cache* cache, const void* q_d
  *   interleaved = 1 (n_{2j}, n_{2j+1}), becomes (a cos a_j - b sin a_j, b cos a_j + a sin a_j).
  * Elements from R on are normed only; R = 0 rotates nothing (pos_dev and turns_dev may be NULL).  R is
  * even, 0 to D; D up to 1024 and Hq + Hkv up to 65535 (PQ_EUNSUPPORTED else); Hq or Hkv may be 0.  Element
- * (t, h, i) of a tensor at t * token stride + h * head stride + i.  Outputs may be the inputs themselves
- * (same pointer, same strides); else they share no element with an input.  turns_dev: R / 2 values of
+ * (t, h, i) of a tensor at t * token stride + h * head stride + i.  An output may be its input itself
+ * (same pointer, same strides); else it shares no element with an input or with the other output: it lies apart as a whole, or between
+ * their heads with their token stride (PQ_EINVAL else).  turns_dev: R / 2 values of
  * palquant_rope_turns_host, whose frequencies are in radians a position; angles are exact to |position| 2^-63
  * turns, positions of either sign.  Squares are summed in fp32, the magnitudes below 2^60.  Bound by HBM: every element read and
  * written once; rows on 16-byte boundaries (R / 2 elements with them) are the fast ones. */

@@ -846,7 +846,7 @@ def qk_norm_rope(q, k, q_out, k_out, positions=None, turns=None, q_weight=None, 
     """Descriptor of a call on queries and keys [tokens, heads, D] (any token and head strides; one of them may be None, with its
     output): norms with a weight for each element (None: ones; norm=False: no norm), rotation of the first 2 * len(turns)
     elements by positions [tokens] (int32; turns=None: no rotation).  An output is its input itself or apart from the
-    inputs.  It keeps positions, turns and weights alive."""
+    inputs and the other output.  It keeps positions, turns and weights alive."""
     import torch
 
     some = q if q is not None else k

@@ -22,7 +22,7 @@ SOURCES = ["api.cu", "conv_tc.cu", "pointwise_tc.cu", "quantize.cu", "watchdog.c
            "kv8_attn_sinks.cu", "kv8_attn_tree.cu", "qk_rope.cu", "linear_w4.cu",
            "linear_w4_f32.cu", "linear_w4_f16.cu", "linear_w4_bf16.cu", "linear_w4_tc.cu"]
 HEADERS = ["pq_device.cuh", "pq_internal.h", "pq_tokens.cuh", "pq_linear.h", "pq_kv8.cuh", "pq_kv8_rows.cuh", "pq_kv8_tiles.cuh",
-           "pq_words.h", "pq_tc.cuh", "pq_w4.cuh", "pq_w4_rows.cuh", "pq_w4_turns.h"]
+           "pq_words.h", "pq_tc.cuh", "pq_w4.cuh", "pq_w4_rows.cuh", "pq_w4_turns.h", "pq_apart.h"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fno-strict-aliasing",
               "-I" + os.path.join(ROOT, "include")]

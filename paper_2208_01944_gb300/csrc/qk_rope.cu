@@ -18,6 +18,7 @@
 #include <cmath>
 
 #include "palquant.h"
+#include "pq_apart.h"
 #include "pq_internal.h"
 #include "pq_tokens.cuh"
 
@@ -311,6 +312,22 @@ bool valid_rope(const pq_qk_rope* d) {
   return true;
 }
 
+// Whether no output lies on an element of another tensor: each is its input itself, or shares nothing with it, and nothing with the others.
+// (A head is written while others are still to be read.)
+bool outputs_apart(const RopeArgs& p) {
+  const pq_qk_rope& d = p.d;
+  const __int128 e = static_cast<__int128>(bytes_of_type(d.type));
+  auto heads = [&](const void* at, int64_t ts, int64_t hs, int n) { return HeadsAt{reinterpret_cast<uintptr_t>(at), ts * e, hs * e, n}; };
+  const HeadsAt in[2] = {heads(p.in[0], d.q_token_stride, d.q_head_stride, d.Hq), heads(p.in[1], d.k_token_stride, d.k_head_stride, d.Hkv)};
+  const HeadsAt out[2] = {heads(p.out[0], d.q_out_token_stride, d.q_out_head_stride, d.Hq),
+                          heads(p.out[1], d.k_out_token_stride, d.k_out_head_stride, d.Hkv)};
+  const int64_t bytes = d.D * static_cast<int64_t>(e);
+  for (int o = 0; o < 2; ++o)
+    for (int i = 0; i < 2; ++i)
+      if (!(o == i && same_heads(out[o], in[i], d.tokens)) && heads_share(out[o], in[i], d.tokens, bytes)) return false;
+  return !heads_share(out[0], out[1], d.tokens, bytes);
+}
+
 }  // namespace
 }  // namespace pq
 
@@ -344,6 +361,7 @@ pq_status palquant_qk_norm_rope(const void* q_dev, const void* k_dev, void* q_ou
     return PQ_EINVAL;
   if (d->D > kMostD || d->tokens > 0x7FFFFFFF || d->Hq + static_cast<int64_t>(d->Hkv) > 65535) return PQ_EUNSUPPORTED;
   RopeArgs p = {*d, {q_dev, k_dev}, {q_out_dev, k_out_dev}, d->Hq + d->Hkv, 1, 1};
+  if (!outputs_apart(p)) return PQ_EINVAL;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t st = d->type == PQ_F32   ? launch_rope<float>(p, s)
                          : d->type == PQ_F16 ? launch_rope<__half>(p, s)

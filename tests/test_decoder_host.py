@@ -322,3 +322,29 @@ def test_w4_scratch_is_a_copy_of_the_tokens_that_need_one(M, K, ldx, x_type, nby
     if nbytes:
         for scratch, n in ((None, nbytes), (72, nbytes), (64, nbytes - 1)):
             _refused(B.palquant_linear_w4, 64, 64, None, 64, w, d, scratch, n)
+
+
+def test_rope_outputs_over_other_heads_are_refused():
+    """Where it is refused for nothing else: aligned addresses, every stride above the heads' length.  (q: 4 heads, k: 2 heads, 5 tokens, bfloat16.)"""
+    at, far = 1 << 20, 1 << 30
+    for q, k, q_out, k_out, kw in (
+            (at, far, at + 128, far, {}),                     # a head further
+            (at, far, at + 1024, far, {}),                    # a token further
+            (at, far, at - 2, far, {}),                       # an element before
+            (at, far, at, far, dict(q_out_head_stride=128)),  # the input's place with other strides
+            (at, far, at, far, dict(q_out_token_stride=640)),
+            (at, far, far, 2 * far, {}),                      # queries over keys, keys over queries, outputs over one another
+            (at, far, 2 * far, at + 128, {}),
+            (at, far, 2 * far, 2 * far + 256, {}),
+            (at, at + 512, at, at + 384, {})):                # in place, but for the keys, which lie in the queries' last head
+        _refused(B.palquant_qk_norm_rope, q, k, q_out, k_out, _rope(**kw))
+    _refused(B.palquant_qk_norm_rope, at, None, at + 128, None, _rope(Hkv=0))
+
+
+def test_rope_views_over_one_another_are_refused():
+    qkv = torch.zeros(6, 8, 64)
+    d = B.qk_norm_rope(qkv[:, :4], None, qkv[:, 1:5], None)
+    d._device = None  # (these tensors are on the CPU: as if they were where they should be)
+    with pytest.raises(B.PalquantError) as e:
+        B.palquant_qk_norm_rope(qkv[:, :4], None, qkv[:, 1:5], None, d, stream=0)
+    assert e.value.status == B.PQ_EINVAL

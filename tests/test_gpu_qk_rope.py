@@ -244,3 +244,28 @@ def test_a_product_past_the_type_stays_its_own(B, D, R, interleaved):
     keep = [d for d in range(D) if d != R + 1]
     want, size = ref.norm_rope(x.cpu().numpy(), w.cpu().numpy(), 1e-6, positions.cpu().numpy(), _frequencies(R), interleaved)
     assert np.all(np.abs(y.cpu().numpy().astype(np.float64) - want)[..., keep] <= ((2.0 ** -24 * np.abs(want) + 14 * 2.0 ** -23 * size))[..., keep])
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_outputs_between_other_heads(B, kind):
+    """In place where queries, keys and values of a head lie side by side; into the heads beside the inputs; heads first."""
+    tokens, H, D = 11, 3, 64
+    f = _frequencies(D)
+    turns, positions = B.rope_turns(f, "cuda"), torch.arange(tokens, dtype=torch.int32, device="cuda") * 13
+
+    def turn(q, k, q_out, k_out):
+        q0, k0 = q.clone(), k.clone()
+        B.palquant_qk_norm_rope(q, k, q_out, k_out, B.qk_norm_rope(q, k, q_out, k_out, positions, turns))
+        _check(q0, q_out, None, 1e-6, positions, f, False, kind)
+        _check(k0, k_out, None, 1e-6, positions, f, False, kind)
+
+    x = torch.randn(tokens, H, 3, D, device="cuda").to(TYPES[kind])
+    values = x[:, :, 2].clone()
+    turn(x[:, :, 0], x[:, :, 1], x[:, :, 0], x[:, :, 1])
+    assert torch.equal(x[:, :, 2], values)
+    x = torch.randn(tokens, 12, D, device="cuda").to(TYPES[kind])
+    before = x.clone()
+    turn(x[:, 0::4], x[:, 1::4], x[:, 2::4], x[:, 3::4])
+    assert torch.equal(x[:, 0::4], before[:, 0::4]) and torch.equal(x[:, 1::4], before[:, 1::4])
+    x = torch.randn(5, tokens, D, device="cuda").to(TYPES[kind]).transpose(0, 1)
+    turn(x[:, :3], x[:, 3:], x[:, :3], x[:, 3:])
