@@ -616,22 +616,39 @@ def _described(t, described, name):
     raise ArgumentError(f"{name}: not as the descriptor has it")
 
 
-def _vector(t, dtype, count, name):
-    """Address of a contiguous tensor of this type with at least `count` elements (None and addresses as they are)."""
+def _vector(t, dtype, count, name, device=None):
+    """Address of a contiguous tensor of this type with at least `count` elements, on the device (its index) if one is known (None and
+    addresses as they are)."""
     if t is None or type(t) is int:
         return t
-    if t.dtype is dtype and t.numel() >= count and t.is_contiguous():
+    if t.dtype is dtype and t.numel() >= count and t.is_contiguous() and (device is None or t.get_device() == device):
         return t.data_ptr()
-    raise ArgumentError(f"{name}: {count} contiguous elements of {dtype}")
+    raise ArgumentError(f"{name}: {count} contiguous elements of {dtype}, on the device of the other tensors")
 
 
-def _span(t, dtype, count, name):
-    """Address of a tensor of this type (None: one that the library refuses) with `count` elements from its first to its last."""
+def _room(t, nbytes, name, device=None):
+    """Address of a buffer of at least `nbytes` contiguous bytes, on the device (its index) if one is known (None and addresses as they are)."""
+    if t is None or type(t) is int:
+        return t
+    if t.is_contiguous() and t.numel() * t.element_size() >= nbytes and (device is None or t.get_device() == device):
+        return t.data_ptr()
+    raise ArgumentError(f"{name}: {nbytes} contiguous bytes on the device of the other tensors")
+
+
+def _device_of(d, of):
+    """Index of the device of the tensor that a descriptor was made for (None: filled by hand)."""
+    layout = getattr(d, of, None)
+    return None if layout is None else layout[3]
+
+
+def _span(t, dtype, count, name, device=None):
+    """Address of a tensor of this type (None: one that the library refuses) with `count` elements from its first to its last, on the
+    device (its index) if one is known."""
     if t is None or type(t) is int or dtype is None:
         return _strided(t)
-    if t.dtype is dtype and 1 + sum((n - 1) * step for n, step in zip(t.shape, t.stride())) >= count:
+    if t.dtype is dtype and 1 + sum((n - 1) * step for n, step in zip(t.shape, t.stride())) >= count and (device is None or t.get_device() == device):
         return t.data_ptr()
-    raise ArgumentError(f"{name}: {count} elements of {dtype}")
+    raise ArgumentError(f"{name}: {count} elements of {dtype}, on the device of the other tensors")
 
 
 def _heads(t, name):
@@ -729,9 +746,10 @@ def _fits_cache(cache, d, of="_heads"):
 def palquant_quantize_tokens(x_dev, x_type, ldx, M, K, code_format, q_dev, ldq, s_dev, stream=None):
     """Signed 8-bit codes and one scale for each token (row); code_format PQ_CODES_INT8 or PQ_CODES_F16."""
     floats, codes, _ = _dtypes()
+    at = x_dev.get_device() if getattr(x_dev, "data_ptr", None) is not None else None
     x, q, s = (_span(x_dev, floats.get(x_type), (M - 1) * ldx + K if M > 0 else 0, "x"),
-               _span(q_dev, codes.get(code_format), (M - 1) * ldq + K if M > 0 else 0, "q"),
-               _vector(s_dev, floats[PQ_F32], M, "s"))
+               _span(q_dev, codes.get(code_format), (M - 1) * ldq + K if M > 0 else 0, "q", at),
+               _vector(s_dev, floats[PQ_F32], M, "s", at))
     _check(lib.palquant_quantize_tokens(x, x_type, ldx, M, K, code_format, q, ldq, s, _stream(stream)),
            "palquant_quantize_tokens")
 
@@ -744,11 +762,11 @@ def palquant_linear_i8(q_dev, code_format, ldq, s_x_dev, w_dev, s_w_dev, bias_de
                        stream=None):
     """Dense layer on token codes: exact int32 sums, scales for each token and output channel."""
     floats, codes, sums = _dtypes()
-    M, N, f32 = d.M, d.N, floats[PQ_F32]
-    q = _span(q_dev, codes.get(code_format), (M - 1) * ldq + d.K if M > 0 else 0, "q")
-    _check(lib.palquant_linear_i8(q, code_format, ldq, _vector(s_x_dev, f32, M, "s_x"), _described(w_dev, getattr(d, "_w", _BY_HAND), "w"),
-                                  _vector(s_w_dev, f32, N, "s_w"), _vector(bias_dev, f32, N, "bias"),
-                                  _vector(acc_dev, sums, M * N, "acc"), _described(y_dev, getattr(d, "_y", _BY_HAND), "y"),
+    M, N, f32, at = d.M, d.N, floats[PQ_F32], _device_of(d, "_w")
+    q = _span(q_dev, codes.get(code_format), (M - 1) * ldq + d.K if M > 0 else 0, "q", at)
+    _check(lib.palquant_linear_i8(q, code_format, ldq, _vector(s_x_dev, f32, M, "s_x", at), _described(w_dev, getattr(d, "_w", _BY_HAND), "w"),
+                                  _vector(s_w_dev, f32, N, "s_w", at), _vector(bias_dev, f32, N, "bias", at),
+                                  _vector(acc_dev, sums, M * N, "acc", at), _described(y_dev, getattr(d, "_y", _BY_HAND), "y"),
                                   ctypes.byref(d), _stream(stream)), "palquant_linear_i8")
 
 
@@ -758,11 +776,11 @@ def palquant_linear_q8_scratch_bytes(d: LinearDesc) -> int:
 
 def palquant_linear_q8(x_dev, w_dev, s_w_dev, bias_dev, y_dev, d: LinearDesc, scratch_dev, scratch_bytes, stream=None):
     """Token quantiser and dense layer: x to y."""
-    N, f32 = d.N, _dtypes()[0][PQ_F32]
+    N, f32, at = d.N, _dtypes()[0][PQ_F32], _device_of(d, "_x")
     _check(lib.palquant_linear_q8(_described(x_dev, getattr(d, "_x", _BY_HAND), "x"), _described(w_dev, getattr(d, "_w", _BY_HAND), "w"),
-                                  _vector(s_w_dev, f32, N, "s_w"), _vector(bias_dev, f32, N, "bias"),
-                                  _described(y_dev, getattr(d, "_y", _BY_HAND), "y"), ctypes.byref(d), _ptr(scratch_dev),
-                                  scratch_bytes, _stream(stream)), "palquant_linear_q8")
+                                  _vector(s_w_dev, f32, N, "s_w", at), _vector(bias_dev, f32, N, "bias", at),
+                                  _described(y_dev, getattr(d, "_y", _BY_HAND), "y"), ctypes.byref(d),
+                                  _room(scratch_dev, scratch_bytes, "scratch", at), scratch_bytes, _stream(stream)), "palquant_linear_q8")
 
 
 def palquant_kv8_append(cache: KV8Cache, k_dev, v_dev, t: KV8Tokens, stream=None):
@@ -790,8 +808,9 @@ def palquant_kv8_attention(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, scratch_de
     """Attention over the cache: single tokens, chunks and prompts, grouped heads."""
     _fits_cache(cache, a, "_queries")
     _check(lib.palquant_kv8_attention(ctypes.byref(cache), _described(q_dev, getattr(a, "_q", _BY_HAND), "q"),
-                                      _described(o_dev, getattr(a, "_o", _BY_HAND), "o"), ctypes.byref(a), _ptr(scratch_dev),
-                                      scratch_bytes, _stream(stream)), "palquant_kv8_attention")
+                                      _described(o_dev, getattr(a, "_o", _BY_HAND), "o"), ctypes.byref(a),
+                                      _room(scratch_dev, scratch_bytes, "scratch", _device_of(a, "_q")), scratch_bytes, _stream(stream)),
+           "palquant_kv8_attention")
 
 
 # ---------------------------------------------------------------- a decoder's operators around the 8-bit cache
@@ -813,15 +832,6 @@ def _here(device):
 
 def _index_of(t):
     return None if t is None or type(t) is int else t.get_device()
-
-
-def _room(t, nbytes, name, device=None):
-    """Address of a buffer of at least `nbytes` contiguous bytes, on the device if one is named (None and addresses as they are)."""
-    if t is None or type(t) is int:
-        return t
-    if t.is_contiguous() and t.numel() * t.element_size() >= nbytes and (device is None or t.get_device() == device):
-        return t.data_ptr()
-    raise ArgumentError(f"{name}: {nbytes} contiguous bytes on the device of the other tensors")
 
 
 def _same_or_apart(src, dst, name):
@@ -975,14 +985,9 @@ def palquant_linear_w4(x_dev, packed_dev, bias_dev, y_dev, w: W4Weights, d: Line
     if nbytes is None:
         nbytes = lib.palquant_w4_packed_bytes(ctypes.byref(w))
     packed = _room(packed_dev, nbytes, "packed", at)
-    _check(lib.palquant_linear_w4(_described(x_dev, getattr(d, "_x", _BY_HAND), "x"), packed, _vector(bias_dev, _dtypes()[0][PQ_F32], d.N, "bias"),
+    _check(lib.palquant_linear_w4(_described(x_dev, getattr(d, "_x", _BY_HAND), "x"), packed, _vector(bias_dev, _dtypes()[0][PQ_F32], d.N, "bias", at),
                                   _described(y_dev, getattr(d, "_y", _BY_HAND), "y"), ctypes.byref(w), ctypes.byref(d),
-                                  _room(scratch_dev, scratch_bytes, "scratch"), scratch_bytes, _stream(stream)), "palquant_linear_w4")
-
-
-def _queries_device(a):
-    q = getattr(a, "_q", None)
-    return None if q is None else q[3]
+                                  _room(scratch_dev, scratch_bytes, "scratch", at), scratch_bytes, _stream(stream)), "palquant_linear_w4")
 
 
 def palquant_kv8_attention_sinks_scratch_bytes(cache: KV8Cache, a: KV8Attn, sinks) -> int:
@@ -991,11 +996,12 @@ def palquant_kv8_attention_sinks_scratch_bytes(cache: KV8Cache, a: KV8Attn, sink
 
 def palquant_kv8_attention_sinks(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, sinks, scratch_dev, scratch_bytes, stream=None):
     """Attention over the cache through a window, with the first `sinks` tokens of every sequence in sight."""
-    _here(_queries_device(a))
+    at = _device_of(a, "_q")
+    _here(at)
     _fits_cache(cache, a, "_queries")
     _check(lib.palquant_kv8_attention_sinks(ctypes.byref(cache), _described(q_dev, getattr(a, "_q", _BY_HAND), "q"),
                                             _described(o_dev, getattr(a, "_o", _BY_HAND), "o"), ctypes.byref(a), sinks,
-                                            _room(scratch_dev, scratch_bytes, "scratch"), scratch_bytes, _stream(stream)),
+                                            _room(scratch_dev, scratch_bytes, "scratch", at), scratch_bytes, _stream(stream)),
            "palquant_kv8_attention_sinks")
 
 
@@ -1019,10 +1025,11 @@ def palquant_kv8_attention_tree_scratch_bytes(cache: KV8Cache, a: KV8Attn, tree:
 
 def palquant_kv8_attention_tree(cache: KV8Cache, q_dev, o_dev, a: KV8Attn, tree: KV8Tree, scratch_dev, scratch_bytes, stream=None):
     """Attention for drafted tokens, the sequences' last cached ones: each sees the text before them and the drafts of its bits."""
-    _here(_queries_device(a))
+    at = _device_of(a, "_q")
+    _here(at)
     _fits_cache(cache, a, "_queries")
     _need(getattr(tree, "_for", None) == getattr(a, "_q", None) or not hasattr(tree, "_for"), "tree: of other queries")
     _check(lib.palquant_kv8_attention_tree(ctypes.byref(cache), _described(q_dev, getattr(a, "_q", _BY_HAND), "q"),
                                            _described(o_dev, getattr(a, "_o", _BY_HAND), "o"), ctypes.byref(a), ctypes.byref(tree),
-                                           _room(scratch_dev, scratch_bytes, "scratch"), scratch_bytes, _stream(stream)),
+                                           _room(scratch_dev, scratch_bytes, "scratch", at), scratch_bytes, _stream(stream)),
            "palquant_kv8_attention_tree")

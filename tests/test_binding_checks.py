@@ -146,3 +146,56 @@ def test_scales_bias_and_codes_of_the_dense_layer_are_looked_at():
     padded = torch.zeros(4, 80)[:, :64]
     with pytest.raises(B.PalquantError):  # rows of a wider matrix: as far as its last element
         tokens(x=padded, ldx=80, format=7)
+
+
+def _elsewhere(d, *layouts):
+    """A descriptor as it would be for the same tensors on cuda:0."""
+    for name in layouts:
+        setattr(d, name, (*getattr(d, name)[:3], 0))
+    if hasattr(d, "_device"):
+        d._device = 0
+    return d
+
+
+def test_tensors_beside_the_described_ones_lie_on_their_device(monkeypatch):
+    """Scales, bias, sums, codes and workspaces on the CPU for a call on a GPU (whose own tensors are given as addresses)."""
+    monkeypatch.setattr(B, "_here", lambda device: None)  # (no GPU is current here)
+    x, w, y = torch.zeros(4, 64), torch.zeros(32, 64, dtype=torch.int8), torch.zeros(4, 32)
+    s_w, bias, s_x, room = torch.zeros(32), torch.zeros(32), torch.zeros(4), torch.zeros(1 << 16, dtype=torch.uint8)
+    d = _elsewhere(B.linear_desc(x, w, y), "_x", "_w", "_y")
+    for i, t in ((2, s_w), (3, bias), (6, room)):
+        args = [64, 64, 64, None, 64, d, 64, 1 << 16]
+        args[i] = t
+        with pytest.raises(ValueError):
+            B.palquant_linear_q8(*args, stream=0)
+    for i, t in ((0, w[:4]), (3, s_x), (5, s_w), (6, bias), (7, torch.zeros(4, 32, dtype=torch.int32))):
+        args = [64, B.PQ_CODES_INT8, 64, 64, 64, 64, None, None, 64, d]
+        args[i] = t
+        with pytest.raises(ValueError):
+            B.palquant_linear_i8(*args, stream=0)
+    w4 = B.w4_weights(32, 64, 32, torch.float16)
+    d4 = _elsewhere(B.linear_w4_desc(x, w4, y), "_x", "_y")
+    for i, t in ((1, room), (2, bias), (6, room)):
+        args = [64, 64, None, 64, w4, d4, 64, 1 << 16]
+        args[i] = t
+        with pytest.raises(ValueError):
+            B.palquant_linear_w4(*args, stream=0)
+    q = torch.zeros(6, 4, 64)
+    a = _elsewhere(B.kv8_attn(q, q.clone(), _i32(3), _i32(2), _i32(2, 2), 4, 32, 0.1), "_q", "_o")
+    tree = B.kv8_tree(_i32(6, 1), B.kv8_attn(q, q.clone(), _i32(3), _i32(2), _i32(2, 2), 4, 32, 0.1))
+    tree._for = a._q
+    with pytest.raises(ValueError):
+        B.palquant_kv8_attention(_cache(), 64, 64, a, room, room.numel(), stream=0)
+    with pytest.raises(ValueError):
+        B.palquant_kv8_attention_sinks(_cache(), 64, 64, a, 4, room, room.numel(), stream=0)
+    with pytest.raises(ValueError):
+        B.palquant_kv8_attention_tree(_cache(), 64, 64, a, tree, room, room.numel(), stream=0)
+
+
+def test_workspaces_are_as_large_as_they_are_said_to_be():
+    q = torch.zeros(6, 4, 64)
+    with pytest.raises(ValueError):
+        B.palquant_kv8_attention(_cache(), q, q.clone(), _queries(q, q.clone()), torch.zeros(8, dtype=torch.uint8), 9, stream=0)
+    x, w, y = torch.zeros(4, 64), torch.zeros(32, 64, dtype=torch.int8), torch.zeros(4, 32)
+    with pytest.raises(ValueError):
+        B.palquant_linear_q8(x, w, torch.zeros(32), None, y, B.linear_desc(x, w, y), torch.zeros(8, dtype=torch.uint8), 9, stream=0)
