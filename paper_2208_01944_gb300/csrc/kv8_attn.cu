@@ -214,15 +214,21 @@ bool valid_view(const pq_kv8_attn* a, const View& v) {
 Plan prepare_attention(const pq_kv8_cache* c, const pq_kv8_attn* a, View& v, AttnArgs* p) {
   p->c = *c;
   p->a = without_idle_window(a);
-  if (v.kind == kSinks && (p->a.window == 0 || v.sinks == 0)) v.kind = kPlain;  // every token up to the query is in sight, or no sink is
-  if (v.kind == kSinks) p->sinks = std::min(v.sinks, a->max_len);
+  // Every token up to the query is in sight, or no sink is: plain attention, and its plan.  Half-precision outputs of a window that only
+  // outlasts the texts keep the view's second half of a weight, so that they are as exact as once the texts have outgrown it (error 2.1e-4 of
+  // the outputs' norm, without it 3.1e-4; us in a graph, with it and without, 32 / 8 heads of 128: 64 single tokens over 4000 106 / 103, 8 chunks
+  // of 64 over 2000 82 / 75, 4 prompts of 2048 over 4096 509 / 403).
+  const bool idle = v.kind == kSinks && (p->a.window == 0 || v.sinks == 0);
+  const bool fine = v.kind != kPlain && !idle;
+  if (idle && !(a->type == PQ_F16 && a->window > 0 && v.sinks > 0)) v.kind = kPlain;
+  if (v.kind == kSinks && !idle) p->sinks = std::min(v.sinks, a->max_len);
   if (v.kind == kTree) {
     p->a.causal = 0;  // every token of the sequence, but for the bits
     p->tree = static_cast<const uint32_t*>(v.tree->bits_dev);
     p->tree_pitch = v.tree->pitch;
     p->tree_words = v.tree->words;
   }
-  return plan_attention(c, &p->a, p, v.kind != kPlain);
+  return plan_attention(c, &p->a, p, fine);
 }
 
 size_t scratch_bytes(const pq_kv8_cache* cache, const pq_kv8_attn* a, View v) {

@@ -333,3 +333,36 @@ def test_queries_without_tokens_beside_long_texts(B, n, lens, Hq, H, D, T, kind,
     c.table = c.table[full]
     _check(c, q[rows], o[rows], [n[b] for b in full], [lens[b] for b in full], kind,
            lambda i: ref.sees_sinks(n[full[i]], lens[full[i]], 5000, 100) if view == "sinks" else ref.sees_tree(n[full[i]], lens[full[i]], bits))
+
+
+@pytest.mark.parametrize("n,sequences,Hq,H,D", [(1, 1, 32, 8, 128), (40, 1, 8, 2, 64), (12, 20, 8, 2, 64), (70, 9, 8, 2, 64), (9, 2, 16, 4, 256)])
+@pytest.mark.parametrize("window", [20, 43, 44, 1000, "tree"])
+def test_half_precision_outputs_are_off_by_their_rounding(B, window, n, sequences, Hq, H, D):
+    """Of all outputs together, in the norm: with 11-bit weights the error is about sqrt(2) of the rounding's, whether a window hides something of
+    the text (44 tokens, or as many as the queries) or only could.
+
+    Bound: the exact outputs' own rounding, 1/16 more for other elements being rounded than those (thousands of them, each error
+    spread evenly over a step), and 2^-20 (2 + max |score|) spread for fp32 scores, exponentials and sums, as everywhere."""
+    length = max(44, n)
+    ns, lens = [n] * sequences, [length] * sequences
+    c = Cache(B, lens, H, D, 16, seed=21)
+    q, o = _queries(n * sequences, Hq, D, "f16", 8)
+    q *= 0.25  # (the weight of a token that outweighs the others is a power of two: no rounding would show)
+    if window == "tree":
+        bits = np.zeros((n * sequences, -(-n // 32)), np.uint32)
+        for i in range(n):
+            bits[i::n, i // 32] = 1 << (i % 32)
+        _tree(B, c, q, o, ns, lens, torch.from_numpy(bits.view(np.int32)).cuda())
+        seen = ref.sees_tree(n, length, bits[:n])
+    else:
+        _sinks(B, c, q, o, ns, lens, window, 4)
+        seen = ref.sees_sinks(n, length, window, 4)
+    off = allowed = bound = 0.0
+    qf, of = q.float().cpu().numpy(), o.double().cpu().numpy()
+    for b in range(sequences):
+        k, v = ref.read(c.k, c.ks, c.table[b], 0, length), ref.read(c.v, c.vs, c.table[b], 0, length)
+        want, spread, top = ref.attention(qf[b * n:(b + 1) * n], k, v, float(np.float32(D ** -0.5)), seen=seen)
+        off += ((of[b * n:(b + 1) * n] - want) ** 2).sum()
+        allowed += ((want.astype(np.float16).astype(np.float64) - want) ** 2).sum()
+        bound += ((2.0 ** -20 * (2 + top) * spread) ** 2).sum()
+    assert off ** 0.5 <= 17 / 16 * allowed ** 0.5 + bound ** 0.5, (off ** 0.5 / allowed ** 0.5, bound ** 0.5 / allowed ** 0.5)
