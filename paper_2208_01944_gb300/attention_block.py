@@ -79,7 +79,9 @@ def weight_codes(w: torch.Tensor, stream: torch.cuda.Stream | None = None):
 
 def weight_codes4(w: torch.Tensor, group: int = 128, scales: torch.dtype = torch.float16, stream: torch.cuda.Stream | None = None):
     """w [N, K] quantised to 4 bits with a scale for each row and `group` (32, 64 or 128) of its columns, and packed: (descriptor,
-    packed bytes) for palquant_linear_w4.  It runs on `stream` as weight_codes does."""
+    packed bytes) for palquant_linear_w4.  `scales` is the type that the scales are held in: a group whose largest weight is below 7 of the
+    type's smallest normal numbers becomes zeros, for float16 4.3e-4 (weights that quiet want bfloat16 or float32 scales).  It runs on
+    `stream` as weight_codes does."""
     if w.dim() != 2 or w.dtype not in _TYPES or w.stride(1) != 1:
         raise ValueError("w: a float matrix with contiguous rows")
     desc = B.w4_weights(w.shape[0], w.shape[1], group, scales)
@@ -124,14 +126,15 @@ class AttentionBlock8:
                  b_qkv: torch.Tensor | None = None, page_tokens: int = 64, window: int = 0,
                  stream: torch.cuda.Stream | None = None, *, sinks: int = 0, rope=None, rope_interleaved: bool = False,
                  q_norm: torch.Tensor | None = None, k_norm: torch.Tensor | None = None, norm_eps: float = 1e-6,
-                 weight_bits: int = 8, weight_group: int = 128):
+                 weight_bits: int = 8, weight_group: int = 128, weight_scales: torch.dtype = torch.float16):
         """w_qkv [(heads + 2 kv_heads) D, hidden] (the rows of q, then k, then v) and w_out [hidden, heads D] on the
         GPU; their type is the activations'.  b_qkv: a value for each row of w_qkv.
 
         sinks: first tokens that a window keeps in sight.  rope: frequencies, in radians a position, of the rotation of the
         first 2 len(rope) elements of every query and key head (pairs half of them apart, or neighbours with
         rope_interleaved).  q_norm, k_norm [D]: weights of a norm of every query and key head before the rotation (both
-        or none).  weight_bits 4: the weights in 4 bits with a scale for each channel and weight_group of inputs."""
+        or none).  weight_bits 4: the weights in 4 bits with a scale for each channel and weight_group of inputs, held as
+        weight_scales (float16 takes groups whose largest weight is below 4.3e-4 for zeros: see weight_codes4)."""
         if w_qkv.dim() != 2 or w_qkv.dtype not in _TYPES or sequences < 1 or max_len < 1 or window < 0 or page_tokens not in (16, 32, 64, 128):
             raise ValueError("w_qkv: a float matrix; at least one sequence and token; window >= 0; page_tokens: 16, 32, 64 or 128")
         if heads < 1 or kv_heads < 1 or heads % kv_heads or w_qkv.shape[0] % (heads + 2 * kv_heads):
@@ -145,8 +148,8 @@ class AttentionBlock8:
             raise ValueError("b_qkv: a value for each row of w_qkv")
         if sinks < 0 or (sinks and not window):
             raise ValueError("sinks: of a window")
-        if weight_bits not in (4, 8) or weight_group not in (32, 64, 128):
-            raise ValueError("weight_bits: 4 or 8; weight_group: 32, 64 or 128")
+        if weight_bits not in (4, 8) or weight_group not in (32, 64, 128) or weight_scales not in _TYPES:
+            raise ValueError("weight_bits: 4 or 8; weight_group: 32, 64 or 128; weight_scales: float32, float16 or bfloat16")
         rope = None if rope is None else [float(f) for f in rope]
         if rope is not None and (2 * len(rope) > self.D or not np.isfinite(rope).all()):
             raise ValueError("rope: finite frequencies, one for each pair of a head's elements at most")
@@ -164,7 +167,7 @@ class AttentionBlock8:
             w_qkv, w_out = w_qkv.contiguous(), w_out.contiguous()
             if weight_bits == 4:
                 # (descriptor, packed) of each; no scales beside them
-                (self.w_qkv_desc, self.w_qkv), (self.w_out_desc, self.w_out) = (weight_codes4(w, weight_group, stream=run) for w in (w_qkv, w_out))
+                (self.w_qkv_desc, self.w_qkv), (self.w_out_desc, self.w_out) = (weight_codes4(w, weight_group, weight_scales, run) for w in (w_qkv, w_out))
                 self.s_qkv = self.s_out = None
             else:
                 self.w_qkv, self.s_qkv = weight_codes(w_qkv, run)

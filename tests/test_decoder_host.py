@@ -348,3 +348,11 @@ def test_rope_views_over_one_another_are_refused():
     with pytest.raises(B.PalquantError) as e:
         B.palquant_qk_norm_rope(qkv[:, :4], None, qkv[:, 1:5], None, d, stream=0)
     assert e.value.status == B.PQ_EINVAL
+
+
+def test_block_scales_refused():
+    from paper_2208_01944_gb300.attention_block import AttentionBlock8
+
+    for scales in (torch.int8, torch.float64, None):
+        with pytest.raises(ValueError):
+            AttentionBlock8(torch.zeros(8 * 64, 256), torch.zeros(256, 4 * 64), 4, 2, 2, 100, weight_bits=4, weight_scales=scales)

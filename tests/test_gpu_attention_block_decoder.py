@@ -222,3 +222,21 @@ def test_refusals(B):
     with pytest.raises(ValueError):
         windowed.draft(x, [[-1, 0, 1], [-1]])
     assert block.draft(x[:0], [[], []]).shape == (0, 256)
+
+
+@pytest.mark.parametrize("scales", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("kind", list(TYPES))
+def test_quiet_weights_in_4_bits(B, kind, scales):
+    """Weights of deviation 1e-5: no group of them is lost where the scales are not held in half precision."""
+    from paper_2208_01944_gb300.attention_block import AttentionBlock8
+
+    g = torch.Generator().manual_seed(17)
+    w = [(torch.randn(*s, generator=g) * 1e-5).to(TYPES[kind]).cuda() for s in ((8 * 64, 256), (256, 4 * 64))]
+    block = AttentionBlock8(*w, 4, 2, 1, 100, weight_bits=4, weight_group=64, weight_scales=scales)
+    x = torch.randn(50, 256, generator=g).to(TYPES[kind]).cuda()
+    block.forward(x, [50])
+    codes, s = ref.w4_quantize(_f32(w[0]), 64, lambda v: torch.from_numpy(v).to(scales).float().numpy())
+    assert (s > 0).all()
+    want, size = ref.linear_w4(_f32(x), codes, s, 64)
+    tol = HALF_ULP[kind] * np.abs(want) + (74 + 2) * 2.0 ** -23 * size + (2.0 ** -25 if kind == "f16" else 0)
+    assert np.all(np.abs(_f32(block.qkv).astype(np.float64) - want) <= tol)
