@@ -225,3 +225,19 @@ def test_three_parts_of_a_token_through_many_stages(B, M, N, K, group):
     y = torch.full((M, N), 7.0, device="cuda")
     for _ in range(3):
         _check(x, _run(B, w, packed, x, y), codes, scales, group, "f32")
+
+
+@pytest.mark.parametrize("kind", list(TYPES))
+@pytest.mark.parametrize("N,K,M", [(300, 4096, 8), (9760, 520, 8), (2064, 700, 16)])
+def test_a_token_has_the_same_bits_in_any_batch_of_one_kernel(B, N, K, M, kind):
+    """Up to 8 tokens, and 16-bit ones from 9 to 16, are one kernel of tiles each; what else is in the batch, and where, does not count."""
+    codes, scales = _weights(N, K, 128, "f16", 9)
+    w, packed = _pack(B, codes, scales, 128)
+    x = torch.randn(M, K, device="cuda").to(TYPES[kind])
+    first = 1 if M <= 8 else 9
+    if kind == "f32" and M > 8:
+        first, M, x = 1, 8, x[:8]
+    whole = _run(B, w, packed, x, torch.empty(M, N, dtype=x.dtype, device="cuda"))
+    for rows in (list(range(first)), list(range(M - first, M)), list(range(M))[::-1], [M - 1] * first, list(range(M))[:first + 2]):
+        part = x[rows].contiguous()
+        assert torch.equal(_run(B, w, packed, part, torch.empty(len(rows), N, dtype=x.dtype, device="cuda")), whole[rows])
