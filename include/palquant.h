@@ -634,7 +634,8 @@ pq_status palquant_kv8_attention(const pq_kv8_cache* cache, const void* q_dev, v
 
 /* The same through a window with sinks: a->causal = 1, and the query at position p sees token j <= p
  * where j > p - window or j < sinks.  sinks >= 0; with no window, or 0 sinks, it is
- * palquant_kv8_attention.  The scratch as there, of this call's own size. */
+ * palquant_kv8_attention.  PQ_F16 carries the rest of a probability in a second half value here and for drafted tokens.  The scratch
+ * as there, of this call's own size. */
 size_t palquant_kv8_attention_sinks_scratch_bytes(const pq_kv8_cache* cache, const pq_kv8_attn* a, int32_t sinks);
 
 pq_status palquant_kv8_attention_sinks(const pq_kv8_cache* cache, const void* q_dev, void* o_dev, const pq_kv8_attn* a,

@@ -5,7 +5,7 @@
 // added in registers, in fp32.  So a weight is never rounded: scaled to 16 bits before the product it would be, by as much as the
 // output is.
 //
-// Tile.  128 output channels (8 packed strips) x BN tokens a block.  Codes stay 4-bit in memory and shared memory; eight warps turn
+// Tile.  128 output channels (8 packed strips) x BN tokens a block.  Codes stay 4-bit in memory and shared memory; sixteen warps turn
 // them into 16-bit operands in tensor memory, which take no shared-memory bandwidth: a lane's packed 16 bytes are, unpacked, the
 // registers of a 16 x 256-bit store, so nothing is exchanged between lanes.  Activations come by TMA in the 128-byte swizzle.
 // The accumulators of groups take turns, so that one is read while others are written.  Few tiles: the blocks of a cluster take
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(kThreads, 1) pq_linear_w4_tc(const __grid_cons
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 104;");
-    // ---- sums and outputs: this thread's channel, half of each accumulator's tokens
+    // ---- sums and outputs: this thread's channel; tiles of 128 tokens: half of each accumulator's
     ctx.err_bits = PQ_ERR_EPILOGUE;
     const int quarter = warp & 3, side = (warp - 20) >> 2;
     const int channel = 32 * quarter + lane, in_strip = channel & 15;

@@ -143,7 +143,9 @@ __device__ __forceinline__ void load4(const T* p, int n, bool wide, T (&v)[4]) {
   }
 }
 
-// Pair i (columns 2 i and 2 i + 1) of a word's codes in the products' type.  The code's sign bit is flipped under the
+// Small integers put under the exponent of a power of two and that power subtracted: a published way of converting 4-bit codes (Kim et
+// al., "Who Says Elephants Can't Run", 2022, arXiv 2211.10017).  Pair i (columns 2 i and 2 i + 1) of a word's codes in the products' type: the
+// code's sign bit is flipped under the
 // exponent of 1024 (128): 1032 + c (136 + c).
 template <typename T, int I>
 __device__ __forceinline__ uint32_t code_pair(uint32_t word) {

@@ -12,7 +12,8 @@
 // that a token's cosines and sines are computed once a block and not once a head; 2^k lanes hold a head,
 // each two 16-byte pieces, so that both members of every pair are in one thread and the sum of squares
 // needs k shuffles.  Whole heads are in registers before they are written: outputs may be the inputs.  Measured: 13003 tokens of 32 + 8
-// heads of 128, bfloat16, 52 us (5.1 TB/s; a warp a head, its partners through shared memory, 404), one token 3.2.
+// heads of 128, bfloat16, 53 us (5.0 TB/s; a warp a head, its partners through shared memory, 404), one token 3.3.  What
+// does not fit these pieces goes through pq_qk_rope_any: 13003 tokens of 32 + 8 heads of 80, 40 rotated, bfloat16, 355 us.
 #include <cuda_runtime.h>
 
 #include <cmath>
